@@ -275,7 +275,7 @@ int lsm_keeps_states(const lsm_params* p);
 /* Static, NUL-terminated description of a status code. */
 const char* lsm_status_string(int status);
 
-/* ABI version, bumped when a signature or struct changes (2: layout and packed input in lsm_params; 3: flags; 4: workspace query of the benchmark aid; 5: lsm_chunk_fwd_noalloc). */
+/* ABI version, bumped when a signature or struct changes (2: layout and packed input in lsm_params; 3: flags; 4: workspace query of the benchmark aid; 5: lsm_chunk_fwd_noalloc; 6: the delta-rule rows; 7: the operators of lsm_block.h). */
 int lsm_version(void);
 
 #ifdef __cplusplus

@@ -1,0 +1,83 @@
+/*
+ * lsm_block.h -- operators around the token mixer of lsm.h in one block of a model: the norm and rotation of the queries
+ * and keys that go into it (forward and backward), the mixture-of-experts layer behind it for a few tokens, and one step
+ * of a beam search with the recurrent states rearranged.
+ *
+ * Conventions of lsm.h: device pointers, 16-byte aligned; the caller owns every buffer; nothing is allocated, kept between
+ * calls or synchronised; all work is enqueued on `stream`; outputs are overwritten and alias neither inputs nor each other
+ * (lsm_state_reorder works in place by design); results are bitwise reproducible (no floating-point atomics); every
+ * argument check comes before the first HIP call.
+ */
+#ifndef LSM_BLOCK_H
+#define LSM_BLOCK_H
+
+#include "lsm.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- per-head norm of queries and keys with the rotation by position ------------------------------------------------ */
+
+typedef enum {
+    LSM_NORM_NONE = 0, /* r = 1                                                                     */
+    LSM_NORM_RMS  = 1, /* r = (mean of x_i^2 + eps)^(-1/2)                                            */
+    LSM_NORM_L2   = 2  /* r = (sum of x_i^2 + eps)^(-1/2): rows of unit length (the delta rule's keys)   */
+} lsm_norm_kind;
+
+/* Which features a rotation takes together, of the first rot_dim. */
+typedef enum {
+    LSM_ROT_HALVES = 0, /* i and i + rot_dim/2 */
+    LSM_ROT_PAIRS  = 1  /* 2i and 2i + 1       */
+} lsm_rotation;
+
+/* Element (b, h, t, i) of a tensor is at b*batch + h*head + t*token + i, in elements. */
+typedef struct { int64_t batch, head, token; } lsm_strides;
+
+typedef struct {
+    uint32_t struct_size;     /* = sizeof(lsm_qk_params)                                                            */
+    int32_t  B, T;            /* sequences and tokens of each (packed input: B = 1)                                 */
+    int32_t  H_q, H_k, d;     /* heads of q and of k (H_k = 0: no k), d in {64,128,256}                               */
+    int32_t  dtype;           /* lsm_dtype of q, k, their outputs and gradients                                     */
+    int32_t  norm, rotation;  /* lsm_norm_kind, lsm_rotation                                                        */
+    int32_t  rot_dim, n_pos;  /* rotated features (0: none; a multiple of 16, at most d) and rows of the table      */
+    float    eps;             /* > 0 where there is a norm                                                          */
+    float    q_scale, k_scale;/* factor of the outputs (the 1/sqrt(d) that lsm.h leaves to its callers)             */
+    int32_t  reserved;        /* 0                                                                                  */
+    lsm_strides q, k;         /* inputs: slices of a fused projection as they stand                                  */
+    lsm_strides q_out, k_out; /* outputs, and their gradients in the backward call                                   */
+    lsm_strides dq, dk;       /* gradients of the inputs (backward only)                                             */
+} lsm_qk_params;
+
+/*
+ * For every row x (one head of one token of q or k):   y = scale * R_p (w * (r x)) ,
+ * R_p the rotation of the token's position p: (a, b) -> (a cos - b sin, b cos + a sin) for the feature pairs of the first
+ * rot_dim features, the others as they are.
+ *   q, k        dtype, by strides; strides of axes longer than 1 in whole 16-byte pieces                       in
+ *   q_weight, k_weight   [d] fp32 or NULL (= 1)                                                                in
+ *   cos_sin     [n_pos, rot_dim] fp32: rot_dim/2 cosines, then rot_dim/2 sines; NULL exactly when rot_dim = 0      in
+ *   positions   [B, T] int32 or NULL (= 0..T-1 in every sequence, T <= n_pos then); not read when rot_dim = 0.
+ *               A position outside [0, n_pos) makes that token's rows NaN (the table is not read for it)       in
+ *   q_out, k_out   dtype, by strides                                                                           out
+ * Squares, sums and the rotation are computed in fp32; a row's elements that are not finite reach that row alone.
+ */
+int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                     const float* cos_sin, const int32_t* positions, void* q_out, void* k_out, void* stream);
+
+/*
+ * Backward of L = <q_out, d_q_out> + <k_out, d_k_out>; only the inputs are needed, nothing saved by the forward call.
+ *   d_q_out, d_k_out   dtype, by the strides q_out, k_out                                                      in
+ *   dq, dk             dtype, by the strides dq, dk                                                            out
+ *   d_q_weight, d_k_weight   [d] fp32; given only where the weight was given, NULL skips it                     out
+ *   workspace          at least lsm_qk_norm_rope_bwd_workspace_bytes(p) (0 for invalid params)
+ */
+size_t lsm_qk_norm_rope_bwd_workspace_bytes(const lsm_qk_params* p);
+int lsm_qk_norm_rope_bwd(const lsm_qk_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                         const float* cos_sin, const int32_t* positions, const void* d_q_out, const void* d_k_out,
+                         void* dq, void* dk, float* d_q_weight, float* d_k_weight,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* LSM_BLOCK_H */

@@ -6,3 +6,6 @@ from .binding import (  # noqa: F401
     lsm_profile_start, lsm_profile_stop, lsm_chunk_workspace, lsm_bench_intra_chunk_workspace,
     lsm_chunk_fwd_noalloc, NOALLOC_SCRATCH_BYTES, lsm_calib_copy, lsm_calib_mfma, lsm_delta_fwd, lsm_delta_bwd, lsm_delta_workspace, lsm_delta_step,
 )
+from .block import (  # noqa: F401
+    NORM_NONE, NORM_RMS, NORM_L2, ROT_HALVES, ROT_PAIRS, lsm_qk_norm_rope, lsm_qk_norm_rope_bwd,
+)

@@ -94,6 +94,12 @@ def library():
     lib.lsm_bench_intra_chunk_workspace_bytes.argtypes = [pp]
     lib.lsm_bench_intra_chunk.restype = ctypes.c_int
     lib.lsm_bench_intra_chunk.argtypes = [pp] + [vp] * 6 + [sz, ctypes.c_int, vp]
+    lib.lsm_qk_norm_rope.restype = ctypes.c_int
+    lib.lsm_qk_norm_rope.argtypes = [vp] * 10
+    lib.lsm_qk_norm_rope_bwd_workspace_bytes.restype = sz
+    lib.lsm_qk_norm_rope_bwd_workspace_bytes.argtypes = [vp]
+    lib.lsm_qk_norm_rope_bwd.restype = ctypes.c_int
+    lib.lsm_qk_norm_rope_bwd.argtypes = [vp] * 14 + [sz, vp]
     _lib = lib
     return lib
 

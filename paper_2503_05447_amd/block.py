@@ -1,0 +1,167 @@
+"""Binding of the operators around the token mixer declared in include/lsm_block.h: norm and rotation of queries and keys.
+
+Argument marshalling only, as in binding.py: every operator runs in the HIP kernels of liblsm_hip.so on ``stream``
+(default: torch's current stream) without synchronising.
+"""
+import ctypes
+import functools
+
+import torch
+
+from .binding import (DTYPE_BF16, DTYPE_F32, LAYOUT_BHTD, LAYOUT_BTHD, LsmError, _alloc_on, _check, _ptr, _stream_handle,
+                      library)
+
+NORM_NONE, NORM_RMS, NORM_L2 = 0, 1, 2
+ROT_HALVES, ROT_PAIRS = 0, 1
+
+_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+class _QkParams(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32)]
+                + [(n, ctypes.c_int32) for n in ("B", "T", "H_q", "H_k", "d", "dtype", "norm", "rotation", "rot_dim", "n_pos")]
+                + [(n, ctypes.c_float) for n in ("eps", "q_scale", "k_scale")] + [("reserved", ctypes.c_int32)]
+                + [(n, ctypes.c_int64 * 3) for n in ("q", "k", "q_out", "k_out", "dq", "dk")])
+
+
+@functools.lru_cache(maxsize=256)
+def _qk_params(sizes, scales, *strides):
+    """Parameter block of a shape (sizes, factors and strides only, read by the library): by reference, and kept, because a
+    decoded token's call costs little more than its marshalling."""
+    strides = [(ctypes.c_int64 * 3)(*s) for s in strides]
+    return ctypes.byref(_QkParams(ctypes.sizeof(_QkParams), *sizes, *scales, 0, *strides))
+
+
+def _dtype(t, name):
+    try:
+        return _DTYPES[t.dtype]
+    except KeyError:
+        raise ValueError("%s must be float32 or bfloat16" % name) from None
+
+
+def _heads(t, layout, name, like=None):
+    """(B, T, H, d), (batch, head, token strides) of a [B,H,T,d], [B,T,H,d] or, for one token, [B,H,d] tensor."""
+    if not t.is_cuda or t.dim() not in (3, 4) or t.stride(-1) != 1 or (like is not None and t.dtype != like):
+        raise ValueError("%s: need a device tensor of 3 or 4 axes%s whose last is dense, got %s %s on %s"
+                         % (name, "" if like is None else " of %s" % like, tuple(t.shape), t.dtype, t.device))
+    if t.dim() == 3:
+        (B, H, d), (sb, sh, _) = t.shape, t.stride()
+        return (B, 1, H, d), (sb, sh, 0)
+    if layout == LAYOUT_BTHD:
+        (B, T, H, d), (sb, st, sh, _) = t.shape, t.stride()
+    else:
+        (B, H, T, d), (sb, sh, st, _) = t.shape, t.stride()
+    return (B, T, H, d), (sb, sh, st)
+
+
+def _shape_of(sizes, layout, dim):
+    B, T, H, d = sizes
+    return (B, H, d) if dim == 3 else (B, T, H, d) if layout == LAYOUT_BTHD else (B, H, T, d)
+
+
+def _qk_setup(q, k, cos_sin, positions, q_weight, k_weight):
+    """Checks what both directions share; (rot_dim, n_pos)."""
+    d = q.shape[-1]
+    _check(q_weight, (d,), torch.float32, "q_weight")
+    _check(k_weight, (d,), torch.float32, "k_weight")
+    if k is None and k_weight is not None:
+        raise ValueError("k_weight without k")
+    if cos_sin is None:
+        return 0, 0
+    _check(cos_sin, cos_sin.shape if cos_sin.dim() == 2 else (0, 0), torch.float32, "cos_sin")
+    return cos_sin.shape[1], cos_sin.shape[0]
+
+
+def _output(given, sizes, layout, dim, like, name):
+    if given is None:
+        return torch.empty(_shape_of(sizes, layout, dim), dtype=like.dtype, device=like.device)
+    if _heads(given, layout, name, like.dtype)[0] != sizes:
+        raise ValueError("%s: need %s, got %s" % (name, _shape_of(sizes, layout, dim), tuple(given.shape)))
+    return given
+
+
+def lsm_qk_norm_rope(q, k=None, cos_sin=None, positions=None, q_weight=None, k_weight=None, norm=NORM_RMS, eps=1e-6,
+                     rotation=ROT_HALVES, q_scale=1.0, k_scale=1.0, layout=LAYOUT_BHTD, out_layout=None, q_out=None,
+                     k_out=None, stream=None):
+    """q_out, k_out = scale * rotation(weight * normalised row), for every head of every token.
+
+    q [B,H_q,T,d], k [B,H_k,T,d] (or None) in ``layout``, float32 or bfloat16, dense along d only: slices of a fused
+    projection go in as they stand; [B,H,d] for one token.  d 64, 128 or 256; H_k may differ from H_q.
+    norm: NORM_RMS (mean of squares), NORM_L2 (sum of squares: unit rows, what the delta rule expects of keys) or
+    NORM_NONE.  q_weight, k_weight: [d] float32 or None.
+    cos_sin: [n_pos, rot_dim] float32, rot_dim/2 cosines and then rot_dim/2 sines a position, or None (no rotation); the
+    first rot_dim features (a multiple of 16) are rotated, as pairs (i, i + rot_dim/2) or, with ROT_PAIRS, (2i, 2i + 1).
+    positions: [B,T] int32 (for q of 3 axes [B]); None: 0..T-1 in every sequence.  A position outside the table makes that
+    token's rows NaN.
+    out_layout: order of the results (default ``layout``); q_out, k_out: tensors to write to."""
+    (B, T, H, d), sq = _heads(q, layout, "q")
+    dt, dim = _dtype(q, "q"), q.dim()
+    out_layout = layout if out_layout is None else out_layout
+    rot, n_pos = _qk_setup(q, k, cos_sin, positions, q_weight, k_weight)
+    if positions is not None:
+        _check(positions, (B,) if dim == 3 else (B, T), torch.int32, "positions")
+    Hk, sk, sko = 0, (0, 0, 0), (0, 0, 0)
+    if k is not None:
+        (Bk, Tk, Hk, dk), sk = _heads(k, layout, "k", q.dtype)
+        if (Bk, Tk, dk) != (B, T, d) or k.dim() != dim:
+            raise ValueError("q and k differ in more than their heads: %s, %s" % (tuple(q.shape), tuple(k.shape)))
+    with _alloc_on(stream):
+        q_out = _output(q_out, (B, T, H, d), out_layout, dim, q, "q_out")
+        if k is not None:
+            k_out = _output(k_out, (B, T, Hk, d), out_layout, dim, q, "k_out")
+            sko = _heads(k_out, out_layout, "k_out")[1]
+    p = _qk_params((B, T, H, Hk, d, dt, norm, rotation, rot, n_pos), (eps, q_scale, k_scale), sq, sk,
+                   _heads(q_out, out_layout, "q_out")[1], sko, (0, 0, 0), (0, 0, 0))
+    rc = library().lsm_qk_norm_rope(p, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin), _ptr(positions),
+                                    _ptr(q_out), _ptr(k_out) if k is not None else None, _stream_handle(stream))
+    if rc != 0:
+        raise LsmError(rc, "lsm_qk_norm_rope")
+    return q_out, k_out
+
+
+def lsm_qk_norm_rope_bwd(q, k, d_q_out, d_k_out, cos_sin=None, positions=None, q_weight=None, k_weight=None, norm=NORM_RMS,
+                         eps=1e-6, rotation=ROT_HALVES, q_scale=1.0, k_scale=1.0, layout=LAYOUT_BHTD, out_layout=None,
+                         dq=None, dk=None, workspace=None, stream=None):
+    """Gradients of L = <q_out, d_q_out> + <k_out, d_k_out>: a dict with dq, dk (like q and k, dense, or written to the
+    tensors given: slices of a fused projection's gradient) and d_q_weight, d_k_weight ([d] float32; None where there is no
+    weight).  The other arguments as in lsm_qk_norm_rope; d_q_out, d_k_out in ``out_layout``, dense along d only."""
+    sizes, sq = _heads(q, layout, "q")
+    B, T, H, d = sizes
+    dt, dim = _dtype(q, "q"), q.dim()
+    out_layout = layout if out_layout is None else out_layout
+    rot, n_pos = _qk_setup(q, k, cos_sin, positions, q_weight, k_weight)
+    if positions is not None:
+        _check(positions, (B,) if dim == 3 else (B, T), torch.int32, "positions")
+    got, sgq = _heads(d_q_out, out_layout, "d_q_out", q.dtype)
+    if got != sizes:
+        raise ValueError("d_q_out: need %s, got %s" % (_shape_of(sizes, out_layout, dim), tuple(d_q_out.shape)))
+    none = (0, 0, 0)
+    Hk, sk, sgk, sdk = 0, none, none, none
+    if k is not None:
+        ksizes, sk = _heads(k, layout, "k", q.dtype)
+        Hk = ksizes[2]
+        if ksizes != (B, T, Hk, d) or k.dim() != dim:
+            raise ValueError("q and k differ in more than their heads: %s, %s" % (tuple(q.shape), tuple(k.shape)))
+        got, sgk = _heads(d_k_out, out_layout, "d_k_out", q.dtype)
+        if got != ksizes:
+            raise ValueError("d_k_out: need %s, got %s" % (_shape_of(ksizes, out_layout, dim), tuple(d_k_out.shape)))
+    elif d_k_out is not None or dk is not None:
+        raise ValueError("d_k_out or dk without k")
+    with _alloc_on(stream):
+        dq = _output(dq, sizes, layout, dim, q, "dq")
+        sdq = _heads(dq, layout, "dq")[1]
+        if k is not None:
+            dk = _output(dk, ksizes, layout, dim, q, "dk")
+            sdk = _heads(dk, layout, "dk")[1]
+        p = _qk_params((B, T, H, Hk, d, dt, norm, rotation, rot, n_pos), (eps, q_scale, k_scale), sq, sk, sgq, sgk, sdq, sdk)
+        if workspace is None:
+            need = library().lsm_qk_norm_rope_bwd_workspace_bytes(p)
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        dqw = None if q_weight is None else torch.empty(d, dtype=torch.float32, device=q.device)
+        dkw = None if k_weight is None else torch.empty(d, dtype=torch.float32, device=q.device)
+    rc = library().lsm_qk_norm_rope_bwd(p, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin), _ptr(positions),
+                                        _ptr(d_q_out), _ptr(d_k_out), _ptr(dq), _ptr(dk), _ptr(dqw), _ptr(dkw),
+                                        _ptr(workspace), workspace.numel(), _stream_handle(stream))
+    if rc != 0:
+        raise LsmError(rc, "lsm_qk_norm_rope_bwd")
+    return dict(dq=dq, dk=dk, d_q_weight=dqw, d_k_weight=dkw)

@@ -1,0 +1,59 @@
+"""Host-side checks of include/lsm_block.h that need no GPU: bad arguments are refused before any HIP call."""
+import ctypes
+
+import paper_2503_05447_amd as pkg
+from paper_2503_05447_amd import block
+
+NULL, SHAPE, UNSUP, ALIGN, WS = -1, -2, -3, -4, -5
+vp = ctypes.c_void_p
+
+
+def qk_params(strides=None, size=None, reserved=0, **kw):
+    c = dict(B=2, T=8, H_q=4, H_k=2, d=128, dtype=1, norm=1, rotation=0, rot_dim=128, n_pos=8, eps=1e-6, q_scale=1.0, k_scale=1.0)
+    c.update(kw)
+    s = {n: (4096, 1024, 128) for n in ("q", "k", "q_out", "k_out", "dq", "dk")}
+    s.update(strides or {})
+    return block._QkParams(ctypes.sizeof(block._QkParams) if size is None else size, *c.values(), reserved,
+                           *[(ctypes.c_int64 * 3)(*v) for v in s.values()])
+
+
+def qk(p, q=0x1000, k=0x2000, qw=0x3000, kw=0x4000, cs=0x5000, pos=0x6000, qo=0x7000, ko=0x8000):
+    return pkg.library().lsm_qk_norm_rope(ctypes.byref(p), vp(q), vp(k), vp(qw), vp(kw), vp(cs), vp(pos), vp(qo), vp(ko), vp(None))
+
+
+def qk_bwd(p, q=0x1000, k=0x2000, qw=0x3000, kw=0x4000, cs=0x5000, gq=0x6000, gk=0x7000, dq=0x8000, dk=0x9000, dqw=0xa000,
+           dkw=0xb000, ws=0x10000, wsb=1 << 40):
+    return pkg.library().lsm_qk_norm_rope_bwd(ctypes.byref(p), vp(q), vp(k), vp(qw), vp(kw), vp(cs), vp(None), vp(gq), vp(gk),
+                                              vp(dq), vp(dk), vp(dqw), vp(dkw), vp(ws), wsb, vp(None))
+
+
+def test_norm_and_rotation_refuse_bad_arguments():
+    P = qk_params
+    assert pkg.library().lsm_qk_norm_rope(None, *[vp(None)] * 9) == NULL
+    for bad in (dict(B=0), dict(T=0), dict(H_q=0), dict(H_k=-1), dict(n_pos=-1), dict(n_pos=0), dict(eps=0.0), dict(eps=-1.0),
+                dict(eps=float("nan")), dict(eps=float("inf")), dict(B=1 << 20, T=1 << 20), dict(H_q=1 << 21), dict(size=8)):
+        assert qk(P(**bad)) == SHAPE, bad
+        assert pkg.library().lsm_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(P(**bad))) == 0
+    for bad in (dict(d=96), dict(dtype=2), dict(norm=3), dict(norm=-1), dict(rotation=2), dict(rot_dim=24), dict(rot_dim=144),
+                dict(reserved=1)):
+        assert qk(P(**bad)) == UNSUP, bad
+    for n in ("q", "k", "q_out", "k_out"):
+        for i in range(3):
+            s = [4096, 1024, 128]
+            s[i] += 4
+            assert qk(P(strides={n: s})) == ALIGN, (n, i)
+    assert qk_bwd(P(strides={"dq": (4096, 1024, 130)})) == ALIGN
+    assert qk(P(strides={"q": (4, 1024, 128)}, B=1), q=0x1008) == ALIGN     # an axis of one: its stride is free, the pointer is not
+    for n in ("q", "qo", "cs", "ko", "k"):
+        assert qk(P(), **{n: None}) == NULL, n
+    assert qk(P(H_k=0)) == NULL and qk(P(H_k=0), k=None, ko=None) == NULL      # a k's weight without a k
+    assert qk(P(rot_dim=0)) == NULL                                            # a table without a rotation
+    assert qk(P(n_pos=7), pos=None) == SHAPE                                   # tokens beyond the table
+    for n in ("q", "k", "qw", "kw", "cs", "pos", "qo", "ko"):
+        assert qk(P(), **{n: 0x1004}) == ALIGN, n
+    for n in ("gq", "gk", "dq", "dk"):
+        assert qk_bwd(P(), **{n: None}) == NULL, n
+    assert qk_bwd(P(), qw=None) == NULL and qk_bwd(P(), kw=None) == NULL       # a gradient without its weight
+    assert qk_bwd(P(), ws=None) == WS and qk_bwd(P(), wsb=16) == WS
+    for n in ("dqw", "dkw", "ws", "gk"):
+        assert qk_bwd(P(), **{n: 0x1004}) == ALIGN, n
