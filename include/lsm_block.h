@@ -77,6 +77,48 @@ int lsm_qk_norm_rope_bwd(const lsm_qk_params* p, const void* q, const void* k, c
                          void* dq, void* dk, float* d_q_weight, float* d_k_weight,
                          void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- one step of a beam search --------------------------------------------------------------------------------------- */
+
+typedef struct {
+    uint32_t struct_size; /* = sizeof(lsm_beam_params)                                                       */
+    int32_t  B, K, V;     /* sequences, beams of each (at most 32), vocabulary; K * V at most 2^30             */
+    int32_t  n_out;       /* candidates wanted of each sequence: 1..32, at most K * V                        */
+    int32_t  dtype;       /* lsm_dtype of the logits                                                         */
+    int32_t  eos;         /* the token that ends a beam, or -1                                               */
+    int32_t  reserved;    /* 0                                                                               */
+    int64_t  row_stride;  /* elements between the logits of consecutive beams, >= V                          */
+} lsm_beam_params;
+
+/*
+ * The n_out best candidates (beam k, token t) of every sequence by
+ *     score(k, t) = scores[k] + ((x_t - m) - log(sum_t exp(x_t - m))) ,   m = max_t x_t ,   x = logits of beam k,
+ * in fp32; a finished beam offers (k, eos) at scores[k] and nothing else (its logits are not read).
+ *   logits     [B, K, V] dtype, rows row_stride apart                                                      in
+ *   scores     [B, K] fp32: the beams' log-probabilities so far (-inf: no such beam)                        in
+ *   finished   [B, K] bytes (0 or not), or NULL; needs eos >= 0                                             in
+ *   out_scores, parent, token   [B, n_out] fp32, int32, int32                                              out
+ *   out_finished   [B, n_out] bytes 0 / 1: the parent was finished or the token is eos; NULL skips it, must be NULL
+ *              where eos < 0                                                                               out
+ *   workspace  at least lsm_beam_select_workspace_bytes(p) (0 for invalid params); contents undefined after the call
+ * Candidates come by falling score, equal ones by rising k * V + t (all K V of them take part, those at -inf too).
+ * A logit that is NaN counts as -inf and +inf as the largest finite number of its type; a score that comes out NaN is -inf.
+ */
+size_t lsm_beam_select_workspace_bytes(const lsm_beam_params* p);
+int lsm_beam_select(const lsm_beam_params* p, const void* logits, const float* scores, const uint8_t* finished,
+                    float* out_scores, int32_t* parent, int32_t* token, uint8_t* out_finished,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The states that belong to the beams follow them, in place: row b K + i of every tensor becomes what row b K + parent[b, i]
+ * was before the call.
+ *   states     HOST array of n_states (1..64) device pointers to [B * K] rows                               in/out
+ *   row_bytes  HOST array: bytes of a row of each, a multiple of 4
+ *   parent     [B, K] int32; a value outside [0, K) fills its row with 0xff bytes (NaN)                      in
+ * Rows that stay where they are (parent[b, i] = i) are not touched.  B at most 65535, K at most 32.
+ */
+int lsm_state_reorder(void* const* states, const size_t* row_bytes, int n_states, const int32_t* parent, int B, int K,
+                      void* stream);
+
 #ifdef __cplusplus
 }
 #endif

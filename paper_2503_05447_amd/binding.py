@@ -100,6 +100,12 @@ def library():
     lib.lsm_qk_norm_rope_bwd_workspace_bytes.argtypes = [vp]
     lib.lsm_qk_norm_rope_bwd.restype = ctypes.c_int
     lib.lsm_qk_norm_rope_bwd.argtypes = [vp] * 14 + [sz, vp]
+    lib.lsm_beam_select.restype = ctypes.c_int
+    lib.lsm_beam_select.argtypes = [vp] * 9 + [sz, vp]
+    lib.lsm_beam_select_workspace_bytes.restype = sz
+    lib.lsm_beam_select_workspace_bytes.argtypes = [vp]
+    lib.lsm_state_reorder.restype = ctypes.c_int
+    lib.lsm_state_reorder.argtypes = [vp, vp, ctypes.c_int, vp, ctypes.c_int, ctypes.c_int, vp]
     _lib = lib
     return lib
 

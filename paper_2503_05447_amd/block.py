@@ -1,4 +1,5 @@
-"""Binding of the operators around the token mixer declared in include/lsm_block.h: norm and rotation of queries and keys.
+"""Binding of the operators around the token mixer declared in include/lsm_block.h: norm and rotation of queries and keys,
+one step of a beam search.
 
 Argument marshalling only, as in binding.py: every operator runs in the HIP kernels of liblsm_hip.so on ``stream``
 (default: torch's current stream) without synchronising.
@@ -165,3 +166,77 @@ def lsm_qk_norm_rope_bwd(q, k, d_q_out, d_k_out, cos_sin=None, positions=None, q
     if rc != 0:
         raise LsmError(rc, "lsm_qk_norm_rope_bwd")
     return dict(dq=dq, dk=dk, d_q_weight=dqw, d_k_weight=dkw)
+
+
+class _BeamParams(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in ("B", "K", "V", "n_out", "dtype", "eos", "reserved")]
+                + [("row_stride", ctypes.c_int64)])
+
+
+@functools.lru_cache(maxsize=256)
+def _beam_params(*sizes):
+    """Parameter block by reference, and the workspace it asks for."""
+    p = ctypes.byref(_BeamParams(ctypes.sizeof(_BeamParams), *sizes))
+    return p, library().lsm_beam_select_workspace_bytes(p)
+
+
+def lsm_beam_select(logits, scores, n_out=None, finished=None, eos=None, workspace=None, stream=None):
+    """scores, parent, token, finished = the n_out (default K, at most 32) best of K x V candidates of each sequence.
+
+    logits [B,K,V] float32 or bfloat16 (dense along V, rows evenly spaced: a padded vocabulary's slice goes in as it is),
+    scores [B,K] float32 log-probabilities of the beams so far (-inf: no such beam).  Candidate (k, t) has
+    scores[k] + log_softmax(logits[k])[t]; a beam marked in ``finished`` ([B,K] bool; needs eos) offers only eos, at its
+    score.  Results [B,n_out], best first, equal scores by rising k V + t: float32 scores, int32 parents and tokens, and with
+    an ``eos`` whether the beam has ended (bool), else None.  A NaN logit counts as -inf."""
+    if not logits.is_cuda or logits.dim() != 3 or logits.stride(2) != 1 or (logits.shape[0] > 1 and logits.shape[1] > 1
+                                                                          and logits.stride(0) != logits.shape[1] * logits.stride(1)):
+        raise ValueError("logits: need a [B,K,V] device tensor, dense along V, its rows evenly spaced, got %s with strides %s on %s"
+                         % (tuple(logits.shape), logits.stride(), logits.device))
+    B, K, V = logits.shape
+    dt = _dtype(logits, "logits")
+    _check(scores, (B, K), torch.float32, "scores")
+    if finished is not None and eos is None:
+        raise ValueError("finished needs eos")
+    _check(finished, (B, K), torch.bool, "finished")
+    n_out = K if n_out is None else n_out
+    row = logits.stride(1) if K > 1 else logits.stride(0) if B > 1 else V
+    p, need = _beam_params(B, K, V, n_out, dt, -1 if eos is None else eos, 0, row)
+    with _alloc_on(stream):
+        if workspace is None:
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=logits.device)
+        out = torch.empty((B, max(n_out, 0)), dtype=torch.float32, device=logits.device)
+        parent = torch.empty_like(out, dtype=torch.int32)
+        token = torch.empty_like(out, dtype=torch.int32)
+        ended = None if eos is None else torch.empty_like(out, dtype=torch.bool)
+    rc = library().lsm_beam_select(p, _ptr(logits), _ptr(scores), _ptr(finished), _ptr(out), _ptr(parent), _ptr(token), _ptr(ended),
+                                   _ptr(workspace), workspace.numel(), _stream_handle(stream))
+    if rc != 0:
+        raise LsmError(rc, "lsm_beam_select")
+    return out, parent, token, ended
+
+
+_MAX_STATES = 64
+
+
+def lsm_state_reorder(states, parent, stream=None):
+    """In place: row b K + i of every tensor in ``states`` (one tensor or a list; first axis B K, or [B,K,...]; dense, rows of
+    whole 4 bytes) becomes its row b K + parent[b,i].  parent [B,K] int32, as lsm_beam_select returns it for n_out = K; a value
+    outside [0, K) fills its row with 0xff bytes (NaN).  Beams that stay are not touched; 64 tensors a launch."""
+    states = [states] if isinstance(states, torch.Tensor) else list(states)
+    if parent.dim() != 2:
+        raise ValueError("parent: need [B,K], got %s" % (tuple(parent.shape),))
+    _check(parent, parent.shape, torch.int32, "parent")
+    B, K = parent.shape
+    at, size = [], []
+    for t in states:
+        if not t.is_cuda or not t.is_contiguous() or t.numel() == 0 or not (
+                t.shape[0] == B * K or (t.dim() > 1 and t.shape[:2] == (B, K))):
+            raise ValueError("states: need contiguous device tensors of %d rows, got %s on %s" % (B * K, tuple(t.shape), t.device))
+        at.append(t.data_ptr())
+        size.append(t.numel() // (B * K) * t.element_size())
+    for i in range(0, len(at), _MAX_STATES):
+        n = min(_MAX_STATES, len(at) - i)
+        rc = library().lsm_state_reorder((ctypes.c_void_p * n)(*at[i:i + n]), (ctypes.c_size_t * n)(*size[i:i + n]), n, _ptr(parent),
+                                         B, K, _stream_handle(stream))
+        if rc != 0:
+            raise LsmError(rc, "lsm_state_reorder")

@@ -57,3 +57,45 @@ def test_norm_and_rotation_refuse_bad_arguments():
     assert qk_bwd(P(), ws=None) == WS and qk_bwd(P(), wsb=16) == WS
     for n in ("dqw", "dkw", "ws", "gk"):
         assert qk_bwd(P(), **{n: 0x1004}) == ALIGN, n
+
+
+def beam_params(size=None, reserved=0, row_stride=None, **kw):
+    c = dict(B=2, K=4, V=100, n_out=4, dtype=0, eos=-1)
+    c.update(kw)
+    return block._BeamParams(ctypes.sizeof(block._BeamParams) if size is None else size, *c.values(), reserved,
+                             c["V"] if row_stride is None else row_stride)
+
+
+def beam(p, x=0x1000, s=0x2000, f=None, o=0x3000, par=0x4000, tok=0x5000, of=None, ws=0x10000, wsb=1 << 40):
+    return pkg.library().lsm_beam_select(ctypes.byref(p), vp(x), vp(s), vp(f), vp(o), vp(par), vp(tok), vp(of), vp(ws), wsb, vp(None))
+
+
+def test_beam_selection_refuses_bad_arguments():
+    P = beam_params
+    need = pkg.library().lsm_beam_select_workspace_bytes
+    assert pkg.library().lsm_beam_select(None, *[vp(None)] * 8, 0, vp(None)) == NULL
+    for bad in (dict(B=0), dict(K=0), dict(V=0), dict(n_out=0), dict(row_stride=99), dict(K=1, V=3, n_out=4), dict(eos=100), dict(eos=-2),
+                dict(K=32, V=1 << 26), dict(size=4), dict(row_stride=1 << 41), dict(B=1 << 30)):
+        assert beam(P(**bad)) == SHAPE, bad
+        assert need(ctypes.byref(P(**bad))) == 0
+    for bad in (dict(dtype=2), dict(K=33), dict(n_out=33), dict(reserved=1)):
+        assert beam(P(**bad)) == UNSUP, bad
+    for n in ("x", "s", "o", "par", "tok"):
+        assert beam(P(), **{n: None}) == NULL, n
+    assert beam(P(), f=0x6000) == NULL and beam(P(), of=0x6000) == NULL        # finished beams without an end token
+    for n in ("x", "s", "o", "par", "tok", "f", "of", "ws"):
+        assert beam(P(eos=1), **{n: 0x1004}) == ALIGN, n
+    assert beam(P(), ws=None) == WS and beam(P(), wsb=need(ctypes.byref(P())) - 1) == WS
+    assert 0 < need(ctypes.byref(P())) < need(ctypes.byref(P(V=50000))) < need(ctypes.byref(P(V=50000, n_out=8)))
+
+
+def test_reordering_states_refuses_bad_arguments():
+    def reorder(at=(0x1000, 0x2000), size=(64, 12), n=None, parent=0x3000, B=2, K=4):
+        a, s = (vp * max(len(at), 1))(*at), (ctypes.c_size_t * max(len(size), 1))(*size)
+        return pkg.library().lsm_state_reorder(a, s, len(at) if n is None else n, vp(parent), B, K, vp(None))
+    assert reorder(parent=None) == NULL and reorder(at=(0x1000, None)) == NULL
+    assert pkg.library().lsm_state_reorder(None, None, 1, vp(0x1000), 1, 1, vp(None)) == NULL
+    assert reorder(n=0) == SHAPE and reorder(at=(0x1000,) * 65, size=(64,) * 65) == SHAPE
+    assert reorder(B=0) == SHAPE and reorder(B=65536) == SHAPE and reorder(K=0) == SHAPE and reorder(K=33) == UNSUP
+    assert reorder(size=(64, 0)) == SHAPE and reorder(size=(64, 6)) == SHAPE
+    assert reorder(at=(0x1000, 0x2004)) == ALIGN and reorder(parent=0x3004) == ALIGN
