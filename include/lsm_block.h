@@ -77,6 +77,36 @@ int lsm_qk_norm_rope_bwd(const lsm_qk_params* p, const void* q, const void* k, c
                          void* dq, void* dk, float* d_q_weight, float* d_k_weight,
                          void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- a mixture-of-experts layer for a few tokens ----------------------------------------------------------------------- */
+
+typedef struct {
+    uint32_t struct_size; /* = sizeof(lsm_moe_params)                                                         */
+    int32_t  n, D, F;     /* tokens (1..128), their width and the experts' (multiples of 8, at most 65536)     */
+    int32_t  E, top_k;    /* experts (1..256) and how many of them a token goes to (1..16, at most E)         */
+    int32_t  dtype;       /* lsm_dtype of everything below                                                    */
+    int32_t  renormalise; /* 1: the chosen experts' weights sum to 1; 0: they are the softmax over all experts */
+} lsm_moe_params;
+
+/*
+ * For every token x:   p = softmax(router x) over the E experts,  S = the top_k experts of largest router output (equal
+ * ones by rising index),  w_e = p_e or p_e / sum_S p,
+ *     y = residual + sum_{e in S} w_e Wd_e (silu(Wg_e x) * (Wu_e x)) ,      silu(z) = z / (1 + exp(-z)) .
+ *   x          [n, D]                                                                               in
+ *   router     [E, D]                                                                               in
+ *   w_gate_up  [E, 2 F, D]: F rows of Wg_e, then F rows of Wu_e                                       in
+ *   w_down     [E, D, F]: Wd_e                                                                       in
+ *   residual   [n, D] or NULL (= 0)                                                                 in
+ *   y          [n, D]                                                                               out
+ *   workspace  at least lsm_moe_step_workspace_bytes(p) (0 for invalid params)
+ * The form for decoding: the active experts' weights are read once, whatever the tokens that share them; for the many tokens
+ * of a prompt a grouped matrix product is the better tool.  Sums are fp32; with bf16 elements the hidden activations are kept
+ * as a bf16 head and a bf16 remainder, so that the one rounding to bf16 is the result's.  A token whose router output is not
+ * finite gets a row of NaN; other tokens are not affected.
+ */
+size_t lsm_moe_step_workspace_bytes(const lsm_moe_params* p);
+int lsm_moe_step(const lsm_moe_params* p, const void* x, const void* router, const void* w_gate_up, const void* w_down,
+                 const void* residual, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- one step of a beam search --------------------------------------------------------------------------------------- */
 
 typedef struct {

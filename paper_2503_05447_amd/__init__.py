@@ -8,5 +8,5 @@ from .binding import (  # noqa: F401
 )
 from .block import (  # noqa: F401
     NORM_NONE, NORM_RMS, NORM_L2, ROT_HALVES, ROT_PAIRS, lsm_qk_norm_rope, lsm_qk_norm_rope_bwd,
-    lsm_beam_select, lsm_state_reorder,
+    lsm_moe_step, lsm_beam_select, lsm_state_reorder,
 )

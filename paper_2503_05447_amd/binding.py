@@ -106,6 +106,10 @@ def library():
     lib.lsm_beam_select_workspace_bytes.argtypes = [vp]
     lib.lsm_state_reorder.restype = ctypes.c_int
     lib.lsm_state_reorder.argtypes = [vp, vp, ctypes.c_int, vp, ctypes.c_int, ctypes.c_int, vp]
+    lib.lsm_moe_step.restype = ctypes.c_int
+    lib.lsm_moe_step.argtypes = [vp] * 8 + [sz, vp]
+    lib.lsm_moe_step_workspace_bytes.restype = sz
+    lib.lsm_moe_step_workspace_bytes.argtypes = [vp]
     _lib = lib
     return lib
 

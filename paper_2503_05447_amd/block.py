@@ -1,5 +1,5 @@
 """Binding of the operators around the token mixer declared in include/lsm_block.h: norm and rotation of queries and keys,
-one step of a beam search.
+a mixture-of-experts layer for a few tokens, one step of a beam search.
 
 Argument marshalling only, as in binding.py: every operator runs in the HIP kernels of liblsm_hip.so on ``stream``
 (default: torch's current stream) without synchronising.
@@ -166,6 +166,50 @@ def lsm_qk_norm_rope_bwd(q, k, d_q_out, d_k_out, cos_sin=None, positions=None, q
     if rc != 0:
         raise LsmError(rc, "lsm_qk_norm_rope_bwd")
     return dict(dq=dq, dk=dk, d_q_weight=dqw, d_k_weight=dkw)
+
+
+class _MoeParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in ("n", "D", "F", "E", "top_k", "dtype", "renormalise")]
+
+
+@functools.lru_cache(maxsize=256)
+def _moe_params(*sizes):
+    """Parameter block by reference, and the workspace it asks for."""
+    p = ctypes.byref(_MoeParams(ctypes.sizeof(_MoeParams), *sizes))
+    return p, library().lsm_moe_step_workspace_bytes(p)
+
+
+def lsm_moe_step(x, router, w_gate_up, w_down, top_k, renormalise=True, residual=None, y=None, workspace=None, stream=None):
+    """y = residual + the mixture of experts of each row of x, for up to 128 tokens (the form for decoding).
+
+    x [n,D], router [E,D], w_gate_up [E,2F,D] (F rows of the gate, F rows of the factor), w_down [E,D,F], residual [n,D] or
+    None, all float32 or all bfloat16; D and F multiples of 8, E at most 256, top_k at most 16.  A token goes to the top_k
+    experts of largest router output (equal ones by index), weighted by the softmax over all experts, with ``renormalise``
+    divided by its sum over the chosen ones: sum_e w_e Wd_e (silu(Wg_e x) * (Wu_e x))."""
+    if x.dim() != 2 or router.dim() != 2 or w_down.dim() != 3:
+        raise ValueError("need x [n,D], router [E,D], w_gate_up [E,2F,D], w_down [E,D,F], got %s" %
+                         ", ".join(str(tuple(t.shape)) for t in (x, router, w_gate_up, w_down)))
+    n, D = x.shape
+    E, F = router.shape[0], w_down.shape[2]
+    dt, dtype = _dtype(x, "x"), x.dtype
+    _check(x, (n, D), dtype, "x")
+    _check(router, (E, D), dtype, "router")
+    _check(w_gate_up, (E, 2 * F, D), dtype, "w_gate_up")
+    _check(w_down, (E, D, F), dtype, "w_down")
+    _check(residual, (n, D), dtype, "residual")
+    p, need = _moe_params(n, D, F, E, top_k, dt, 1 if renormalise else 0)
+    with _alloc_on(stream):
+        if workspace is None:
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
+        if y is None:
+            y = torch.empty_like(x)
+        else:
+            _check(y, (n, D), dtype, "y")
+    rc = library().lsm_moe_step(p, _ptr(x), _ptr(router), _ptr(w_gate_up), _ptr(w_down), _ptr(residual), _ptr(y), _ptr(workspace),
+                                workspace.numel(), _stream_handle(stream))
+    if rc != 0:
+        raise LsmError(rc, "lsm_moe_step")
+    return y
 
 
 class _BeamParams(ctypes.Structure):

@@ -157,14 +157,14 @@ __global__ __launch_bounds__(256) void k_beam_slices(BeamArgs a) {
     const uint32_t mine = ordered(top);
     _Pragma("unroll") for (int bit = 31; bit >= 16; --bit) {
         const uint32_t trial = bound | (1u << bit);
-        if (__popcll(__ballot(mine >= trial)) >= keep) bound = trial;
+        if (lanes(__ballot(mine >= trial)) >= keep) bound = trial;
     }
     if (sizeof(TIO) == 2) {
         bound |= bound & 0x80000000u ? 0u : 0xffffu;
-    } else if (__popcll(__ballot(mine >= bound)) > 2 * keep) {
+    } else if (lanes(__ballot(mine >= bound)) > 2 * keep) {
         for (int bit = 15; bit >= 0; --bit) {
             const uint32_t trial = bound | (1u << bit);
-            if (__popcll(__ballot(mine >= trial)) >= keep) bound = trial;
+            if (lanes(__ballot(mine >= trial)) >= keep) bound = trial;
         }
     }
     if (lane == 0) {
@@ -304,8 +304,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
         u64 bound = 0;
         for (int bit = 63; bit >= 0; --bit) {
             const u64 trial = bound | (u64(1) << bit);
-            if (__popcll(__ballot(top >= trial)) >= n) bound = trial;
-            if (bit == 32 && __popcll(__ballot(top >= bound)) <= 2 * n) break;
+            if (lanes(__ballot(top >= trial)) >= n) bound = trial;
+            if (bit == 32 && lanes(__ballot(top >= bound)) <= 2 * n) break;
         }
         if (lane == 0) wave_bound[wave] = bound;
         __syncthreads();
@@ -374,14 +374,14 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
                     hit = ordered(y) == bar;
                 }
                 const u64 hits = __ballot(hit);
-                if (lane == 0) counts[wave] = __popcll(hits);
+                if (lane == 0) counts[wave] = lanes(hits);
                 __syncthreads();
                 int before = 0, all = 0;
                 _Pragma("unroll") for (int w = 0; w < kMergeWaves; ++w) {
                     before += w < wave ? counts[w] : 0;
                     all += counts[w];
                 }
-                const int place = found + before + __popcll(hits & ((u64(1) << lane) - 1));
+                const int place = found + before + lanes(hits & ((u64(1) << lane) - 1));
                 if (hit && place < n) put(place, bar, uint32_t(k) * uint32_t(a.V) + uint32_t(t));
                 found += all;
                 __syncthreads();

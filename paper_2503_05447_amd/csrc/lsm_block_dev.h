@@ -35,6 +35,9 @@ __device__ __forceinline__ u32x4 pack(const float (&x)[4]) {
     return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
 }
 
+// lanes set in a ballot (HIP's own returns an unsigned number)
+__device__ __forceinline__ int lanes(unsigned long long mask) { return __builtin_popcountll(mask); }
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
     return __uint_as_float(__builtin_amdgcn_mov_dpp(int(__float_as_uint(x)), CTRL, 0xf, 0xf, true));

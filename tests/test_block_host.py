@@ -99,3 +99,31 @@ def test_reordering_states_refuses_bad_arguments():
     assert reorder(B=0) == SHAPE and reorder(B=65536) == SHAPE and reorder(K=0) == SHAPE and reorder(K=33) == UNSUP
     assert reorder(size=(64, 0)) == SHAPE and reorder(size=(64, 6)) == SHAPE
     assert reorder(at=(0x1000, 0x2004)) == ALIGN and reorder(parent=0x3004) == ALIGN
+
+
+def moe_params(size=None, **kw):
+    c = dict(n=4, D=64, F=32, E=8, top_k=2, dtype=1, renormalise=1)
+    c.update(kw)
+    return block._MoeParams(ctypes.sizeof(block._MoeParams) if size is None else size, *c.values())
+
+
+def moe(p, x=0x1000, r=0x2000, gu=0x3000, d=0x4000, res=0x5000, y=0x6000, ws=0x10000, wsb=1 << 40):
+    return pkg.library().lsm_moe_step(ctypes.byref(p), vp(x), vp(r), vp(gu), vp(d), vp(res), vp(y), vp(ws), wsb, vp(None))
+
+
+def test_mixture_of_experts_refuses_bad_arguments():
+    P = moe_params
+    need = pkg.library().lsm_moe_step_workspace_bytes
+    assert pkg.library().lsm_moe_step(None, *[vp(None)] * 7, 0, vp(None)) == NULL
+    for bad in (dict(n=0), dict(D=0), dict(F=0), dict(E=0), dict(top_k=0), dict(top_k=9), dict(size=4)):
+        assert moe(P(**bad)) == SHAPE, bad
+        assert need(ctypes.byref(P(**bad))) == 0
+    for bad in (dict(n=129), dict(E=257), dict(top_k=17, E=32), dict(D=60), dict(F=36), dict(D=65544), dict(F=65544), dict(dtype=2),
+                dict(renormalise=2)):
+        assert moe(P(**bad)) == UNSUP, bad
+    for n in ("x", "r", "gu", "d", "y"):
+        assert moe(P(), **{n: None}) == NULL, n
+    for n in ("x", "r", "gu", "d", "res", "y", "ws"):
+        assert moe(P(), **{n: 0x1004}) == ALIGN, n
+    assert moe(P(), ws=None) == WS and moe(P(), wsb=need(ctypes.byref(P())) - 1) == WS
+    assert 0 < need(ctypes.byref(P())) < need(ctypes.byref(P(n=8))) < need(ctypes.byref(P(n=8, dtype=0, F=64)))
