@@ -1,19 +1,22 @@
-// A mixture-of-experts layer for a few tokens (include/lsm_block.h), in four launches:
-//   k_moe_router   a workgroup per 16 tokens: router outputs, softmax, the top_k experts of each token
-//   k_moe_gate_up  a workgroup per active expert and 16 hidden features: h = w silu(Wg x) * (Wu x) for the expert's tokens
-//   k_moe_down     a workgroup per active expert and 16 output features: Wd h, one row for each (token, expert) pair
+// A mixture-of-experts layer for a few tokens (include/lsm_block.h), in five launches:
+//   k_moe_router   a workgroup per expert and 16 tokens: router outputs
+//   k_moe_route    a wave per token: softmax, the top_k experts, their weights; a bit per token in each expert's mask
+//   k_moe_gate_up  a workgroup per active expert and tile of hidden features: h = w silu(Wg x) * (Wu x) for the expert's tokens
+//   k_moe_down     a workgroup per active expert and tile of output features: Wd h, one row for each (token, expert) pair
 //   k_moe_sum      y = residual + the sum of a token's rows, in the order of the experts
 //
 // Bound: the active experts' weights, read once from HBM: with a token or two an expert there are a few operations to a byte.
 // A weight matrix is the first operand of 16 x 16 matrix products (its rows are the product's rows; a lane loads 16 bytes of
 // a row straight into the operand's registers, no staging), the expert's tokens are the columns: up to 16 tokens cost what one
-// does.  Four waves share the tile's rows by splitting the contraction and are summed through LDS in a fixed order.
+// does.  What is requested for a step is used a step later, so that a wave always has a request under way.
 #include "lsm_block_dev.h"
 
 namespace lsm {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+typedef unsigned long long u64;
 
 constexpr int kMaxTokens = 128, kMaxExperts = 256, kMaxTop = 16;
 
@@ -31,55 +34,55 @@ __device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, f32x4 c
 struct MoeArgs {
     const void *x, *router, *w_gate_up, *w_down, *residual;
     void* y;
+    float* logits;    // [n][E]
     int* chosen;      // [n][top_k] experts, rising
-    float* weight;    // [n][top_k]
+    f32x2* place;     // [n][E], where chosen: the weight, and (as an int) the place in `chosen`
+    u64* mask;        // [E][2] the tokens of each expert
     void *h, *h_rem;  // [n top_k][F] hidden activations times the expert's weight (bf16: head and remainder)
     float* part;      // [n top_k][D]
     int n, D, F, E, top_k, renormalise;
     bool by_pair;     // fewer (token, expert) pairs than experts: the grid counts pairs
 };
 
-// 16 bytes of row `row` from element k on; 0 beyond the row's K elements
+// Router outputs of 16 tokens for one expert: a thread takes 16 bytes of the expert's row at a time for all the tokens.  (As 16 x 16
+// products by one workgroup for all experts: 22 us where the rows are 4 KiB apart and meet in one channel; this way 4.)
 template <typename TIO>
-__device__ __forceinline__ u32x4 operand(const TIO* m, size_t row, int K, int k) {
-    if (k >= K) return u32x4{0, 0, 0, 0};
-    return *reinterpret_cast<const u32x4*>(m + row * size_t(K) + k);
-}
-
-// Router of 16 tokens: 16 waves take the tiles of 16 experts, several waves a tile splitting the contraction where there are
-// fewer tiles than waves.  Then a wave per token: softmax over the experts, four to a lane, and the top_k by the bits of the
-// top_k-th largest output, found one by one by counting.  Experts of equal output go by index.
-template <typename TIO>
-__global__ __launch_bounds__(1024) void k_moe_router(MoeArgs a) {
-    constexpr int E = kPiece<TIO>, STEP = 4 * E;
-    __shared__ f32x4 part[16][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t0 = int(blockIdx.x) * 16;
-    const int tiles = (a.E + 15) / 16, split = 16 / tiles;
-    {
-        const int tile = wave / split, piece = wave % split;
-        f32x4 c = {0.f, 0.f, 0.f, 0.f};
-        if (tile < tiles) {
-            const int steps = (a.D + STEP - 1) / STEP, per = (steps + split - 1) / split;
-            const size_t er = min(tile * 16 + (lane & 15), a.E - 1), tr = min(t0 + (lane & 15), a.n - 1);
-            const int k0 = E * (lane >> 4);
-            constexpr int U = 4;
-            for (int s = piece * per; s < min(steps, (piece + 1) * per); s += U) {
-                u32x4 wr[U], xr[U];
-                const int last = min(steps, (piece + 1) * per);
-                _Pragma("unroll") for (int u = 0; u < U; ++u) {
-                    const int k = s + u < last ? (s + u) * STEP + k0 : a.D;
-                    wr[u] = operand(static_cast<const TIO*>(a.router), er, a.D, k);
-                    xr[u] = operand(static_cast<const TIO*>(a.x), tr, a.D, k);
-                }
-                _Pragma("unroll") for (int u = 0; u < U; ++u) c = product(wr[u], xr[u], c, TIO());
+__global__ __launch_bounds__(256) void k_moe_router(MoeArgs a) {
+    constexpr int E = kPiece<TIO>;
+    __shared__ float part[4][16];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, e = blockIdx.x, t0 = int(blockIdx.y) * 16, n = min(16, a.n - t0);
+    const TIO* w = static_cast<const TIO*>(a.router) + size_t(e) * a.D;
+    const TIO* x = static_cast<const TIO*>(a.x) + size_t(t0) * a.D;
+    float sum[16];
+    _Pragma("unroll") for (int t = 0; t < 16; ++t) sum[t] = 0.f;
+    for (int k = tid * E; k < a.D; k += 256 * E) {
+        float wr[E];
+        unpack(*reinterpret_cast<const u32x4*>(w + k), wr);
+        _Pragma("unroll") for (int t = 0; t < 16; ++t) {
+            if (t < n) {
+                float xr[E];
+                unpack(*reinterpret_cast<const u32x4*>(x + size_t(t) * a.D + k), xr);
+                _Pragma("unroll") for (int i = 0; i < E; ++i) sum[t] += wr[i] * xr[i];
             }
         }
-        part[wave][lane] = c;
+    }
+    _Pragma("unroll") for (int t = 0; t < 16; ++t) {
+        if (t < n) {
+            sum[t] = group_sum<64>(sum[t]);
+            if (lane == 0) part[wave][t] = sum[t];
+        }
     }
     __syncthreads();
-    const int t = t0 + wave;
+    if (t0 == 0 && tid < 2) a.mask[2 * e + tid] = 0;  // filled by the next kernel
+    if (tid < n) a.logits[size_t(t0 + tid) * a.E + e] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+}
+
+// A wave per token: softmax over the experts, R to a lane, and the top_k by the bits of the top_k-th largest output, found one
+// by one by counting.  Experts of equal output go by index.
+template <int R>
+__global__ __launch_bounds__(256) void k_moe_route(MoeArgs a) {
+    const int lane = threadIdx.x & 63, t = int(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (t >= a.n) return;
-    constexpr int R = kMaxExperts / 64;
     float out[R], p[R];
     uint32_t key[R];
     float m = -__builtin_inff();
@@ -88,8 +91,7 @@ __global__ __launch_bounds__(1024) void k_moe_router(MoeArgs a) {
         out[r] = -__builtin_inff();
         key[r] = 0;
         if (e < a.E) {
-            float s = 0.f;
-            for (int i = 0; i < split; ++i) s += part[(e / 16) * split + i][16 * ((e % 16) / 4) + wave][e % 4];
+            const float s = a.logits[size_t(t) * a.E + e];
             out[r] = s;
             const uint32_t u = __float_as_uint(s + 0.f);
             key[r] = s == s ? u ^ (uint32_t(int(u) >> 31) | 0x80000000u) : 1u;  // not a number: after all numbers
@@ -127,151 +129,198 @@ __global__ __launch_bounds__(1024) void k_moe_router(MoeArgs a) {
     _Pragma("unroll") for (int r = 0; r < R; ++r) {
         const unsigned long long who = __ballot(in[r]);
         if (in[r]) {
-            const int i = place + lanes(who & below);
-            a.chosen[i] = 64 * r + lane;
-            a.weight[i] = p[r] / over;
+            const int i = place + lanes(who & below), e = 64 * r + lane;
+            a.chosen[i] = e;
+            a.place[size_t(t) * a.E + e] = f32x2{p[r] / over, __int_as_float(i)};
+            atomicOr(a.mask + 2 * e + (t >> 6), u64(1) << (t & 63));  // bits: the order of the tokens does not matter
         }
         place += lanes(who);
     }
 }
 
-// The pairs (token * top_k + place) of this workgroup's expert in the order of the tokens; -1: nothing to do for it.
-__device__ __forceinline__ int expert_pairs(const MoeArgs& a, int y, int* pairs, int* counts, int* expert) {
-    constexpr int M = kMaxTokens * kMaxTop / 256;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, total = a.n * a.top_k;
-    const int e = a.by_pair ? a.chosen[y] : y;
-    unsigned long long who[M];
-    _Pragma("unroll") for (int i = 0; i < M; ++i) {
-        const int at = i * 256 + tid;
-        who[i] = __ballot(i * 256 < total && at < total && a.chosen[at < total ? at : 0] == e);
-        if (lane == 0) counts[i * 4 + wave] = lanes(who[i]);
+// The tokens of this workgroup's expert.
+struct Tokens {
+    u64 low, high;
+    int e, m;  // expert and how many; 0: nothing to do here
+    __device__ __forceinline__ explicit Tokens(const MoeArgs& a) {
+        const int y = blockIdx.y;
+        e = a.by_pair ? a.chosen[y] : y;
+        low = a.mask[2 * e];
+        high = a.mask[2 * e + 1];
+        m = lanes(low) + lanes(high);
+        if (a.by_pair && m > 0 && (low ? __builtin_ctzll(low) : 64 + __builtin_ctzll(high)) != y / a.top_k) m = 0;  // an earlier pair has it
     }
-    __syncthreads();
-    int n = 0;
-    _Pragma("unroll") for (int i = 0; i < M; ++i)
-        _Pragma("unroll") for (int w = 0; w < 4; ++w) {
-            if (w == wave && (who[i] >> lane & 1)) pairs[n + lanes(who[i] & ((1ull << lane) - 1))] = i * 256 + tid;
-            n += counts[i * 4 + w];
+    // the i-th of them, i < m: the position of a bit by halves
+    __device__ __forceinline__ int at(int i) const {
+        int n = lanes(low), t = 0;
+        u64 w = low;
+        if (i >= n) { i -= n; w = high; t = 64; }
+        n = lanes(w & 0xffffffffu);
+        uint32_t v = uint32_t(w);
+        if (i >= n) { i -= n; v = uint32_t(w >> 32); t += 32; }
+        _Pragma("unroll") for (int half = 16; half > 0; half /= 2) {
+            n = __builtin_popcount(v & ((1u << half) - 1));
+            if (i >= n) { i -= n; v >>= half; t += half; }
         }
-    __syncthreads();
-    *expert = e;
-    if (n == 0 || (a.by_pair && pairs[0] != y)) return -1;
-    return n;
-}
+        return t;
+    }
+};
 
-constexpr int kSteps = 4;  // steps of the contraction requested at a time
+constexpr int kSteps = 2;  // steps of the contraction in a request
 
-// NG: groups of 16 tokens that an expert may have
-template <typename TIO, int NG>
+// A workgroup of either product takes NT tiles of 16 rows (of the gate and of the factor half each, or all of the down matrix), so
+// that a request of the columns serves them all; its four waves split the contraction and are summed through LDS.
+// NG: groups of 16 columns at a time; an expert with more tokens takes another pass.  PLANES: of the columns (head, remainder).
+template <typename TIO, int NT, int NG, int PLANES>
+struct Product {
+    static constexpr int E = kPiece<TIO>, STEP = 4 * E;
+    f32x4 c[NT][NG];
+    const TIO *w[NT], *col[PLANES][NG];  // this lane's row of each tile and its columns, from the first element that it loads
+    int K, first, last, groups;
+
+    struct Request { u32x4 w[NT][kSteps], x[PLANES][NG][kSteps]; };
+
+    __device__ __forceinline__ void range(int contraction, int wave) {
+        K = contraction;
+        const int steps = (K + STEP - 1) / STEP, per = (steps + 3) / 4;
+        first = wave * per;
+        last = min(steps, first + per);
+    }
+    __device__ __forceinline__ void request(Request& r, int s) const {
+        const int k = s * STEP;
+        if (s + kSteps <= last && k + kSteps * STEP <= K) {
+            _Pragma("unroll") for (int u = 0; u < kSteps; ++u)
+                _Pragma("unroll") for (int n = 0; n < NT; ++n) r.w[n][u] = *reinterpret_cast<const u32x4*>(w[n] + k + u * STEP);
+            _Pragma("unroll") for (int g = 0; g < NG; ++g) {
+                if (g >= groups) break;
+                _Pragma("unroll") for (int u = 0; u < kSteps; ++u)
+                    _Pragma("unroll") for (int n = 0; n < PLANES; ++n)
+                        r.x[n][g][u] = *reinterpret_cast<const u32x4*>(col[n][g] + k + u * STEP);
+            }
+            return;
+        }
+        const int mine = E * int((threadIdx.x & 63) >> 4);  // beyond the end of the contraction: zeros
+        _Pragma("unroll") for (int u = 0; u < kSteps; ++u) {
+            const bool in = s + u < last && k + u * STEP + mine < K;
+            const u32x4 zero = {0, 0, 0, 0};
+            _Pragma("unroll") for (int n = 0; n < NT; ++n) r.w[n][u] = in ? *reinterpret_cast<const u32x4*>(w[n] + k + u * STEP) : zero;
+            _Pragma("unroll") for (int g = 0; g < NG; ++g) {
+                if (g >= groups) break;
+                _Pragma("unroll") for (int n = 0; n < PLANES; ++n)
+                    r.x[n][g][u] = in ? *reinterpret_cast<const u32x4*>(col[n][g] + k + u * STEP) : zero;
+            }
+        }
+    }
+    __device__ __forceinline__ void take(const Request& r) {
+        _Pragma("unroll") for (int g = 0; g < NG; ++g) {
+            if (g >= groups) break;
+            _Pragma("unroll") for (int u = 0; u < kSteps; ++u)
+                _Pragma("unroll") for (int n = 0; n < PLANES; ++n)
+                    _Pragma("unroll") for (int i = 0; i < NT; ++i) c[i][g] = product(r.w[i][u], r.x[n][g][u], c[i][g], TIO());
+        }
+    }
+    __device__ __forceinline__ void walk() {
+        _Pragma("unroll") for (int g = 0; g < NG; ++g)
+            _Pragma("unroll") for (int i = 0; i < NT; ++i) c[i][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (first >= last) return;
+        Request a, b;
+        request(a, first);
+        for (int s = first;;) {
+            s += kSteps;
+            if (s < last) request(b, s);
+            take(a);
+            if (s >= last) break;
+            s += kSteps;
+            if (s < last) request(a, s);
+            take(b);
+            if (s >= last) break;
+        }
+    }
+    __device__ __forceinline__ void join(f32x4 (*part)[NT * NG][64], int wave, int lane, bool again) {
+        if (again) __syncthreads();
+        _Pragma("unroll") for (int g = 0; g < NG; ++g)
+            _Pragma("unroll") for (int i = 0; i < NT; ++i) part[wave][NT * g + i][lane] = c[i][g];
+        __syncthreads();
+    }
+    __device__ __forceinline__ static f32x4 sum(const f32x4 (*part)[NT * NG][64], int i, int g, int lane) {
+        const int at = NT * g + i;
+        return (part[0][at][lane] + part[1][at][lane]) + (part[2][at][lane] + part[3][at][lane]);
+    }
+};
+
+template <typename TIO, int NT, int NG>
 __global__ __launch_bounds__(256) void k_moe_gate_up(MoeArgs a) {
-    constexpr int E = kPiece<TIO>, STEP = 4 * E;
-    __shared__ int pairs[kMaxTokens], counts[kMaxTokens * kMaxTop / 64];
-    __shared__ f32x4 part[4][2 * NG][64];
-    int e;
-    const int m = expert_pairs(a, blockIdx.y, pairs, counts, &e);
-    if (m < 0) return;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, groups = (m + 15) / 16;
-    const int f0 = int(blockIdx.x) * 16;
-    const size_t row = size_t(e) * 2 * a.F + min(f0 + (lane & 15), a.F - 1);
-    const TIO* w = static_cast<const TIO*>(a.w_gate_up);
-    const TIO* x = static_cast<const TIO*>(a.x);
-    size_t token[NG];
-    _Pragma("unroll") for (int g = 0; g < NG; ++g) token[g] = pairs[min(g * 16 + (lane & 15), m - 1)] / a.top_k;
-    f32x4 c[2][NG];
-    _Pragma("unroll") for (int g = 0; g < NG; ++g) c[0][g] = c[1][g] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int steps = (a.D + STEP - 1) / STEP, per = (steps + 3) / 4, last = min(steps, (wave + 1) * per);
-    for (int s = wave * per; s < last; s += kSteps) {
-        u32x4 wr[2][kSteps];
-        int k[kSteps];
-        _Pragma("unroll") for (int u = 0; u < kSteps; ++u) {
-            k[u] = s + u < last ? (s + u) * STEP + E * (lane >> 4) : a.D;
-            wr[0][u] = operand(w, row, a.D, k[u]);
-            wr[1][u] = operand(w, row + a.F, a.D, k[u]);
-        }
+    constexpr int HT = NT / 2;  // tiles of the gate, and of the factor
+    __shared__ f32x4 part[4][NT * NG][64];
+    const Tokens tok(a);
+    if (tok.m == 0) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    typedef Product<TIO, NT, NG, 1> P;
+    P p;
+    p.range(a.D, wave);
+    const int row0 = int(blockIdx.x) * 16 * HT, mine = P::E * (lane >> 4);
+    _Pragma("unroll") for (int i = 0; i < HT; ++i) {
+        p.w[i] = static_cast<const TIO*>(a.w_gate_up) + (size_t(tok.e) * 2 * a.F + min(row0 + 16 * i + (lane & 15), a.F - 1)) * a.D + mine;
+        p.w[HT + i] = p.w[i] + size_t(a.F) * a.D;
+    }
+    for (int i0 = 0; i0 < tok.m; i0 += 16 * NG) {
+        p.groups = min(NG, (tok.m - i0 + 15) / 16);
+        int token[NG];
         _Pragma("unroll") for (int g = 0; g < NG; ++g) {
-            if (g >= groups) break;
-            u32x4 xr[kSteps];
-            _Pragma("unroll") for (int u = 0; u < kSteps; ++u) xr[u] = operand(x, token[g], a.D, k[u]);
-            _Pragma("unroll") for (int u = 0; u < kSteps; ++u) {
-                c[0][g] = product(wr[0][u], xr[u], c[0][g], TIO());
-                c[1][g] = product(wr[1][u], xr[u], c[1][g], TIO());
-            }
+            token[g] = tok.at(min(i0 + g * 16 + (lane & 15), tok.m - 1));
+            p.col[0][g] = static_cast<const TIO*>(a.x) + size_t(token[g]) * a.D + mine;
         }
-    }
-    _Pragma("unroll") for (int g = 0; g < NG; ++g) {
-        part[wave][2 * g][lane] = c[0][g];
-        part[wave][2 * g + 1][lane] = c[1][g];
-    }
-    __syncthreads();
-    const int f = f0 + 4 * (lane >> 4);  // F is a multiple of 8: the four features of a lane are all there or none
-    for (int g = wave; g < groups; g += 4) {
-        const int i = g * 16 + (lane & 15);
-        if (i >= m || f >= a.F) continue;
-        f32x4 s[2];
-        _Pragma("unroll") for (int n = 0; n < 2; ++n)
-            s[n] = (part[0][2 * g + n][lane] + part[1][2 * g + n][lane]) + (part[2][2 * g + n][lane] + part[3][2 * g + n][lane]);
-        const int pair = pairs[i];
-        const float p = a.weight[pair];
-        float h[4];
-        _Pragma("unroll") for (int j = 0; j < 4; ++j) h[j] = p * (s[0][j] / (1.f + expf(-s[0][j])) * s[1][j]);
-        const size_t at = size_t(pair) * a.F + f;
-        if (sizeof(TIO) == 4) {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(a.h) + at) = f32x4{h[0], h[1], h[2], h[3]};
-        } else {
-            const u32x2 hi = {pack2(h[0], h[1]), pack2(h[2], h[3])};
-            *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.h) + at) = hi;
-            *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.h_rem) + at) =
-                u32x2{pack2(h[0] - bf16_lo(hi.x), h[1] - bf16_hi(hi.x)), pack2(h[2] - bf16_lo(hi.y), h[3] - bf16_hi(hi.y))};
+        p.walk();
+        p.join(part, wave, lane, i0 > 0);
+        _Pragma("unroll") for (int u = 0; u < NG * HT; ++u) {
+            const int g = u / HT, i = u % HT, f = row0 + 16 * i + 4 * (lane >> 4);  // F is a multiple of 8: a lane's four are all there or none
+            if (g >= p.groups || u % 4 != wave || i0 + g * 16 + (lane & 15) >= tok.m || f >= a.F) continue;
+            const f32x4 gate = P::sum(part, i, g, lane), up = P::sum(part, HT + i, g, lane);
+            const f32x2 to = a.place[size_t(token[g]) * a.E + tok.e];
+            float h[4];
+            _Pragma("unroll") for (int j = 0; j < 4; ++j) h[j] = to.x * (gate[j] / (1.f + expf(-gate[j])) * up[j]);
+            const size_t at = size_t(__float_as_int(to.y)) * a.F + f;
+            if (sizeof(TIO) == 4) {
+                *reinterpret_cast<f32x4*>(static_cast<float*>(a.h) + at) = f32x4{h[0], h[1], h[2], h[3]};
+            } else {
+                const u32x2 hi = {pack2(h[0], h[1]), pack2(h[2], h[3])};
+                *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.h) + at) = hi;
+                *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.h_rem) + at) =
+                    u32x2{pack2(h[0] - bf16_lo(hi.x), h[1] - bf16_hi(hi.x)), pack2(h[2] - bf16_lo(hi.y), h[3] - bf16_hi(hi.y))};
+            }
         }
     }
 }
 
-template <typename TIO, int NG>
+template <typename TIO, int NT, int NG>
 __global__ __launch_bounds__(256) void k_moe_down(MoeArgs a) {
-    constexpr int E = kPiece<TIO>, STEP = 4 * E;
-    constexpr bool REM = sizeof(TIO) == 2;
-    __shared__ int pairs[kMaxTokens], counts[kMaxTokens * kMaxTop / 64];
-    __shared__ f32x4 part[4][NG][64];
-    int e;
-    const int m = expert_pairs(a, blockIdx.y, pairs, counts, &e);
-    if (m < 0) return;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, groups = (m + 15) / 16;
-    const int d0 = int(blockIdx.x) * 16;
-    const size_t row = size_t(e) * a.D + min(d0 + (lane & 15), a.D - 1);
-    const TIO* w = static_cast<const TIO*>(a.w_down);
-    size_t pair[NG];
-    _Pragma("unroll") for (int g = 0; g < NG; ++g) pair[g] = pairs[min(g * 16 + (lane & 15), m - 1)];
-    f32x4 c[NG];
-    _Pragma("unroll") for (int g = 0; g < NG; ++g) c[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int steps = (a.F + STEP - 1) / STEP, per = (steps + 3) / 4, last = min(steps, (wave + 1) * per);
-    for (int s = wave * per; s < last; s += kSteps) {
-        u32x4 wr[kSteps];
-        int k[kSteps];
-        _Pragma("unroll") for (int u = 0; u < kSteps; ++u) {
-            k[u] = s + u < last ? (s + u) * STEP + E * (lane >> 4) : a.F;
-            wr[u] = operand(w, row, a.F, k[u]);
-        }
+    __shared__ f32x4 part[4][NT * NG][64];
+    const Tokens tok(a);
+    if (tok.m == 0) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    constexpr int PLANES = sizeof(TIO) == 2 ? 2 : 1;
+    typedef Product<TIO, NT, NG, PLANES> P;
+    P p;
+    p.range(a.F, wave);
+    const int row0 = int(blockIdx.x) * 16 * NT, mine = P::E * (lane >> 4);
+    _Pragma("unroll") for (int i = 0; i < NT; ++i)
+        p.w[i] = static_cast<const TIO*>(a.w_down) + (size_t(tok.e) * a.D + min(row0 + 16 * i + (lane & 15), a.D - 1)) * a.F + mine;
+    for (int i0 = 0; i0 < tok.m; i0 += 16 * NG) {
+        p.groups = min(NG, (tok.m - i0 + 15) / 16);
+        int pair[NG];
         _Pragma("unroll") for (int g = 0; g < NG; ++g) {
-            if (g >= groups) break;
-            u32x4 hr[kSteps], rr[kSteps];
-            _Pragma("unroll") for (int u = 0; u < kSteps; ++u) {
-                hr[u] = operand(static_cast<const TIO*>(a.h), pair[g], a.F, k[u]);
-                if (REM) rr[u] = operand(static_cast<const TIO*>(a.h_rem), pair[g], a.F, k[u]);
-            }
-            _Pragma("unroll") for (int u = 0; u < kSteps; ++u) {
-                c[g] = product(wr[u], hr[u], c[g], TIO());
-                if (REM) c[g] = product(wr[u], rr[u], c[g], TIO());
-            }
+            const int token = tok.at(min(i0 + g * 16 + (lane & 15), tok.m - 1));
+            pair[g] = __float_as_int(a.place[size_t(token) * a.E + tok.e].y);
+            p.col[0][g] = static_cast<const TIO*>(a.h) + size_t(pair[g]) * a.F + mine;
+            if (PLANES == 2) p.col[PLANES - 1][g] = static_cast<const TIO*>(a.h_rem) + size_t(pair[g]) * a.F + mine;
         }
-    }
-    _Pragma("unroll") for (int g = 0; g < NG; ++g) part[wave][g][lane] = c[g];
-    __syncthreads();
-    const int d = d0 + 4 * (lane >> 4);
-    for (int g = wave; g < groups; g += 4) {
-        const int i = g * 16 + (lane & 15);
-        if (i >= m || d >= a.D) continue;
-        *reinterpret_cast<f32x4*>(a.part + size_t(pairs[i]) * a.D + d) =
-            (part[0][g][lane] + part[1][g][lane]) + (part[2][g][lane] + part[3][g][lane]);
+        p.walk();
+        p.join(part, wave, lane, i0 > 0);
+        _Pragma("unroll") for (int u = 0; u < NG * NT; ++u) {
+            const int g = u / NT, i = u % NT, d = row0 + 16 * i + 4 * (lane >> 4);
+            if (g >= p.groups || u % 4 != wave || i0 + g * 16 + (lane & 15) >= tok.m || d >= a.D) continue;
+            *reinterpret_cast<f32x4*>(a.part + size_t(pair[g]) * a.D + d) = P::sum(part, i, g, lane);
+        }
     }
 }
 
@@ -304,38 +353,49 @@ int check(const lsm_moe_params* p) {
     if (p->renormalise != 0 && p->renormalise != 1) return LSM_ERR_UNSUPPORTED;
     return LSM_OK;
 }
-struct MoeSpace { size_t chosen, weight, h, h_rem, part, bytes; };
+struct MoeSpace { size_t logits, chosen, place, mask, h, h_rem, part, bytes; };
 MoeSpace space(const lsm_moe_params& p) {
     const size_t pairs = size_t(p.n) * p.top_k, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4;
     MoeSpace s{};
-    s.chosen = 0;
-    s.weight = align256(pairs * 4);
-    s.h = s.weight + align256(pairs * 4);
+    s.logits = 0;
+    s.chosen = s.logits + align256(size_t(p.n) * p.E * 4);
+    s.place = s.chosen + align256(pairs * 4);
+    s.mask = s.place + align256(size_t(p.n) * p.E * sizeof(f32x2));
+    s.h = s.mask + align256(size_t(p.E) * 2 * sizeof(u64));
     s.h_rem = s.h + align256(pairs * p.F * el);
     s.part = s.h_rem + (el == 2 ? align256(pairs * p.F * el) : 0);
     s.bytes = s.part + align256(pairs * p.D * 4);
     return s;
 }
-template <typename TIO, int NG>
+template <typename TIO, int NT, int NG>
 void launch_experts(const MoeArgs& a, hipStream_t st) {
     const int y = a.by_pair ? a.n * a.top_k : a.E;
     {
         ProfScope ps(KID_MOE_GATE_UP, st);
-        hipLaunchKernelGGL((k_moe_gate_up<TIO, NG>), dim3((a.F + 15) / 16, y), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG>), dim3((a.F + 8 * NT - 1) / (8 * NT), y), dim3(256), 0, st, a);
     }
     ProfScope ps(KID_MOE_DOWN, st);
-    hipLaunchKernelGGL((k_moe_down<TIO, NG>), dim3((a.D + 15) / 16, y), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_moe_down<TIO, NT, NG>), dim3((a.D + 16 * NT - 1) / (16 * NT), y), dim3(256), 0, st, a);
 }
 template <typename TIO>
 void launch(const MoeArgs& a, hipStream_t st) {
     {
         ProfScope ps(KID_MOE_ROUTER, st);
-        hipLaunchKernelGGL((k_moe_router<TIO>), dim3((a.n + 15) / 16), dim3(1024), 0, st, a);
+        hipLaunchKernelGGL((k_moe_router<TIO>), dim3(a.E, (a.n + 15) / 16), dim3(256), 0, st, a);
     }
-    if (a.n <= 16) launch_experts<TIO, 1>(a, st);
-    else if (a.n <= 32) launch_experts<TIO, 2>(a, st);
-    else if (a.n <= 64) launch_experts<TIO, 4>(a, st);
-    else launch_experts<TIO, 8>(a, st);
+    {
+        ProfScope ps(KID_MOE_ROUTER, st);
+        if (a.E <= 64) hipLaunchKernelGGL((k_moe_route<1>), dim3((a.n + 3) / 4), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_moe_route<kMaxExperts / 64>), dim3((a.n + 3) / 4), dim3(256), 0, st, a);
+    }
+    // Columns: as many groups of 16 as an expert has tokens, give or take the spread of chance (more take another pass; with
+    // groups that are rarely used the registers would be missing: 128 tokens, 12 an expert: 4 groups 296 us, 2 groups 259).
+    // Tiles: four where columns are half full, so that they are requested half as often (the same case 277 -> 259 us); two
+    // where an expert has a token or two and the number of workgroups counts (16 tokens 167 -> 162, one token 28 -> 25).
+    const float mean = float(a.n) * a.top_k / a.E, most = mean + 2.f * sqrtf(mean);
+    if (a.n <= 16) mean < 8.f ? launch_experts<TIO, 2, 1>(a, st) : launch_experts<TIO, 4, 1>(a, st);
+    else if (a.n <= 32 || most <= 32.f) mean < 8.f ? launch_experts<TIO, 2, 2>(a, st) : launch_experts<TIO, 4, 2>(a, st);
+    else launch_experts<TIO, 4, 4>(a, st);
     ProfScope ps(KID_MOE_SUM, st);
     hipLaunchKernelGGL((k_moe_sum<TIO>), dim3(unsigned((size_t(a.n) * a.D / 4 + 255) / 256)), dim3(256), 0, st, a);
 }
@@ -362,9 +422,10 @@ int lsm_moe_step(const lsm_moe_params* p, const void* x, const void* router, con
     const MoeSpace s = space(*p);
     if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
-    const MoeArgs a{x, router, w_gate_up, w_down, residual, y, reinterpret_cast<int*>(ws + s.chosen),
-                    reinterpret_cast<float*>(ws + s.weight), ws + s.h, ws + s.h_rem, reinterpret_cast<float*>(ws + s.part),
-                    p->n, p->D, p->F, p->E, p->top_k, p->renormalise, p->n * p->top_k < p->E};
+    const MoeArgs a{x, router, w_gate_up, w_down, residual, y, reinterpret_cast<float*>(ws + s.logits),
+                    reinterpret_cast<int*>(ws + s.chosen), reinterpret_cast<f32x2*>(ws + s.place), reinterpret_cast<u64*>(ws + s.mask),
+                    ws + s.h, ws + s.h_rem, reinterpret_cast<float*>(ws + s.part), p->n, p->D, p->F, p->E, p->top_k, p->renormalise,
+                    p->n * p->top_k < p->E};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (p->dtype == LSM_DTYPE_BF16) launch<uint16_t>(a, st);
     else launch<float>(a, st);
