@@ -111,7 +111,7 @@ int lsm_moe_step(const lsm_moe_params* p, const void* x, const void* router, con
 
 typedef struct {
     uint32_t struct_size; /* = sizeof(lsm_beam_params)                                                       */
-    int32_t  B, K, V;     /* sequences, beams of each (at most 32), vocabulary; K * V at most 2^30             */
+    int32_t  B, K, V;     /* sequences, beams of each (at most 32), vocabulary; K * V at most 2^25             */
     int32_t  n_out;       /* candidates wanted of each sequence: 1..32, at most K * V                        */
     int32_t  dtype;       /* lsm_dtype of the logits                                                         */
     int32_t  eos;         /* the token that ends a beam, or -1                                               */
@@ -123,7 +123,7 @@ typedef struct {
  * The n_out best candidates (beam k, token t) of every sequence by
  *     score(k, t) = scores[k] + ((x_t - m) - log(sum_t exp(x_t - m))) ,   m = max_t x_t ,   x = logits of beam k,
  * in fp32; a finished beam offers (k, eos) at scores[k] and nothing else (its logits are not read).
- *   logits     [B, K, V] dtype, rows row_stride apart                                                      in
+ *   logits     [B, K, V] dtype, rows row_stride apart (what lies between them is read but not used)             in
  *   scores     [B, K] fp32: the beams' log-probabilities so far (-inf: no such beam)                        in
  *   finished   [B, K] bytes (0 or not), or NULL; needs eos >= 0                                             in
  *   out_scores, parent, token   [B, n_out] fp32, int32, int32                                              out

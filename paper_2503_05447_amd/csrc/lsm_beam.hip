@@ -1,17 +1,19 @@
 // One step of a beam search: the best candidates of beams x vocabulary, and the beams' states rearranged (include/lsm_block.h).
 //
-// Selection is two kernels.  k_beam_slices: a workgroup reads a slice of one beam's logits once, into registers, and leaves the
-// slice's maximum, its sum of exponentials and its n_out + 1 best logits (value descending, token ascending).  k_beam_merge: a
-// workgroup per sequence joins the slices' sums to each beam's log-normaliser, turns the kept logits into scores and takes the
-// n_out best.  Scores fall with the logits of a beam, but not strictly (rounding makes equal scores of close logits), and equal
-// scores go by token: where a slice's last kept score reaches the n_out-th best, dropped ones might be due, and the merge takes
-// the candidates at exactly that score from the logits themselves, in order.
+// Selection is two kernels.  k_beam_slices: a workgroup reads a slice of one beam's logits once and leaves the slice's maximum, its
+// sum of exponentials and its n_out + 1 best logits (value descending, token ascending).  k_beam_merge: a workgroup per sequence
+// joins the slices' sums to each beam's log-normaliser, turns the kept logits into scores and takes the n_out best.  Scores fall
+// with the logits of a beam, but not strictly (rounding makes equal scores of close logits), and equal scores go by token: where a
+// slice's last kept score reaches the n_out-th best, dropped ones might be due, and the merge takes the candidates at exactly
+// that score from the logits themselves, in order.
 //
-// To find the best n of what a wave holds without sorting it: the n-th largest of its 64 lanes' maxima bounds the n-th best from
-// below; its upper bits come from counting lanes above a trial value, bit by bit (a comparison and a population count
-// each).  Few elements reach the bound; they are collected in LDS and ranked by counting.
+// To find the best n of what a workgroup holds without sorting it: the n-th largest of its lanes' maxima bounds the n-th best from
+// below; its bits come one by one from counting the maxima above a trial value (a comparison and a population count each).  Few
+// elements reach the bound; they are collected in LDS and ranked by counting.  The merge does the same with the slices' lists: the
+// n-th largest of their first entries, say, is a bound.
 //
-// Bound: HBM (the logits once) for large batches; a latency of two launches for small ones.
+// Bound: HBM (the logits once) for large batches, with the instructions for an exponential a logit close behind; the latency of
+// two launches for small ones.
 #include "lsm_block_dev.h"
 
 namespace lsm {
@@ -19,11 +21,12 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr float kInf = __builtin_inff();
+constexpr float kInf = __builtin_inff(), kLog2E = 1.44269504f;
 constexpr float kLargest = 3.402823466e38f;
 template <typename TIO> constexpr float kLargestOf = sizeof(TIO) == 4 ? kLargest : 3.389531390e38f;  // finite, of the logits' type
 constexpr int kMaxOut = 32;      // n_out and K
-constexpr int kSliceList = 1024; // candidates of a slice that are ranked at once
+constexpr int kWaveList = 512;   // a wave's candidates
+constexpr int kPieces = 4;       // 16-byte pieces that a lane holds: tiles of 8192 logits, in fp32 4096
 
 // unsigned numbers in the order of the floats (no NaN); -0 counts as 0
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -55,6 +58,18 @@ __device__ __forceinline__ float wave_max(float x) {
     return fmaxf(x, __shfl_xor(x, 32, 64));
 }
 
+// how many of a list's n keys are above x; eight are on their way at a time
+__device__ __forceinline__ int rank_in(const u64* list, int n, u64 x) {
+    int rank = 0, k = 0;
+    for (; k + 8 <= n; k += 8) {
+        u64 y[8];
+        _Pragma("unroll") for (int i = 0; i < 8; ++i) y[i] = list[k + i];
+        _Pragma("unroll") for (int i = 0; i < 8; ++i) rank += y[i] > x ? 1 : 0;
+    }
+    for (; k < n; ++k) rank += list[k] > x ? 1 : 0;
+    return rank;
+}
+
 struct BeamArgs {
     const char* logits;
     const float* scores;
@@ -65,172 +80,262 @@ struct BeamArgs {
     f32x2* sums;      // [B K][slices] maximum and sum of exponentials
     u64* kept;        // [B K][slices][n_out + 1] keys of logits, descending; 0 = none
     int64_t row_bytes;
-    int K, V, n_out, eos, slices, bf16, per_slice;
+    int rows, K, V, n_out, eos, bf16, slices, tiles, row_tiles;  // tiles of a slice and of a row
 };
 
 // The pieces of 16 bytes that a beam's logits lie in, counted from the one with its first logit; `lead` elements of that one
 // come before it.  Elements that are not the beam's read as -inf, which is never kept and adds nothing to a sum.
 template <typename TIO>
 struct Row {
+    static constexpr int E = kPiece<TIO>;
     const char* p;
     int lead, end;
+    bool tail;  // nothing may be read behind this row's last logit
     __device__ __forceinline__ Row(const BeamArgs& a, int row) {
         const char* x = a.logits + row * a.row_bytes;
         lead = int(reinterpret_cast<uintptr_t>(x) & 15u) / int(sizeof(TIO));
         p = x - lead * int(sizeof(TIO));
         end = lead + a.V;
+        tail = row == a.rows - 1;
     }
-    __device__ __forceinline__ u32x4 piece(int at) const {  // at: its first element, a multiple of kPiece<TIO>
-        constexpr int E = kPiece<TIO>;
-        if (at >= lead && at + E <= end) return *reinterpret_cast<const u32x4*>(p + size_t(at) * sizeof(TIO));
-        u32x4 v;
+    // `at`: a piece's first element, a multiple of E
+    __device__ __forceinline__ u32x4 whole(int at) const { return *reinterpret_cast<const u32x4*>(p + size_t(at) * sizeof(TIO)); }
+    __device__ __forceinline__ u32x4 part(int at) const {
+        constexpr uint32_t none = sizeof(TIO) == 4 ? 0xff800000u : 0xff80ff80u;
+        u32x4 v = {none, none, none, none};
+        if (at >= end) return v;
+        if (at + E <= end || !tail) {
+            v = whole(at);
+        } else {
+            TIO e[E];
+            _Pragma("unroll") for (int i = 0; i < E; ++i) e[i] = reinterpret_cast<const TIO*>(p)[min(at + i, end - 1)];
+            __builtin_memcpy(&v, e, 16);
+        }
         _Pragma("unroll") for (int i = 0; i < 4; ++i) {
             if (sizeof(TIO) == 4) {
-                v[i] = at + i >= lead && at + i < end ? reinterpret_cast<const uint32_t*>(p)[at + i] : 0xff800000u;
+                if (at + i < lead || at + i >= end) v[i] = none;
             } else {
-                uint32_t w = 0;
-                _Pragma("unroll") for (int j = 0; j < 2; ++j) {
-                    const int e = at + 2 * i + j;
-                    w |= (e >= lead && e < end ? uint32_t(reinterpret_cast<const uint16_t*>(p)[e]) : 0xff80u) << (16 * j);
-                }
-                v[i] = w;
+                const int e = at + 2 * i;
+                if (e < lead || e >= end) v[i] = (v[i] & 0xffff0000u) | 0xff80u;
+                if (e + 1 < lead || e + 1 >= end) v[i] = (v[i] & 0xffffu) | 0xff800000u;
             }
         }
         return v;
     }
 };
 
-// A workgroup's list of candidates; `count` goes on beyond its end.
-template <int CAP>
-__device__ __forceinline__ void append(u64* list, int* count, u64 key) {
-    const int at = atomicAdd(count, 1);
-    if (at < CAP) list[at] = key;
+// The k-th largest of the values that a wave's lanes hold, W each, or something a little below it: of fp32 the upper 16 bits do,
+// unless many lanes share them (bf16 has no others).
+template <typename TIO, int W>
+__device__ __forceinline__ uint32_t kth_largest(const uint32_t (&v)[W], int k) {
+    auto above = [&](uint32_t x) {
+        int c = 0;
+        _Pragma("unroll") for (int i = 0; i < W; ++i) c += lanes(__ballot(v[i] >= x));
+        return c;
+    };
+    uint32_t bound = 0;
+    _Pragma("unroll") for (int bit = 31; bit >= 16; --bit)
+        if (above(bound | (1u << bit)) >= k) bound |= 1u << bit;
+    if (sizeof(TIO) == 2) return bound | (bound & 0x80000000u ? 0u : 0xffffu);
+    if (above(bound) > 2 * k)
+        for (int bit = 15; bit >= 0; --bit)
+            if (above(bound | (1u << bit)) >= k) bound |= 1u << bit;
+    return bound;
 }
 
-template <typename TIO, int NP>
+template <typename TIO>
 __global__ __launch_bounds__(256) void k_beam_slices(BeamArgs a) {
-    constexpr int E = kPiece<TIO>;
-    __shared__ u64 list[kSliceList];
+    constexpr int E = kPiece<TIO>, NP = kPieces, TILE = 256 * E * NP;
+    __shared__ u64 list[4][kWaveList];
+    __shared__ uint32_t lane_top[256], wave_bound[4];
     __shared__ f32x2 wave_sum[4];
-    __shared__ uint32_t wave_bound[4];
+    __shared__ int wave_count[4];
     __shared__ u64 wave_best[4];
-    __shared__ int count;
     const int row = int(blockIdx.x) / a.slices, slice = int(blockIdx.x) - row * a.slices;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, keep = a.n_out + 1;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, keep = a.n_out + 1, quarter = (keep + 3) / 4;
+    const u64 below = (u64(1) << lane) - 1;
     if (a.finished && a.finished[row]) return;
-    if (tid == 0) count = 0;
     const Row<TIO> r(a, row);
-    const int at0 = (slice * NP * 256 + tid) * E;  // this lane's pieces are 256 pieces apart
-    u32x4 raw[NP];
-    _Pragma("unroll") for (int j = 0; j < NP; ++j) raw[j] = r.piece(at0 + j * 256 * E);
-
-    float top = -kInf, m = 0.f, s = 0.f;
-    auto normaliser = [&]() {
-        top = -kInf;
-        _Pragma("unroll") for (int j = 0; j < NP; ++j) {
-            float x[E];
-            unpack(raw[j], x);
-            _Pragma("unroll") for (int i = 0; i < E; i += 2) top = max3(top, x[i], x[i + 1]);
+    const int tile0 = slice * a.tiles, tiles = min(a.tiles, a.row_tiles - tile0);
+    auto first_of = [&](int tile, int j) { return tile * TILE + (j * 256 + tid) * E; };  // element of a lane's piece j
+    auto fetch = [&](u32x4 (&raw)[NP], int tile) {
+        if (tile * TILE >= r.lead && (tile + 1) * TILE <= r.end) {
+            _Pragma("unroll") for (int j = 0; j < NP; ++j) raw[j] = r.whole(first_of(tile, j));
+        } else {
+            _Pragma("unroll") for (int j = 0; j < NP; ++j) raw[j] = r.part(first_of(tile, j));
         }
-        m = wave_max(top);
-        const float from = fmaxf(m, -kLargest);
-        s = 0.f;
-        _Pragma("unroll") for (int j = 0; j < NP; ++j) {
-            float x[E];
-            unpack(raw[j], x);
-            _Pragma("unroll") for (int i = 0; i < E; ++i) s += __builtin_amdgcn_exp2f((x[i] - from) * 1.44269504f);
-        }
-        s = group_sum<64>(s);
     };
-    normaliser();
-    if (s != s) {  // a NaN or +inf among the wave's logits (the sum is the same in all lanes)
+    auto make_sane = [&](u32x4 (&raw)[NP]) {
         _Pragma("unroll") for (int j = 0; j < NP; ++j) {
             float x[E];
             unpack(raw[j], x);
             _Pragma("unroll") for (int i = 0; i < E; ++i) x[i] = sane(x[i], kLargestOf<TIO>);
             raw[j] = pack(x);
         }
-        normaliser();
-    }
-    // bound: the keep-th largest lane maximum; in fp32 its upper 16 bits do, unless many lanes share them
-    uint32_t bound = 0;
-    const uint32_t mine = ordered(top);
-    _Pragma("unroll") for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t trial = bound | (1u << bit);
-        if (lanes(__ballot(mine >= trial)) >= keep) bound = trial;
-    }
-    if (sizeof(TIO) == 2) {
-        bound |= bound & 0x80000000u ? 0u : 0xffffu;
-    } else if (lanes(__ballot(mine >= bound)) > 2 * keep) {
-        for (int bit = 15; bit >= 0; --bit) {
-            const uint32_t trial = bound | (1u << bit);
-            if (lanes(__ballot(mine >= trial)) >= keep) bound = trial;
+    };
+    int count = 0;       // candidates of this wave; beyond the list's end they are only counted
+    bool fits = true;
+    f32x2 sums[4];
+    bool not_numbers = false;  // a NaN or +inf among the slice's logits: seen by the sum, and then all of it once more with those replaced
+    for (;;) {
+        float m = -kInf, from = -kLargest, s = 0.f, least = 0.f;
+        float best = -kInf;  // this lane's largest so far
+        int equal = 0;       // elements met at the bound
+        bool in_order = true;
+        for (int t = 0; t < tiles; ++t) {
+            u32x4 raw[NP];
+            fetch(raw, tile0 + t);
+            if (not_numbers) make_sane(raw);
+            float top = -kInf, piece_top[NP];
+            _Pragma("unroll") for (int j = 0; j < NP; ++j) {
+                float x[E];
+                unpack(raw[j], x);
+                piece_top[j] = max3(x[0], x[1], x[2]);
+                _Pragma("unroll") for (int i = 3; i < E; i += 2) piece_top[j] = max3(piece_top[j], x[i], x[i + 1 < E ? i + 1 : i]);
+                top = fmaxf(top, piece_top[j]);
+            }
+            if (__ballot(top > m)) {
+                m = fmaxf(m, wave_max(top));
+                const float to = fmaxf(m, -kLargest);
+                s *= __builtin_amdgcn_exp2f((from - to) * kLog2E);
+                from = to;
+            }
+            _Pragma("unroll") for (int j = 0; j < NP; ++j) {
+                float x[E];
+                unpack(raw[j], x);
+                _Pragma("unroll") for (int i = 0; i < E; ++i) s += __builtin_amdgcn_exp2f((x[i] - from) * kLog2E);
+            }
+            // Bound: of the first tile the keep-th largest of the workgroup's 256 lane maxima.  Later also a value that quarter =
+            // ceil(keep / 4) lanes of each wave have reached so far; the waves' own only rise, so an old one of another wave will do.
+            best = fmaxf(best, top);
+            if (t == 0) {
+                lane_top[tid] = ordered(top);
+                if (lane == 0) wave_bound[wave] = 0;
+                __syncthreads();
+                uint32_t tops[4];
+                _Pragma("unroll") for (int i = 0; i < 4; ++i) tops[i] = lane_top[64 * i + lane];
+                least = from_ordered(max(kth_largest<TIO>(tops, keep), kOrderedNegInf));
+            } else if (__ballot(top > least)) {
+                const uint32_t bests[1] = {ordered(best)};
+                uint32_t all = kth_largest<TIO>(bests, quarter);
+                if (lane == 0) __atomic_store_n(&wave_bound[wave], all, __ATOMIC_RELAXED);
+                _Pragma("unroll") for (int w = 0; w < 4; ++w)
+                    if (w != wave) all = min(all, __atomic_load_n(&wave_bound[w], __ATOMIC_RELAXED));
+                if (all > ordered(least)) {
+                    least = from_ordered(all);
+                    equal = 0;
+                    in_order = false;
+                }
+            }
+            // Elements above the bound, and of those at it the wave's first `keep` (a mask's value may stand in every place).  At the first
+            // tile's bound `keep` have come before those of later tiles; another wave may have met a later bound further on.
+            const bool at_bound = (t == 0 || !in_order) && least > -kInf;
+            _Pragma("unroll") for (int j = 0; j < NP; ++j) {
+                if (__ballot(piece_top[j] >= least) == 0) continue;
+                float x[E];
+                unpack(raw[j], x);
+                const uint32_t token0 = uint32_t(first_of(tile0 + t, j) - r.lead);
+                int same = 0;
+                _Pragma("unroll") for (int i = 0; i < E; ++i) {
+                    const u64 who = __ballot(x[i] > least);
+                    if (who) {
+                        const int at = count + lanes(who & below);
+                        if (x[i] > least && at < kWaveList) list[wave][at] = make_key(x[i], token0 + i);
+                        count += lanes(who);
+                    }
+                }
+                if (!at_bound || equal >= keep) continue;
+                _Pragma("unroll") for (int i = 0; i < E; ++i) same += x[i] == least ? 1 : 0;
+                if (__ballot(same > 0) == 0) continue;
+                int upto = same;
+                _Pragma("unroll") for (int off = 1; off < 64; off <<= 1) {
+                    const int before = __shfl_up(upto, off, 64);
+                    if (lane >= off) upto += before;
+                }
+                int place = equal + upto - same;
+                const int all = __builtin_amdgcn_readlane(upto, 63);
+                _Pragma("unroll") for (int i = 0; i < E; ++i)
+                    if (x[i] == least) {
+                        const int at = count + place - equal;
+                        if (place < keep && at < kWaveList) list[wave][at] = make_key(x[i], token0 + i);
+                        ++place;
+                    }
+                count += min(all, keep - equal);
+                equal += all;
+            }
+            fits = fits && count <= kWaveList;
+            if (fits && count > kWaveList / 2) {  // only the wave's own best go on
+                constexpr int M = kWaveList / 64;
+                u64 key[M];
+                int rank[M];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                _Pragma("unroll") for (int i = 0; i < M; ++i) {
+                    key[i] = 64 * i + lane < count ? list[wave][64 * i + lane] : 0;
+                    rank[i] = 0;
+                }
+                for (int k = 0; k < count; ++k) {
+                    const u64 other = list[wave][k];
+                    _Pragma("unroll") for (int i = 0; i < M; ++i) rank[i] += other > key[i] ? 1 : 0;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                _Pragma("unroll") for (int i = 0; i < M; ++i)
+                    if (key[i] != 0 && rank[i] < keep) list[wave][rank[i]] = key[i];
+                count = keep;
+            }
         }
+        s = group_sum<64>(s);
+        if (lane == 0) {
+            wave_sum[wave] = f32x2{m, s};
+            wave_count[wave] = fits ? count : kWaveList + 1;
+        }
+        __syncthreads();
+        _Pragma("unroll") for (int w = 0; w < 4; ++w) sums[w] = wave_sum[w];
+        const float any = sums[0].y + sums[1].y + sums[2].y + sums[3].y;
+        if (any == any || not_numbers) break;
+        not_numbers = true;
+        count = 0;
+        fits = true;
+        __syncthreads();
     }
-    if (lane == 0) {
-        wave_sum[wave] = f32x2{m, s};
-        wave_bound[wave] = bound;
-    }
-    __syncthreads();
-    bound = max(max(wave_bound[0], wave_bound[1]), max(wave_bound[2], wave_bound[3]));
     if (tid == 0) {
         float all = -kInf, sum = 0.f;
-        _Pragma("unroll") for (int w = 0; w < 4; ++w) all = fmaxf(all, wave_sum[w].x);
+        _Pragma("unroll") for (int w = 0; w < 4; ++w) all = fmaxf(all, sums[w].x);
         if (all > -kInf)
-            _Pragma("unroll") for (int w = 0; w < 4; ++w) sum += wave_sum[w].y * expf(wave_sum[w].x - all);
+            _Pragma("unroll") for (int w = 0; w < 4; ++w) sum += sums[w].y * expf(sums[w].x - all);
         a.sums[blockIdx.x] = f32x2{all, sum};
     }
-    // Elements above the bound, and of those at it the wave's first `keep` (a mask's value may stand in every place).
-    const float least = from_ordered(max(bound, kOrderedNegInf + 1));
-    int equal = 0;
-    _Pragma("unroll") for (int j = 0; j < NP; ++j) {
-        float x[E], best = -kInf;
-        unpack(raw[j], x);
-        _Pragma("unroll") for (int i = 0; i < E; i += 2) best = max3(best, x[i], x[i + 1]);
-        if (__ballot(best >= least) == 0) continue;
-        const uint32_t token0 = uint32_t(at0 + j * 256 * E - r.lead);
-        int same = 0;
-        _Pragma("unroll") for (int i = 0; i < E; ++i) {
-            if (x[i] > least) append<kSliceList>(list, &count, make_key(x[i], token0 + i));
-            same += x[i] == least ? 1 : 0;
-        }
-        if (equal >= keep || __ballot(same > 0) == 0) continue;
-        int upto = same;
-        _Pragma("unroll") for (int off = 1; off < 64; off <<= 1) {
-            const int t = __shfl_up(upto, off, 64);
-            if (lane >= off) upto += t;
-        }
-        int place = equal + upto - same;
-        _Pragma("unroll") for (int i = 0; i < E; ++i)
-            if (x[i] == least) {
-                if (place < keep) append<kSliceList>(list, &count, make_key(x[i], token0 + i));
-                ++place;
-            }
-        equal += __builtin_amdgcn_readlane(upto, 63);
-    }
-    __syncthreads();
     u64* out = a.kept + size_t(blockIdx.x) * keep;
-    const int n = count;
-    if (n <= kSliceList) {
-        for (int i = tid; i < n; i += 256) {
-            const u64 key = list[i];
+    int n = 0;
+    fits = true;
+    _Pragma("unroll") for (int w = 0; w < 4; ++w) {
+        n += wave_count[w];
+        fits = fits && wave_count[w] <= kWaveList;
+    }
+    if (fits) {
+        for (int i = lane; i < count; i += 64) {
+            const u64 key = list[wave][i];
             int rank = 0;
-            for (int k = 0; k < n; ++k) rank += list[k] > key ? 1 : 0;
+            _Pragma("unroll") for (int w = 0; w < 4; ++w) rank += rank_in(list[w], wave_count[w], key);
             if (rank < keep) out[rank] = key;
         }
         for (int i = n + tid; i < keep; i += 256) out[i] = 0;
         return;
     }
-    // More than the list holds above one bound (long runs of neighbours among the largest): the best one by one.
+    // More than a list holds above one bound (whole lanes of the largest): the best one by one, from the logits.
     u64 last = ~u64(0);
     for (int k = 0; k < keep; ++k) {
         u64 best = 0;
-        _Pragma("unroll") for (int j = 0; j < NP; ++j) {
-            float x[E];
-            unpack(raw[j], x);
-            _Pragma("unroll") for (int i = 0; i < E; ++i) {
-                const u64 key = make_key(x[i], uint32_t(at0 + j * 256 * E - r.lead + i));
-                if (x[i] > -kInf && key < last && key > best) best = key;
+        for (int t = 0; t < tiles; ++t) {
+            u32x4 raw[NP];
+            fetch(raw, tile0 + t);
+            if (not_numbers) make_sane(raw);
+            _Pragma("unroll") for (int j = 0; j < NP; ++j) {
+                float x[E];
+                unpack(raw[j], x);
+                _Pragma("unroll") for (int i = 0; i < E; ++i) {
+                    const u64 key = make_key(x[i], uint32_t(first_of(tile0 + t, j) - r.lead + i));
+                    if (x[i] > -kInf && key < last && key > best) best = key;
+                }
             }
         }
         _Pragma("unroll") for (int off = 1; off < 64; off <<= 1) {
@@ -246,32 +351,57 @@ __global__ __launch_bounds__(256) void k_beam_slices(BeamArgs a) {
     }
 }
 
-constexpr int kMergeThreads = 1024, kMergePer = 8, kMergeWaves = kMergeThreads / 64;
+constexpr int kMergeThreads = 512, kMergeWaves = kMergeThreads / 64;
+constexpr int kMergeAhead = 8;    // lists requested at once by a lane
+constexpr int kMaxLists = 4160;   // K * slices, see check()
+constexpr int kFewLists = 256;    // with so many, bounds from up to six depths of the lists
+constexpr int kMergeList = kMaxOut * (kMaxOut + 2);  // candidates that can reach the bound, see there
 
 __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
-    __shared__ u64 list[kMaxOut + kMergeThreads * kMergePer];
-    __shared__ u64 best[kMaxOut];
-    __shared__ u64 wave_bound[kMergeWaves];
+    __shared__ u64 nth_of[kMaxLists], list[kMergeList], best[kMaxOut], the_bound;
     __shared__ float row_max[kMaxOut], row_log[kMaxOut], row_score[kMaxOut];
     __shared__ int row_done[kMaxOut], counts[kMergeWaves], count, hazard;
     const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, K = a.K, n = a.n_out, keep = n + 1;
-    if (tid == 0) { count = 0; hazard = 0; }
+    const int lists = K * a.slices;
+    if (tid == 0) { count = 0; hazard = 0; the_bound = 0; }
+    // What comes from memory is requested first: entries of the lists (see the bound below) and this wave's first lists.  Those of a
+    // finished beam's lists are not written and not used.
+    const int r0 = min(n, (n + lists - 1) / lists);
+    int levels = 1;
+    while (lists <= kFewLists && (r0 << (levels - 1)) < n) ++levels;
+    const u64* kept = a.kept + size_t(b) * lists * keep;
+    auto nth_entry = [&](int i) { return kept[size_t(i % lists) * keep + min(n, r0 << (i / lists)) - 1]; };
+    u64 ahead[kMergeAhead];
+    const u64 my_nth = tid < levels * lists ? nth_entry(tid) : 0;
+    const int at_once = 64 / keep, mine = lane / keep, nth = lane - mine * keep;  // lists that a wave takes at once
+    auto request = [&](int l0) {
+        _Pragma("unroll") for (int j = 0; j < kMergeAhead; ++j) {
+            const int l = l0 + j * kMergeWaves * at_once + mine;
+            ahead[j] = mine < at_once && l < lists ? kept[size_t(l) * keep + nth] : 0;
+        }
+    };
+    request(wave * at_once);
     for (int k = wave; k < K; k += kMergeWaves) {
         const int row = b * K + k;
         const bool done = a.finished && a.finished[row];
+        const float so_far = a.scores[row];
         float m = -kInf, s = 0.f;
         if (!done) {
             const f32x2* p = a.sums + size_t(row) * a.slices;
-            for (int i = lane; i < a.slices; i += 64) m = fmaxf(m, p[i].x);
+            for (int i = lane; i < a.slices; i += 64) {  // joined as they come
+                const f32x2 x = p[i];
+                const float to = fmaxf(m, x.x);
+                if (to > -kInf) s = s * expf(m - to) + x.y * expf(x.x - to);
+                m = to;
+            }
+            const float mine = m;
             m = wave_max(m);
-            if (m > -kInf)
-                for (int i = lane; i < a.slices; i += 64) s += p[i].y * expf(p[i].x - m);
-            s = group_sum<64>(s);
+            s = group_sum<64>(mine > -kInf ? s * expf(mine - m) : 0.f);
         }
         if (lane == 0) {
             row_max[k] = m;
             row_log[k] = logf(s);
-            row_score[k] = a.scores[row];
+            row_score[k] = so_far;
             row_done[k] = done;
         }
     }
@@ -280,53 +410,57 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
         const float y = row_score[k] + ((x - row_max[k]) - row_log[k]);
         return y == y ? y : -kInf;
     };
-    int have = 0;  // best[0 .. have): the best so far, descending
-    if (tid < K && row_done[tid]) {
+    const float inverse = 1.f / float(a.slices);
+    auto row_of = [&](int l) {  // l / slices: below 2^24, so the product is at most one off
+        int k = int(float(l) * inverse);
+        if (k * a.slices > l) --k;
+        if ((k + 1) * a.slices <= l) ++k;
+        return k;
+    };
+    // a kept logit of list l as a key of scores; 0: none
+    auto scored = [&](int l, u64 kept) {
+        const int k = row_of(l);
+        if (kept == 0 || row_done[k]) return u64(0);
+        return make_key(score(k, from_ordered(uint32_t(kept >> 32))), uint32_t(k) * uint32_t(a.V) + key_index(kept));
+    };
+    // Bound: ceil(n / r) lists have their first r entries at or above the ceil(n / r)-th largest of the lists' r-th entries, so this
+    // bounds the n-th best from below; the largest of these over some r does.  (r = 1 alone leaves 800 candidates where the best
+    // beams' lists hold most of them.)  At most n (n + 1) candidates reach it: r = 1: n lists reach it with an entry or more.
+    // r0 > 1: there are fewer than n lists.  (Nothing bounds from below where too few lists have r entries: then there are no more
+    // candidates than that either.)
+    for (int i = tid; i < levels * lists; i += kMergeThreads) nth_of[i] = scored(i % lists, i == tid ? my_nth : nth_entry(i));
+    if (tid < K && row_done[tid]) {  // a finished beam's one candidate
         const float y = row_score[tid];
-        append<kMaxOut>(list, &count, make_key(y == y ? y : -kInf, uint32_t(tid) * uint32_t(a.V) + uint32_t(a.eos)));
+        list[atomicAdd(&count, 1)] = make_key(y == y ? y : -kInf, uint32_t(tid) * uint32_t(a.V) + uint32_t(a.eos));
     }
     __syncthreads();
-    const int per_row = a.slices * keep, total = K * per_row;
-    uint32_t last_kept = 0;  // largest score at which a slice of this thread's stopped keeping
-    for (int base = 0; base == 0 || base < total; base += kMergeThreads * kMergePer) {
-        u64 key[kMergePer], top = 0;
-        _Pragma("unroll") for (int j = 0; j < kMergePer; ++j) {
-            const int i = base + tid + j * kMergeThreads, k = i / per_row;
-            key[j] = 0;
-            if (i >= total || row_done[k]) continue;
-            const u64 kept = a.kept[size_t(b) * total + i];
-            if (kept == 0) continue;
-            key[j] = make_key(score(k, from_ordered(uint32_t(kept >> 32))), uint32_t(k) * uint32_t(a.V) + key_index(kept));
-            top = key[j] > top ? key[j] : top;
-            if (i % keep == n) last_kept = max(last_kept, uint32_t(key[j] >> 32));
-        }
-        // bound: the n-th largest of the lanes' best, down to the last bit only where many lanes share its score
-        u64 bound = 0;
-        for (int bit = 63; bit >= 0; --bit) {
-            const u64 trial = bound | (u64(1) << bit);
-            if (lanes(__ballot(top >= trial)) >= n) bound = trial;
-            if (bit == 32 && lanes(__ballot(top >= bound)) <= 2 * n) break;
-        }
-        if (lane == 0) wave_bound[wave] = bound;
-        __syncthreads();
-        _Pragma("unroll") for (int w = 0; w < kMergeWaves; ++w) bound = wave_bound[w] > bound ? wave_bound[w] : bound;
-        if (bound == 0) bound = 1;
-        _Pragma("unroll") for (int j = 0; j < kMergePer; ++j)
-            if (key[j] >= bound) append<kMaxOut + kMergeThreads * kMergePer>(list, &count, key[j]);
-        __syncthreads();
-        const int c = count;
-        for (int i = tid; i < c; i += kMergeThreads) {
-            const u64 x = list[i];
-            int rank = 0;
-            for (int k = 0; k < c; ++k) rank += list[k] > x ? 1 : 0;
-            if (rank < n) best[rank] = x;
-        }
-        __syncthreads();
-        have = min(c, n);
-        if (tid < have) list[tid] = best[tid];
-        if (tid == 0) count = have;
-        __syncthreads();
+    for (int i = tid; i < levels * lists; i += kMergeThreads) {
+        const int level = i / lists, r = min(n, r0 << level);
+        const u64 x = nth_of[i];
+        // (a list is in the order of its logits: its first r entries reach the r-th one's score, not its key)
+        if (x != 0 && rank_in(nth_of + level * lists, lists, x) == (n + r - 1) / r - 1)
+            atomicMax(&the_bound, r == 1 ? x : x & ~u64(0xffffffffu));
     }
+    __syncthreads();
+    const u64 bound = the_bound;
+    uint32_t last_kept = 0;  // largest score at which a list of this lane's stopped keeping
+    for (int l0 = wave * at_once; l0 < lists; l0 += kMergeAhead * kMergeWaves * at_once) {
+        if (l0 != wave * at_once) request(l0);
+        _Pragma("unroll") for (int j = 0; j < kMergeAhead; ++j) {
+            if (ahead[j] == 0) continue;
+            const u64 key = scored(l0 + j * kMergeWaves * at_once + mine, ahead[j]);
+            if (key != 0 && nth == n) last_kept = max(last_kept, uint32_t(key >> 32));
+            if (key != 0 && key >= bound) list[atomicAdd(&count, 1)] = key;
+        }
+    }
+    __syncthreads();
+    const int c = count, have = min(c, n);
+    for (int i = tid; i < c; i += kMergeThreads) {
+        const u64 x = list[i];
+        const int rank = rank_in(list, c, x);
+        if (rank < n) best[rank] = x;
+    }
+    __syncthreads();
     const uint32_t bar = have == n ? uint32_t(best[n - 1] >> 32) : kOrderedNegInf;
     if (last_kept >= bar || bar <= kOrderedNegInf) hazard = 1;
     __syncthreads();
@@ -353,7 +487,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
             const size_t slot = size_t(b * K + k) * a.slices + s;
             // a slice of the first kernel starts at a whole piece of 16 bytes
             const int lead = int(reinterpret_cast<uintptr_t>(x) & 15u) / (a.bf16 ? 2 : 4);
-            const int t0 = max(s * a.per_slice - lead, 0), t1 = min((s + 1) * a.per_slice - lead, a.V);
+            const int per_slice = a.tiles * 256 * kPieces * (a.bf16 ? 8 : 4);
+            const int t0 = max(s * per_slice - lead, 0), t1 = min((s + 1) * per_slice - lead, a.V);
             if (bar > kOrderedNegInf && row_done[k]) {
                 if (a.eos < t0 || a.eos >= t1) continue;
             } else if (bar > kOrderedNegInf) {
@@ -430,16 +565,18 @@ __global__ __launch_bounds__(256) void k_state_reorder(ReorderArgs a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-constexpr int kFewPieces = 2, kManyPieces = 8;  // 16-byte pieces a lane (in fp32 twice as many): slices of 4096 or 16384 logits
-
-struct BeamPlan { int per_slice, slices; bool many; };
+constexpr int kSlices = 1024, kMaxTiles = 8;
+// Slices of so many tiles that there are a few workgroups for each compute unit, or of one.
+struct BeamPlan { int row_tiles, tiles, slices; };
 BeamPlan plan(const lsm_beam_params& p) {
-    const int piece = p.dtype == LSM_DTYPE_BF16 ? 8 : 4;
-    auto slices = [&](int64_t n) { return int64_t(p.V + piece - 1 + n - 1) / n; };  // a row may start inside a piece
-    const int few = 256 * 8 * kFewPieces, large = 256 * 8 * kManyPieces;
-    const bool many = int64_t(p.B) * p.K * slices(large) >= 512;
-    const int n = many ? large : few;
-    return BeamPlan{n, int(slices(n)), many};
+    const int piece = p.dtype == LSM_DTYPE_BF16 ? 8 : 4, tile = 256 * piece * kPieces;
+    BeamPlan pl{};
+    pl.row_tiles = int((int64_t(p.V) + piece - 1 + tile - 1) / tile);  // a row may start inside a piece
+    const int64_t all = int64_t(p.B) * p.K * pl.row_tiles;
+    pl.tiles = int(all < 2 * kSlices ? 1 : all / kSlices < kMaxTiles ? all / kSlices : kMaxTiles);
+    if (pl.tiles > pl.row_tiles) pl.tiles = pl.row_tiles;
+    pl.slices = (pl.row_tiles + pl.tiles - 1) / pl.tiles;
+    return pl;
 }
 int check(const lsm_beam_params* p) {
     if (!p) return LSM_ERR_NULL;
@@ -448,18 +585,13 @@ int check(const lsm_beam_params* p) {
     if (p->dtype != LSM_DTYPE_F32 && p->dtype != LSM_DTYPE_BF16) return LSM_ERR_UNSUPPORTED;
     if (p->K > kMaxOut || p->n_out > kMaxOut || p->reserved != 0) return LSM_ERR_UNSUPPORTED;
     const int64_t all = int64_t(p->K) * p->V;
-    if (all > (int64_t(1) << 30) || p->n_out > all || p->eos < -1 || p->eos >= p->V) return LSM_ERR_SHAPE;
-    if (p->row_stride > (int64_t(1) << 40) || int64_t(p->B) * p->K * plan(*p).slices > 0x7fffffff) return LSM_ERR_SHAPE;
+    if (all > (int64_t(1) << 25) || p->n_out > all || p->eos < -1 || p->eos >= p->V) return LSM_ERR_SHAPE;
+    // a sequence's lists: one a tile where there are fewer than 2 kSlices tiles, else a fraction of at most 2^25 / 4096 + K tiles
+    static_assert(2 * kSlices <= kMaxLists && ((1 << 25) / 4096 + kMaxOut) / 2 + kMaxOut <= kMaxLists, "lists of a sequence");
+    if (p->row_stride > (int64_t(1) << 40) || int64_t(p->B) * p->K * plan(*p).row_tiles > 0x7fffffff) return LSM_ERR_SHAPE;
     return LSM_OK;
 }
 size_t sums_bytes(const lsm_beam_params& p, const BeamPlan& pl) { return align256(size_t(p.B) * p.K * pl.slices * sizeof(f32x2)); }
-
-template <typename TIO, int F>
-void launch_slices(const BeamArgs& a, bool many, unsigned blocks, hipStream_t st) {
-    ProfScope ps(KID_BEAM_SLICES, st);
-    if (many) hipLaunchKernelGGL((k_beam_slices<TIO, F * kManyPieces>), dim3(blocks), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_beam_slices<TIO, F * kFewPieces>), dim3(blocks), dim3(256), 0, st, a);
-}
 
 }  // namespace
 }  // namespace lsm
@@ -489,11 +621,14 @@ int lsm_beam_select(const lsm_beam_params* p, const void* logits, const float* s
     const bool bf16 = p->dtype == LSM_DTYPE_BF16;
     const BeamArgs a{static_cast<const char*>(logits), scores, finished, out_scores, parent, token, out_finished,
                      static_cast<f32x2*>(workspace), reinterpret_cast<u64*>(static_cast<char*>(workspace) + sums_bytes(*p, pl)),
-                     p->row_stride * (bf16 ? 2 : 4), p->K, p->V, p->n_out, p->eos, pl.slices, bf16, pl.per_slice};
+                     p->row_stride * (bf16 ? 2 : 4), p->B * p->K, p->K, p->V, p->n_out, p->eos, bf16, pl.slices, pl.tiles, pl.row_tiles};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const unsigned blocks = unsigned(p->B) * p->K * pl.slices;
-    if (bf16) launch_slices<uint16_t, 1>(a, pl.many, blocks, st);
-    else launch_slices<float, 2>(a, pl.many, blocks, st);
+    {
+        ProfScope ps(KID_BEAM_SLICES, st);
+        if (bf16) hipLaunchKernelGGL((k_beam_slices<uint16_t>), dim3(blocks), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_beam_slices<float>), dim3(blocks), dim3(256), 0, st, a);
+    }
     {
         ProfScope ps(KID_BEAM_MERGE, st);
         hipLaunchKernelGGL(k_beam_merge, dim3(p->B), dim3(kMergeThreads), 0, st, a);

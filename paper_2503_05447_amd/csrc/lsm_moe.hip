@@ -44,37 +44,44 @@ struct MoeArgs {
     bool by_pair;     // fewer (token, expert) pairs than experts: the grid counts pairs
 };
 
-// Router outputs of 16 tokens for one expert: a thread takes 16 bytes of the expert's row at a time for all the tokens.  (As 16 x 16
-// products by one workgroup for all experts: 22 us where the rows are 4 KiB apart and meet in one channel; this way 4.)
+// Router outputs of 16 tokens for one expert, four tokens a wave: lanes along the row, 16 bytes each, four pieces of the expert's row
+// and of every token's requested at a time.  (As 16 x 16 products by one workgroup for all experts: 22 us at a hidden size of
+// 2048, where the rows are 4 KiB apart and meet in one channel.)
 template <typename TIO>
 __global__ __launch_bounds__(256) void k_moe_router(MoeArgs a) {
-    constexpr int E = kPiece<TIO>;
-    __shared__ float part[4][16];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, e = blockIdx.x, t0 = int(blockIdx.y) * 16, n = min(16, a.n - t0);
+    constexpr int E = kPiece<TIO>, U = 4;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, e = blockIdx.x, t0 = int(blockIdx.y) * 16 + wave;
+    if (blockIdx.y == 0 && threadIdx.x < 2) a.mask[2 * e + threadIdx.x] = 0;  // filled by the next kernel
+    if (t0 >= a.n) return;
     const TIO* w = static_cast<const TIO*>(a.router) + size_t(e) * a.D;
-    const TIO* x = static_cast<const TIO*>(a.x) + size_t(t0) * a.D;
-    float sum[16];
-    _Pragma("unroll") for (int t = 0; t < 16; ++t) sum[t] = 0.f;
-    for (int k = tid * E; k < a.D; k += 256 * E) {
-        float wr[E];
-        unpack(*reinterpret_cast<const u32x4*>(w + k), wr);
-        _Pragma("unroll") for (int t = 0; t < 16; ++t) {
-            if (t < n) {
-                float xr[E];
-                unpack(*reinterpret_cast<const u32x4*>(x + size_t(t) * a.D + k), xr);
-                _Pragma("unroll") for (int i = 0; i < E; ++i) sum[t] += wr[i] * xr[i];
+    const TIO* x[4];
+    float sum[4];
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        x[i] = static_cast<const TIO*>(a.x) + size_t(min(t0 + 4 * i, a.n - 1)) * a.D;
+        sum[i] = 0.f;
+    }
+    for (int k0 = lane * E; k0 < a.D; k0 += U * 64 * E) {
+        u32x4 wr[U], xr[4][U];
+        _Pragma("unroll") for (int u = 0; u < U; ++u) {
+            const int k = min(k0 + u * 64 * E, a.D - E);
+            wr[u] = *reinterpret_cast<const u32x4*>(w + k);
+            _Pragma("unroll") for (int i = 0; i < 4; ++i) xr[i][u] = *reinterpret_cast<const u32x4*>(x[i] + k);
+        }
+        _Pragma("unroll") for (int u = 0; u < U; ++u) {
+            if (k0 + u * 64 * E >= a.D) break;
+            float wf[E];
+            unpack(wr[u], wf);
+            _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+                float xf[E];
+                unpack(xr[i][u], xf);
+                _Pragma("unroll") for (int c = 0; c < E; ++c) sum[i] += wf[c] * xf[c];
             }
         }
     }
-    _Pragma("unroll") for (int t = 0; t < 16; ++t) {
-        if (t < n) {
-            sum[t] = group_sum<64>(sum[t]);
-            if (lane == 0) part[wave][t] = sum[t];
-        }
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        sum[i] = group_sum<64>(sum[i]);
+        if (lane == 0 && t0 + 4 * i < a.n) a.logits[size_t(t0 + 4 * i) * a.E + e] = sum[i];
     }
-    __syncthreads();
-    if (t0 == 0 && tid < 2) a.mask[2 * e + tid] = 0;  // filled by the next kernel
-    if (tid < n) a.logits[size_t(t0 + tid) * a.E + e] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
 }
 
 // A wave per token: softmax over the experts, R to a lane, and the top_k by the bits of the top_k-th largest output, found one

@@ -75,7 +75,7 @@ def test_beam_selection_refuses_bad_arguments():
     need = pkg.library().lsm_beam_select_workspace_bytes
     assert pkg.library().lsm_beam_select(None, *[vp(None)] * 8, 0, vp(None)) == NULL
     for bad in (dict(B=0), dict(K=0), dict(V=0), dict(n_out=0), dict(row_stride=99), dict(K=1, V=3, n_out=4), dict(eos=100), dict(eos=-2),
-                dict(K=32, V=1 << 26), dict(size=4), dict(row_stride=1 << 41), dict(B=1 << 30)):
+                dict(K=32, V=(1 << 20) + 1), dict(size=4), dict(row_stride=1 << 41), dict(B=1 << 30)):
         assert beam(P(**bad)) == SHAPE, bad
         assert need(ctypes.byref(P(**bad))) == 0
     for bad in (dict(dtype=2), dict(K=33), dict(n_out=33), dict(reserved=1)):

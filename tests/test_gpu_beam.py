@@ -54,6 +54,7 @@ def check(logits, scores, n_out=None, finished=None, eos=None):
     got, parent, token, ended = (t if t is None else t.cpu().numpy() for t in select(logits, scores, n_out, finished, eos))
     largest = torch.finfo(logits.dtype).max
     true = true_scores(logits, scores, finished, eos, largest)
+    x = logits.float().cpu().numpy()
     size = 2.0 ** -20 * (1 + np.abs(np.where(np.isfinite(true), true, 0)) + np.abs(scores.double().cpu().numpy()).clip(max=1e30).max() + math.log(V))
     for b in range(B):
         index = parent[b].astype(np.int64) * V + token[b]
@@ -67,6 +68,12 @@ def check(logits, scores, n_out=None, finished=None, eos=None):
         for i in range(n - 1):
             if got[b][i] == got[b][i + 1]:
                 assert index[i] < index[i + 1], "equal scores out of order"
+        # equal logits of a beam have one score: whoever is in, those before it are too
+        for i in np.nonzero(fin)[0]:
+            k, tk = parent[b][i], token[b][i]
+            if finished is None or not finished[b, k]:
+                same = np.nonzero(x[b, k, :tk] == x[b, k, tk])[0]
+                assert set((k * V + same).tolist()) <= set(index.tolist()), "an equal logit before it was left out"
         # nothing left out is better than the last one by more than the rounding
         rest = true[b].copy()
         rest[index] = -INF
@@ -217,6 +224,36 @@ def test_rising_logits(dtype):
     big[0, 0, lanes] = (100 + torch.rand(int(lanes.sum()), device="cuda", generator=torch.Generator("cuda").manual_seed(1)) * 50).to(dt)
     check(big, torch.zeros(1, 1, device="cuda"), 32)
     check(big.expand(600, 1, -1).contiguous()[:, :, :16383], torch.zeros(600, 1, device="cuda"), 32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_slices_of_several_tiles(dtype):
+    """Enough beams for a workgroup to take several tiles of a row: what a later tile holds against the first one's bound."""
+    import torch
+    B, K, V = 64, 8, 40001
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    low = torch.finfo(dt).min
+    at = torch.arange(V, device="cuda")
+    logits, scores = random_case(B, K, V, dtype, 1, seed=12)
+    scores = torch.where(torch.arange(K, device="cuda") == 5, scores + 30, scores).contiguous()   # one beam has nearly all
+    for n in (8, 32):
+        check(logits, scores, n)
+        late = logits.clone()
+        late[:, :, :V // 3] = -INF                                   # nothing in the first tiles
+        check(late, scores, n)
+        late[:, :, V // 3:] = low                                    # ... and the lowest number in all the others
+        late[:, 5, V - 2] = 0
+        check(late, scores, n)
+        late[:, :, 100], late[:, :, 200] = 1, low
+        check(late, scores, n)
+        ties = logits * 0 + (at // 5003 % 3).to(dt)                  # blocks of equal ones, the largest in the third and sixth
+        check(ties, scores, n)
+        ties = logits * 0 - 3
+        ties[:, :, 30000:] = 2                                       # more than a list holds, in later tiles only
+        ties[:, :, 39990:] = 2.5
+        check(ties, scores, n)
+        check((at * 2.0 ** -9).to(dt).expand(B, K, V).contiguous(), scores, n)
+    check(torch.where(torch.rand(B, K, V, device="cuda", generator=torch.Generator("cuda").manual_seed(3)) < 1e-3, logits, -INF), scores, 32)
 
 
 def test_offsets_beyond_32_bits():
