@@ -84,12 +84,11 @@ __global__ __launch_bounds__(256) void k_moe_router(MoeArgs a) {
     }
 }
 
-// A wave per token: softmax over the experts, R to a lane, and the top_k by the bits of the top_k-th largest output, found one
-// by one by counting.  Experts of equal output go by index.
-template <int R>
-__global__ __launch_bounds__(256) void k_moe_route(MoeArgs a) {
-    const int lane = threadIdx.x & 63, t = int(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (t >= a.n) return;
+// The experts of token t, by a wave: softmax over the experts, R to a lane, and the top_k by the bits of the top_k-th largest
+// output, found one by one by counting.  Experts of equal output go by index.  emit(place, expert, weight), places rising with
+// the experts.
+template <int R, typename Emit>
+__device__ __forceinline__ void route(const MoeArgs& a, int t, int lane, Emit emit) {
     float out[R], p[R];
     uint32_t key[R];
     float m = -__builtin_inff();
@@ -132,23 +131,57 @@ __global__ __launch_bounds__(256) void k_moe_route(MoeArgs a) {
     }
     sum = group_sum<64>(sum);
     const float over = all == all ? (a.renormalise ? sum : all) : all;
-    int place = t * a.top_k;
+    int place = 0;
     _Pragma("unroll") for (int r = 0; r < R; ++r) {
         const unsigned long long who = __ballot(in[r]);
-        if (in[r]) {
-            const int i = place + lanes(who & below), e = 64 * r + lane;
-            a.chosen[i] = e;
-            a.place[size_t(t) * a.E + e] = f32x2{p[r] / over, __int_as_float(i)};
-            atomicOr(a.mask + 2 * e + (t >> 6), u64(1) << (t & 63));  // bits: the order of the tokens does not matter
-        }
+        if (in[r]) emit(place + lanes(who & below), 64 * r + lane, p[r] / over);
         place += lanes(who);
     }
+}
+constexpr int kWide = kMaxExperts / 64;
+
+template <int R>
+__global__ __launch_bounds__(256) void k_moe_route(MoeArgs a) {
+    const int lane = threadIdx.x & 63, t = int(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (t >= a.n) return;
+    route<R>(a, t, lane, [&](int i, int e, float w) {
+        a.chosen[t * a.top_k + i] = e;
+        a.place[size_t(t) * a.E + e] = f32x2{w, __int_as_float(t * a.top_k + i)};
+        atomicOr(a.mask + 2 * e + (t >> 6), u64(1) << (t & 63));  // bits: the order of the tokens does not matter
+    });
 }
 
 // The tokens of this workgroup's expert.
 struct Tokens {
     u64 low, high;
     int e, m;  // expert and how many; 0: nothing to do here
+    // For up to four tokens, which every workgroup of the first product routes for itself (a wave per token; a launch less): low is
+    // the set of the expert's pairs.  The first workgroup leaves what the next kernel needs.
+    __device__ __forceinline__ Tokens(const MoeArgs& a, int* chosen, float* weight) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, pairs = a.n * a.top_k;
+        auto emit = [&](int i, int e_, float w) {
+            chosen[wave * a.top_k + i] = e_;
+            weight[wave * a.top_k + i] = w;
+        };
+        if (wave < a.n) a.E <= 64 ? route<1>(a, wave, lane, emit) : route<kWide>(a, wave, lane, emit);
+        __syncthreads();
+        const int mine = lane < pairs ? chosen[lane] : -1;
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < pairs) {
+            u64 mask = 0;
+            for (int i = 0; i < pairs; ++i) mask |= u64(chosen[i] == mine ? 1 : 0) << (i / a.top_k);
+            a.chosen[lane] = mine;
+            a.place[size_t(lane / a.top_k) * a.E + mine] = f32x2{weight[lane], __int_as_float(lane)};
+            a.mask[2 * mine] = mask;
+            a.mask[2 * mine + 1] = 0;
+        }
+        const int y = blockIdx.y;
+        e = __builtin_amdgcn_readfirstlane(chosen[a.by_pair ? y : 0]);
+        if (!a.by_pair) e = y;
+        low = __ballot(mine == e);
+        high = 0;
+        m = lanes(low);
+        if (a.by_pair && __builtin_ctzll(low) != y) m = 0;  // an earlier pair has the expert
+    }
     __device__ __forceinline__ explicit Tokens(const MoeArgs& a) {
         const int y = blockIdx.y;
         e = a.by_pair ? a.chosen[y] : y;
@@ -255,11 +288,14 @@ struct Product {
     }
 };
 
-template <typename TIO, int NT, int NG>
+// ROUTE: at most four tokens, see Tokens
+template <typename TIO, int NT, int NG, bool ROUTE>
 __global__ __launch_bounds__(256) void k_moe_gate_up(MoeArgs a) {
     constexpr int HT = NT / 2;  // tiles of the gate, and of the factor
     __shared__ f32x4 part[4][NT * NG][64];
-    const Tokens tok(a);
+    __shared__ int chosen[ROUTE ? 4 * kMaxTop : 1];
+    __shared__ float weight[ROUTE ? 4 * kMaxTop : 1];
+    Tokens tok = ROUTE ? Tokens(a, chosen, weight) : Tokens(a);
     if (tok.m == 0) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     typedef Product<TIO, NT, NG, 1> P;
@@ -274,8 +310,8 @@ __global__ __launch_bounds__(256) void k_moe_gate_up(MoeArgs a) {
         p.groups = min(NG, (tok.m - i0 + 15) / 16);
         int token[NG];
         _Pragma("unroll") for (int g = 0; g < NG; ++g) {
-            token[g] = tok.at(min(i0 + g * 16 + (lane & 15), tok.m - 1));
-            p.col[0][g] = static_cast<const TIO*>(a.x) + size_t(token[g]) * a.D + mine;
+            token[g] = tok.at(min(i0 + g * 16 + (lane & 15), tok.m - 1));  // with ROUTE the pair
+            p.col[0][g] = static_cast<const TIO*>(a.x) + size_t(ROUTE ? token[g] / a.top_k : token[g]) * a.D + mine;
         }
         p.walk();
         p.join(part, wave, lane, i0 > 0);
@@ -283,7 +319,7 @@ __global__ __launch_bounds__(256) void k_moe_gate_up(MoeArgs a) {
             const int g = u / HT, i = u % HT, f = row0 + 16 * i + 4 * (lane >> 4);  // F is a multiple of 8: a lane's four are all there or none
             if (g >= p.groups || u % 4 != wave || i0 + g * 16 + (lane & 15) >= tok.m || f >= a.F) continue;
             const f32x4 gate = P::sum(part, i, g, lane), up = P::sum(part, HT + i, g, lane);
-            const f32x2 to = a.place[size_t(token[g]) * a.E + tok.e];
+            const f32x2 to = ROUTE ? f32x2{weight[token[g]], __int_as_float(token[g])} : a.place[size_t(token[g]) * a.E + tok.e];
             float h[4];
             _Pragma("unroll") for (int j = 0; j < 4; ++j) h[j] = to.x * (gate[j] / (1.f + expf(-gate[j])) * up[j]);
             const size_t at = size_t(__float_as_int(to.y)) * a.F + f;
@@ -374,15 +410,23 @@ MoeSpace space(const lsm_moe_params& p) {
     s.bytes = s.part + align256(pairs * p.D * 4);
     return s;
 }
+constexpr int kRouteAlong = 4;  // tokens that the first product's workgroups route themselves
+
 template <typename TIO, int NT, int NG>
 void launch_experts(const MoeArgs& a, hipStream_t st) {
     const int y = a.by_pair ? a.n * a.top_k : a.E;
     {
         ProfScope ps(KID_MOE_GATE_UP, st);
-        hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG>), dim3((a.F + 8 * NT - 1) / (8 * NT), y), dim3(256), 0, st, a);
+        const dim3 grid((a.F + 8 * NT - 1) / (8 * NT), y);
+        if (NG == 1 && a.n <= kRouteAlong) hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, NG == 1>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, false>), grid, dim3(256), 0, st, a);
     }
-    ProfScope ps(KID_MOE_DOWN, st);
-    hipLaunchKernelGGL((k_moe_down<TIO, NT, NG>), dim3((a.D + 16 * NT - 1) / (16 * NT), y), dim3(256), 0, st, a);
+    {
+        ProfScope ps(KID_MOE_DOWN, st);
+        hipLaunchKernelGGL((k_moe_down<TIO, NT, NG>), dim3((a.D + 16 * NT - 1) / (16 * NT), y), dim3(256), 0, st, a);
+    }
+    ProfScope ps(KID_MOE_SUM, st);
+    hipLaunchKernelGGL((k_moe_sum<TIO>), dim3(unsigned((size_t(a.n) * a.D / 4 + 255) / 256)), dim3(256), 0, st, a);
 }
 template <typename TIO>
 void launch(const MoeArgs& a, hipStream_t st) {
@@ -390,10 +434,10 @@ void launch(const MoeArgs& a, hipStream_t st) {
         ProfScope ps(KID_MOE_ROUTER, st);
         hipLaunchKernelGGL((k_moe_router<TIO>), dim3(a.E, (a.n + 15) / 16), dim3(256), 0, st, a);
     }
-    {
+    if (a.n > kRouteAlong) {
         ProfScope ps(KID_MOE_ROUTER, st);
         if (a.E <= 64) hipLaunchKernelGGL((k_moe_route<1>), dim3((a.n + 3) / 4), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((k_moe_route<kMaxExperts / 64>), dim3((a.n + 3) / 4), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_moe_route<kWide>), dim3((a.n + 3) / 4), dim3(256), 0, st, a);
     }
     // Columns: as many groups of 16 as an expert has tokens, give or take the spread of chance (more take another pass; with
     // groups that are rarely used the registers would be missing: 128 tokens, 12 an expert: 4 groups 296 us, 2 groups 259).
@@ -403,8 +447,6 @@ void launch(const MoeArgs& a, hipStream_t st) {
     if (a.n <= 16) mean < 8.f ? launch_experts<TIO, 2, 1>(a, st) : launch_experts<TIO, 4, 1>(a, st);
     else if (a.n <= 32 || most <= 32.f) mean < 8.f ? launch_experts<TIO, 2, 2>(a, st) : launch_experts<TIO, 4, 2>(a, st);
     else launch_experts<TIO, 4, 4>(a, st);
-    ProfScope ps(KID_MOE_SUM, st);
-    hipLaunchKernelGGL((k_moe_sum<TIO>), dim3(unsigned((size_t(a.n) * a.D / 4 + 255) / 256)), dim3(256), 0, st, a);
 }
 
 }  // namespace
