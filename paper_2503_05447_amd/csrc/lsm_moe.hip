@@ -206,7 +206,6 @@ struct Tokens {
     }
 };
 
-constexpr int kSteps = 2;  // steps of the contraction in a request
 
 // A workgroup of either product takes NT tiles of 16 rows (of the gate and of the factor half each, or all of the down matrix), so
 // that a request of the columns serves them all; its four waves split the contraction and are summed through LDS.
@@ -214,6 +213,7 @@ constexpr int kSteps = 2;  // steps of the contraction in a request
 template <typename TIO, int NT, int NG, int PLANES>
 struct Product {
     static constexpr int E = kPiece<TIO>, STEP = 4 * E;
+    static constexpr int kSteps = NT == 1 ? 4 : 2;  // steps of the contraction in a request
     f32x4 c[NT][NG];
     const TIO *w[NT], *col[PLANES][NG];  // this lane's row of each tile and its columns, from the first element that it loads
     int K, first, last, groups;
@@ -291,7 +291,9 @@ struct Product {
 // ROUTE: at most four tokens, see Tokens
 template <typename TIO, int NT, int NG, bool ROUTE>
 __global__ __launch_bounds__(256) void k_moe_gate_up(MoeArgs a) {
-    constexpr int HT = NT / 2;  // tiles of the gate, and of the factor
+    // Tiles of the gate, and of the factor; NT = 1: one tile of eight rows of either.
+    constexpr bool SHARED = NT == 1;
+    constexpr int HT = SHARED ? 1 : NT / 2, ROWS = SHARED ? 8 : 16;
     __shared__ f32x4 part[4][NT * NG][64];
     __shared__ int chosen[ROUTE ? 4 * kMaxTop : 1];
     __shared__ float weight[ROUTE ? 4 * kMaxTop : 1];
@@ -301,10 +303,15 @@ __global__ __launch_bounds__(256) void k_moe_gate_up(MoeArgs a) {
     typedef Product<TIO, NT, NG, 1> P;
     P p;
     p.range(a.D, wave);
-    const int row0 = int(blockIdx.x) * 16 * HT, mine = P::E * (lane >> 4);
-    _Pragma("unroll") for (int i = 0; i < HT; ++i) {
-        p.w[i] = static_cast<const TIO*>(a.w_gate_up) + (size_t(tok.e) * 2 * a.F + min(row0 + 16 * i + (lane & 15), a.F - 1)) * a.D + mine;
-        p.w[HT + i] = p.w[i] + size_t(a.F) * a.D;
+    const int row0 = int(blockIdx.x) * ROWS * HT, mine = P::E * (lane >> 4);
+    const TIO* w = static_cast<const TIO*>(a.w_gate_up) + size_t(tok.e) * 2 * a.F * a.D + mine;
+    if (SHARED) {
+        p.w[0] = w + size_t((lane & 8 ? a.F : 0) + row0 + (lane & 7)) * a.D;  // F is a multiple of 8
+    } else {
+        _Pragma("unroll") for (int i = 0; i < HT; ++i) {
+            p.w[i] = w + size_t(min(row0 + 16 * i + (lane & 15), a.F - 1)) * a.D;
+            p.w[(HT + i) % NT] = p.w[i] + size_t(a.F) * a.D;
+        }
     }
     for (int i0 = 0; i0 < tok.m; i0 += 16 * NG) {
         p.groups = min(NG, (tok.m - i0 + 15) / 16);
@@ -317,8 +324,8 @@ __global__ __launch_bounds__(256) void k_moe_gate_up(MoeArgs a) {
         p.join(part, wave, lane, i0 > 0);
         _Pragma("unroll") for (int u = 0; u < NG * HT; ++u) {
             const int g = u / HT, i = u % HT, f = row0 + 16 * i + 4 * (lane >> 4);  // F is a multiple of 8: a lane's four are all there or none
-            if (g >= p.groups || u % 4 != wave || i0 + g * 16 + (lane & 15) >= tok.m || f >= a.F) continue;
-            const f32x4 gate = P::sum(part, i, g, lane), up = P::sum(part, HT + i, g, lane);
+            if (g >= p.groups || u % 4 != wave || i0 + g * 16 + (lane & 15) >= tok.m || f >= a.F || (SHARED && lane >= 32)) continue;
+            const f32x4 gate = P::sum(part, i, g, lane), up = SHARED ? P::sum(part, 0, g, lane + 32) : P::sum(part, HT + i, g, lane);
             const f32x2 to = ROUTE ? f32x2{weight[token[g]], __int_as_float(token[g])} : a.place[size_t(token[g]) * a.E + tok.e];
             float h[4];
             _Pragma("unroll") for (int j = 0; j < 4; ++j) h[j] = to.x * (gate[j] / (1.f + expf(-gate[j])) * up[j]);
@@ -418,7 +425,8 @@ void launch_experts(const MoeArgs& a, hipStream_t st) {
     {
         ProfScope ps(KID_MOE_GATE_UP, st);
         const dim3 grid((a.F + 8 * NT - 1) / (8 * NT), y);
-        if (NG == 1 && a.n <= kRouteAlong) hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, NG == 1>), grid, dim3(256), 0, st, a);
+        constexpr bool ALONG = NG == 1 && NT < 4;
+        if (ALONG && a.n <= kRouteAlong) hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, ALONG>), grid, dim3(256), 0, st, a);
         else hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, false>), grid, dim3(256), 0, st, a);
     }
     {
@@ -444,7 +452,10 @@ void launch(const MoeArgs& a, hipStream_t st) {
     // Tiles: four where columns are half full, so that they are requested half as often (the same case 277 -> 259 us); two
     // where an expert has a token or two and the number of workgroups counts (16 tokens 167 -> 162, one token 28 -> 25).
     const float mean = float(a.n) * a.top_k / a.E, most = mean + 2.f * sqrtf(mean);
-    if (a.n <= 16) mean < 8.f ? launch_experts<TIO, 2, 1>(a, st) : launch_experts<TIO, 4, 1>(a, st);
+    // One, with eight rows of the gate and of the factor in it, for few tokens in fp32, whose rows are twice as long (8 experts of
+    // 776 x 1024, one token 22.2 -> 18.6 us, 2000 x 3000, four tokens 117 -> 102; in bf16 it is slower, 38 -> 40).
+    if (a.n <= 16 && sizeof(TIO) == 4) launch_experts<TIO, sizeof(TIO) == 4 ? 1 : 2, 1>(a, st);
+    else if (a.n <= 16) mean < 8.f ? launch_experts<TIO, 2, 1>(a, st) : launch_experts<TIO, 4, 1>(a, st);
     else if (a.n <= 32 || most <= 32.f) mean < 8.f ? launch_experts<TIO, 2, 2>(a, st) : launch_experts<TIO, 4, 2>(a, st);
     else launch_experts<TIO, 4, 4>(a, st);
 }
