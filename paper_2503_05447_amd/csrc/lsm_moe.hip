@@ -420,19 +420,42 @@ MoeSpace space(const lsm_moe_params& p) {
 constexpr int kRouteAlong = 4;  // tokens that the first product's workgroups route themselves
 
 template <typename TIO, int NT, int NG>
-void launch_experts(const MoeArgs& a, hipStream_t st) {
-    const int y = a.by_pair ? a.n * a.top_k : a.E;
-    {
-        ProfScope ps(KID_MOE_GATE_UP, st);
-        const dim3 grid((a.F + 8 * NT - 1) / (8 * NT), y);
-        constexpr bool ALONG = NG == 1 && NT < 4;
-        if (ALONG && a.n <= kRouteAlong) hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, ALONG>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, false>), grid, dim3(256), 0, st, a);
+void launch_gate_up(const MoeArgs& a, int y, hipStream_t st) {
+    ProfScope ps(KID_MOE_GATE_UP, st);
+    const dim3 grid((a.F + 8 * NT - 1) / (8 * NT), y);
+    constexpr bool ALONG = NG == 1 && NT < 4;
+    if (ALONG && a.n <= kRouteAlong) hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, ALONG>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, false>), grid, dim3(256), 0, st, a);
+}
+template <typename TIO, int NT, int NG>
+void launch_down(const MoeArgs& a, int y, hipStream_t st) {
+    ProfScope ps(KID_MOE_DOWN, st);
+    hipLaunchKernelGGL((k_moe_down<TIO, NT, NG>), dim3((a.D + 16 * NT - 1) / (16 * NT), y), dim3(256), 0, st, a);
+}
+// Tiles: four where columns are half full, so that they are requested half as often (128 tokens, 12 an expert: 277 -> 259 us), else
+// two (16 tokens 167 -> 162 us, one token 28 -> 25).  Half as many where the workgroups are too few for the chip, or few and long, so
+// that a compute unit with one more than another has much more to do (110 tokens, 8 experts of 168 x 376, all active: 33.5 -> 29.6 us;
+// 64 tokens, 8 experts of 1024 x 1024 in fp32: 59 -> 49; 4 tokens, 8 of 2000 x 3000 in fp32: 117 -> 102).  Not where they are few
+// but short: the columns would be requested more often (90 tokens, 8 of 648 x 472, first product 11.1 -> 13.5 us).
+int tiles(int rows, int experts, bool half_full, int64_t row_bytes) {
+    int nt = half_full ? 4 : 2;
+    for (; nt > 1; nt /= 2) {
+        const int64_t groups = int64_t(experts) * ((rows + 16 * nt - 1) / (16 * nt)), bytes = 16 * nt * row_bytes;
+        if (groups >= 128 && (groups >= 512 || bytes <= (96 << 10)) && (groups >= 2048 || bytes <= (256 << 10))) break;
     }
-    {
-        ProfScope ps(KID_MOE_DOWN, st);
-        hipLaunchKernelGGL((k_moe_down<TIO, NT, NG>), dim3((a.D + 16 * NT - 1) / (16 * NT), y), dim3(256), 0, st, a);
-    }
+    return nt;
+}
+template <typename TIO, int NG>
+void launch_experts(const MoeArgs& a, bool half_full, hipStream_t st) {
+    const int pairs = a.n * a.top_k, y = a.by_pair ? pairs : a.E;
+    const int up = tiles(2 * a.F, y, half_full, int64_t(a.D) * int(sizeof(TIO))),
+              down = tiles(a.D, y, half_full, int64_t(a.F) * int(sizeof(TIO)));
+    if (up == 4) launch_gate_up<TIO, 4, NG>(a, y, st);
+    else if (up == 2) launch_gate_up<TIO, 2, NG>(a, y, st);
+    else launch_gate_up<TIO, 1, NG>(a, y, st);
+    if (down == 4) launch_down<TIO, 4, NG>(a, y, st);
+    else if (down == 2) launch_down<TIO, 2, NG>(a, y, st);
+    else launch_down<TIO, 1, NG>(a, y, st);
     ProfScope ps(KID_MOE_SUM, st);
     hipLaunchKernelGGL((k_moe_sum<TIO>), dim3(unsigned((size_t(a.n) * a.D / 4 + 255) / 256)), dim3(256), 0, st, a);
 }
@@ -449,15 +472,11 @@ void launch(const MoeArgs& a, hipStream_t st) {
     }
     // Columns: as many groups of 16 as an expert has tokens, give or take the spread of chance (more take another pass; with
     // groups that are rarely used the registers would be missing: 128 tokens, 12 an expert: 4 groups 296 us, 2 groups 259).
-    // Tiles: four where columns are half full, so that they are requested half as often (the same case 277 -> 259 us); two
-    // where an expert has a token or two and the number of workgroups counts (16 tokens 167 -> 162, one token 28 -> 25).
     const float mean = float(a.n) * a.top_k / a.E, most = mean + 2.f * sqrtf(mean);
-    // One, with eight rows of the gate and of the factor in it, for few tokens in fp32, whose rows are twice as long (8 experts of
-    // 776 x 1024, one token 22.2 -> 18.6 us, 2000 x 3000, four tokens 117 -> 102; in bf16 it is slower, 38 -> 40).
-    if (a.n <= 16 && sizeof(TIO) == 4) launch_experts<TIO, sizeof(TIO) == 4 ? 1 : 2, 1>(a, st);
-    else if (a.n <= 16) mean < 8.f ? launch_experts<TIO, 2, 1>(a, st) : launch_experts<TIO, 4, 1>(a, st);
-    else if (a.n <= 32 || most <= 32.f) mean < 8.f ? launch_experts<TIO, 2, 2>(a, st) : launch_experts<TIO, 4, 2>(a, st);
-    else launch_experts<TIO, 4, 4>(a, st);
+    const bool half_full = mean >= 8.f;
+    if (a.n <= 16) launch_experts<TIO, 1>(a, half_full, st);
+    else if (a.n <= 32 || most <= 32.f) launch_experts<TIO, 2>(a, half_full, st);
+    else launch_experts<TIO, 4>(a, half_full, st);
 }
 
 }  // namespace
