@@ -232,21 +232,25 @@ __global__ __launch_bounds__(256) void k_beam_slices(BeamArgs a) {
             // Elements above the bound, and of those at it the wave's first `keep` (a mask's value may stand in every place).  At the first
             // tile's bound `keep` have come before those of later tiles; another wave may have met a later bound further on.
             const bool at_bound = (t == 0 || !in_order) && least > -kInf;
+            const float bar = at_bound ? least : from_ordered(ordered(least) + 1);
             _Pragma("unroll") for (int j = 0; j < NP; ++j) {
-                if (__ballot(piece_top[j] >= least) == 0) continue;
+                const int hit = lanes(__ballot(piece_top[j] >= bar));
+                if (hit == 0) continue;
                 float x[E];
                 unpack(raw[j], x);
                 const uint32_t token0 = uint32_t(first_of(tile0 + t, j) - r.lead);
+                const bool few = !at_bound || hit <= 8;  // all of those at the bound will do
+                const float from_here = few ? bar : from_ordered(ordered(least) + 1);
                 int same = 0;
                 _Pragma("unroll") for (int i = 0; i < E; ++i) {
-                    const u64 who = __ballot(x[i] > least);
+                    const u64 who = __ballot(x[i] >= from_here);
                     if (who) {
                         const int at = count + lanes(who & below);
-                        if (x[i] > least && at < kWaveList) list[wave][at] = make_key(x[i], token0 + i);
+                        if (x[i] >= from_here && at < kWaveList) list[wave][at] = make_key(x[i], token0 + i);
                         count += lanes(who);
                     }
                 }
-                if (!at_bound || equal >= keep) continue;
+                if (few || equal >= keep) continue;
                 _Pragma("unroll") for (int i = 0; i < E; ++i) same += x[i] == least ? 1 : 0;
                 if (__ballot(same > 0) == 0) continue;
                 int upto = same;
