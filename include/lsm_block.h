@@ -100,8 +100,9 @@ typedef struct {
  *   workspace  at least lsm_moe_step_workspace_bytes(p) (0 for invalid params)
  * The form for decoding: the active experts' weights are read once, whatever the tokens that share them; for the many tokens
  * of a prompt a grouped matrix product is the better tool.  Sums are fp32; with bf16 elements the hidden activations are kept
- * as a bf16 head and a bf16 remainder, so that the one rounding to bf16 is the result's.  A token whose router output is not
- * finite gets a row of NaN; other tokens are not affected.
+ * as a bf16 head and a bf16 remainder, so that the one rounding to bf16 is the result's.  A token with a router output of
+ * NaN or +inf, or with none above -inf, gets a row of NaN (beside finite ones an expert of -inf has the weight 0); other tokens
+ * are not affected.
  */
 size_t lsm_moe_step_workspace_bytes(const lsm_moe_params* p);
 int lsm_moe_step(const lsm_moe_params* p, const void* x, const void* router, const void* w_gate_up, const void* w_down,

@@ -12,8 +12,8 @@
 // elements reach the bound; they are collected in LDS and ranked by counting.  The merge does the same with the slices' lists: the
 // n-th largest of their first entries, say, is a bound.
 //
-// Bound: large batches: instructions (17 vector instructions a logit, of which 8 are the exponential, the sum and the maximum), the
-// logits' bytes would take half of the time.  16 x 16 beams of 131071 bf16 logits, 32 candidates: k_beam_slices 25 us (2.7 TB/s),
+// Bound: large batches: instructions (16 vector instructions a logit, of which 8 are the exponential, the sum and the maximum), the
+// logits' bytes would take half of the time.  16 x 16 beams of 131071 bf16 logits, 32 candidates: k_beam_slices 23 us (2.9 TB/s),
 // k_beam_merge 9.  Small ones: the latency of two launches (one sequence of 4 beams: 5.5 and 4.7 us, the host needs 14).
 // k_state_reorder: HBM, 5.2 TB/s on 1 GiB of states.
 #include "lsm_block_dev.h"
@@ -92,13 +92,13 @@ struct Row {
     static constexpr int E = kPiece<TIO>;
     const char* p;
     int lead, end;
-    bool tail;  // nothing may be read behind this row's last logit
+    bool tail;  // so near the end of all logits that nothing may be read behind this row's last one
     __device__ __forceinline__ Row(const BeamArgs& a, int row) {
         const char* x = a.logits + row * a.row_bytes;
         lead = int(reinterpret_cast<uintptr_t>(x) & 15u) / int(sizeof(TIO));
         p = x - lead * int(sizeof(TIO));
         end = lead + a.V;
-        tail = row == a.rows - 1;
+        tail = (a.rows - 1 - row) * a.row_bytes < 16;
     }
     // `at`: a piece's first element, a multiple of E
     __device__ __forceinline__ u32x4 whole(int at) const { return *reinterpret_cast<const u32x4*>(p + size_t(at) * sizeof(TIO)); }
