@@ -15,6 +15,7 @@ from .binding import (DTYPE_BF16, DTYPE_F32, LAYOUT_BHTD, LAYOUT_BTHD, LsmError,
 NORM_NONE, NORM_RMS, NORM_L2 = 0, 1, 2
 ROT_HALVES, ROT_PAIRS = 0, 1
 
+_ERR_SHAPE, _ERR_ALIGN = -2, -4  # of lsm_status
 _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
 
 
@@ -292,12 +293,14 @@ def lsm_state_reorder(states, parent, stream=None):
     _check(parent, parent.shape, torch.int32, "parent")
     B, K = parent.shape
     at, size = [], []
-    for t in states:
-        if not t.is_cuda or not t.is_contiguous() or t.numel() == 0 or not (
+    for t in states:  # all of them before the first launch: nothing is moved if one is refused
+        if not t.is_cuda or not t.is_contiguous() or t.dim() == 0 or t.numel() == 0 or not (
                 t.shape[0] == B * K or (t.dim() > 1 and t.shape[:2] == (B, K))):
             raise ValueError("states: need contiguous device tensors of %d rows, got %s on %s" % (B * K, tuple(t.shape), t.device))
         at.append(t.data_ptr())
         size.append(t.numel() // (B * K) * t.element_size())
+        if size[-1] % 4 or at[-1] % 16:
+            raise LsmError(_ERR_SHAPE if size[-1] % 4 else _ERR_ALIGN, "lsm_state_reorder")
     for i in range(0, len(at), _MAX_STATES):
         n = min(_MAX_STATES, len(at) - i)
         rc = library().lsm_state_reorder((ctypes.c_void_p * n)(*at[i:i + n]), (ctypes.c_size_t * n)(*size[i:i + n]), n, _ptr(parent),

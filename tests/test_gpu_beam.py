@@ -369,3 +369,18 @@ def test_refusals():
         pkg.lsm_state_reorder(s, parent.view(-1))
     with pytest.raises(pkg.LsmError):
         pkg.lsm_state_reorder(torch.zeros(8, 3, device="cuda", dtype=torch.bfloat16), parent)
+
+
+def test_nothing_is_moved_when_one_of_many_states_is_refused():
+    import torch
+    pkg = lsm()
+    parent = torch.tensor([[1, 1, 0, 3]], dtype=torch.int32, device="cuda")
+    start = torch.arange(4 * 4, dtype=torch.float32, device="cuda").view(4, 4)
+    shifted = torch.zeros(4 * 4 + 1, device="cuda")[1:].view(4, 4)
+    for bad in (torch.zeros(4, 3, device="cuda", dtype=torch.bfloat16), shifted):
+        states = [start.clone() for _ in range(70)]
+        with pytest.raises(pkg.LsmError):
+            pkg.lsm_state_reorder(states + [bad], parent)
+        assert all(torch.equal(s, start) for s in states)
+    with pytest.raises(ValueError):
+        pkg.lsm_state_reorder(torch.zeros((), device="cuda"), parent)
