@@ -269,6 +269,11 @@ bool stride_ok(const lsm_qk_params& p, const lsm_strides& s, int H) {
     return (p.B == 1 || s.batch % piece == 0) && (H == 1 || s.head % piece == 0) && (p.T == 1 || s.token % piece == 0);
 }
 
+// a result's rows are not each other's (inputs may repeat: an expanded gradient has strides of 0)
+bool writable(const lsm_qk_params& p, const lsm_strides& s, int H) {
+    return (p.B == 1 || s.batch != 0) && (H == 1 || s.head != 0) && (p.T == 1 || s.token != 0);
+}
+
 int check(const lsm_qk_params* p, bool backward) {
     if (!p) return LSM_ERR_NULL;
     if (p->struct_size != sizeof(lsm_qk_params)) return LSM_ERR_SHAPE;
@@ -341,6 +346,7 @@ int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const
     if (rc != LSM_OK) return rc;
     if (!q_out || (p->H_k > 0) != (k_out != nullptr)) return LSM_ERR_NULL;
     if (misaligned(q_out) || misaligned(k_out)) return LSM_ERR_ALIGN;
+    if (!writable(*p, p->q_out, p->H_q) || (p->H_k && !writable(*p, p->k_out, p->H_k))) return LSM_ERR_SHAPE;
     QkArgs a = arguments(*p, q, k, q_weight, k_weight, cos_sin, positions);
     a.side[0].y = q_out;
     a.side[1].y = k_out;
@@ -372,6 +378,7 @@ int lsm_qk_norm_rope_bwd(const lsm_qk_params* p, const void* q, const void* k, c
     if (misaligned(d_q_out) || misaligned(d_k_out) || misaligned(dq) || misaligned(dk) || misaligned(d_q_weight) ||
         misaligned(d_k_weight) || misaligned(workspace))
         return LSM_ERR_ALIGN;
+    if (!writable(*p, p->dq, p->H_q) || (has_k && !writable(*p, p->dk, p->H_k))) return LSM_ERR_SHAPE;
     if (!workspace || workspace_bytes < lsm_qk_norm_rope_bwd_workspace_bytes(p)) return LSM_ERR_WORKSPACE;
     QkArgs a = arguments(*p, q, k, q_weight, k_weight, cos_sin, positions);
     a.side[0].g = d_q_out; a.side[0].y = dq; a.side[0].ys = p->dq;

@@ -46,6 +46,12 @@ def test_norm_and_rotation_refuse_bad_arguments():
     assert qk(P(strides={"q": (4, 1024, 128)}, B=1), q=0x1008) == ALIGN     # an axis of one: its stride is free, the pointer is not
     for n in ("q", "qo", "cs", "ko", "k"):
         assert qk(P(), **{n: None}) == NULL, n
+    for i in range(3):                                                         # rows that would be written more than once
+        s = [4096, 1024, 128]
+        s[i] = 0
+        assert qk(P(strides={"q_out": s})) == SHAPE and qk(P(strides={"k_out": s})) == SHAPE
+        assert qk_bwd(P(strides={"dq": s})) == SHAPE and qk_bwd(P(strides={"dk": s})) == SHAPE
+        assert qk_bwd(P(strides={"q_out": s, "q": s}), wsb=16) == WS           # inputs may repeat
     assert qk(P(H_k=0)) == NULL and qk(P(H_k=0), k=None, ko=None) == NULL      # a k's weight without a k
     assert qk(P(rot_dim=0)) == NULL                                            # a table without a rotation
     assert qk(P(n_pos=7), pos=None) == SHAPE                                   # tokens beyond the table

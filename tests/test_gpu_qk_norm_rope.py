@@ -187,6 +187,29 @@ def test_results_into_slices_of_given_tensors():
     assert not d_fused[:, :, 6:].any()
 
 
+def test_repeated_inputs_and_results_in_place():
+    import torch
+    pkg = lsm()
+    cs, w = table(11, 64).cuda(), torch.linspace(0.5, 1.5, 64, device="cuda")
+    one = torch.randn(1, 1, 11, 64, device="cuda")
+    q, g = one.expand(3, 4, 11, 64), torch.randn(3, 4, 1, 64, device="cuda").expand(3, 4, 11, 64)
+    got, ref = pkg.lsm_qk_norm_rope(q, q, cs, None, w), pkg.lsm_qk_norm_rope(q.contiguous(), q.contiguous(), cs, None, w)
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    got, plain = pkg.lsm_qk_norm_rope_bwd(q, q, g, g, cs, None, w), pkg.lsm_qk_norm_rope_bwd(q.contiguous(), q.contiguous(), g.contiguous(),
+                                                                                          g.contiguous(), cs, None, w)
+    for n in ("dq", "dk", "d_q_weight"):
+        assert torch.equal(got[n], plain[n]), n
+    for bad in (torch.zeros(1, 4, 11, 64, device="cuda").expand(3, 4, 11, 64), torch.zeros(3, 1, 11, 64, device="cuda").expand(3, 4, 11, 64)):
+        with pytest.raises(pkg.LsmError):
+            pkg.lsm_qk_norm_rope(q, q, cs, None, w, q_out=bad)
+        with pytest.raises(pkg.LsmError):
+            pkg.lsm_qk_norm_rope_bwd(q, q, g, g, cs, None, w, dk=bad)
+    mine = q.contiguous()
+    other = mine.clone()
+    out = pkg.lsm_qk_norm_rope(mine, other, cs, None, w, q_out=mine, k_out=other)
+    assert out[0] is mine and torch.equal(mine, ref[0]) and torch.equal(other, ref[1])
+
+
 @pytest.mark.parametrize("pairs", [0, 1])
 def test_gradient_is_the_slope_of_the_forward_formula(pairs):
     """Central differences of the forward formula in 64 bits against the kernel's gradients in fp32."""
