@@ -14,7 +14,8 @@
 //
 // Bound: large batches: instructions (16 vector instructions a logit, of which 8 are the exponential, the sum and the maximum), the
 // logits' bytes would take half of the time.  16 x 16 beams of 131071 bf16 logits, 32 candidates: k_beam_slices 23 us (2.9 TB/s),
-// k_beam_merge 9.  Small ones: the latency of two launches (one sequence of 4 beams: 5.5 and 4.7 us, the host needs 14).
+// k_beam_merge 7.5, a workgroup a sequence: its chain of loads and barriers.  Small ones: the latency of two launches (one sequence
+// of 4 beams: 5.6 and 4.8 us, the host needs 15).
 // k_state_reorder: HBM, 5.2 TB/s on 1 GiB of states.
 #include "lsm_block_dev.h"
 
@@ -51,13 +52,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
-__device__ __forceinline__ float wave_max(float x) {
+__device__ __forceinline__ float group_max(float x, int width) {  // of 16, 32 or 64 lanes
     x = fmaxf(x, dpp<0xB1>(x));
     x = fmaxf(x, dpp<0x4E>(x));
     x = fmaxf(x, dpp<0x141>(x));
     x = fmaxf(x, dpp<0x140>(x));
-    x = fmaxf(x, __shfl_xor(x, 16, 64));
-    return fmaxf(x, __shfl_xor(x, 32, 64));
+    if (width >= 32) x = fmaxf(x, __shfl_xor(x, 16, 64));
+    if (width >= 64) x = fmaxf(x, __shfl_xor(x, 32, 64));
+    return x;
 }
 
 // how many of a list's n keys are above x; eight are on their way at a time
@@ -197,7 +199,7 @@ __global__ __launch_bounds__(256) void k_beam_slices(BeamArgs a) {
                 top = fmaxf(top, piece_top[j]);
             }
             if (__ballot(top > m)) {
-                m = fmaxf(m, wave_max(top));
+                m = fmaxf(m, group_max(top, 64));
                 const float to = fmaxf(m, -kLargest);
                 s *= __builtin_amdgcn_exp2f((from - to) * kLog2E);
                 from = to;
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(256) void k_beam_slices(BeamArgs a) {
 }
 
 constexpr int kMergeThreads = 512, kMergeWaves = kMergeThreads / 64;
-constexpr int kMergeAhead = 8;    // lists requested at once by a lane
+constexpr int kMergeAhead = 8;    // entries of the lists requested at once by a lane
 constexpr int kMaxLists = 4160;   // K * slices, see check()
 constexpr int kFewLists = 256;    // with so many, bounds from up to six depths of the lists
 constexpr int kMergeList = kMaxOut * (kMaxOut + 2);  // candidates that can reach the bound, see there
@@ -370,8 +372,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
     const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, K = a.K, n = a.n_out, keep = n + 1;
     const int lists = K * a.slices;
     if (tid == 0) { count = 0; hazard = 0; the_bound = 0; }
-    // What comes from memory is requested first: entries of the lists (see the bound below) and this wave's first lists.  Those of a
-    // finished beam's lists are not written and not used.
+    // What comes from memory is requested first: entries of the lists (see the bound below), and the lists from their beginning.  Those
+    // of a finished beam's lists are not written and not used.
     const int r0 = min(n, (n + lists - 1) / lists);
     int levels = 1;
     while (lists <= kFewLists && (r0 << (levels - 1)) < n) ++levels;
@@ -379,32 +381,34 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
     auto nth_entry = [&](int i) { return kept[size_t(i % lists) * keep + min(n, r0 << (i / lists)) - 1]; };
     u64 ahead[kMergeAhead];
     const u64 my_nth = tid < levels * lists ? nth_entry(tid) : 0;
-    const int at_once = 64 / keep, mine = lane / keep, nth = lane - mine * keep;  // lists that a wave takes at once
-    auto request = [&](int l0) {
+    auto request = [&](int i0) {
         _Pragma("unroll") for (int j = 0; j < kMergeAhead; ++j) {
-            const int l = l0 + j * kMergeWaves * at_once + mine;
-            ahead[j] = mine < at_once && l < lists ? kept[size_t(l) * keep + nth] : 0;
+            const int i = i0 + j * kMergeThreads + tid;
+            ahead[j] = i < lists * keep ? kept[i] : 0;
         }
     };
-    request(wave * at_once);
-    for (int k = wave; k < K; k += kMergeWaves) {
+    request(0);
+    const int width = K > 16 ? 16 : K > 8 ? 32 : 64, k = tid / width;  // lanes to a beam: all beams at once (one after another 2 us more for 16)
+    if (k < K) {
         const int row = b * K + k;
         const bool done = a.finished && a.finished[row];
         const float so_far = a.scores[row];
         float m = -kInf, s = 0.f;
         if (!done) {
             const f32x2* p = a.sums + size_t(row) * a.slices;
-            for (int i = lane; i < a.slices; i += 64) {  // joined as they come
+            for (int i = tid % width; i < a.slices; i += width) {  // joined as they come
                 const f32x2 x = p[i];
                 const float to = fmaxf(m, x.x);
                 if (to > -kInf) s = s * expf(m - to) + x.y * expf(x.x - to);
                 m = to;
             }
             const float mine = m;
-            m = wave_max(m);
-            s = group_sum<64>(mine > -kInf ? s * expf(mine - m) : 0.f);
+            m = group_max(m, width);
+            s = group_sum<16>(mine > -kInf ? s * expf(mine - m) : 0.f);
+            if (width >= 32) s += __shfl_xor(s, 16, 64);
+            if (width >= 64) s += __shfl_xor(s, 32, 64);
         }
-        if (lane == 0) {
+        if (tid % width == 0) {
             row_max[k] = m;
             row_log[k] = logf(s);
             row_score[k] = so_far;
@@ -416,16 +420,16 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
         const float y = row_score[k] + ((x - row_max[k]) - row_log[k]);
         return y == y ? y : -kInf;
     };
-    const float inverse = 1.f / float(a.slices);
-    auto row_of = [&](int l) {  // l / slices: below 2^24, so the product is at most one off
-        int k = int(float(l) * inverse);
-        if (k * a.slices > l) --k;
-        if ((k + 1) * a.slices <= l) ++k;
-        return k;
+    const float per_list = 1.f / float(a.slices), per_entry = 1.f / float(keep);
+    auto quotient = [](int x, int by, float inverse) {  // below 2^24: the product is at most one off
+        int q = int(float(x) * inverse);
+        if (q * by > x) --q;
+        if ((q + 1) * by <= x) ++q;
+        return q;
     };
     // a kept logit of list l as a key of scores; 0: none
     auto scored = [&](int l, u64 kept) {
-        const int k = row_of(l);
+        const int k = quotient(l, a.slices, per_list);
         if (kept == 0 || row_done[k]) return u64(0);
         return make_key(score(k, from_ordered(uint32_t(kept >> 32))), uint32_t(k) * uint32_t(a.V) + key_index(kept));
     };
@@ -450,12 +454,13 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
     __syncthreads();
     const u64 bound = the_bound;
     uint32_t last_kept = 0;  // largest score at which a list of this lane's stopped keeping
-    for (int l0 = wave * at_once; l0 < lists; l0 += kMergeAhead * kMergeWaves * at_once) {
-        if (l0 != wave * at_once) request(l0);
+    for (int i0 = 0; i0 < lists * keep; i0 += kMergeAhead * kMergeThreads) {
+        if (i0 > 0) request(i0);
         _Pragma("unroll") for (int j = 0; j < kMergeAhead; ++j) {
             if (ahead[j] == 0) continue;
-            const u64 key = scored(l0 + j * kMergeWaves * at_once + mine, ahead[j]);
-            if (key != 0 && nth == n) last_kept = max(last_kept, uint32_t(key >> 32));
+            const int i = i0 + j * kMergeThreads + tid, l = quotient(i, keep, per_entry);
+            const u64 key = scored(l, ahead[j]);
+            if (key != 0 && i - l * keep == n) last_kept = max(last_kept, uint32_t(key >> 32));
             if (key != 0 && key >= bound) list[atomicAdd(&count, 1)] = key;
         }
     }
