@@ -388,7 +388,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
         }
     };
     request(0);
-    const int width = K > 16 ? 16 : K > 8 ? 32 : 64, k = tid / width;  // lanes to a beam: all beams at once (one after another 2 us more for 16)
+    const int width = K > 16 ? 16 : K > 8 ? 32 : 64, k = tid / width;  // lanes to a beam: all beams at once
     if (k < K) {
         const int row = b * K + k;
         const bool done = a.finished && a.finished[row];
