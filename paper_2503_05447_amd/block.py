@@ -6,6 +6,7 @@ Argument marshalling only, as in binding.py: every operator runs in the HIP kern
 """
 import ctypes
 import functools
+from operator import index
 
 import torch
 
@@ -58,7 +59,8 @@ def _dense(shape):
 
 
 # What follows from shapes and strides alone is worked out once and kept (sizes only, no pointers): a decoded token's call costs
-# little more than its marshalling.  4 sequences, 16 heads: 14 -> 11 us a call.
+# little more than its marshalling.  4 sequences, 16 heads: 14 -> 11 us a call.  Every number comes in as a Python one, here and in
+# the caches below: a tensor of one element would be found again by its identity, whatever it holds by then.
 @functools.lru_cache(maxsize=256)
 def _qk_plan(q, k, given, grads, table, dtype, norm, rotation, eps, q_scale, k_scale, layout, out_layout):
     """Parameter block by reference, its workspace's size, shapes of q's and k's results (None where they are given), of the
@@ -121,6 +123,12 @@ def _qk_tables(cos_sin, positions, q_weight, k_weight, k, pos_shape, w_shape):
         raise ValueError("k_weight without k")
 
 
+def _choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout):
+    layout = index(layout)
+    return (index(norm), index(rotation), float(eps), float(q_scale), float(k_scale), layout,
+            layout if out_layout is None else index(out_layout))
+
+
 def _table(cos_sin):
     if cos_sin is None:
         return None
@@ -145,7 +153,7 @@ def lsm_qk_norm_rope(q, k=None, cos_sin=None, positions=None, q_weight=None, k_w
     out_layout: order of the results (default ``layout``); q_out, k_out: tensors to write to."""
     p, _, q_new, k_new, pos_shape, w_shape = _qk_plan(
         _form(q, q, "q"), _form(k, q, "k"), (_form(q_out, q, "q_out"), _form(k_out, q, "k_out")), None, _table(cos_sin), _dtype(q, "q"),
-        norm, rotation, eps, q_scale, k_scale, layout, layout if out_layout is None else out_layout)
+        *_choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout))
     _qk_tables(cos_sin, positions, q_weight, k_weight, k, pos_shape, w_shape)
     with _alloc_on(stream):
         if q_new is not None:
@@ -170,7 +178,7 @@ def lsm_qk_norm_rope_bwd(q, k, d_q_out, d_k_out, cos_sin=None, positions=None, q
     p, need, q_new, k_new, pos_shape, w_shape = _qk_plan(
         _form(q, q, "q"), _form(k, q, "k"), (_form(dq, q, "dq"), _form(dk, q, "dk")),
         (_form(d_q_out, q, "d_q_out"), _form(d_k_out, q, "d_k_out")), _table(cos_sin), _dtype(q, "q"),
-        norm, rotation, eps, q_scale, k_scale, layout, layout if out_layout is None else out_layout)
+        *_choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout))
     _qk_tables(cos_sin, positions, q_weight, k_weight, k, pos_shape, w_shape)
     with _alloc_on(stream):
         if q_new is not None:
@@ -218,7 +226,7 @@ def lsm_moe_step(x, router, w_gate_up, w_down, top_k, renormalise=True, residual
     _check(w_gate_up, (E, 2 * F, D), dtype, "w_gate_up")
     _check(w_down, (E, D, F), dtype, "w_down")
     _check(residual, (n, D), dtype, "residual")
-    p, need = _moe_params(n, D, F, E, top_k, dt, 1 if renormalise else 0)
+    p, need = _moe_params(n, D, F, E, index(top_k), dt, 1 if renormalise else 0)
     with _alloc_on(stream):
         if workspace is None:
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
@@ -263,9 +271,9 @@ def lsm_beam_select(logits, scores, n_out=None, finished=None, eos=None, workspa
     if finished is not None and eos is None:
         raise ValueError("finished needs eos")
     _check(finished, (B, K), torch.bool, "finished")
-    n_out = K if n_out is None else n_out
+    n_out = K if n_out is None else index(n_out)
     row = logits.stride(1) if K > 1 else logits.stride(0) if B > 1 else V
-    p, need = _beam_params(B, K, V, n_out, dt, -1 if eos is None else eos, 0, row)
+    p, need = _beam_params(B, K, V, n_out, dt, -1 if eos is None else index(eos), 0, row)
     with _alloc_on(stream):
         if workspace is None:
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=logits.device)
