@@ -58,8 +58,8 @@ typedef struct {
  *   cos_sin     [n_pos, rot_dim] fp32: rot_dim/2 cosines, then rot_dim/2 sines; NULL exactly when rot_dim = 0      in
  *   positions   [B, T] int32 or NULL (= 0..T-1 in every sequence, T <= n_pos then); not read when rot_dim = 0.
  *               A position outside [0, n_pos) makes that token's rows NaN (the table is not read for it)       in
- *   q_out, k_out   dtype, by strides, none of them 0 along an axis longer than 1 (nor of dq, dk; inputs and
- *               d_q_out, d_k_out may repeat); may be q, k themselves                                          out
+ *   q_out, k_out   dtype, by strides with which no two rows share an element (nor with those of dq, dk; rows of
+ *               inputs and of d_q_out, d_k_out may repeat); may be q, k themselves                            out
  * Squares, sums and the rotation are computed in fp32; a row's elements that are not finite reach that row alone.
  */
 int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,

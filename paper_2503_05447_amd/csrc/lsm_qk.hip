@@ -11,6 +11,8 @@
 // bf16: forward 107 us (5.2 TB/s), backward 168 (4.9 TB/s) and 3 for the weights' sums: the rate of a large copy.
 #include "lsm_block_dev.h"
 
+#include <algorithm>
+
 namespace lsm {
 namespace {
 
@@ -269,9 +271,34 @@ bool stride_ok(const lsm_qk_params& p, const lsm_strides& s, int H) {
     return (p.B == 1 || s.batch % piece == 0) && (H == 1 || s.head % piece == 0) && (p.T == 1 || s.token % piece == 0);
 }
 
-// a result's rows are not each other's (inputs may repeat: an expanded gradient has strides of 0)
+// Whether no two of a result's rows share an element (those of inputs may: an expanded gradient has strides of 0).
 bool writable(const lsm_qk_params& p, const lsm_strides& s, int H) {
-    return (p.B == 1 || s.batch != 0) && (H == 1 || s.head != 0) && (p.T == 1 || s.token != 0);
+    struct Axis { int64_t n; __int128 step; };
+    Axis axis[3] = {{p.B, s.batch}, {H, s.head}, {p.T, s.token}};
+    for (Axis& a : axis) a.step = a.n == 1 ? 0 : a.step < 0 ? -a.step : a.step;
+    // Axes in which each holds all of what the smaller ones reach: any order of a dense tensor, and slices of it.
+    std::sort(axis, axis + 3, [](const Axis& x, const Axis& y) { return x.step < y.step; });
+    __int128 reach = p.d;
+    bool nested = true;
+    for (const Axis& a : axis) {
+        nested = nested && (a.n == 1 || a.step >= reach);
+        reach += a.step * (a.n - 1);
+    }
+    if (nested) return true;
+    if (__int128(p.B) * H * p.T * p.d > reach) return false;
+    // Two rows are apart by (x, y, z) steps of the axes: for every x, y of the two shorter axes the z that brings them nearest.
+    std::sort(axis, axis + 3, [](const Axis& x, const Axis& y) { return x.n < y.n; });
+    const Axis& last = axis[2];
+    if (last.step < p.d) return false;
+    for (int64_t x = 0; x < axis[0].n; ++x)
+        for (int64_t y = 1 - axis[1].n; y < axis[1].n; ++y) {
+            if (x == 0 && y == 0) continue;
+            const __int128 at = axis[0].step * x + axis[1].step * y, size = at < 0 ? -at : at;
+            __int128 z = size / last.step;
+            if (z > last.n - 1) z = last.n - 1;
+            if (size - z * last.step < p.d || (z + 1 < last.n && (z + 1) * last.step - size < p.d)) return false;
+        }
+    return true;
 }
 
 int check(const lsm_qk_params* p, bool backward) {
@@ -345,8 +372,8 @@ int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const
     if (rc == LSM_OK) rc = check_pointers(*p, q, k, q_weight, k_weight, cos_sin, positions);
     if (rc != LSM_OK) return rc;
     if (!q_out || (p->H_k > 0) != (k_out != nullptr)) return LSM_ERR_NULL;
-    if (misaligned(q_out) || misaligned(k_out)) return LSM_ERR_ALIGN;
     if (!writable(*p, p->q_out, p->H_q) || (p->H_k && !writable(*p, p->k_out, p->H_k))) return LSM_ERR_SHAPE;
+    if (misaligned(q_out) || misaligned(k_out)) return LSM_ERR_ALIGN;
     QkArgs a = arguments(*p, q, k, q_weight, k_weight, cos_sin, positions);
     a.side[0].y = q_out;
     a.side[1].y = k_out;

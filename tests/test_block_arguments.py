@@ -107,3 +107,60 @@ def test_numbers_of_experts_and_beams_that_change_between_calls_are_read_again(s
                 lambda: block.lsm_beam_select(tensor(1, 3, 50), tensor(1, 3), 2, eos=5.0)):
         with pytest.raises(TypeError):
             bad()
+
+
+def qk_status(entry, q_out, k_out, q_at=0x100000, q_out_at=0x200000, sizes=(3, 5, 4, 64), **strides):
+    """Status of a call on B, T, H heads of d elements with the results' strides given."""
+    B, T, H, d = sizes
+    plain = (H * T * d, T * d, d)
+    s = dict(q=plain, k=plain, q_out=plain, k_out=plain, dq=plain, dk=plain)
+    s.update({"fwd": dict(q_out=q_out, k_out=k_out), "bwd": dict(dq=q_out, dk=k_out)}[entry])
+    s.update(strides)
+    p = block._QkParams(ctypes.sizeof(block._QkParams), B, T, H, H, d, 1, 1, 0, 0, 0, 1e-6, 1.0, 1.0, 0,
+                        *[(ctypes.c_int64 * 3)(*x) for x in s.values()])
+    at = [ctypes.c_void_p(x) for x in (q_at, 0x300000, None, None, None, None)]
+    if entry == "fwd":
+        return pkg.library().lsm_qk_norm_rope(ctypes.byref(p), *at, ctypes.c_void_p(q_out_at), ctypes.c_void_p(0x400001), None)
+    return pkg.library().lsm_qk_norm_rope_bwd(ctypes.byref(p), *at, *[ctypes.c_void_p(x) for x in (0x500000, 0x600000, q_out_at, 0x400000)],
+                                              None, None, ctypes.c_void_p(0x700000), 1, None)
+
+
+def meet(sizes, strides):
+    """Whether two rows of d elements share one, by going through all of them."""
+    B, T, H, d = sizes
+    at = sorted(b * strides[0] + h * strides[1] + t * strides[2] for b in range(B) for h in range(H) for t in range(T))
+    return any(y - x < d for x, y in zip(at, at[1:]))
+
+
+def test_results_whose_rows_share_elements_are_refused():
+    """Against every row's place: a forward call that passes this check ends at the misaligned k_out, a backward call at its workspace."""
+    import itertools
+    import random
+    rng = random.Random(0)
+    passed = {"fwd": -4, "bwd": -5}
+    seen = {True: 0, False: 0}
+    for n in range(3000):
+        sizes = (rng.randint(1, 4), rng.randint(1, 4), rng.randint(1, 4), 64)
+        if n % 3 == 0:   # an order of the axes, perhaps with gaps, perhaps a little too near each other
+            strides, step = [0, 0, 0], 64
+            for axis in rng.sample(range(3), 3):
+                step += 8 * rng.choice([0, 0, 0, 1, 5, -1])
+                strides[axis] = step
+                step *= (sizes[0], sizes[2], sizes[1])[axis]
+        else:
+            strides = [8 * rng.choice([-1, 1, 1, 1]) * rng.randint(0, 40) for _ in range(3)]
+        want = meet(sizes, strides)
+        seen[want] += 1
+        plain = (sizes[2] * sizes[1] * 64, sizes[1] * 64, 64)
+        for entry, which in itertools.product(("fwd", "bwd"), (0, 1)):
+            outs = [plain, plain]
+            outs[which] = strides
+            if which == 1 and entry == "fwd":
+                continue  # k_out stands for the call's end here
+            assert qk_status(entry, *outs, sizes=sizes) == (SHAPE if want else passed[entry]), (entry, which, sizes, strides)
+    assert min(seen.values()) > 500
+    # long axes: heads beside each other in a token, heads that begin before the last one's end, more rows than fit
+    for entry in ("fwd", "bwd"):
+        assert qk_status(entry, (0, 64, 192), (0, 64000, 64), sizes=(1, 1000, 3, 64)) == passed[entry]
+        assert qk_status(entry, (0, 64 * 999, 64), (0, 64000, 64), sizes=(1, 1000, 3, 64)) == SHAPE
+        assert qk_status(entry, (64 * 3, 64 * 1001, 64 * 7), (700 * 51200, 51200, 64), sizes=(900, 800, 700, 64)) == SHAPE
