@@ -5,8 +5,8 @@
  *
  * Conventions of lsm.h: device pointers, 16-byte aligned; the caller owns every buffer; nothing is allocated, kept between
  * calls or synchronised; all work is enqueued on `stream`; outputs are overwritten and alias neither inputs nor each other
- * (lsm_state_reorder works in place by design); results are bitwise reproducible (no floating-point atomics); every
- * argument check comes before the first HIP call.
+ * (but the results of lsm_qk_norm_rope may take its inputs' place, and lsm_state_reorder works in place); results are
+ * bitwise reproducible (no floating-point atomics); every argument check comes before the first HIP call.
  */
 #ifndef LSM_BLOCK_H
 #define LSM_BLOCK_H
@@ -59,7 +59,7 @@ typedef struct {
  *   positions   [B, T] int32 or NULL (= 0..T-1 in every sequence, T <= n_pos then); not read when rot_dim = 0.
  *               A position outside [0, n_pos) makes that token's rows NaN (the table is not read for it)       in
  *   q_out, k_out   dtype, by strides with which no two rows share an element (nor with those of dq, dk; rows of
- *               inputs and of d_q_out, d_k_out may repeat); may be q, k themselves                            out
+ *               inputs and of d_q_out, d_k_out may repeat); may be q, k themselves, with their strides            out
  * Squares, sums and the rotation are computed in fp32; a row's elements that are not finite reach that row alone.
  */
 int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,

@@ -150,7 +150,8 @@ def lsm_qk_norm_rope(q, k=None, cos_sin=None, positions=None, q_weight=None, k_w
     first rot_dim features (a multiple of 16) are rotated, as pairs (i, i + rot_dim/2) or, with ROT_PAIRS, (2i, 2i + 1).
     positions: [B,T] int32 (for q of 3 axes [B]); None: 0..T-1 in every sequence.  A position outside the table makes that
     token's rows NaN.
-    out_layout: order of the results (default ``layout``); q_out, k_out: tensors to write to."""
+    out_layout: order of the results (default ``layout``); q_out, k_out: tensors to write to (q, k themselves in ``layout``
+    too)."""
     p, _, q_new, k_new, pos_shape, w_shape = _qk_plan(
         _form(q, q, "q"), _form(k, q, "k"), (_form(q_out, q, "q_out"), _form(k_out, q, "k_out")), None, _table(cos_sin), _dtype(q, "q"),
         *_choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout))

@@ -301,6 +301,11 @@ bool writable(const lsm_qk_params& p, const lsm_strides& s, int H) {
     return true;
 }
 
+// Results at their input's own address: the same rows in the same places, or some wave's results meet rows that another has yet to read.
+bool in_place_ok(const lsm_qk_params& p, const void* x, const lsm_strides& xs, const void* y, const lsm_strides& ys, int H) {
+    return x != y || ((p.B == 1 || xs.batch == ys.batch) && (H == 1 || xs.head == ys.head) && (p.T == 1 || xs.token == ys.token));
+}
+
 int check(const lsm_qk_params* p, bool backward) {
     if (!p) return LSM_ERR_NULL;
     if (p->struct_size != sizeof(lsm_qk_params)) return LSM_ERR_SHAPE;
@@ -373,6 +378,8 @@ int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const
     if (rc != LSM_OK) return rc;
     if (!q_out || (p->H_k > 0) != (k_out != nullptr)) return LSM_ERR_NULL;
     if (!writable(*p, p->q_out, p->H_q) || (p->H_k && !writable(*p, p->k_out, p->H_k))) return LSM_ERR_SHAPE;
+    if (!in_place_ok(*p, q, p->q, q_out, p->q_out, p->H_q) || (p->H_k && !in_place_ok(*p, k, p->k, k_out, p->k_out, p->H_k)))
+        return LSM_ERR_SHAPE;
     if (misaligned(q_out) || misaligned(k_out)) return LSM_ERR_ALIGN;
     QkArgs a = arguments(*p, q, k, q_weight, k_weight, cos_sin, positions);
     a.side[0].y = q_out;

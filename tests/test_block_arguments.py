@@ -164,3 +164,30 @@ def test_results_whose_rows_share_elements_are_refused():
         assert qk_status(entry, (0, 64, 192), (0, 64000, 64), sizes=(1, 1000, 3, 64)) == passed[entry]
         assert qk_status(entry, (0, 64 * 999, 64), (0, 64000, 64), sizes=(1, 1000, 3, 64)) == SHAPE
         assert qk_status(entry, (64 * 3, 64 * 1001, 64 * 7), (700 * 51200, 51200, 64), sizes=(900, 800, 700, 64)) == SHAPE
+
+
+def test_results_in_place_have_the_inputs_strides():
+    """q_out = q with heads and tokens exchanged would overwrite rows that other waves have yet to read.  (A call that passes ends
+    at the misaligned k_out.)"""
+    bhtd, bthd, sizes = (4096, 512, 64), (4096, 64, 512), (2, 8, 8, 64)
+    kw = dict(q_at=0x100000, sizes=sizes)
+    assert qk_status("fwd", bhtd, bhtd, q_out_at=0x100000, q=bhtd, **kw) == -4
+    assert qk_status("fwd", bthd, bhtd, q_out_at=0x100000, q=bthd, **kw) == -4
+    assert qk_status("fwd", bthd, bhtd, q_out_at=0x100000, q=bhtd, **kw) == SHAPE
+    assert qk_status("fwd", bhtd, bhtd, q_out_at=0x100000, q=bthd, **kw) == SHAPE
+    assert qk_status("fwd", bhtd, bhtd, q_out_at=0x100000, q=(0, 512, 64), **kw) == SHAPE     # a repeated input is no place for results
+    assert qk_status("fwd", bthd, bhtd, q_out_at=0x200000, q=bhtd, **kw) == -4                # two tensors: any order
+    # the stride of an axis of one is never used
+    assert qk_status("fwd", (8, 512, 64), bhtd, q_out_at=0x100000, q=(4096, 512, 64), q_at=0x100000, sizes=(1, 8, 8, 64)) == -4
+
+
+def test_a_transposition_in_place_is_refused_through_the_binding(monkeypatch):
+    monkeypatch.setattr(block, "_stream_handle", lambda stream: None)
+    q = torch.zeros(1, 8, 8, 64).as_subclass(OnDevice)
+    with pytest.raises(pkg.LsmError) as e:
+        block.lsm_qk_norm_rope(q, None, layout=block.LAYOUT_BHTD, out_layout=block.LAYOUT_BTHD, q_out=q)
+    assert e.value.status == SHAPE
+    k = q.clone()
+    with pytest.raises(pkg.LsmError) as e:
+        block.lsm_qk_norm_rope(q.clone(), k, layout=block.LAYOUT_BTHD, out_layout=block.LAYOUT_BHTD, q_out=q, k_out=k)
+    assert e.value.status == SHAPE
