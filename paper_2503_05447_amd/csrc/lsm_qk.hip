@@ -44,6 +44,7 @@ struct QkLane {
     bool live;
     int b, t, partner;
     float cs[E], sn[E];  // cosine, and the sine with the sign that it has for this side of the pair
+    uint32_t turned;     // all bits where this lane's features are rotated: what they are not turned with counts as 0, an infinity too
 
     __device__ __forceinline__ QkLane(const QkArgs& a, int group, bool pairs) {
         const int lane = threadIdx.x & 63;
@@ -54,6 +55,7 @@ struct QkLane {
         b = token / a.T;
         t = token - b * a.T;
         partner = lane;
+        turned = 0;
         _Pragma("unroll") for (int i = 0; i < E; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
         if (a.rot == 0) return;
         const int pos = a.positions ? a.positions[token] : t;
@@ -62,6 +64,7 @@ struct QkLane {
             return;
         }
         if (f0 >= a.rot) return;
+        turned = 0xffffffffu;
         const int half = a.rot / 2;
         const float* row = a.cos_sin + size_t(pos) * a.rot;
         if (pairs) {
@@ -91,14 +94,17 @@ __device__ __forceinline__ u32x4 row_load(const TIO* p) { return *reinterpret_ca
 template <typename TIO>
 __device__ __forceinline__ void row_store(TIO* p, const u32x4& v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p)); }
 
-// the elements that a lane's elements are turned with
+// the elements that a lane's elements are turned with, 0 where they are not
 template <bool PAIRS, int E>
-__device__ __forceinline__ void partners(const u32x4& raw, const float (&x)[E], int partner, float (&xp)[E]) {
+__device__ __forceinline__ void partners(const u32x4& raw, int partner, uint32_t turned, float (&xp)[E]) {
+    u32x4 o;
+    _Pragma("unroll") for (int i = 0; i < 4; ++i)
+        o[i] = (PAIRS ? raw[i] : uint32_t(__builtin_amdgcn_ds_bpermute(4 * partner, int(raw[i])))) & turned;
     if (PAIRS) {
+        float x[E];
+        unpack(o, x);
         _Pragma("unroll") for (int i = 0; i < E; ++i) xp[i] = x[i ^ 1];
     } else {
-        u32x4 o;
-        _Pragma("unroll") for (int i = 0; i < 4; ++i) o[i] = uint32_t(__builtin_amdgcn_ds_bpermute(4 * partner, int(raw[i])));
         unpack(o, xp);
     }
 }
@@ -134,7 +140,7 @@ __global__ __launch_bounds__(256) void k_qk(QkArgs a) {
                 if (h + u >= h1) break;
                 float v[E], vp[E];
                 unpack(raw[u], v);
-                partners<PAIRS>(raw[u], v, ln.partner, vp);
+                partners<PAIRS>(raw[u], ln.partner, ln.turned, vp);
                 float r = 1.f;
                 if (a.norm != LSM_NORM_NONE) {
                     float ss = 0.f;
@@ -192,7 +198,7 @@ __global__ __launch_bounds__(256) void k_qk_bwd(QkArgs a) {
                     float v[E], z[E], zp[E];
                     unpack(rx[u], v);
                     unpack(rg[u], z);
-                    partners<PAIRS>(rg[u], z, ln.partner, zp);
+                    partners<PAIRS>(rg[u], ln.partner, ln.turned, zp);
                     float ss = 0.f, along = 0.f, r = 1.f;
                     _Pragma("unroll") for (int i = 0; i < E; ++i) {
                         z[i] = z[i] * ct[i] + zp[i] * st[i];
