@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void k_qk(QkArgs a) {
     }
 }
 
-// Backward: u = scale R_p^T dy, z = w * u, dx = r (z - r x (r x . z) / d) (L2: without the 1 / d), dw = sum over rows of u * r x.
+// Backward: u = scale R_p^T dy, z = w * u, dx = r (z - r x (r x . z) / d) (L2: without the 1 / d; no norm: z), dw = sum over rows of u * r x.
 // The rows of x and dy are read once; a lane adds up its features' part of dw over all its rows, the workgroup's lanes are
 // joined at its end and k_qk_weights sums the workgroups in a fixed order.
 template <typename TIO, int D, bool PAIRS>
@@ -210,12 +210,11 @@ __global__ __launch_bounds__(256) void k_qk_bwd(QkArgs a) {
                         along = group_sum<Lane::L>(along);
                         r = rsqrtf((a.norm == LSM_NORM_RMS ? ss * (1.f / D) : ss) + a.eps);
                         along *= a.norm == LSM_NORM_RMS ? r * r * (1.f / D) : r * r;
-                    } else {
-                        along = 0.f;
                     }
                     _Pragma("unroll") for (int i = 0; i < E; ++i) {
                         dw[n][i] += z[i] * (r * v[i]);
-                        z[i] = r * (z[i] * w[i] - v[i] * along);
+                        // without a norm x does not enter, whatever it is
+                        z[i] = a.norm != LSM_NORM_NONE ? r * (z[i] * w[i] - v[i] * along) : z[i] * w[i];
                     }
                     if (ln.live) row_store(dx + (h + u) * s.ys.head, pack(z));
                 }
