@@ -36,7 +36,8 @@ typedef struct { int64_t batch, head, token; } lsm_strides;
 
 typedef struct {
     uint32_t struct_size;     /* = sizeof(lsm_qk_params)                                                            */
-    int32_t  B, T;            /* sequences and tokens of each (packed input: B = 1)                                 */
+    int32_t  B, T;            /* sequences and tokens of each (packed input: B = 1), B * T at most 2^30 and, forward,
+                                 the rows of one head at most 2^36 - 4096 bytes (LSM_ERR_SHAPE beyond)               */
     int32_t  H_q, H_k, d;     /* heads of q and of k (H_k = 0: no k), d in {64,128,256}                               */
     int32_t  dtype;           /* lsm_dtype of q, k, their outputs and gradients                                     */
     int32_t  norm, rotation;  /* lsm_norm_kind, lsm_rotation                                                        */
@@ -113,7 +114,8 @@ int lsm_moe_step(const lsm_moe_params* p, const void* x, const void* router, con
 
 typedef struct {
     uint32_t struct_size; /* = sizeof(lsm_beam_params)                                                       */
-    int32_t  B, K, V;     /* sequences, beams of each (at most 32), vocabulary; K * V at most 2^25             */
+    int32_t  B, K, V;     /* sequences (below 2^23), beams of each (at most 32), vocabulary; K * V at most 2^25;
+                             B * K * ceil(V / 4096) below 2^24 will do always (LSM_ERR_SHAPE beyond a launch) */
     int32_t  n_out;       /* candidates wanted of each sequence: 1..32, at most K * V                        */
     int32_t  dtype;       /* lsm_dtype of the logits                                                         */
     int32_t  eos;         /* the token that ends a beam, or -1                                               */

@@ -599,7 +599,8 @@ int check(const lsm_beam_params* p) {
     if (all > (int64_t(1) << 25) || p->n_out > all || p->eos < -1 || p->eos >= p->V) return LSM_ERR_SHAPE;
     // a sequence's lists: one a tile where there are fewer than 2 kSlices tiles, else a fraction of at most 2^25 / 4096 + K tiles
     static_assert(2 * kSlices <= kMaxLists && ((1 << 25) / 4096 + kMaxOut) / 2 + kMaxOut <= kMaxLists, "lists of a sequence");
-    if (p->row_stride > (int64_t(1) << 40) || int64_t(p->B) * p->K * plan(*p).row_tiles > 0x7fffffff) return LSM_ERR_SHAPE;
+    if (p->row_stride > (int64_t(1) << 40)) return LSM_ERR_SHAPE;
+    if (int64_t(p->B) * p->K * plan(*p).slices * 256 > kAxisThreads || int64_t(p->B) * kMergeThreads > kAxisThreads) return LSM_ERR_SHAPE;
     return LSM_OK;
 }
 size_t sums_bytes(const lsm_beam_params& p, const BeamPlan& pl) { return align256(size_t(p.B) * p.K * pl.slices * sizeof(f32x2)); }

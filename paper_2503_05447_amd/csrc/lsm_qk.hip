@@ -382,17 +382,18 @@ int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const
     if (rc == LSM_OK) rc = check_pointers(*p, q, k, q_weight, k_weight, cos_sin, positions);
     if (rc != LSM_OK) return rc;
     if (!q_out || (p->H_k > 0) != (k_out != nullptr)) return LSM_ERR_NULL;
+    QkArgs a = arguments(*p, q, k, q_weight, k_weight, cos_sin, positions);
+    const int64_t blocks = (int64_t(a.groups) * a.splits + 3) / 4;
+    if (blocks * 256 > kAxisThreads) return LSM_ERR_SHAPE;
     if (!writable(*p, p->q_out, p->H_q) || (p->H_k && !writable(*p, p->k_out, p->H_k))) return LSM_ERR_SHAPE;
     if (!in_place_ok(*p, q, p->q, q_out, p->q_out, p->H_q) || (p->H_k && !in_place_ok(*p, k, p->k, k_out, p->k_out, p->H_k)))
         return LSM_ERR_SHAPE;
     if (misaligned(q_out) || misaligned(k_out)) return LSM_ERR_ALIGN;
-    QkArgs a = arguments(*p, q, k, q_weight, k_weight, cos_sin, positions);
     a.side[0].y = q_out;
     a.side[1].y = k_out;
-    const int blocks = int((int64_t(a.groups) * a.splits + 3) / 4);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p->dtype == LSM_DTYPE_BF16) launch<uint16_t>(*p, a, false, blocks, st);
-    else launch<float>(*p, a, false, blocks, st);
+    if (p->dtype == LSM_DTYPE_BF16) launch<uint16_t>(*p, a, false, int(blocks), st);
+    else launch<float>(*p, a, false, int(blocks), st);
     return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_LAUNCH;
 }
 

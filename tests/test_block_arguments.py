@@ -191,3 +191,26 @@ def test_a_transposition_in_place_is_refused_through_the_binding(monkeypatch):
     with pytest.raises(pkg.LsmError) as e:
         block.lsm_qk_norm_rope(q.clone(), k, layout=block.LAYOUT_BTHD, out_layout=block.LAYOUT_BHTD, q_out=q, k_out=k)
     assert e.value.status == SHAPE
+
+
+def beam_status(B, K, V, **kw):
+    """Status of a selection whose last check, the alignment of a result, fails."""
+    c = dict(n_out=1, dtype=1, eos=-1)
+    c.update(kw)
+    p = block._BeamParams(ctypes.sizeof(block._BeamParams), B, K, V, c["n_out"], c["dtype"], c["eos"], 0, V)
+    at = [ctypes.c_void_p(x) for x in (0x1000, 0x2000, None, 0x3000, 0x4000, 0x5001, None, 0x6000)]
+    return pkg.library().lsm_beam_select(ctypes.byref(p), *at, 1 << 62, None), pkg.library().lsm_beam_select_workspace_bytes(ctypes.byref(p))
+
+
+def test_launches_of_more_threads_than_an_axis_takes_are_refused():
+    """Fewer than 2^32 threads along an axis of a launch: 2^24 - 1 workgroups of 256, 2^23 - 1 of 512."""
+    row = lambda T, d: ((T * d, T * d, d),) * 2
+    at = dict(q_at=0x100000)
+    most = ((1 << 24) - 1) * 16                               # tokens of 128 bf16 features, 16 to a workgroup
+    for T, want in ((1 << 27, -4), (most, -4), (most + 1, SHAPE), (1 << 29, SHAPE), (1 << 30, SHAPE)):
+        assert qk_status("fwd", *row(T, 128), sizes=(1, T, 1, 128), **at) == want, T
+    assert qk_status("bwd", *row(1 << 30, 128), sizes=(1, 1 << 30, 1, 128), **at) == -5        # its workgroups take what there is in turn
+    for B, K, V, want in (((1 << 23) - 1, 1, 1, -4), (1 << 23, 1, 1, SHAPE), ((1 << 19) - 1, 32, 1, -4), (1 << 19, 32, 1, SHAPE),
+                          (1 << 18, 32, 1 << 14, -4), ((1 << 19) - 1, 32, 1 << 18, SHAPE)):
+        status, need = beam_status(B, K, V)
+        assert status == want and (need > 0) == (want != SHAPE), (B, K, V)
