@@ -641,11 +641,12 @@ int lsm_beam_select(const lsm_beam_params* p, const void* logits, const float* s
         if (bf16) hipLaunchKernelGGL((k_beam_slices<uint16_t>), dim3(blocks), dim3(256), 0, st, a);
         else hipLaunchKernelGGL((k_beam_slices<float>), dim3(blocks), dim3(256), 0, st, a);
     }
+    if (!launched()) return LSM_ERR_LAUNCH;
     {
         ProfScope ps(KID_BEAM_MERGE, st);
         hipLaunchKernelGGL(k_beam_merge, dim3(p->B), dim3(kMergeThreads), 0, st, a);
     }
-    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_LAUNCH;
+    return launched() ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 int lsm_state_reorder(void* const* states, const size_t* row_bytes, int n_states, const int32_t* parent, int B, int K,
@@ -676,7 +677,7 @@ int lsm_state_reorder(void* const* states, const size_t* row_bytes, int n_states
     else if (K <= 8) hipLaunchKernelGGL((k_state_reorder<8>), grid, block, 0, st, a);
     else if (K <= 16) hipLaunchKernelGGL((k_state_reorder<16>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((k_state_reorder<32>), grid, block, 0, st, a);
-    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_LAUNCH;
+    return launched() ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 }  // extern "C"

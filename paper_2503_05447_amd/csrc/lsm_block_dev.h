@@ -12,6 +12,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// After each launch that others of a call follow: they take addresses from what it writes.
+inline bool launched() { return hipGetLastError() == hipSuccess; }
+
 constexpr int64_t kAxisThreads = 0xffffffff;  // most threads of a launch along an axis
 
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }

@@ -428,18 +428,21 @@ MoeSpace space(const lsm_moe_params& p) {
 }
 constexpr int kRouteAlong = 4;  // tokens that the first product's workgroups route themselves
 
+// The launches: whether each could be enqueued, and nothing after one that could not.
 template <typename TIO, int NT, int NG>
-void launch_gate_up(const MoeArgs& a, int y, hipStream_t st) {
+bool launch_gate_up(const MoeArgs& a, int y, hipStream_t st) {
     ProfScope ps(KID_MOE_GATE_UP, st);
     const dim3 grid((a.F + 8 * NT - 1) / (8 * NT), y);
     constexpr bool ALONG = NG == 1 && NT < 4;
     if (ALONG && a.n <= kRouteAlong) hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, ALONG>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_moe_gate_up<TIO, NT, NG, false>), grid, dim3(256), 0, st, a);
+    return launched();
 }
 template <typename TIO, int NT, int NG>
-void launch_down(const MoeArgs& a, int y, hipStream_t st) {
+bool launch_down(const MoeArgs& a, int y, hipStream_t st) {
     ProfScope ps(KID_MOE_DOWN, st);
     hipLaunchKernelGGL((k_moe_down<TIO, NT, NG>), dim3((a.D + 16 * NT - 1) / (16 * NT), y), dim3(256), 0, st, a);
+    return launched();
 }
 // Tiles: four where columns are half full, so that they are requested half as often (128 tokens, 12 an expert: 277 -> 259 us), else
 // two (16 tokens 167 -> 162 us, one token 28 -> 25).  Half as many where the workgroups are too few for the chip, or few and long, so
@@ -455,37 +458,40 @@ int tiles(int rows, int experts, bool half_full, int64_t row_bytes) {
     return nt;
 }
 template <typename TIO, int NG>
-void launch_experts(const MoeArgs& a, bool half_full, hipStream_t st) {
+bool launch_experts(const MoeArgs& a, bool half_full, hipStream_t st) {
     const int pairs = a.n * a.top_k, y = a.by_pair ? pairs : a.E;
     const int up = tiles(2 * a.F, y, half_full, int64_t(a.D) * int(sizeof(TIO))),
               down = tiles(a.D, y, half_full, int64_t(a.F) * int(sizeof(TIO)));
-    if (up == 4) launch_gate_up<TIO, 4, NG>(a, y, st);
-    else if (up == 2) launch_gate_up<TIO, 2, NG>(a, y, st);
-    else launch_gate_up<TIO, 1, NG>(a, y, st);
-    if (down == 4) launch_down<TIO, 4, NG>(a, y, st);
-    else if (down == 2) launch_down<TIO, 2, NG>(a, y, st);
-    else launch_down<TIO, 1, NG>(a, y, st);
+    if (!(up == 4 ? launch_gate_up<TIO, 4, NG>(a, y, st) : up == 2 ? launch_gate_up<TIO, 2, NG>(a, y, st)
+                                                                   : launch_gate_up<TIO, 1, NG>(a, y, st)))
+        return false;
+    if (!(down == 4 ? launch_down<TIO, 4, NG>(a, y, st) : down == 2 ? launch_down<TIO, 2, NG>(a, y, st)
+                                                                    : launch_down<TIO, 1, NG>(a, y, st)))
+        return false;
     ProfScope ps(KID_MOE_SUM, st);
     hipLaunchKernelGGL((k_moe_sum<TIO>), dim3(unsigned((size_t(a.n) * a.D / 4 + 255) / 256)), dim3(256), 0, st, a);
+    return launched();
 }
 template <typename TIO>
-void launch(const MoeArgs& a, hipStream_t st) {
+bool launch(const MoeArgs& a, hipStream_t st) {
     {
         ProfScope ps(KID_MOE_ROUTER, st);
         hipLaunchKernelGGL((k_moe_router<TIO>), dim3(a.E, (a.n + 15) / 16), dim3(256), 0, st, a);
     }
+    if (!launched()) return false;
     if (a.n > kRouteAlong) {
         ProfScope ps(KID_MOE_ROUTER, st);
         if (a.E <= 64) hipLaunchKernelGGL((k_moe_route<1>), dim3((a.n + 3) / 4), dim3(256), 0, st, a);
         else hipLaunchKernelGGL((k_moe_route<kWide>), dim3((a.n + 3) / 4), dim3(256), 0, st, a);
+        if (!launched()) return false;
     }
     // Columns: as many groups of 16 as an expert has tokens, give or take the spread of chance (more take another pass; with
     // groups that are rarely used the registers would be missing: 128 tokens, 12 an expert: 4 groups 296 us, 2 groups 259).
     const float mean = float(a.n) * a.top_k / a.E, most = mean + 2.f * sqrtf(mean);
     const bool half_full = mean >= 8.f;
-    if (a.n <= 16) launch_experts<TIO, 1>(a, half_full, st);
-    else if (a.n <= 32 || most <= 32.f) launch_experts<TIO, 2>(a, half_full, st);
-    else launch_experts<TIO, 4>(a, half_full, st);
+    if (a.n <= 16) return launch_experts<TIO, 1>(a, half_full, st);
+    if (a.n <= 32 || most <= 32.f) return launch_experts<TIO, 2>(a, half_full, st);
+    return launch_experts<TIO, 4>(a, half_full, st);
 }
 
 }  // namespace
@@ -515,9 +521,7 @@ int lsm_moe_step(const lsm_moe_params* p, const void* x, const void* router, con
                     ws + s.h, ws + s.h_rem, reinterpret_cast<float*>(ws + s.part), p->n, p->D, p->F, p->E, p->top_k, p->renormalise,
                     p->n * p->top_k < p->E};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p->dtype == LSM_DTYPE_BF16) launch<uint16_t>(a, st);
-    else launch<float>(a, st);
-    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_LAUNCH;
+    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, st) : launch<float>(a, st)) ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 }  // extern "C"

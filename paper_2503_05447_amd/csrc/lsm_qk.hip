@@ -394,7 +394,7 @@ int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (p->dtype == LSM_DTYPE_BF16) launch<uint16_t>(*p, a, false, int(blocks), st);
     else launch<float>(*p, a, false, int(blocks), st);
-    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_LAUNCH;
+    return launched() ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 size_t lsm_qk_norm_rope_bwd_workspace_bytes(const lsm_qk_params* p) {
@@ -429,11 +429,13 @@ int lsm_qk_norm_rope_bwd(const lsm_qk_params* p, const void* q, const void* k, c
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (p->dtype == LSM_DTYPE_BF16) launch<uint16_t>(*p, a, true, blocks, st);
     else launch<float>(*p, a, true, blocks, st);
+    if (!launched()) return LSM_ERR_LAUNCH;
     if (weights) {
         ProfScope ps(KID_QK_WEIGHTS, st);
         hipLaunchKernelGGL(k_qk_weights, dim3(p->d / 16, 2), dim3(1024), 0, st, a.part, blocks, p->d, d_q_weight, d_k_weight);
+        if (!launched()) return LSM_ERR_LAUNCH;
     }
-    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_LAUNCH;
+    return LSM_OK;
 }
 
 }  // extern "C"

@@ -214,3 +214,54 @@ def test_launches_of_more_threads_than_an_axis_takes_are_refused():
                           (1 << 18, 32, 1 << 14, -4), ((1 << 19) - 1, 32, 1 << 18, SHAPE)):
         status, need = beam_status(B, K, V)
         assert status == want and (need > 0) == (want != SHAPE), (B, K, V)
+
+
+SHIM = """
+/* HIP's launch replaced: the n-th one fails, all of them are counted. */
+static int calls, fail_at, last;
+int __hipPushCallConfiguration(void) { return 0; }
+int __hipPopCallConfiguration(void) { return 0; }
+int hipLaunchKernel(void) { return ++calls == fail_at ? (last = 9) : 0; }
+int hipGetLastError(void) { int e = last; last = 0; return e; }
+void shim_reset(int at) { calls = last = 0; fail_at = at; }
+int shim_calls(void) { return calls; }
+"""
+AFTER_A_FAILED_LAUNCH = """
+import ctypes, sys
+shim = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+sys.path.insert(0, sys.argv[2])
+from paper_2503_05447_amd import block
+lib, vp, P = block.library(), ctypes.c_void_p, lambda *a: [ctypes.c_void_p(0x1000 * (i + 1)) for i in a]
+beam = block._BeamParams(ctypes.sizeof(block._BeamParams), 1, 2, 100, 2, 0, -1, 0, 100)
+moe = lambda n: block._MoeParams(ctypes.sizeof(block._MoeParams), n, 64, 32, 8, 2, 1, 1)
+s = (ctypes.c_int64 * 3)(1024, 512, 64)
+qk = block._QkParams(ctypes.sizeof(block._QkParams), 1, 8, 2, 2, 64, 1, 1, 0, 0, 0, 1e-6, 1.0, 1.0, 0, s, s, s, s, s, s)
+calls = dict(
+    beam=(2, lambda: lib.lsm_beam_select(ctypes.byref(beam), *P(0, 1), None, *P(2, 3, 4), None, *P(5), 1 << 40, None)),
+    moe_2=(4, lambda: lib.lsm_moe_step(ctypes.byref(moe(2)), *P(0, 1, 2, 3, 4, 5, 6), 1 << 40, None)),
+    moe_9=(5, lambda: lib.lsm_moe_step(ctypes.byref(moe(9)), *P(0, 1, 2, 3, 4, 5, 6), 1 << 40, None)),
+    qk_bwd=(2, lambda: lib.lsm_qk_norm_rope_bwd(ctypes.byref(qk), *P(0, 1, 2, 3), None, None, *P(4, 5, 6, 7, 8, 9, 10), 1 << 40, None)))
+for name, (launches, call) in calls.items():
+    for at in range(launches + 1):
+        shim.shim_reset(at)
+        status = call()
+        want = (0, launches) if at == 0 else (-6, at)
+        assert (status, shim.shim_calls()) == want, (name, at, status, shim.shim_calls())
+print("done")
+"""
+
+
+def test_nothing_is_launched_after_a_launch_that_failed(tmp_path):
+    """What a kernel left out would have written is where the next ones find their addresses."""
+    import os
+    import shutil
+    import subprocess
+    import sys
+    if shutil.which("gcc") is None:
+        pytest.skip("no host compiler for the launch counter")
+    (tmp_path / "shim.c").write_text(SHIM)
+    subprocess.run(["gcc", "-shared", "-fPIC", "-o", tmp_path / "shim.so", tmp_path / "shim.c"], check=True)
+    pkg.library()
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-W", "ignore", "-c", AFTER_A_FAILED_LAUNCH, str(tmp_path / "shim.so"), root], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "done", r.stderr[-2000:]
