@@ -399,7 +399,7 @@ int lsm_qk_norm_rope(const lsm_qk_params* p, const void* q, const void* k, const
 
 size_t lsm_qk_norm_rope_bwd_workspace_bytes(const lsm_qk_params* p) {
     using namespace lsm;
-    if (check(p, false) != LSM_OK) return 0;
+    if (check(p, true) != LSM_OK) return 0;
     QkArgs a{};
     plan(*p, a);
     return align256(size_t(2) * bwd_groups(a) * p->d * sizeof(float));

@@ -265,3 +265,12 @@ def test_nothing_is_launched_after_a_launch_that_failed(tmp_path):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-W", "ignore", "-c", AFTER_A_FAILED_LAUNCH, str(tmp_path / "shim.so"), root], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "done", r.stderr[-2000:]
+
+
+def test_the_backward_workspace_of_invalid_strides_is_0():
+    s = (4096, 512, 64)
+    for bad in ("q", "k", "q_out", "k_out", "dq", "dk"):
+        strides = {n: (4096, 512, 68) if n == bad else s for n in ("q", "k", "q_out", "k_out", "dq", "dk")}
+        p = block._QkParams(ctypes.sizeof(block._QkParams), 2, 8, 8, 8, 64, 1, 1, 0, 0, 0, 1e-6, 1.0, 1.0, 0,
+                            *[(ctypes.c_int64 * 3)(*x) for x in strides.values()])
+        assert pkg.library().lsm_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(p)) == 0, bad
