@@ -123,6 +123,14 @@ def _qk_tables(cos_sin, positions, q_weight, k_weight, k, pos_shape, w_shape):
         raise ValueError("k_weight without k")
 
 
+def _workspace(workspace, need, like):
+    """The caller's workspace, or a new one beside `like`."""
+    if workspace is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+    _check(workspace, workspace.shape, workspace.dtype, "workspace")
+    return workspace
+
+
 def _choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout):
     layout = index(layout)
     return (index(norm), index(rotation), float(eps), float(q_scale), float(k_scale), layout,
@@ -186,8 +194,7 @@ def lsm_qk_norm_rope_bwd(q, k, d_q_out, d_k_out, cos_sin=None, positions=None, q
             dq = torch.empty(q_new, dtype=q.dtype, device=q.device)
         if k_new is not None:
             dk = torch.empty(k_new, dtype=q.dtype, device=q.device)
-        if workspace is None:
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = _workspace(workspace, need, q)
         dqw = None if q_weight is None else torch.empty(w_shape, dtype=torch.float32, device=q.device)
         dkw = None if k_weight is None else torch.empty(w_shape, dtype=torch.float32, device=q.device)
     rc = library().lsm_qk_norm_rope_bwd(p, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin), _ptr(positions),
@@ -229,8 +236,7 @@ def lsm_moe_step(x, router, w_gate_up, w_down, top_k, renormalise=True, residual
     _check(residual, (n, D), dtype, "residual")
     p, need = _moe_params(n, D, F, E, index(top_k), dt, 1 if renormalise else 0)
     with _alloc_on(stream):
-        if workspace is None:
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
+        workspace = _workspace(workspace, need, x)
         if y is None:
             y = torch.empty_like(x)
         else:
@@ -276,8 +282,7 @@ def lsm_beam_select(logits, scores, n_out=None, finished=None, eos=None, workspa
     row = logits.stride(1) if K > 1 else logits.stride(0) if B > 1 else V
     p, need = _beam_params(B, K, V, n_out, dt, -1 if eos is None else index(eos), 0, row)
     with _alloc_on(stream):
-        if workspace is None:
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=logits.device)
+        workspace = _workspace(workspace, need, logits)
         out = torch.empty((B, max(n_out, 0)), dtype=torch.float32, device=logits.device)
         parent = torch.empty_like(out, dtype=torch.int32)
         token = torch.empty_like(out, dtype=torch.int32)

@@ -274,3 +274,19 @@ def test_the_backward_workspace_of_invalid_strides_is_0():
         p = block._QkParams(ctypes.sizeof(block._QkParams), 2, 8, 8, 8, 64, 1, 1, 0, 0, 0, 1e-6, 1.0, 1.0, 0,
                             *[(ctypes.c_int64 * 3)(*x) for x in strides.values()])
         assert pkg.library().lsm_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(p)) == 0, bad
+
+
+def test_a_workspace_that_is_not_all_there_on_the_device_is_refused(seen):
+    """Host memory, or one byte repeated: the kernels would write outside it."""
+    q = tensor(1, 2, 8, 64)
+    calls = (lambda ws: block.lsm_qk_norm_rope_bwd(q, q, q, q, workspace=ws),
+             lambda ws: block.lsm_moe_step(tensor(3, 16), tensor(8, 16), tensor(8, 16, 16), tensor(8, 16, 8), 2, workspace=ws),
+             lambda ws: block.lsm_beam_select(tensor(1, 3, 50), tensor(1, 3), workspace=ws))
+    for call in calls:
+        for bad in (torch.zeros(1 << 20, dtype=torch.uint8), tensor(1, dtype=torch.uint8).expand(1 << 20), tensor(1 << 20, 2, dtype=torch.uint8)[:, 0]):
+            with pytest.raises(ValueError):
+                call(bad)
+        assert not seen
+    for call in calls:
+        call(tensor(1 << 20, dtype=torch.uint8))
+    assert len(seen) == len(calls)
