@@ -145,7 +145,7 @@ int lsm_beam_select(const lsm_beam_params* p, const void* logits, const float* s
 /*
  * The states that belong to the beams follow them, in place: row b K + i of every tensor becomes what row b K + parent[b, i]
  * was before the call.
- *   states     HOST array of n_states (1..64) device pointers to [B * K] rows                               in/out
+ *   states     HOST array of n_states (1..64) device pointers to [B * K] rows, no two tensors sharing memory  in/out
  *   row_bytes  HOST array: bytes of a row of each, a multiple of 4
  *   parent     [B, K] int32; a value outside [0, K) fills its row with 0xff bytes (NaN)                      in
  * Rows that stay where they are (parent[b, i] = i) are not touched.  B at most 65535, K at most 32.

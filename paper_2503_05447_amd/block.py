@@ -300,7 +300,8 @@ _MAX_STATES = 64
 def lsm_state_reorder(states, parent, stream=None):
     """In place: row b K + i of every tensor in ``states`` (one tensor or a list; first axis B K, or [B,K,...]; dense, rows of
     whole 4 bytes) becomes its row b K + parent[b,i].  parent [B,K] int32, as lsm_beam_select returns it for n_out = K; a value
-    outside [0, K) fills its row with 0xff bytes (NaN).  Beams that stay are not touched; 64 tensors a launch."""
+    outside [0, K) fills its row with 0xff bytes (NaN).  Beams that stay are not touched; 64 tensors a launch, none of which
+    shares memory with another or with parent."""
     states = [states] if isinstance(states, torch.Tensor) else list(states)
     if parent.dim() != 2:
         raise ValueError("parent: need [B,K], got %s" % (tuple(parent.shape),))
@@ -315,6 +316,10 @@ def lsm_state_reorder(states, parent, stream=None):
         size.append(t.numel() // (B * K) * t.element_size())
         if size[-1] % 4 or at[-1] % 16:
             raise LsmError(_ERR_SHAPE if size[-1] % 4 else _ERR_ALIGN, "lsm_state_reorder")
+    if len(at) > _MAX_STATES:  # of one launch's the library sees it itself
+        places = sorted(zip(at, size))
+        if any(a + n * B * K > b for (a, n), (b, _) in zip(places, places[1:])):
+            raise LsmError(_ERR_SHAPE, "lsm_state_reorder")
     for i in range(0, len(at), _MAX_STATES):
         n = min(_MAX_STATES, len(at) - i)
         rc = library().lsm_state_reorder((ctypes.c_void_p * n)(*at[i:i + n]), (ctypes.c_size_t * n)(*size[i:i + n]), n, _ptr(parent),

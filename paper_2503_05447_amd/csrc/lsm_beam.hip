@@ -19,6 +19,8 @@
 // k_state_reorder: HBM, 5.2 TB/s on 1 GiB of states.
 #include "lsm_block_dev.h"
 
+#include <algorithm>
+
 namespace lsm {
 namespace {
 
@@ -659,15 +661,24 @@ int lsm_state_reorder(void* const* states, const size_t* row_bytes, int n_states
     size_t columns = 0;
     for (int i = 0; i < n_states; ++i) {
         if (!states[i]) return LSM_ERR_NULL;
-        if (misaligned(states[i])) return LSM_ERR_ALIGN;
         if (row_bytes[i] == 0 || row_bytes[i] % 4 != 0) return LSM_ERR_SHAPE;
         a.state[i] = static_cast<char*>(states[i]);
         a.row_bytes[i] = row_bytes[i];
         const size_t c = row_bytes[i] / (row_bytes[i] % 16 == 0 ? 16 : 4);
         columns = c > columns ? c : columns;
     }
-    if (misaligned(parent)) return LSM_ERR_ALIGN;
     if (columns > (size_t(1) << 31)) return LSM_ERR_SHAPE;
+    // Tensors that share memory, with each other or with the parents, would be read while others' workgroups change them.
+    struct Range { uintptr_t from, to; } range[kMaxStates + 1];
+    const auto place = [](const void* p, size_t bytes) { return Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes}; };
+    for (int i = 0; i < n_states; ++i) range[i] = place(states[i], row_bytes[i] * size_t(B) * K);
+    range[n_states] = place(parent, size_t(B) * K * sizeof(int32_t));
+    std::sort(range, range + n_states + 1, [](const Range& x, const Range& y) { return x.from < y.from; });
+    for (int i = 0; i < n_states; ++i)
+        if (range[i].to > range[i + 1].from) return LSM_ERR_SHAPE;
+    for (int i = 0; i < n_states; ++i)
+        if (misaligned(states[i])) return LSM_ERR_ALIGN;
+    if (misaligned(parent)) return LSM_ERR_ALIGN;
     a.parent = parent;
     a.K = K;
     const dim3 grid(unsigned((columns + 255) / 256), B, n_states), block(256);

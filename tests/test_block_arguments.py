@@ -290,3 +290,34 @@ def test_a_workspace_that_is_not_all_there_on_the_device_is_refused(seen):
     for call in calls:
         call(tensor(1 << 20, dtype=torch.uint8))
     assert len(seen) == len(calls)
+
+
+def reorder_status(at, size, parent=0x300000, B=2, K=4):
+    """Status of a call whose last state is misaligned: one that passes what comes before it."""
+    a, s = (ctypes.c_void_p * len(at))(*at), (ctypes.c_size_t * len(size))(*size)
+    return pkg.library().lsm_state_reorder(a, s, len(at), ctypes.c_void_p(parent), B, K, None)
+
+
+def test_states_that_share_memory_are_refused(monkeypatch):
+    """Each is moved by its own workgroups: two that meet, or one that meets the parents, would be read while they change."""
+    rows = 8
+    assert reorder_status((0x10000, 0x10000), (64, 64)) == SHAPE
+    assert reorder_status((0x20000, 0x10000, 0x10000 + rows * 64 - 16), (64, 64, 16)) == SHAPE
+    assert reorder_status((0x10000, 0x10000 + rows * 64 - 32, 0x20000), (64, 64, 4)) == SHAPE
+    assert reorder_status((0x300000 - rows * 64 + 16, 0x10000), (64, 64)) == SHAPE
+    assert reorder_status((0x300000 + 16,), (4,)) == SHAPE
+    # neighbours are not refused for it (but for a last row of 6 bytes)
+    assert reorder_status((0x10000, 0x10000 + rows * 64, 0x300000 + rows * 4, 0x300000 - rows * 16, 0x50008), (64, 64, 16, 16, 8)) == -4
+    # more than one launch takes
+    monkeypatch.setattr(block, "_stream_handle", lambda stream: None)
+    moved = []
+    monkeypatch.setattr(block, "library", lambda: type("L", (), {"lsm_state_reorder": staticmethod(lambda *a: moved.append(a) or 0),
+                                                                "lsm_status_string": staticmethod(pkg.library().lsm_status_string)}))
+    states = [tensor(8, 4) for _ in range(70)]
+    parent = tensor(2, 4, dtype=torch.int32)
+    for extra in (states[3], states[3].view(-1)[:16].view(8, 2)):
+        with pytest.raises(pkg.LsmError) as e:
+            block.lsm_state_reorder(states + [extra], parent)
+        assert e.value.status == SHAPE and not moved
+    block.lsm_state_reorder(states, parent)
+    assert len(moved) == 2
