@@ -131,12 +131,6 @@ def _workspace(workspace, need, like):
     return workspace
 
 
-def _choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout):
-    layout = index(layout)
-    return (index(norm), index(rotation), float(eps), float(q_scale), float(k_scale), layout,
-            layout if out_layout is None else index(out_layout))
-
-
 def _table(cos_sin):
     if cos_sin is None:
         return None
@@ -160,9 +154,10 @@ def lsm_qk_norm_rope(q, k=None, cos_sin=None, positions=None, q_weight=None, k_w
     token's rows NaN.
     out_layout: order of the results (default ``layout``); q_out, k_out: tensors to write to (q, k themselves in ``layout``
     too)."""
+    layout = index(layout)
     p, _, q_new, k_new, pos_shape, w_shape = _qk_plan(
         _form(q, q, "q"), _form(k, q, "k"), (_form(q_out, q, "q_out"), _form(k_out, q, "k_out")), None, _table(cos_sin), _dtype(q, "q"),
-        *_choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout))
+        index(norm), index(rotation), float(eps), float(q_scale), float(k_scale), layout, layout if out_layout is None else index(out_layout))
     _qk_tables(cos_sin, positions, q_weight, k_weight, k, pos_shape, w_shape)
     with _alloc_on(stream):
         if q_new is not None:
@@ -184,10 +179,11 @@ def lsm_qk_norm_rope_bwd(q, k, d_q_out, d_k_out, cos_sin=None, positions=None, q
     weight).  The other arguments as in lsm_qk_norm_rope; d_q_out, d_k_out in ``out_layout``, dense along d only."""
     if d_q_out is None:
         raise ValueError("d_q_out is required")
+    layout = index(layout)
     p, need, q_new, k_new, pos_shape, w_shape = _qk_plan(
         _form(q, q, "q"), _form(k, q, "k"), (_form(dq, q, "dq"), _form(dk, q, "dk")),
         (_form(d_q_out, q, "d_q_out"), _form(d_k_out, q, "d_k_out")), _table(cos_sin), _dtype(q, "q"),
-        *_choices(norm, rotation, eps, q_scale, k_scale, layout, out_layout))
+        index(norm), index(rotation), float(eps), float(q_scale), float(k_scale), layout, layout if out_layout is None else index(out_layout))
     _qk_tables(cos_sin, positions, q_weight, k_weight, k, pos_shape, w_shape)
     with _alloc_on(stream):
         if q_new is not None:
