@@ -2,7 +2,8 @@
 a mixture-of-experts layer for a few tokens, one step of a beam search.
 
 Argument marshalling only, as in binding.py: every operator runs in the HIP kernels of liblsm_hip.so on ``stream``
-(default: torch's current stream) without synchronising.
+(default: torch's current stream) without synchronising.  Every tensor begins at a multiple of 16 bytes, as torch allocates
+them; a view that begins elsewhere (a row of a [steps, B] table of positions) is refused, and copied by the caller.
 """
 import ctypes
 import functools

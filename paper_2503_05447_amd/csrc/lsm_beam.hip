@@ -12,11 +12,14 @@
 // elements reach the bound; they are collected in LDS and ranked by counting.  The merge does the same with the slices' lists: the
 // n-th largest of their first entries, say, is a bound.
 //
-// Bound: large batches: instructions (16 vector instructions a logit, of which 8 are the exponential, the sum and the maximum), the
-// logits' bytes would take half of the time.  16 x 16 beams of 131071 bf16 logits, 32 candidates: k_beam_slices 23 us (2.9 TB/s),
-// k_beam_merge 7.5, a workgroup a sequence: its chain of loads and barriers.  Small ones: the latency of two launches (one sequence
-// of 4 beams: 5.6 and 4.8 us, the host needs 15).
-// k_state_reorder: HBM, 5.2 TB/s on 1 GiB of states.
+// Bound, large batches: vector instructions and waiting, each in part.  Counted for 16 x 16 beams of 131071 bf16 logits, 32
+// candidates: 16.6 vector instructions a logit (8 of them the exponential, the sum and the maximum) fill about two thirds of the
+// kernel's cycles; a wave waits in 55 % of its own, since nothing is requested while a tile is worked on.  k_beam_slices 24.6 us
+// (2.7 TB/s; the bytes alone would take 13), k_beam_merge 7.8, a workgroup a sequence: its chain of loads and barriers.  Small
+// ones: the latency of two launches (one sequence of 4 beams: 6.0 and 4.6 us, the host needs 15).
+// k_state_reorder: 391 us for 32 x 8 beams with 1 GiB of states, of which 1.25 GB have to move (about 220 rows of 256 change, 76 are
+// some other beam's parent): 3.2 TB/s.  Not HBM: for K <= 8 a thread's loads, each under its own condition, are compiled to one
+// after the other.
 #include "lsm_block_dev.h"
 
 #include <algorithm>
@@ -539,7 +542,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a) {
 }
 
 // ---- the states follow their beams ---------------------------------------------------------------------------------
-// A thread owns the same 16 bytes (or 4) of the K rows of a sequence: it requests what each row is to become, from the rows of the
+// A thread owns the same 16 bytes (or 4) of the K rows of a sequence: it has read what each row is to become, from the rows of the
 // parents, before it stores the first one, so that the rows can change in place.  Nothing is moved for a beam that stays.
 constexpr int kMaxStates = 64;
 struct ReorderArgs {

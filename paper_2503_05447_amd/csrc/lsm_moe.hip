@@ -11,9 +11,9 @@
 // a row straight into the operand's registers, no staging), the expert's tokens are the columns: up to 16 tokens cost what one
 // does.  What is requested for a step is used a step later, so that a wave always has a request under way.
 //
-// Measured, bf16: 128 tokens, 64 experts of 1536 x 2048, 6 a token: k_moe_gate_up 146 us (5.5 TB/s), k_moe_down 89 (4.5: it reads
-// its columns, head and remainder, beside the weights), the other three 16; 16 tokens, 64 of 1032 x 2048, 8 a token: 86 and 54; one
-// token, 64 of 1024 x 1024: 9.4 and 6.7, 3.6 each for the other two.  A read-only stream reaches 6.1 TB/s here.
+// Measured, bf16: 128 tokens, 64 experts of 1536 x 2048, 6 a token: k_moe_gate_up 148 us (5.4 TB/s), k_moe_down 91 (4.4: it reads
+// its columns, head and remainder, beside the weights), the other three 17; 16 tokens, 64 of 1032 x 2048, 8 a token: 86 and 54; one
+// token, 64 of 1024 x 1024: 10.4 and 6.2, 3.6 and 3.8 for the other two.  A read-only stream reaches 6.1 TB/s here.
 //
 // Not kept: the sum by the last workgroup of a tile (the fences across the dies cost more than they save: 128 tokens 250 -> 650 us);
 // all experts' rows of 16 outputs by one workgroup (one token: 64 workgroups, 5 us more than both kernels); an expert's tiles on

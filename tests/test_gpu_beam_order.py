@@ -1,9 +1,9 @@
 """Beam selection where some scores are huge or infinite: the first step, masks of large negative numbers, masked ends of a row.
 
-Every candidate is judged by its own size.  A score c + ((x - m) - log s) is four roundings of 2^-24 of numbers no larger than
+Every candidate is held to its own size.  A score c + ((x - m) - log s) is four roundings of 2^-24 of numbers no larger than
 |c| + |x - m| + log V, and log s, whose sum's terms and trees are off by 2^-20 at most: so a candidate of score y is within
 e = 2^-20 (1 + |y| + |c| + log V), an infinite y or c counting as 0.  Of two candidates the one returned may be worse than the one left
-out by the two e, no more; in one beam, where scores fall with the logits, not at all.  The judge itself is tried on wrong results."""
+out by the two e, no more; in one beam, where scores fall with the logits, not at all.  The check itself is tried on wrong results."""
 import math
 
 import pytest
@@ -24,7 +24,7 @@ def definition(x, scores, finished, eos):
     return s
 
 
-def judge(x, scores, finished, eos, got, parent, token, ended):
+def verify(x, scores, finished, eos, got, parent, token, ended):
     """x [B, K, V], scores [B, K] in 64 bits, the rest as returned: raises AssertionError unless it is the n best, best first."""
     B, K, V = x.shape
     n = got.shape[1]
@@ -89,12 +89,12 @@ def host_case(kind):
 
 
 @pytest.mark.parametrize("kind", list(masks(0)))
-def test_the_judge_accepts_the_definition_and_refuses_what_is_wrong(kind):
+def test_the_check_accepts_the_definition_and_refuses_what_is_wrong(kind):
     x, scores = host_case(kind)
     B, K, V = x.shape
     n = 6
     good = ideal(x, scores, n + 1, None, None)
-    judge(x, scores, None, None, *[a[:, :n] if a is not None else None for a in good])
+    verify(x, scores, None, None, *[a[:, :n] if a is not None else None for a in good])
     low, worst = (a[:, :n] for a in definition(x, scores, None, None).view(B, K * V).sort(dim=1, stable=True))
     without = lambda i: [torch.cat((a[:, :i], a[:, i + 1:]), 1) for a in good[:3]] + [None]
     wrong = {
@@ -107,31 +107,31 @@ def test_the_judge_accepts_the_definition_and_refuses_what_is_wrong(kind):
     }
     for what, result in wrong.items():
         with pytest.raises(AssertionError):
-            judge(x, scores, None, None, *result)
+            verify(x, scores, None, None, *result)
             pytest.fail("accepted: " + what, pytrace=False)
 
 
-def test_the_judge_knows_ties_and_finished_beams():
+def test_the_check_knows_ties_and_finished_beams():
     x, scores = torch.zeros(1, 2, 9).double(), torch.zeros(1, 2).double()
-    judge(x, scores, None, None, *ideal(x, scores, 4, None, None))
+    verify(x, scores, None, None, *ideal(x, scores, 4, None, None))
     s, parent, token, _ = ideal(x, scores, 4, None, None)
     with pytest.raises(AssertionError):
-        judge(x, scores, None, None, s, parent, token + 1, None)         # the first one of equal ones left out
+        verify(x, scores, None, None, s, parent, token + 1, None)         # the first one of equal ones left out
     done = torch.tensor([[True, False]])
-    judge(x, scores, done, 3, *ideal(x, scores, 4, done, 3))
+    verify(x, scores, done, 3, *ideal(x, scores, 4, done, 3))
     s, parent, token, ended = ideal(x, scores, 4, done, 3)
     with pytest.raises(AssertionError):
-        judge(x, scores, done, 3, s, parent, token, ~ended)
+        verify(x, scores, done, 3, s, parent, token, ~ended)
     none = torch.full((1, 2), -INF).double()
     s, parent, token, _ = ideal(x, none, 4, None, None)
-    judge(x, none, None, None, s, parent, token, None)
+    verify(x, none, None, None, s, parent, token, None)
     with pytest.raises(AssertionError):
-        judge(x, none, None, None, s, parent, token + 1, None)
+        verify(x, none, None, None, s, parent, token + 1, None)
 
 
 def check(logits, scores, n=None, finished=None, eos=None):
     import paper_2503_05447_amd as lsm
-    judge(logits.double(), scores.double(), finished, eos, *lsm.lsm_beam_select(logits, scores, n, finished, eos))
+    verify(logits.double(), scores.double(), finished, eos, *lsm.lsm_beam_select(logits, scores, n, finished, eos))
 
 
 def device_case(B, K, V, dtype, seed, pad=1):
