@@ -175,8 +175,8 @@ def _own_experts(s):
     plan = lsm.lsm_moe_plan(s["chosen"], s["E"])
     if not s["train"]:
         return dict(y=lsm.lsm_moe_experts(s["x"], s["weights"], plan, s["w_gate_up"], s["w_down"], residual=s["skip"]))
-    y, hidden = lsm.lsm_moe_experts(s["x"], s["weights"], plan, s["w_gate_up"], s["w_down"], residual=s["skip"], save_hidden=True)
-    return dict(lsm.lsm_moe_experts_bwd(s["x"], s["weights"], plan, s["w_gate_up"], s["w_down"], hidden, s["d_y"]), y=y)
+    y = lsm.lsm_moe_experts(s["x"], s["weights"], plan, s["w_gate_up"], s["w_down"], residual=s["skip"])
+    return dict(lsm.lsm_moe_experts_bwd(s["x"], s["weights"], plan, s["w_gate_up"], s["w_down"], s["d_y"]), y=y)
 
 
 def _own_loss(s):
