@@ -10,3 +10,7 @@ from .block import (  # noqa: F401
     NORM_NONE, NORM_RMS, NORM_L2, ROT_HALVES, ROT_PAIRS, lsm_qk_norm_rope, lsm_qk_norm_rope_bwd,
     lsm_moe_step, lsm_beam_select, lsm_state_reorder,
 )
+from .train import (  # noqa: F401
+    lsm_moe_route, lsm_moe_route_bwd, lsm_moe_plan, lsm_moe_experts, lsm_moe_experts_bwd,
+    lsm_linear_cross_entropy, lsm_linear_cross_entropy_bwd, lsm_linear_distill, lsm_linear_distill_bwd,
+)

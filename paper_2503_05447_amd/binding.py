@@ -110,6 +110,15 @@ def library():
     lib.lsm_moe_step.argtypes = [vp] * 8 + [sz, vp]
     lib.lsm_moe_step_workspace_bytes.restype = sz
     lib.lsm_moe_step_workspace_bytes.argtypes = [vp]
+    for name, pointers in (("lsm_moe_plan", 6), ("lsm_moe_experts", 11), ("lsm_moe_experts_bwd", 14), ("lsm_vocab_loss", 8),
+                           ("lsm_vocab_loss_bwd", 10)):
+        call, space = getattr(lib, name), getattr(lib, name + "_workspace_bytes")
+        call.restype, call.argtypes = ctypes.c_int, [vp] * pointers + [sz, vp]
+        space.restype, space.argtypes = sz, [vp]
+    lib.lsm_moe_route.restype = ctypes.c_int
+    lib.lsm_moe_route.argtypes = [vp] * 5
+    lib.lsm_moe_route_bwd.restype = ctypes.c_int
+    lib.lsm_moe_route_bwd.argtypes = [vp] * 6
     _lib = lib
     return lib
 

@@ -1,0 +1,484 @@
+// The experts' products for many tokens, forward and backward (include/lsm_train.h), over pairs sorted by expert (lsm_route.hip):
+//   k_up           h = silu(Wg x) * (Wu x) of every pair, x taken through the plan's order
+//   k_down         Wd h, fp32, a row a pair
+//   k_sum          the weighted sum of a token's pairs and the residual; backward the sum of dx and of the weights' gradients
+//   k_hidden_grad  both products of the hidden layer again and t = Wd^T dy; from them the gradients of gate and factor, the
+//                  activations times their weight, and the part of <t, h> that belongs to the tile
+//   k_dx           the gradients of gate and factor times Wg, Wu, fp32, a row a pair
+//   k_dw           both weights' gradients, an expert's pairs being the long axis
+// An expert's rows are whole tiles but the last; a workgroup finds its expert and tile from the offsets.
+#include "lsm_product_dev.h"
+#include "lsm_train_dev.h"
+
+namespace lsm {
+namespace {
+
+struct ExpertArgs {
+    const void *x, *w_gate_up, *w_down, *residual, *d_y;
+    const float* weights;
+    const int32_t *offsets, *order, *place;
+    void *y, *d_w_gate_up, *d_w_down;
+    float* d_weights;
+    void *h, *da;           // [pairs][F]: activations (backward: times their weight); [pairs][2 F]
+    float *part, *weight_part;  // [pairs][D]; [tiles of F][pairs]
+    int n, D, F, E, top_k, parts;
+    uint32_t x_bytes, dy_bytes;  // between rows
+};
+
+// What the plan says, kept inside the buffers whatever stands there.
+__device__ __forceinline__ int offset_of(const ExpertArgs& a, int e) { return min(max(a.offsets[e], 0), a.n * a.top_k); }
+__device__ __forceinline__ uint32_t pair_of(const ExpertArgs& a, int at) { return min(uint32_t(a.order[at]), uint32_t(a.n * a.top_k - 1)); }
+__device__ __forceinline__ uint32_t token_of(const ExpertArgs& a, int at) { return pair_of(a, at) / uint32_t(a.top_k); }
+
+struct Where { int e, first, count, r, c; };  // expert, its first place and its pairs, the tile's number along rows and columns
+
+// The tile of this workgroup, of all experts' tiles of BR rows x `cols` columns in the order expert, column, row.  Workgroups are dealt out
+// to the eight dies in turn; a die gets neighbouring tiles, which share operands in its L2.  False: there is none left.
+template <int BR>
+__device__ __forceinline__ bool find_tile(const ExpertArgs& a, int cols, Where& w) {
+    const int lane = threadIdx.x & 63;
+    int o[5], tiles[4], own = 0;
+    _Pragma("unroll") for (int i = 0; i < 5; ++i) o[i] = offset_of(a, min(4 * lane + i, a.E));
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        tiles[i] = max(o[i + 1] - o[i] + BR - 1, 0) / BR;
+        own += tiles[i];
+    }
+    int upto = own;
+    for (int off = 1; off < 64; off <<= 1) {
+        const int t = __shfl_up(upto, off, 64);
+        if (lane >= off) upto += t;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63) * cols, die = (all + 7) / 8;
+    const int slot = int(blockIdx.x) / 8, id = (int(blockIdx.x) % 8) * die + slot;
+    if (slot >= die || id >= all) return false;
+    const int at = lanes(__ballot(upto * cols <= id));
+    int rest = id - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at)) * cols;
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        const int t = __builtin_amdgcn_readlane(tiles[i], at);
+        if (rest < t * cols) {
+            w.e = 4 * at + i;
+            w.first = __builtin_amdgcn_readlane(o[i], at);
+            w.count = __builtin_amdgcn_readlane(o[i + 1], at) - w.first;
+            w.c = rest / t;
+            w.r = rest - w.c * t;
+            return true;
+        }
+        rest -= t * cols;
+    }
+    return false;
+}
+
+template <typename T>
+__device__ __forceinline__ void clear(f32x16 (&acc)[T::TC][T::TR]) {
+    _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
+            _Pragma("unroll") for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+}
+
+// The rows of gate and factor for the same features are blocks i and i + TC / 2 of one wave.
+template <typename T>
+__device__ __forceinline__ uint32_t gate_up_row(const ExpertArgs& a, int c, int q) {
+    constexpr int HALF = T::TC / 2;
+    const int wave = q / (T::TC * 32), i = q / 32 % T::TC, f = c * (T::BC / 2) + (wave * HALF + i % HALF) * 32 + q % 32;
+    return f < a.F ? uint32_t((i >= HALF ? a.F : 0) + f) * uint32_t(a.D) * uint32_t(sizeof(typename T::TIO)) : kBeyond;
+}
+template <typename T>
+__device__ __forceinline__ void start_gate_up(T& t, const ExpertArgs& a, const Where& w) {
+    typedef typename T::TIO TIO;
+    t.r.start_rows(a.x, t.wave, t.lane, [&](int i) {
+        const int at = w.r * T::BR + i;
+        return at < w.count ? token_of(a, w.first + at) * a.x_bytes : kBeyond;
+    });
+    t.c.start_rows(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, t.wave, t.lane,
+                   [&](int q) { return gate_up_row<T>(a, w.c, q); });
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
+    typedef typename T::TIO TIO;
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    Where w;
+    if (!find_tile<T::BR>(a, (a.F + T::BC / 2 - 1) / (T::BC / 2), w)) return;
+    T t(shared);
+    start_gate_up(t, a, w);
+    f32x16 acc[T::TC][T::TR];
+    clear<T>(acc);
+    t.walk(acc, a.D);
+    constexpr int HALF = T::TC / 2;
+    const int f0 = w.c * (T::BC / 2) + t.wc * HALF * 32;
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        t.template put<HALF>([&](int i, int g) {
+            f32x4 h;
+            _Pragma("unroll") for (int e = 0; e < 4; ++e) {
+                const float gate = acc[i][j][4 * g + e];
+                h[e] = gate / (1.f + expf(-gate)) * acc[i + HALF][j][4 * g + e];
+            }
+            return h;
+        });
+        t.template take<HALF, TIO>(j, a.F - f0, [&](int r) {
+            const int at = w.r * T::BR + r;
+            return at < w.count ? static_cast<TIO*>(a.h) + size_t(w.first + at) * a.F + f0 : nullptr;
+        });
+    }
+}
+
+// rows of `parts` [pairs][D] = rows of R [pairs][K] times C^T
+template <typename T>
+__device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, const Where& w, f32x16 (&acc)[T::TC][T::TR]) {
+    const int d0 = w.c * T::BC + t.wc * T::TC * 32;
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        t.template put<T::TC>([&](int i, int g) { return f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]}; });
+        t.template take<T::TC, float>(j, a.D - d0, [&](int r) {
+            const int at = w.r * T::BR + r;
+            return at < w.count ? a.part + size_t(w.first + at) * a.D + d0 : nullptr;
+        });
+    }
+}
+// rows of the pairs of this tile, `bytes` each, one after the other
+template <typename T>
+__device__ __forceinline__ void start_pairs(T& t, const void* rows, const Where& w, uint32_t bytes) {
+    t.r.start_rows(static_cast<const char*>(rows) + size_t(w.first + w.r * T::BR) * bytes, t.wave, t.lane,
+                   [&](int i) { return w.r * T::BR + i < w.count ? uint32_t(i) * bytes : kBeyond; });
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::THREADS) void k_down(ExpertArgs a) {
+    typedef typename T::TIO TIO;
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    Where w;
+    if (!find_tile<T::BR>(a, (a.D + T::BC - 1) / T::BC, w)) return;
+    T t(shared);
+    const uint32_t bytes = uint32_t(a.F) * uint32_t(sizeof(TIO));
+    start_pairs(t, a.h, w, bytes);
+    t.c.start_rows(static_cast<const TIO*>(a.w_down) + size_t(w.e) * a.D * a.F, t.wave, t.lane, [&](int q) {
+        const int d = w.c * T::BC + q;
+        return d < a.D ? uint32_t(d) * bytes : kBeyond;
+    });
+    f32x16 acc[T::TC][T::TR];
+    clear<T>(acc);
+    t.walk(acc, a.F);
+    finish_part(t, a, w, acc);
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::THREADS) void k_dx(ExpertArgs a) {
+    typedef typename T::TIO TIO;
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    Where w;
+    if (!find_tile<T::BR>(a, (a.D + T::BC - 1) / T::BC, w)) return;
+    T t(shared);
+    start_pairs(t, a.da, w, 2 * uint32_t(a.F) * uint32_t(sizeof(TIO)));
+    t.c.start_cols(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, a.D * int(sizeof(TIO)), w.c * T::BC, a.D, t.wave, t.lane, 0);
+    f32x16 acc[T::TC][T::TR];
+    clear<T>(acc);
+    t.walk(acc, 2 * a.F);
+    finish_part(t, a, w, acc);
+}
+
+// H: the products of gate and factor; T: that of dy with the columns of Wd for the same features.
+template <typename H, typename T>
+__global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
+    typedef typename T::TIO TIO;
+    static_assert(H::TC == 2 * T::TC && H::TR == T::TR && H::WC == T::WC && H::WR == T::WR, "the same features in the same lanes");
+    __shared__ __attribute__((aligned(1024))) char shared[H::LDS > T::LDS ? H::LDS : T::LDS];
+    Where w;
+    if (!find_tile<T::BR>(a, (a.F + T::BC - 1) / T::BC, w)) return;
+    f32x16 gu[H::TC][H::TR], tt[T::TC][T::TR];
+    {
+        H t(shared);
+        start_gate_up(t, a, w);
+        clear<H>(gu);
+        t.walk(gu, a.D);
+    }
+    T t(shared);
+    t.r.start_rows(a.d_y, t.wave, t.lane, [&](int i) {
+        const int at = w.r * T::BR + i;
+        return at < w.count ? token_of(a, w.first + at) * a.dy_bytes : kBeyond;
+    });
+    t.c.start_cols(static_cast<const TIO*>(a.w_down) + size_t(w.e) * a.D * a.F, a.F * int(sizeof(TIO)), w.c * T::BC, a.F, t.wave, t.lane, 0);
+    clear<T>(tt);
+    t.walk(tt, a.D);
+    const int f0 = w.c * T::BC + t.wc * T::TC * 32;
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        const int at = w.r * T::BR + t.row(j);
+        const float p = at < w.count ? a.weights[pair_of(a, w.first + at)] : 0.f;
+        float along = 0.f;
+        _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+            _Pragma("unroll") for (int r = 0; r < 16; ++r) {
+                const float gate = gu[i][j][r], up = gu[i + T::TC][j][r], d = tt[i][j][r];
+                const float sig = 1.f / (1.f + expf(-gate)), s = gate * sig, h = s * up, dh = p * d;
+                along += d * h;
+                gu[i][j][r] = dh * up * (sig + s * (1.f - sig));
+                gu[i + T::TC][j][r] = dh * s;
+                tt[i][j][r] = p * h;
+            }
+        along += __shfl_xor(along, 32, 64);
+        if (t.lane < 32 && at < w.count) a.weight_part[size_t(w.c * T::WC + t.wc) * (size_t(a.n) * a.top_k) + w.first + at] = along;
+        const auto line = [&](void* base, int length, int shift) {
+            return [=, &w](int r) {
+                const int q = w.r * T::BR + r;
+                return q < w.count ? static_cast<TIO*>(base) + size_t(w.first + q) * length + shift + f0 : nullptr;
+            };
+        };
+        _Pragma("unroll") for (int half = 0; half < 2; ++half) {
+            t.template put<T::TC>([&](int i, int g) {
+                const f32x16& v = gu[half * T::TC + i][j];
+                return f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+            });
+            t.template take<T::TC, TIO>(j, a.F - f0, line(a.da, 2 * a.F, half * a.F));
+        }
+        t.template put<T::TC>([&](int i, int g) { return f32x4{tt[i][j][4 * g], tt[i][j][4 * g + 1], tt[i][j][4 * g + 2], tt[i][j][4 * g + 3]}; });
+        t.template take<T::TC, TIO>(j, a.F - f0, line(a.h, a.F, 0));
+    }
+}
+
+// DOWN: d_w_down [D][F] = sum over the expert's pairs of dy (rows) and weighted activations (columns); else d_w_gate_up [2 F][D] of the
+// gradients of gate and factor (rows) and x (columns).
+template <typename T, bool DOWN>
+__global__ __launch_bounds__(T::THREADS) void k_dw(ExpertArgs a, int row_tiles, int col_tiles) {
+    typedef typename T::TIO TIO;
+    constexpr int EL = int(sizeof(TIO));
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    const int all = a.E * row_tiles * col_tiles, die = (all + 7) / 8, slot = int(blockIdx.x) / 8, id = (int(blockIdx.x) % 8) * die + slot;
+    if (slot >= die || id >= all) return;
+    const int e = id / (row_tiles * col_tiles), rest = id - e * row_tiles * col_tiles, c = rest / row_tiles, r0 = rest - c * row_tiles;
+    const int first = uniform(offset_of(a, e)), count = max(uniform(offset_of(a, e + 1)) - first, 0);
+    const int rows = DOWN ? a.D : 2 * a.F, cols = DOWN ? a.F : a.D;
+    T t(shared);
+    if (DOWN) {
+        t.r.start_cols(a.d_y, int(a.dy_bytes), r0 * T::BR, rows, t.wave, t.lane, t.list_at());
+        t.c.start_cols(static_cast<const TIO*>(a.h) + size_t(first) * a.F, a.F * EL, c * T::BC, cols, t.wave, t.lane, 0);
+    } else {
+        t.r.start_cols(static_cast<const TIO*>(a.da) + size_t(first) * 2 * a.F, 2 * a.F * EL, r0 * T::BR, rows, t.wave, t.lane, 0);
+        t.c.start_cols(a.x, int(a.x_bytes), c * T::BC, cols, t.wave, t.lane, t.list_at());
+    }
+    f32x16 acc[T::TC][T::TR];
+    clear<T>(acc);
+    t.walk(acc, count, [&](int k) { return token_of(a, first + k); });
+    TIO* out = static_cast<TIO*>(DOWN ? a.d_w_down : a.d_w_gate_up) + size_t(e) * rows * cols;
+    const int c0 = c * T::BC + t.wc * T::TC * 32;
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        t.template put<T::TC>([&](int i, int g) { return f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]}; });
+        t.template take<T::TC, TIO>(j, cols - c0, [&](int r) {
+            const int row = r0 * T::BR + r;
+            return row < rows ? out + size_t(row) * cols + c0 : nullptr;
+        });
+    }
+}
+
+// Four (fp32) or eight (bf16) neighbouring elements of a token; WEIGHTED: forward.
+template <typename TIO, bool WEIGHTED>
+__global__ __launch_bounds__(256) void k_sum(ExpertArgs a) {
+    constexpr int E = kPiece<TIO>;
+    const int pieces = a.D / E;
+    const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (!WEIGHTED && id < int64_t(a.n) * a.top_k) {
+        const int at = a.place[id];
+        float s = 0.f;
+        if (uint32_t(at) < uint32_t(a.n * a.top_k))
+            for (int b = 0; b < a.parts; ++b) s += a.weight_part[size_t(b) * (size_t(a.n) * a.top_k) + at];
+        a.d_weights[id] = s;
+    }
+    if (id >= int64_t(a.n) * pieces) return;
+    const int t = int(id / pieces), d = int(id - int64_t(t) * pieces) * E;
+    float s[E];
+    if (WEIGHTED && a.residual) unpack(*reinterpret_cast<const u32x4*>(static_cast<const TIO*>(a.residual) + size_t(t) * a.D + d), s);
+    else _Pragma("unroll") for (int e = 0; e < E; ++e) s[e] = 0.f;
+    for (int j = 0; j < a.top_k; ++j) {
+        const int at = a.place[size_t(t) * a.top_k + j];
+        if (uint32_t(at) >= uint32_t(a.n * a.top_k)) continue;
+        const float p = WEIGHTED ? a.weights[size_t(t) * a.top_k + j] : 1.f;
+        const f32x4* z = reinterpret_cast<const f32x4*>(a.part + size_t(at) * a.D + d);
+        _Pragma("unroll") for (int q = 0; q < E / 4; ++q) {
+            const f32x4 v = z[q];
+            _Pragma("unroll") for (int e = 0; e < 4; ++e) s[4 * q + e] += p * v[e];
+        }
+    }
+    *reinterpret_cast<u32x4*>(static_cast<TIO*>(a.y) + size_t(t) * a.D + d) = pack(s);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+int check(const lsm_experts_params* p, bool backward) {
+    if (!p) return LSM_ERR_NULL;
+    if (p->struct_size != sizeof(lsm_experts_params)) return LSM_ERR_SHAPE;
+    if (p->n < 1 || p->D < 1 || p->F < 1 || p->E < 1 || p->top_k < 1 || p->top_k > p->E) return LSM_ERR_SHAPE;
+    if (p->dtype != LSM_DTYPE_F32 && p->dtype != LSM_DTYPE_BF16) return LSM_ERR_UNSUPPORTED;
+    if (p->E > kMostExperts || p->top_k > kMostTop || p->D % 8 || p->F % 8 || p->D > 65536 || p->F > 65536 || p->reserved != 0)
+        return LSM_ERR_UNSUPPORTED;
+    const int64_t el = p->dtype == LSM_DTYPE_BF16 ? 2 : 4;
+    if (int64_t(p->n) * p->top_k > kMostPairs || 2 * int64_t(p->F) * p->D * el >= int64_t(kBeyond)) return LSM_ERR_SHAPE;
+    for (const int64_t s : {p->x_stride, backward ? p->dy_stride : int64_t(p->x_stride)}) {
+        if (s < p->D || s > (int64_t(1) << 31) || p->n * s * el >= int64_t(kBeyond)) return LSM_ERR_SHAPE;
+        if (s % 8) return LSM_ERR_ALIGN;
+    }
+    return LSM_OK;
+}
+
+// Tiles of 256 columns; rows by the pairs of an expert.
+template <typename TIO, Layout LC, Layout LR, int BR> struct TileOf;
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 256> { typedef Tile<TIO, LC, LR, 2, 4, 4, 2, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 128> { typedef Tile<TIO, LC, LR, 4, 2, 2, 2, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 64> { typedef Tile<TIO, LC, LR, 4, 1, 2, 2, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 32> { typedef Tile<TIO, LC, LR, 4, 1, 2, 1, 4> type; };
+template <typename TIO, int BR> struct HalfTileOf;  // the same rows, half the columns
+template <typename TIO> struct HalfTileOf<TIO, 256> { typedef Tile<TIO, BY_COLS, BY_ROWS, 2, 4, 2, 2, 4> type; };
+template <typename TIO> struct HalfTileOf<TIO, 128> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 2, 1, 2, 4> type; };
+template <typename TIO> struct HalfTileOf<TIO, 64> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 1, 2, 4> type; };
+template <typename TIO> struct HalfTileOf<TIO, 32> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 1, 1, 4> type; };
+
+int rows_of_tile(const lsm_experts_params& p) {
+    const int64_t mean = int64_t(p.n) * p.top_k / p.E;
+    return mean >= 192 ? 256 : mean >= 56 ? 128 : mean >= 28 ? 64 : 32;
+}
+int weight_parts(const lsm_experts_params& p) {  // waves along the features
+    const int br = rows_of_tile(p), wc = br == 256 ? 2 : 4;
+    return (p.F + 127) / 128 * wc;
+}
+// The most tiles there can be: every expert's last one may be almost empty.
+unsigned grid_of(const lsm_experts_params& p, int br, int cols) {
+    const int64_t pairs = int64_t(p.n) * p.top_k, tiles = pairs / br + (pairs < p.E ? pairs : int64_t(p.E));
+    return unsigned((tiles * cols + 7) / 8 * 8);
+}
+
+struct Space { size_t h, da, part, weight_part, bytes; };
+Space space(const lsm_experts_params& p, bool backward) {
+    const size_t pairs = size_t(p.n) * p.top_k, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4;
+    Space s{};
+    s.h = 0;
+    s.part = align256(pairs * p.F * el);
+    s.da = s.part + align256(pairs * p.D * 4);
+    s.weight_part = s.da + (backward ? align256(pairs * 2 * p.F * el) : 0);
+    s.bytes = s.weight_part + (backward ? align256(pairs * weight_parts(p) * 4) : 0);
+    return s;
+}
+
+template <typename TIO, bool WEIGHTED>
+bool launch_sum(const ExpertArgs& a, hipStream_t st) {
+    int64_t items = int64_t(a.n) * (a.D / kPiece<TIO>);
+    if (!WEIGHTED && items < int64_t(a.n) * a.top_k) items = int64_t(a.n) * a.top_k;
+    ProfScope ps(KID_EXPERTS_SUM, st);
+    hipLaunchKernelGGL((k_sum<TIO, WEIGHTED>), dim3(unsigned((items + 255) / 256)), dim3(256), 0, st, a);
+    return launched();
+}
+
+template <typename TIO, int BR>
+bool launch_fwd(const lsm_experts_params& p, const ExpertArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type T;
+    {
+        ProfScope ps(KID_EXPERTS_UP, st);
+        hipLaunchKernelGGL((k_up<T>), dim3(grid_of(p, BR, (a.F + T::BC / 2 - 1) / (T::BC / 2))), dim3(T::THREADS), 0, st, a);
+    }
+    if (!launched()) return false;
+    {
+        ProfScope ps(KID_EXPERTS_DOWN, st);
+        hipLaunchKernelGGL((k_down<T>), dim3(grid_of(p, BR, (a.D + T::BC - 1) / T::BC)), dim3(T::THREADS), 0, st, a);
+    }
+    return launched() && launch_sum<TIO, true>(a, st);
+}
+
+template <typename T, bool DOWN>
+bool launch_dw(const ExpertArgs& a, hipStream_t st) {
+    const int rows = DOWN ? a.D : 2 * a.F, cols = DOWN ? a.F : a.D, rt = (rows + T::BR - 1) / T::BR, ct = (cols + T::BC - 1) / T::BC;
+    ProfScope ps(KID_EXPERTS_DW, st);
+    hipLaunchKernelGGL((k_dw<T, DOWN>), dim3(unsigned((int64_t(a.E) * rt * ct + 7) / 8 * 8)), dim3(T::THREADS), 0, st, a, rt, ct);
+    return launched();
+}
+template <typename TIO, int BR>
+bool launch_bwd(const lsm_experts_params& p, const ExpertArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type H;
+    typedef typename HalfTileOf<TIO, BR>::type T;
+    {
+        ProfScope ps(KID_EXPERTS_HIDDEN_GRAD, st);
+        hipLaunchKernelGGL((k_hidden_grad<H, T>), dim3(grid_of(p, BR, (a.F + T::BC - 1) / T::BC)), dim3(T::THREADS), 0, st, a);
+    }
+    if (!launched()) return false;
+    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, BR>::type X;
+    {
+        ProfScope ps(KID_EXPERTS_DX, st);
+        hipLaunchKernelGGL((k_dx<X>), dim3(grid_of(p, BR, (a.D + X::BC - 1) / X::BC)), dim3(X::THREADS), 0, st, a);
+    }
+    if (!launched() || !launch_sum<TIO, false>(a, st)) return false;
+    if (!a.d_w_down) return true;
+    return launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 4, 2, 4, true, false>, false>(a, st) &&
+           launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 4, 2, 4, false, true>, true>(a, st);
+}
+
+template <typename TIO>
+bool launch(const lsm_experts_params& p, const ExpertArgs& a, bool backward, hipStream_t st) {
+    switch (rows_of_tile(p)) {
+        case 256: return backward ? launch_bwd<TIO, 256>(p, a, st) : launch_fwd<TIO, 256>(p, a, st);
+        case 128: return backward ? launch_bwd<TIO, 128>(p, a, st) : launch_fwd<TIO, 128>(p, a, st);
+        case 64: return backward ? launch_bwd<TIO, 64>(p, a, st) : launch_fwd<TIO, 64>(p, a, st);
+        default: return backward ? launch_bwd<TIO, 32>(p, a, st) : launch_fwd<TIO, 32>(p, a, st);
+    }
+}
+
+}  // namespace
+}  // namespace lsm
+
+extern "C" {
+
+size_t lsm_moe_experts_workspace_bytes(const lsm_experts_params* p) {
+    using namespace lsm;
+    return check(p, false) == LSM_OK ? space(*p, false).bytes : 0;
+}
+size_t lsm_moe_experts_bwd_workspace_bytes(const lsm_experts_params* p) {
+    using namespace lsm;
+    return check(p, true) == LSM_OK ? space(*p, true).bytes : 0;
+}
+
+int lsm_moe_experts(const lsm_experts_params* p, const void* x, const float* weights, const int32_t* offsets, const int32_t* order,
+                    const int32_t* place, const void* w_gate_up, const void* w_down, const void* residual, void* y,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace lsm;
+    const int rc = check(p, false);
+    if (rc != LSM_OK) return rc;
+    if (!x || !weights || !offsets || !order || !place || !w_gate_up || !w_down || !y) return LSM_ERR_NULL;
+    for (const void* q : {x, static_cast<const void*>(weights), static_cast<const void*>(offsets), static_cast<const void*>(order),
+                          static_cast<const void*>(place), w_gate_up, w_down, residual, static_cast<const void*>(y), static_cast<const void*>(workspace)})
+        if (misaligned(q)) return LSM_ERR_ALIGN;
+    const Space s = space(*p, false);
+    if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    const uint32_t el = p->dtype == LSM_DTYPE_BF16 ? 2 : 4;
+    ExpertArgs a{};
+    a.x = x; a.w_gate_up = w_gate_up; a.w_down = w_down; a.residual = residual; a.weights = weights;
+    a.offsets = offsets; a.order = order; a.place = place; a.y = y;
+    a.h = ws + s.h; a.part = reinterpret_cast<float*>(ws + s.part);
+    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k;
+    a.x_bytes = uint32_t(p->x_stride) * el;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return (el == 2 ? launch<uint16_t>(*p, a, false, st) : launch<float>(*p, a, false, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+}
+
+int lsm_moe_experts_bwd(const lsm_experts_params* p, const void* x, const float* weights, const int32_t* offsets,
+                        const int32_t* order, const int32_t* place, const void* w_gate_up, const void* w_down, const void* d_y,
+                        void* dx, float* d_weights, void* d_w_gate_up, void* d_w_down,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace lsm;
+    const int rc = check(p, true);
+    if (rc != LSM_OK) return rc;
+    if (!x || !weights || !offsets || !order || !place || !w_gate_up || !w_down || !d_y || !dx || !d_weights || !d_w_gate_up != !d_w_down)
+        return LSM_ERR_NULL;
+    for (const void* q : {x, static_cast<const void*>(weights), static_cast<const void*>(offsets), static_cast<const void*>(order),
+                          static_cast<const void*>(place), w_gate_up, w_down, d_y, static_cast<const void*>(dx), static_cast<const void*>(d_weights),
+                          static_cast<const void*>(d_w_gate_up), static_cast<const void*>(d_w_down), static_cast<const void*>(workspace)})
+        if (misaligned(q)) return LSM_ERR_ALIGN;
+    const Space s = space(*p, true);
+    if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    const uint32_t el = p->dtype == LSM_DTYPE_BF16 ? 2 : 4;
+    ExpertArgs a{};
+    a.x = x; a.w_gate_up = w_gate_up; a.w_down = w_down; a.d_y = d_y; a.weights = weights;
+    a.offsets = offsets; a.order = order; a.place = place; a.y = dx; a.d_weights = d_weights;
+    a.d_w_gate_up = d_w_gate_up; a.d_w_down = d_w_down;
+    a.h = ws + s.h; a.part = reinterpret_cast<float*>(ws + s.part);
+    a.da = ws + s.da; a.weight_part = reinterpret_cast<float*>(ws + s.weight_part);
+    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k; a.parts = weight_parts(*p);
+    a.x_bytes = uint32_t(p->x_stride) * el;
+    a.dy_bytes = uint32_t(p->dy_stride) * el;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return (el == 2 ? launch<uint16_t>(*p, a, true, st) : launch<float>(*p, a, true, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -151,7 +151,9 @@ enum KernelId {
     KID_GEN_STATE = 0, KID_GEN_SCAN, KID_GEN_OUTPUT, KID_GEN_DG, KID_GEN_GRAD,
     KID_HEAD_REDUCE, KID_MFMA_STATE, KID_MFMA_OUTPUT, KID_MFMA_STATE_BWD, KID_MFMA_DSTATE, KID_MFMA_GRAD, KID_MFMA_PREP, KID_MFMA_VEC_PREP, KID_MFMA_VEC_DV, KID_STEP,
     KID_WALK_SUMMARY, KID_WALK_SCAN, KID_WALK_FWD, KID_WALK_GRAD, KID_DELTA_PREP, KID_DELTA_WALK, KID_DELTA_RWALK, KID_DELTA_SUMMARY, KID_DELTA_COMBINE,
-    KID_QK, KID_QK_BWD, KID_QK_WEIGHTS, KID_BEAM_SLICES, KID_BEAM_MERGE, KID_REORDER, KID_MOE_ROUTER, KID_MOE_GATE_UP, KID_MOE_DOWN, KID_MOE_SUM, KID_COUNT
+    KID_QK, KID_QK_BWD, KID_QK_WEIGHTS, KID_BEAM_SLICES, KID_BEAM_MERGE, KID_REORDER, KID_MOE_ROUTER, KID_MOE_GATE_UP, KID_MOE_DOWN, KID_MOE_SUM,
+    KID_ROUTE, KID_PLAN, KID_EXPERTS_UP, KID_EXPERTS_DOWN, KID_EXPERTS_HIDDEN_GRAD, KID_EXPERTS_DX, KID_EXPERTS_DW, KID_EXPERTS_SUM,
+    KID_VOCAB_ROWS, KID_VOCAB_LOGITS, KID_VOCAB_JOIN, KID_VOCAB_GRAD, KID_VOCAB_DX, KID_VOCAB_DW, KID_COUNT
 };
 // Bracket a kernel launch with events when timing is switched on (no-ops otherwise).
 void prof_begin(int kernel_id, hipStream_t stream);

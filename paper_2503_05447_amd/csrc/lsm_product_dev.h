@@ -1,0 +1,273 @@
+// Matrix products of the training operators (lsm_train.h): one workgroup forms a tile out[r][c] = sum_k R[r][k] C[c][k], the c
+// of which lie next to each other in memory, with either operand by rows ([i][k], k contiguous) or by columns ([k][i], i
+// contiguous), rows taken through a list where one is given.
+//
+// The product is formed as C R^T: c is the first operand of the 32 x 32 matrix instructions, so that a lane holds one row r and four
+// neighbouring c's in four registers, and what is done along a row (maximum, sum, gate with factor) stays in the lane.
+//
+// Pieces of 64 bytes of k a row (32 of bf16, 16 of fp32) go straight from memory into LDS, NBUF of them in a ring, 16 bytes a lane;
+// a lane that has nothing to load (behind the last row, behind the last k) asks beyond the buffer's bound and gets zeros.
+// Where a lane's 16 bytes land is fixed by the hardware (one after the other), so rows are spread over the banks by which
+// 16 bytes of the row a lane asks for: slot s of row i holds piece s ^ f(i).
+//
+// Within a step t the operands of the next half step are read while the matrix instructions of this one run, across the barrier
+// too: piece t + 1 is complete before step t begins, and piece t + NBUF - 1 is requested in it.
+#pragma once
+#include "lsm_block_dev.h"
+
+namespace lsm {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t kBeyond = 0xfffff000u;  // offset and size of a buffer: at or behind it nothing is read and zeros come
+constexpr int kStepBytes = 64;             // of k, a row and step
+
+enum Layout { BY_ROWS, BY_COLS };
+
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+__device__ __forceinline__ void fence_schedule() { __builtin_amdgcn_sched_barrier(0); }
+
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+    return uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(x))))) |
+           uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(x >> 32))))) << 32;
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// 16 bytes a lane from base + offset to LDS address `to` + 16 lane.  `base` and `to` are the same in all lanes.  (In assembly, so that the
+// waits are those written below and not one for every read of LDS.  m0 is set and used here; nothing else in these kernels
+// holds a value in it: no register is indexed by a variable.)
+__device__ __forceinline__ void load_to_lds(uint64_t base, uint32_t offset, uint32_t to) {
+    const uint64_t from = uniform(base);
+    const u32x4 buffer = {uint32_t(from), uint32_t(from >> 32) & 0xffffu, kBeyond, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer)
+                 : "memory");
+}
+// One half step of a 32 x 32 product.
+__device__ __forceinline__ f32x16 product(const u32x4& a, const u32x4& b, f32x16 c, uint16_t) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 product(const u32x4& a, const u32x4& b, f32x16 c, float) {
+    _Pragma("unroll") for (int i = 0; i < 4; ++i)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+    return c;
+}
+
+typedef __attribute__((address_space(3))) char* lds_t;
+
+// N rows of an operand and a step's k of each, as a workgroup of WAVES waves brings them to LDS and reads them.
+template <typename TIO, Layout L, int N, int WAVES, bool LISTED>
+struct Operand {
+    static constexpr int EL = int(sizeof(TIO)), KSTEP = kStepBytes / EL, BYTES = N * kStepBytes;
+    static constexpr int PIECES = N / 16, LOADS = PIECES >= WAVES ? PIECES / WAVES : 1;  // 1 KiB a load; of a wave
+    static_assert(N % 32 == 0 && (PIECES % WAVES == 0 || WAVES % PIECES == 0), "even shares");
+    static constexpr int LINE = L == BY_ROWS ? kStepBytes : N * EL;   // bytes of a line in LDS
+    static constexpr int LANES = LINE / 16, LINES = 64 / LANES;       // lanes of a line, lines of a load
+    // by columns: which 16 bytes of its line k a slot holds
+    static __device__ __forceinline__ int turn(int k) { return EL == 4 || LINE < 128 ? 0 : LINE >= 256 ? 4 * (k & 3) : 4 * ((k >> 1) & 1); }
+
+    uint64_t base;
+    uint32_t off[LOADS];
+    int row_bytes;
+    int list;  // LDS address of the list of rows (LISTED, by columns)
+
+    __device__ __forceinline__ static int piece(int wave, int j) { return (wave * LOADS + j) % PIECES; }
+    // the row (by rows) or the first of eight (four) neighbouring ones (by columns) that load j of this lane brings
+    __device__ __forceinline__ static int mine(int wave, int lane, int j) {
+        if (L == BY_ROWS) return piece(wave, j) * LINES + lane / LANES;
+        return ((lane % LANES) ^ turn(line(wave, lane, j))) * (16 / EL);
+    }
+    __device__ __forceinline__ static int line(int wave, int lane, int j) { return piece(wave, j) * LINES + lane / LANES; }
+    __device__ __forceinline__ static int k_piece(int lane) { return (lane & 3) ^ ((lane >> 3) & 3); }
+
+    // By rows: row_at(i) is the row's offset in bytes from `from` (kBeyond: none) for i of the tile.
+    template <typename RowAt>
+    __device__ __forceinline__ void start_rows(const void* from, int wave, int lane, RowAt row_at) {
+        base = uniform(reinterpret_cast<uint64_t>(from));
+        _Pragma("unroll") for (int j = 0; j < LOADS; ++j) {
+            const uint32_t at = row_at(mine(wave, lane, j));
+            off[j] = at == kBeyond ? kBeyond : at + 16 * k_piece(lane);
+        }
+    }
+    // By columns: columns first .. first + N of [k][..] rows of `stride` bytes, `width` columns in all.
+    __device__ __forceinline__ void start_cols(const void* from, int stride, int first, int width, int wave, int lane, int rows_at) {
+        base = uniform(reinterpret_cast<uint64_t>(from)) + uint64_t(first) * EL;
+        row_bytes = stride;
+        list = rows_at;
+        _Pragma("unroll") for (int j = 0; j < LOADS; ++j) {
+            const int c = mine(wave, lane, j);
+            off[j] = first + c < width ? uint32_t(c * EL) + (LISTED ? 0u : uint32_t(line(wave, lane, j)) * uint32_t(stride)) : kBeyond;
+        }
+    }
+    // Request the pieces of step `step` of `K` k's; nothing behind the last.
+    __device__ __forceinline__ void request(uint32_t to, int step, int K, int wave, int lane) {
+        const int k0 = step * KSTEP;
+        _Pragma("unroll") for (int j = 0; j < LOADS; ++j) {
+            uint32_t o = off[j];
+            if (L == BY_ROWS) {
+                if (k0 + k_piece(lane) * (16 / EL) >= K) o = kBeyond;
+                load_to_lds(base + uint64_t(k0) * EL, o, uniform(int(to + piece(wave, j) * 1024)));
+            } else {
+                const int k = k0 + line(wave, lane, j);
+                if (LISTED) {
+                    const uint32_t row = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(list + 4 * (k % kList)));
+                    o = o == kBeyond ? kBeyond : o + row * uint32_t(row_bytes);
+                }
+                if (k >= K) o = kBeyond;
+                load_to_lds(LISTED ? base : base + uint64_t(k0) * uint64_t(uint32_t(row_bytes)), o, uniform(int(to + piece(wave, j) * 1024)));
+            }
+        }
+    }
+    static constexpr int kList = 2048;  // rows of a list that are in LDS at a time
+
+    // Rows first .. first + 32 of half step `half_step` as an operand: lane l holds row l % 32, 16 bytes of k from l / 32 on.
+    __device__ __forceinline__ static u32x4 read(uint32_t at, int first, int half_step, int lane) {
+        const int half = lane >> 5;
+        if (L == BY_ROWS) {
+            const int x = (lane >> 1) & 3;
+            return *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(
+                uintptr_t(at + first * kStepBytes + (lane & 31) * kStepBytes + (((2 * half_step + half) ^ x) * 16)));
+        }
+        if (EL == 4) {
+            u32x4 v;
+            _Pragma("unroll") for (int i = 0; i < 4; ++i)
+                v[i] = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(
+                    uintptr_t(at + (8 * half_step + 4 * half + i) * LINE + (first + (lane & 31)) * 4));
+            return v;
+        }
+        const int r = lane & 15, k = 16 * half_step + 8 * half + (r >> 2);
+        const int slot = ((first >> 3) + 2 * ((lane >> 4) & 1) + ((r >> 1) & 1)) ^ turn(r >> 2);
+        const uint32_t p = at + k * LINE + slot * 16 + 8 * (r & 1);
+        typedef s16x4 __attribute__((address_space(3))) * tr_t;
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(uintptr_t(p))));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(uintptr_t(p + 4 * LINE))));
+        return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+};
+
+// A tile: WC x WR waves of TC x TR blocks of 32 x 32.
+template <typename TIO_, Layout LC, Layout LR, int WC_, int WR_, int TC_, int TR_, int NBUF_, bool LIST_C = false, bool LIST_R = false>
+struct Tile {
+    typedef TIO_ TIO;
+    static constexpr int WC = WC_, WR = WR_, TC = TC_, TR = TR_, NBUF = NBUF_, WAVES = WC * WR, THREADS = 64 * WAVES;
+    static constexpr int BC = WC * TC * 32, BR = WR * TR * 32;
+    typedef Operand<TIO, LC, BC, WAVES, LIST_C> C;
+    typedef Operand<TIO, LR, BR, WAVES, LIST_R> R;
+    static constexpr int STAGE = C::BYTES + R::BYTES, LOADS = C::LOADS + R::LOADS, AHEAD = NBUF - 1;
+    static constexpr int LIST = LIST_C || LIST_R ? 4 * C::kList : 0;
+    // results on their way out: 32 rows of a wave's blocks at a time, in fp32, padded by 16 bytes a row; each wave has its own place
+    static constexpr int OUT = 32 * (TC * 128 + 16), RING = NBUF * STAGE;
+    static constexpr int LDS = (RING > WAVES * OUT ? RING : WAVES * OUT) + LIST;
+    static_assert(LDS <= 160 * 1024 && NBUF >= 3, "LDS");
+
+    C c;
+    R r;
+    int wave, lane, wc, wr;
+    uint32_t lds;
+
+    __device__ __forceinline__ Tile(const char* shared) {
+        wave = uniform(int(threadIdx.x >> 6));
+        lane = threadIdx.x & 63;
+        wc = wave % WC;
+        wr = wave / WC;
+        lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)shared));
+    }
+    __device__ __forceinline__ uint32_t list_at() const { return lds + (LDS - LIST); }
+    __device__ __forceinline__ void request(int step, int K) {
+        const uint32_t at = lds + uint32_t(step % NBUF) * STAGE;
+        c.request(at, step, K, wave, lane);
+        r.request(at + C::BYTES, step, K, wave, lane);
+    }
+    __device__ __forceinline__ void read(u32x4 (&a)[TC], u32x4 (&b)[TR], int step, int half_step) const {
+        const uint32_t at = lds + uint32_t(step % NBUF) * STAGE;
+        _Pragma("unroll") for (int i = 0; i < TC; ++i) a[i] = C::read(at, (wc * TC + i) * 32, half_step, lane);
+        _Pragma("unroll") for (int j = 0; j < TR; ++j) b[j] = R::read(at + C::BYTES, (wr * TR + j) * 32, half_step, lane);
+    }
+    static __device__ __forceinline__ void multiply(f32x16 (&acc)[TC][TR], const u32x4 (&a)[TC], const u32x4 (&b)[TR]) {
+        _Pragma("unroll") for (int j = 0; j < TR; ++j)
+            _Pragma("unroll") for (int i = 0; i < TC; ++i) acc[i][j] = product(a[i], b[j], acc[i][j], TIO());
+    }
+    // The rows of k0 .. k0 + n - 1 for an operand that is taken through a list.
+    template <typename RowOf>
+    __device__ __forceinline__ void fill(RowOf row_of, int k0, int n, int K) const {
+        for (int k = k0 + int(threadIdx.x); k < min(k0 + n, K); k += THREADS)
+            *reinterpret_cast<__attribute__((address_space(3))) uint32_t*>(uintptr_t(list_at() + 4 * (k % C::kList))) = row_of(k);
+    }
+    __device__ __forceinline__ void walk(f32x16 (&acc)[TC][TR], int K) {
+        walk(acc, K, [](int) { return 0u; });
+    }
+    // acc += the product over k = 0 .. K - 1; row_of(k): the row of k in a list.  Begins and ends with LDS free.
+    template <typename RowOf>
+    __device__ __forceinline__ void walk(f32x16 (&acc)[TC][TR], int K, RowOf row_of) {
+        const int steps = (K + C::KSTEP - 1) / C::KSTEP;
+        if (steps == 0) return;
+        if (LIST) {
+            fill(row_of, 0, C::kList, K);
+            wait_lds();
+            barrier();
+        }
+        u32x4 a0[TC], b0[TR], a1[TC], b1[TR];
+        _Pragma("unroll") for (int s = 0; s < AHEAD; ++s) request(s, K);
+        wait_loads<(AHEAD - 2) * LOADS>();
+        barrier();
+        read(a0, b0, 0, 0);
+        for (int t = 0; t < steps; ++t) {
+            fence_schedule();
+            if (LIST) {  // the next half of the list, a step before its first row is wanted; the half that it replaces is used up
+                const int k = (t + AHEAD + 1) * C::KSTEP;
+                if (k >= C::kList && k % (C::kList / 2) == 0) fill(row_of, k, C::kList / 2, K);
+            }
+            request(t + AHEAD, K);
+            read(a1, b1, t, 1);
+            multiply(acc, a0, b0);
+            fence_schedule();
+            wait_lds();  // nothing of piece t is on its way any more: it may be overwritten behind the barrier
+            read(a0, b0, t + 1, 0);
+            multiply(acc, a1, b1);
+            fence_schedule();
+            wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
+            barrier();
+        }
+        wait_lds();
+        wait_loads<0>();
+        barrier();
+    }
+    // Values of block (i, j): register 4 g + e of a lane is row(j), column col(i, g) + e of the tile.
+    __device__ __forceinline__ int row(int j) const { return (wr * TR + j) * 32 + (lane & 31); }
+    __device__ __forceinline__ int col(int i, int g) const { return (wc * TC + i) * 32 + 8 * g + 4 * (lane >> 5); }
+
+    // Results to memory, whole lines at a time: block j of this wave's rows goes through the wave's own place in LDS (the caller has
+    // seen to it that LDS is free) and leaves in 16-byte pieces.  value(i, g): four results of block i < NB; line(r): where row r of
+    // the tile goes, first column of this wave included, or null; width: columns that there are from that column on.
+    __device__ __forceinline__ uint32_t own_place() const { return lds + uint32_t(wave) * OUT; }
+    template <int NB> __device__ __forceinline__ uint32_t cell(int row32, int column) const {
+        return own_place() + uint32_t(row32) * (NB * 128 + 16) + uint32_t(column) * 4;
+    }
+    template <int NB, typename Value>
+    __device__ __forceinline__ void put(Value value) const {
+        _Pragma("unroll") for (int i = 0; i < NB; ++i)
+            _Pragma("unroll") for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<NB>(lane & 31, i * 32 + 8 * g + 4 * (lane >> 5)))) = value(i, g);
+    }
+    template <int NB, typename TOUT, typename Line>
+    __device__ __forceinline__ void take(int j, int width, Line line) const {
+        constexpr int E = 16 / int(sizeof(TOUT)), LANES = NB * 32 / E, ROWS = 64 / LANES;
+        _Pragma("unroll") for (int it = 0; it < 32 / ROWS; ++it) {
+            const int row = it * ROWS + lane / LANES, c = (lane % LANES) * E;
+            float v[E];
+            _Pragma("unroll") for (int q = 0; q < E / 4; ++q) {
+                const f32x4 x = *reinterpret_cast<__attribute__((address_space(3))) const f32x4*>(uintptr_t(cell<NB>(row, c + 4 * q)));
+                _Pragma("unroll") for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
+            }
+            TOUT* to = line((wr * TR + j) * 32 + row);
+            if (to && c < width) *reinterpret_cast<u32x4*>(to + c) = pack(v);
+        }
+    }
+};
+
+}  // namespace
+}  // namespace lsm
