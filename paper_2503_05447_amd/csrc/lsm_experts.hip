@@ -68,13 +68,6 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int cols, Where& 
     return false;
 }
 
-template <typename T>
-__device__ __forceinline__ void clear(f32x16 (&acc)[T::TC][T::TR]) {
-    _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-        _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
-            _Pragma("unroll") for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-}
-
 // The rows of gate and factor for the same features are blocks i and i + TC / 2 of one wave.
 template <typename T>
 __device__ __forceinline__ uint32_t gate_up_row(const ExpertArgs& a, int c, int q) {
@@ -127,7 +120,7 @@ template <typename T>
 __device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, const Where& w, f32x16 (&acc)[T::TC][T::TR]) {
     const int d0 = w.c * T::BC + t.wc * T::TC * 32;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i, int g) { return f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]}; });
+        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
         t.template take<T::TC, float>(j, a.D - d0, [&](int r) {
             const int at = w.r * T::BR + r;
             return at < w.count ? a.part + size_t(w.first + at) * a.D + d0 : nullptr;
@@ -221,13 +214,10 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
             };
         };
         _Pragma("unroll") for (int half = 0; half < 2; ++half) {
-            t.template put<T::TC>([&](int i, int g) {
-                const f32x16& v = gu[half * T::TC + i][j];
-                return f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
-            });
+            t.template put<T::TC>([&](int i, int g) { return four(gu[half * T::TC + i][j], g); });
             t.template take<T::TC, TIO>(j, a.F - f0, line(a.da, 2 * a.F, half * a.F));
         }
-        t.template put<T::TC>([&](int i, int g) { return f32x4{tt[i][j][4 * g], tt[i][j][4 * g + 1], tt[i][j][4 * g + 2], tt[i][j][4 * g + 3]}; });
+        t.template put<T::TC>([&](int i, int g) { return four(tt[i][j], g); });
         t.template take<T::TC, TIO>(j, a.F - f0, line(a.h, a.F, 0));
     }
 }
@@ -258,7 +248,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(ExpertArgs a, int row_tiles, 
     TIO* out = static_cast<TIO*>(DOWN ? a.d_w_down : a.d_w_gate_up) + size_t(e) * rows * cols;
     const int c0 = c * T::BC + t.wc * T::TC * 32;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i, int g) { return f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]}; });
+        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
         t.template take<T::TC, TIO>(j, cols - c0, [&](int r) {
             const int row = r0 * T::BR + r;
             return row < rows ? out + size_t(row) * cols + c0 : nullptr;
@@ -314,12 +304,6 @@ int check(const lsm_experts_params* p, bool backward) {
     return LSM_OK;
 }
 
-// Tiles of 256 columns; rows by the pairs of an expert.
-template <typename TIO, Layout LC, Layout LR, int BR> struct TileOf;
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 256> { typedef Tile<TIO, LC, LR, 2, 4, 4, 2, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 128> { typedef Tile<TIO, LC, LR, 4, 2, 2, 2, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 64> { typedef Tile<TIO, LC, LR, 4, 1, 2, 2, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 32> { typedef Tile<TIO, LC, LR, 4, 1, 2, 1, 4> type; };
 template <typename TIO, int BR> struct HalfTileOf;  // the same rows, half the columns
 template <typename TIO> struct HalfTileOf<TIO, 256> { typedef Tile<TIO, BY_COLS, BY_ROWS, 2, 4, 2, 2, 4> type; };
 template <typename TIO> struct HalfTileOf<TIO, 128> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 2, 1, 2, 4> type; };

@@ -253,7 +253,8 @@ struct Tile {
             _Pragma("unroll") for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<NB>(lane & 31, i * 32 + 8 * g + 4 * (lane >> 5)))) = value(i, g);
     }
-    template <int NB, typename TOUT, typename Line>
+    // ADD: to what is there already (fp32).
+    template <int NB, typename TOUT, bool ADD = false, typename Line>
     __device__ __forceinline__ void take(int j, int width, Line line) const {
         constexpr int E = 16 / int(sizeof(TOUT)), LANES = NB * 32 / E, ROWS = 64 / LANES;
         _Pragma("unroll") for (int it = 0; it < 32 / ROWS; ++it) {
@@ -264,10 +265,31 @@ struct Tile {
                 _Pragma("unroll") for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
             }
             TOUT* to = line((wr * TR + j) * 32 + row);
-            if (to && c < width) *reinterpret_cast<u32x4*>(to + c) = pack(v);
+            if (!to || c >= width) continue;
+            if (ADD) {
+                float old[E];
+                unpack(*reinterpret_cast<const u32x4*>(to + c), old);
+                _Pragma("unroll") for (int e = 0; e < E; ++e) v[e] += old[e];
+            }
+            *reinterpret_cast<u32x4*>(to + c) = pack(v);
         }
     }
 };
+
+template <typename T>
+__device__ __forceinline__ void clear(f32x16 (&acc)[T::TC][T::TR]) {
+    _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
+            _Pragma("unroll") for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+}
+__device__ __forceinline__ f32x4 four(const f32x16& v, int g) { return f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]}; }
+
+// Tiles of 256 columns and BR rows.
+template <typename TIO, Layout LC, Layout LR, int BR> struct TileOf;
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 256> { typedef Tile<TIO, LC, LR, 2, 4, 4, 2, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 128> { typedef Tile<TIO, LC, LR, 4, 2, 2, 2, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 64> { typedef Tile<TIO, LC, LR, 4, 1, 2, 2, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 32> { typedef Tile<TIO, LC, LR, 4, 1, 2, 1, 4> type; };
 
 }  // namespace
 }  // namespace lsm

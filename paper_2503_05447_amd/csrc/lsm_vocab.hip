@@ -1,0 +1,532 @@
+// Losses over a large vocabulary without its logits (include/lsm_train.h).
+//   k_teacher   a wave per token: the teacher's probabilities and their entropy, entry by entry; whether the token counts
+//   (plan)      the tokens that count, in their order (lsm_route.hip, one group): everything below works on these alone
+//   k_logits    a tile of x w^T: of each row the maximum, the sum of exponentials and the logits at its entries
+//   k_join      a token's loss from its tiles' maxima and sums
+//   k_grad      a tile of x w^T again: the logits' gradient, for a piece of the vocabulary
+//   k_dw        gradient^T x for the piece, all tokens being the long axis
+//   k_dx        gradient w, the piece's vocabulary being the long axis, in several shares of it, added to the pieces before
+//   k_dx_join   the shares' sum
+// Bound: the matrix products, three forward and backward and a fourth for the logits formed again; for few tokens the weights, read once.
+#include "lsm_product_dev.h"
+#include "lsm_train_dev.h"
+
+namespace lsm {
+namespace {
+
+struct VocabArgs {
+    const void *x, *w;
+    const int32_t *index, *offsets, *order, *place;
+    const float *teacher, *lse_in, *d_loss;
+    int32_t *count, *entry;   // [n] 0: counts, -1: not; [K][n] tokens
+    float *share, *entropy;   // [K][n] probabilities; [n]
+    f32x2* stats;             // [parts][n] maximum, sum
+    float* at_entry;          // [max(K, 1)][n] logits
+    float *loss, *lse;
+    void *grad, *dx, *dw;     // gradient [n][piece]
+    float* part;              // [shares][n][D]
+    int n, D, V, K, parts, piece, v0, shares;
+    uint32_t x_bytes;
+    float scale;              // 1 / temperature
+};
+
+__device__ __forceinline__ int rows_of(const VocabArgs& a) { return uniform(min(max(a.offsets[1], 0), a.n)); }
+__device__ __forceinline__ uint32_t token_of(const VocabArgs& a, int at) { return min(uint32_t(a.order[at]), uint32_t(a.n - 1)); }
+
+// exp: 24 bits for fp32 elements; for bf16 the hardware's power of two, whose argument's rounding costs 2^-24 of its size (2^-19 at most
+// where the result is not negligible).
+__device__ __forceinline__ float exponential(float x, float) { return expf(x); }
+__device__ __forceinline__ float exponential(float x, uint16_t) { return __builtin_amdgcn_exp2f(x * 1.442695041f); }
+
+__global__ __launch_bounds__(256) void k_teacher(VocabArgs a) {
+    const int t = int(blockIdx.x) * 4 + int(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (t >= a.n) return;
+    float z[4], m = -__builtin_inff();
+    int v[4];
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        const int j = 64 * i + lane;
+        v[i] = -1;
+        z[i] = -__builtin_inff();
+        if (j < a.K) {
+            v[i] = a.index[size_t(t) * a.K + j];
+            z[i] = a.teacher[size_t(t) * a.K + j];
+            if (z[i] != z[i] || v[i] < 0 || v[i] >= a.V) z[i] = -__builtin_inff();
+            z[i] = fminf(z[i], 3.402823466e38f);
+            if (z[i] == -__builtin_inff()) v[i] = -1;
+        }
+        m = fmaxf(m, z[i]);
+    }
+    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    const bool counts = m > -__builtin_inff();
+    float sum = 0.f, d[4];
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        d[i] = v[i] >= 0 ? (z[i] - m) * a.scale : -__builtin_inff();
+        sum += v[i] >= 0 ? expf(d[i]) : 0.f;
+    }
+    sum = group_sum<64>(sum);
+    const float log_sum = logf(sum);
+    float entropy = 0.f;
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        const int j = 64 * i + lane;
+        const float p = v[i] >= 0 ? expf(d[i]) / sum : 0.f;
+        if (p > 0.f) entropy += p * (d[i] - log_sum);
+        if (j < a.K) {
+            a.entry[size_t(j) * a.n + t] = p > 0.f ? v[i] : -1;
+            a.share[size_t(j) * a.n + t] = p;
+        }
+    }
+    entropy = group_sum<64>(entropy);
+    if (lane == 0) {
+        a.count[t] = counts ? 0 : -1;
+        a.entropy[t] = entropy;
+    }
+}
+
+// Tile number id of rt x ct: eight rows of tiles at a time, the column changing more slowly than the row among them, so that the workgroups of
+// a die, whose numbers are neighbours, hold a block of about eight by four tiles.
+__device__ __forceinline__ void tile_at(int id, int rt, int ct, int& r, int& c) {
+    const int band = id / (8 * ct), rest = id - band * 8 * ct, rows = min(8, rt - 8 * band);
+    c = rest / rows;
+    r = 8 * band + rest - c * rows;
+}
+__device__ __forceinline__ int number_of_tile(int all) {  // -1: none left.  A die's numbers are neighbours
+    const int die = (all + 7) / 8, slot = int(blockIdx.x) / 8, id = (int(blockIdx.x) % 8) * die + slot;
+    return slot < die && id < all ? id : -1;
+}
+
+// x (rows that count) times w^T from vocabulary column v0 on
+template <typename T>
+__device__ __forceinline__ void form_logits(T& t, const VocabArgs& a, int rows, int r0, int v0, int end, f32x16 (&acc)[T::TC][T::TR]) {
+    typedef typename T::TIO TIO;
+    const uint32_t bytes = uint32_t(a.D) * uint32_t(sizeof(TIO));
+    t.r.start_rows(a.x, t.wave, t.lane, [&](int i) { return r0 + i < rows ? token_of(a, r0 + i) * a.x_bytes : kBeyond; });
+    t.c.start_rows(static_cast<const TIO*>(a.w) + size_t(v0) * a.D, t.wave, t.lane, [&](int q) { return v0 + q < end ? uint32_t(q) * bytes : kBeyond; });
+    clear<T>(acc);
+    t.walk(acc, a.D);
+}
+
+template <typename T, bool TEACHER>
+__global__ __launch_bounds__(T::THREADS) void k_logits(VocabArgs a) {
+    typedef typename T::TIO TIO;
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    const int rows = rows_of(a), rt = (rows + T::BR - 1) / T::BR, ct = (a.V + T::BC - 1) / T::BC, id = number_of_tile(rt * ct);
+    if (id < 0) return;
+    int r, c;
+    tile_at(id, rt, ct, r, c);
+    const int r0 = r * T::BR;
+    T t(shared);
+    f32x16 acc[T::TC][T::TR];
+    form_logits(t, a, rows, r0, c * T::BC, a.V, acc);
+    const int first = c * T::BC + t.wc * T::TC * 32, mine = first + 4 * (t.lane >> 5);  // of the wave, of the lane
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        const int at = r0 + t.row(j);
+        float m = -__builtin_inff(), sum = 0.f;
+        _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+            _Pragma("unroll") for (int q = 0; q < 16; ++q) {
+                float z = acc[i][j][q] * a.scale;
+                if (mine + i * 32 + 8 * (q / 4) + q % 4 >= a.V) z = -__builtin_inff();
+                acc[i][j][q] = z;
+                m = fmaxf(m, z);
+            }
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float top = m == -__builtin_inff() ? 0.f : m;
+        _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+            _Pragma("unroll") for (int q = 0; q < 16; ++q) sum += exponential(acc[i][j][q] - top, TIO());
+        sum += __shfl_xor(sum, 32, 64);
+        if (t.lane < 32 && at < rows) a.stats[size_t(c * T::WC + t.wc) * a.n + at] = f32x2{m, sum};
+        const int token = at < rows ? int(token_of(a, at)) : -1;
+        if (!TEACHER) {
+            const int want = token < 0 ? -1 : a.index[token];
+            if (__ballot(uint32_t(want - first) < uint32_t(T::TC * 32)) == 0) continue;
+            _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+                _Pragma("unroll") for (int q = 0; q < 16; ++q)
+                    if (want == mine + i * 32 + 8 * (q / 4) + q % 4) a.at_entry[at] = acc[i][j][q];
+        } else {  // either half of the wave looks for every other entry of its lane's row
+            t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
+            if (token < 0) continue;
+            for (int e = t.lane >> 5; e < a.K; e += 2) {
+                const int d = a.entry[size_t(e) * a.n + token] - first;
+                if (uint32_t(d) < uint32_t(T::TC * 32))
+                    a.at_entry[size_t(e) * a.n + at] =
+                        *reinterpret_cast<__attribute__((address_space(3))) const float*>(uintptr_t(t.template cell<T::TC>(t.lane & 31, d)));
+            }
+        }
+    }
+}
+
+// 64 tokens by a workgroup, every 16th part (and entry) by a thread
+__global__ __launch_bounds__(1024) void k_join(VocabArgs a) {
+    __shared__ float top[16][64], total[16][64];
+    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, token = int(blockIdx.x) * 64 + lane;
+    const int at = token < a.n ? a.place[token] : -1;
+    float m = -__builtin_inff(), s = 0.f;
+    if (at >= 0 && at < a.n) {
+        for (int p = slice; p < a.parts; p += 16) m = fmaxf(m, a.stats[size_t(p) * a.n + at].x);
+        const float mm = m == -__builtin_inff() ? 0.f : m;
+        for (int p = slice; p < a.parts; p += 16) {
+            const f32x2 v = a.stats[size_t(p) * a.n + at];
+            s += v.y * expf(v.x - mm);
+        }
+    }
+    top[slice][lane] = m;
+    __syncthreads();
+    float all = top[0][lane];
+    _Pragma("unroll") for (int i = 1; i < 16; ++i) all = fmaxf(all, top[i][lane]);
+    const float base = all == -__builtin_inff() ? 0.f : all;
+    total[slice][lane] = m == -__builtin_inff() ? s : s * expf(m - base);
+    __syncthreads();
+    float sum = 0.f;
+    _Pragma("unroll") for (int i = 0; i < 16; ++i) sum += total[i][lane];
+    const float lse = base + logf(sum);
+    __syncthreads();
+    float part = 0.f, shares = 0.f;
+    if (a.K > 0 && at >= 0)
+        for (int e = slice; e < a.K; e += 16) {
+            const float p = a.share[size_t(e) * a.n + token];
+            if (!(p > 0.f)) continue;
+            shares += p;
+            part += p * (lse - a.at_entry[size_t(e) * a.n + at]);
+        }
+    top[slice][lane] = part;
+    __syncthreads();
+    if (slice != 0 || token >= a.n) return;
+    float loss = 0.f;
+    if (a.K > 0) {
+        loss = a.entropy[token];
+        _Pragma("unroll") for (int i = 0; i < 16; ++i) loss += top[i][lane];
+    } else if (at >= 0) {
+        loss = lse - a.at_entry[at];
+    }
+    a.loss[token] = at >= 0 ? loss : 0.f;
+    a.lse[token] = at >= 0 ? lse : 0.f;
+}
+
+template <typename T, bool TEACHER>
+__global__ __launch_bounds__(T::THREADS) void k_grad(VocabArgs a) {
+    typedef typename T::TIO TIO;
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    const int end = min(a.V, a.v0 + a.piece);
+    const int rows = rows_of(a), rt = (rows + T::BR - 1) / T::BR, ct = (end - a.v0 + T::BC - 1) / T::BC, id = number_of_tile(rt * ct);
+    if (id < 0) return;
+    int r, c;
+    tile_at(id, rt, ct, r, c);
+    const int r0 = r * T::BR;
+    T t(shared);
+    f32x16 acc[T::TC][T::TR];
+    form_logits(t, a, rows, r0, a.v0 + c * T::BC, end, acc);
+    const int column = c * T::BC + t.wc * T::TC * 32, first = a.v0 + column, mine = first + 4 * (t.lane >> 5);
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        const int at = r0 + t.row(j), token = at < rows ? int(token_of(a, at)) : -1;
+        const float lse = token < 0 ? 0.f : a.lse_in[token], weight = token < 0 ? 0.f : a.d_loss[token] * a.scale;
+        const int want = TEACHER || token < 0 ? -1 : a.index[token];
+        t.template put<T::TC>([&](int i, int g) {
+            f32x4 v;
+            _Pragma("unroll") for (int e = 0; e < 4; ++e) {
+                const int col = mine + i * 32 + 8 * g + e;
+                float p = exponential(acc[i][j][4 * g + e] * a.scale - lse, TIO());
+                if (!TEACHER && col == want) p -= 1.f;
+                v[e] = col < end && token >= 0 ? weight * p : 0.f;
+            }
+            return v;
+        });
+        if (TEACHER && token >= 0 && t.lane < 32)  // a row's entries one after the other: some may be the same
+            for (int e = 0; e < a.K; ++e) {
+                const int d = a.entry[size_t(e) * a.n + token] - first;
+                if (uint32_t(d) < uint32_t(T::TC * 32) && d + first < end) {
+                    auto* p = reinterpret_cast<__attribute__((address_space(3))) float*>(uintptr_t(t.template cell<T::TC>(t.lane, d)));
+                    *p = *p - weight * a.share[size_t(e) * a.n + token];
+                }
+            }
+        // the columns behind the vocabulary's end are zeros that the next products read
+        t.template take<T::TC, TIO>(j, a.piece - column, [&](int q) {
+            return r0 + q < rows ? static_cast<TIO*>(a.grad) + size_t(r0 + q) * a.piece + column : nullptr;
+        });
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::THREADS) void k_dw(VocabArgs a) {
+    typedef typename T::TIO TIO;
+    constexpr int EL = int(sizeof(TIO));
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    const int width = min(a.V - a.v0, a.piece), rows = rows_of(a);
+    const int rt = (width + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, id = number_of_tile(rt * ct);
+    if (id < 0) return;
+    int r, c;
+    tile_at(id, rt, ct, r, c);
+    T t(shared);
+    t.r.start_cols(a.grad, a.piece * EL, r * T::BR, a.piece, t.wave, t.lane, 0);
+    t.c.start_cols(a.x, int(a.x_bytes), c * T::BC, a.D, t.wave, t.lane, t.list_at());
+    f32x16 acc[T::TC][T::TR];
+    clear<T>(acc);
+    t.walk(acc, rows, [&](int k) { return token_of(a, k); });
+    const int c0 = c * T::BC + t.wc * T::TC * 32;
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
+        t.template take<T::TC, TIO>(j, a.D - c0, [&](int q) {
+            const int v = r * T::BR + q;
+            return v < width ? static_cast<TIO*>(a.dw) + size_t(a.v0 + v) * a.D + c0 : nullptr;
+        });
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
+    typedef typename T::TIO TIO;
+    constexpr int EL = int(sizeof(TIO)), STEP = kStepBytes / EL;
+    __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    const int width = min(a.V - a.v0, a.piece), rows = rows_of(a);
+    const int rt = (rows + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, id = number_of_tile(rt * ct * a.shares);
+    if (id < 0) return;
+    const int share = id / (rt * ct);
+    int r, c;
+    tile_at(id - share * rt * ct, rt, ct, r, c);
+    const int steps = (width + STEP - 1) / STEP, k0 = steps * share / a.shares * STEP, k1 = min(width, steps * (share + 1) / a.shares * STEP);
+    const int r0 = r * T::BR;
+    const uint32_t bytes = uint32_t(a.piece) * EL;
+    T t(shared);
+    t.r.start_rows(static_cast<const TIO*>(a.grad) + size_t(r0) * a.piece + k0, t.wave, t.lane,
+                   [&](int i) { return r0 + i < rows ? uint32_t(i) * bytes : kBeyond; });
+    t.c.start_cols(static_cast<const TIO*>(a.w) + size_t(a.v0 + k0) * a.D, a.D * EL, c * T::BC, a.D, t.wave, t.lane, 0);
+    f32x16 acc[T::TC][T::TR];
+    clear<T>(acc);
+    t.walk(acc, k1 - k0);
+    const int c0 = c * T::BC + t.wc * T::TC * 32;
+    const auto line = [&](int q) { return r0 + q < rows ? a.part + (size_t(share) * a.n + r0 + q) * a.D + c0 : nullptr; };
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
+        if (a.v0 == 0) t.template take<T::TC, float>(j, a.D - c0, line);
+        else t.template take<T::TC, float, true>(j, a.D - c0, line);
+    }
+}
+
+template <typename TIO>
+__global__ __launch_bounds__(256) void k_dx_join(VocabArgs a) {
+    constexpr int E = kPiece<TIO>;
+    const int pieces = a.D / E;
+    const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (id >= int64_t(a.n) * pieces) return;
+    const int token = int(id / pieces), d = int(id - int64_t(token) * pieces) * E, at = a.place[token];
+    float s[E];
+    _Pragma("unroll") for (int e = 0; e < E; ++e) s[e] = 0.f;
+    if (at >= 0 && at < a.n)
+        for (int q = 0; q < a.shares; ++q) {
+            const f32x4* z = reinterpret_cast<const f32x4*>(a.part + (size_t(q) * a.n + at) * a.D + d);
+            _Pragma("unroll") for (int i = 0; i < E / 4; ++i)
+                _Pragma("unroll") for (int e = 0; e < 4; ++e) s[4 * i + e] += z[i][e];
+        }
+    *reinterpret_cast<u32x4*>(static_cast<TIO*>(a.dx) + size_t(token) * a.D + d) = pack(s);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+constexpr int kMostEntries = 256;
+constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of the logits' gradient at a time: what the memory-side cache holds
+
+int check(const lsm_vocab_params* p) {
+    if (!p) return LSM_ERR_NULL;
+    if (p->struct_size != sizeof(lsm_vocab_params)) return LSM_ERR_SHAPE;
+    if (p->n < 1 || p->D < 1 || p->V < 1 || p->K < 0 || p->n > kMostPairs || p->V > (1 << 24)) return LSM_ERR_SHAPE;
+    if (!(p->temperature > 0.f) || !(1.f / p->temperature < 3.4e38f) || !(1.f / p->temperature > 0.f)) return LSM_ERR_SHAPE;
+    if (p->dtype != LSM_DTYPE_F32 && p->dtype != LSM_DTYPE_BF16) return LSM_ERR_UNSUPPORTED;
+    if (p->K > kMostEntries || p->D % 8 || p->D > 65536 || p->reserved != 0) return LSM_ERR_UNSUPPORTED;
+    const int64_t el = p->dtype == LSM_DTYPE_BF16 ? 2 : 4;
+    if (p->x_stride < p->D || p->x_stride > (int64_t(1) << 31) || p->n * p->x_stride * el >= int64_t(kBeyond)) return LSM_ERR_SHAPE;
+    if (p->x_stride % 8) return LSM_ERR_ALIGN;
+    return LSM_OK;
+}
+int rows_of_tile(const lsm_vocab_params& p) { return p.n > 160 ? 256 : p.n > 64 ? 128 : p.n > 32 ? 64 : 32; }
+int waves_along(int br) { return br == 256 ? 2 : 4; }
+int up(int64_t x, int64_t to) { return int((x + to - 1) / to); }
+
+struct Split { int piece, shares; };
+Split split(const lsm_vocab_params& p) {
+    const int64_t el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4;
+    int64_t most = kPieceBytes / (p.n * el) / 256 * 256;
+    if (most < 256) most = 256;
+    const int pieces = up(p.V, most);
+    Split s{up(up(p.V, pieces), 256) * 256, 1};
+    // shares of a piece's vocabulary: the fewest with which the last round of workgroups is nine tenths full, or the best of eight
+    const int br = rows_of_tile(p), room = br >= 128 ? 256 : 512;
+    const int64_t tiles = int64_t(up(p.n, br)) * up(p.D, 256);
+    double best = 0;
+    for (int k = 1; k <= 64 && k * 512 <= s.piece + 511; ++k) {
+        const double full = double(tiles * k) / (double(up(tiles * k, room)) * room);
+        if (full > best + 0.02) { best = full; s.shares = k; }
+        if (best >= 0.9 || (k >= 8 && tiles * k >= room)) break;
+    }
+    return s;
+}
+
+struct Space { size_t offsets, order, place, hist, count, entry, share, entropy, stats, at_entry, grad, part, bytes; };
+Space space(const lsm_vocab_params& p, bool backward) {
+    const size_t n = p.n, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4, K = p.K;
+    Space s{};
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
+    s.offsets = take(8);
+    s.order = take(n * 4);
+    s.place = take(n * 4);
+    s.hist = take(plan_space(p.n, 1));
+    s.count = take(K ? n * 4 : 0);
+    s.entry = take(K * n * 4);
+    s.share = take(K * n * 4);
+    s.entropy = take(K ? n * 4 : 0);
+    if (!backward) {
+        s.stats = take(size_t(up(p.V, 256)) * waves_along(rows_of_tile(p)) * n * sizeof(f32x2));
+        s.at_entry = take((K ? K : 1) * n * 4);
+    } else {
+        const Split q = split(p);
+        s.grad = take(n * q.piece * el);
+        s.part = take(size_t(q.shares) * n * p.D * 4);
+    }
+    s.bytes = at;
+    return s;
+}
+
+VocabArgs arguments(const lsm_vocab_params& p, const Space& s, char* ws, const void* x, const void* w, const int32_t* index, const float* teacher) {
+    VocabArgs a{};
+    a.x = x; a.w = w; a.index = index; a.teacher = teacher;
+    a.offsets = reinterpret_cast<int32_t*>(ws + s.offsets);
+    a.order = reinterpret_cast<int32_t*>(ws + s.order);
+    a.place = reinterpret_cast<int32_t*>(ws + s.place);
+    a.count = reinterpret_cast<int32_t*>(ws + s.count);
+    a.entry = reinterpret_cast<int32_t*>(ws + s.entry);
+    a.share = reinterpret_cast<float*>(ws + s.share);
+    a.entropy = reinterpret_cast<float*>(ws + s.entropy);
+    a.stats = reinterpret_cast<f32x2*>(ws + s.stats);
+    a.at_entry = reinterpret_cast<float*>(ws + s.at_entry);
+    a.grad = ws + s.grad;
+    a.part = reinterpret_cast<float*>(ws + s.part);
+    a.n = p.n; a.D = p.D; a.V = p.V; a.K = p.K;
+    a.x_bytes = uint32_t(p.x_stride) * (p.dtype == LSM_DTYPE_BF16 ? 2 : 4);
+    a.scale = 1.f / p.temperature;
+    a.parts = up(p.V, 256) * waves_along(rows_of_tile(p));
+    return a;
+}
+// The tokens that count.
+bool enqueue_rows(const VocabArgs& a, const Space& s, char* ws, hipStream_t st) {
+    if (a.K > 0) {
+        ProfScope ps(KID_VOCAB_ROWS, st);
+        hipLaunchKernelGGL(k_teacher, dim3(up(a.n, 4)), dim3(256), 0, st, a);
+        if (!launched()) return false;
+    }
+    return enqueue_plan(a.K ? a.count : a.index, a.n, 1, a.K ? 1 : a.V, reinterpret_cast<int32_t*>(ws + s.offsets),
+                        reinterpret_cast<int32_t*>(ws + s.order), reinterpret_cast<int32_t*>(ws + s.place),
+                        reinterpret_cast<int32_t*>(ws + s.hist), st);
+}
+unsigned grid_of(int64_t tiles) { return unsigned((tiles + 7) / 8 * 8); }
+
+template <typename TIO, int BR>
+bool launch_fwd(const VocabArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type T;
+    {
+        ProfScope ps(KID_VOCAB_LOGITS, st);
+        const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(a.V, T::BC));
+        if (a.K) hipLaunchKernelGGL((k_logits<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
+        else hipLaunchKernelGGL((k_logits<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
+    }
+    if (!launched()) return false;
+    ProfScope ps(KID_VOCAB_JOIN, st);
+    hipLaunchKernelGGL(k_join, dim3(up(a.n, 64)), dim3(1024), 0, st, a);
+    return launched();
+}
+
+template <typename TIO, int BR>
+bool launch_bwd(VocabArgs a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type T;
+    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, BR>::type X;
+    typedef Tile<TIO, BY_COLS, BY_COLS, 2, 4, 4, 2, 4, true, false> W;
+    for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
+        const int width = a.V - a.v0 < a.piece ? a.V - a.v0 : a.piece;
+        {
+            ProfScope ps(KID_VOCAB_GRAD, st);
+            const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(width, T::BC));
+            if (a.K) hipLaunchKernelGGL((k_grad<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
+            else hipLaunchKernelGGL((k_grad<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
+        }
+        if (!launched()) return false;
+        if (a.dw) {
+            ProfScope ps(KID_VOCAB_DW, st);
+            hipLaunchKernelGGL((k_dw<W>), dim3(grid_of(int64_t(up(width, W::BR)) * up(a.D, W::BC))), dim3(W::THREADS), 0, st, a);
+            if (!launched()) return false;
+        }
+        ProfScope ps(KID_VOCAB_DX, st);
+        hipLaunchKernelGGL((k_dx<X>), dim3(grid_of(int64_t(up(a.n, X::BR)) * up(a.D, X::BC) * a.shares)), dim3(X::THREADS), 0, st, a);
+        if (!launched()) return false;
+    }
+    ProfScope ps(KID_VOCAB_JOIN, st);
+    hipLaunchKernelGGL((k_dx_join<TIO>), dim3(up(int64_t(a.n) * (a.D / kPiece<TIO>), 256)), dim3(256), 0, st, a);
+    return launched();
+}
+template <typename TIO>
+bool launch(const VocabArgs& a, int br, bool backward, hipStream_t st) {
+    switch (br) {
+        case 256: return backward ? launch_bwd<TIO, 256>(a, st) : launch_fwd<TIO, 256>(a, st);
+        case 128: return backward ? launch_bwd<TIO, 128>(a, st) : launch_fwd<TIO, 128>(a, st);
+        case 64: return backward ? launch_bwd<TIO, 64>(a, st) : launch_fwd<TIO, 64>(a, st);
+        default: return backward ? launch_bwd<TIO, 32>(a, st) : launch_fwd<TIO, 32>(a, st);
+    }
+}
+
+}  // namespace
+}  // namespace lsm
+
+extern "C" {
+
+size_t lsm_vocab_loss_workspace_bytes(const lsm_vocab_params* p) {
+    using namespace lsm;
+    return check(p) == LSM_OK ? space(*p, false).bytes : 0;
+}
+size_t lsm_vocab_loss_bwd_workspace_bytes(const lsm_vocab_params* p) {
+    using namespace lsm;
+    return check(p) == LSM_OK ? space(*p, true).bytes : 0;
+}
+
+int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,
+                   float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace lsm;
+    const int rc = check(p);
+    if (rc != LSM_OK) return rc;
+    if (!x || !w || !index || !teacher != !p->K || !loss || !lse) return LSM_ERR_NULL;
+    if (misaligned(x) || misaligned(w) || misaligned(index) || misaligned(teacher) || misaligned(loss) || misaligned(lse) || misaligned(workspace))
+        return LSM_ERR_ALIGN;
+    const Space s = space(*p, false);
+    if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    VocabArgs a = arguments(*p, s, ws, x, w, index, teacher);
+    a.loss = loss;
+    a.lse = lse;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!enqueue_rows(a, s, ws, st)) return LSM_ERR_LAUNCH;
+    const int br = rows_of_tile(*p);
+    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, br, false, st) : launch<float>(a, br, false, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+}
+
+int lsm_vocab_loss_bwd(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,
+                       const float* lse, const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes,
+                       void* stream) {
+    using namespace lsm;
+    const int rc = check(p);
+    if (rc != LSM_OK) return rc;
+    if (!x || !w || !index || !teacher != !p->K || !lse || !d_loss || !dx) return LSM_ERR_NULL;
+    if (misaligned(x) || misaligned(w) || misaligned(index) || misaligned(teacher) || misaligned(lse) || misaligned(d_loss) || misaligned(dx) ||
+        misaligned(dw) || misaligned(workspace))
+        return LSM_ERR_ALIGN;
+    const Space s = space(*p, true);
+    if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    VocabArgs a = arguments(*p, s, ws, x, w, index, teacher);
+    const Split q = split(*p);
+    a.piece = q.piece;
+    a.shares = q.shares;
+    a.lse_in = lse;
+    a.d_loss = d_loss;
+    a.dx = dx;
+    a.dw = dw;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!enqueue_rows(a, s, ws, st)) return LSM_ERR_LAUNCH;
+    const int br = rows_of_tile(*p);
+    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, br, true, st) : launch<float>(a, br, true, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+}
+
+}  // extern "C"
