@@ -111,7 +111,7 @@ int lsm_moe_experts_bwd(const lsm_experts_params* p, const void* x, const float*
 typedef struct {
     uint32_t struct_size; /* = sizeof(lsm_vocab_params)                                                       */
     int32_t  n, D, V;     /* tokens (1..2^24), their width (a multiple of 8, at most 65536), vocabulary (1..2^24)  */
-    int32_t  K;           /* 0: one target a token; 1..256: so many logits of a teacher                       */
+    int32_t  K;           /* 0: one target a token; 1..256: so many logits of a teacher, n * K at most 2^28       */
     int32_t  dtype;       /* lsm_dtype of x, w and their gradients                                            */
     float    temperature; /* > 0: divides the logits, the teacher's too                                       */
     int32_t  reserved;    /* 0                                                                               */

@@ -72,7 +72,7 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int cols, Where& 
 template <typename T>
 __device__ __forceinline__ uint32_t gate_up_row(const ExpertArgs& a, int c, int q) {
     constexpr int HALF = T::TC / 2;
-    const int wave = q / (T::TC * 32), i = q / 32 % T::TC, f = c * (T::BC / 2) + (wave * HALF + i % HALF) * 32 + q % 32;
+    const int wave = q / (T::TC * 16), i = q / 16 % T::TC, f = c * (T::BC / 2) + (wave * HALF + i % HALF) * 16 + q % 16;
     return f < a.F ? uint32_t((i >= HALF ? a.F : 0) + f) * uint32_t(a.D) * uint32_t(sizeof(typename T::TIO)) : kBeyond;
 }
 template <typename T>
@@ -94,17 +94,17 @@ __global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
     if (!find_tile<T::BR>(a, (a.F + T::BC / 2 - 1) / (T::BC / 2), w)) return;
     T t(shared);
     start_gate_up(t, a, w);
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     clear<T>(acc);
     t.walk(acc, a.D);
     constexpr int HALF = T::TC / 2;
-    const int f0 = w.c * (T::BC / 2) + t.wc * HALF * 32;
+    const int f0 = w.c * (T::BC / 2) + t.wc * HALF * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<HALF>([&](int i, int g) {
+        t.template put<HALF>([&](int i) {
             f32x4 h;
             _Pragma("unroll") for (int e = 0; e < 4; ++e) {
-                const float gate = acc[i][j][4 * g + e];
-                h[e] = gate / (1.f + expf(-gate)) * acc[i + HALF][j][4 * g + e];
+                const float gate = acc[i][j][e];
+                h[e] = gate * sigmoid(gate, TIO()) * acc[i + HALF][j][e];
             }
             return h;
         });
@@ -117,10 +117,10 @@ __global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
 
 // rows of `parts` [pairs][D] = rows of R [pairs][K] times C^T
 template <typename T>
-__device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, const Where& w, f32x16 (&acc)[T::TC][T::TR]) {
-    const int d0 = w.c * T::BC + t.wc * T::TC * 32;
+__device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, const Where& w, f32x4 (&acc)[T::TC][T::TR]) {
+    const int d0 = w.c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
+        t.template put<T::TC>([&](int i) { return acc[i][j]; });
         t.template take<T::TC, float>(j, a.D - d0, [&](int r) {
             const int at = w.r * T::BR + r;
             return at < w.count ? a.part + size_t(w.first + at) * a.D + d0 : nullptr;
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(T::THREADS) void k_down(ExpertArgs a) {
         const int d = w.c * T::BC + q;
         return d < a.D ? uint32_t(d) * bytes : kBeyond;
     });
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     clear<T>(acc);
     t.walk(acc, a.F);
     finish_part(t, a, w, acc);
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(ExpertArgs a) {
     T t(shared);
     start_pairs(t, a.da, w, 2 * uint32_t(a.F) * uint32_t(sizeof(TIO)));
     t.c.start_cols(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, a.D * int(sizeof(TIO)), w.c * T::BC, a.D, t.wave, t.lane, 0);
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     clear<T>(acc);
     t.walk(acc, 2 * a.F);
     finish_part(t, a, w, acc);
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
     __shared__ __attribute__((aligned(1024))) char shared[H::LDS > T::LDS ? H::LDS : T::LDS];
     Where w;
     if (!find_tile<T::BR>(a, (a.F + T::BC - 1) / T::BC, w)) return;
-    f32x16 gu[H::TC][H::TR], tt[T::TC][T::TR];
+    f32x4 gu[H::TC][H::TR], tt[T::TC][T::TR];
     {
         H t(shared);
         start_gate_up(t, a, w);
@@ -191,22 +191,22 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
     t.c.start_cols(static_cast<const TIO*>(a.w_down) + size_t(w.e) * a.D * a.F, a.F * int(sizeof(TIO)), w.c * T::BC, a.F, t.wave, t.lane, 0);
     clear<T>(tt);
     t.walk(tt, a.D);
-    const int f0 = w.c * T::BC + t.wc * T::TC * 32;
+    const int f0 = w.c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
         const int at = w.r * T::BR + t.row(j);
         const float p = at < w.count ? a.weights[pair_of(a, w.first + at)] : 0.f;
         float along = 0.f;
         _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-            _Pragma("unroll") for (int r = 0; r < 16; ++r) {
+            _Pragma("unroll") for (int r = 0; r < 4; ++r) {
                 const float gate = gu[i][j][r], up = gu[i + T::TC][j][r], d = tt[i][j][r];
-                const float sig = 1.f / (1.f + expf(-gate)), s = gate * sig, h = s * up, dh = p * d;
+                const float sig = sigmoid(gate, TIO()), s = gate * sig, h = s * up, dh = p * d;
                 along += d * h;
                 gu[i][j][r] = dh * up * (sig + s * (1.f - sig));
                 gu[i + T::TC][j][r] = dh * s;
                 tt[i][j][r] = p * h;
             }
-        along += __shfl_xor(along, 32, 64);
-        if (t.lane < 32 && at < w.count) a.weight_part[size_t(w.c * T::WC + t.wc) * (size_t(a.n) * a.top_k) + w.first + at] = along;
+        along = T::row_sum(along);
+        if (t.lane < 16 && at < w.count) a.weight_part[size_t(w.c * T::WC + t.wc) * (size_t(a.n) * a.top_k) + w.first + at] = along;
         const auto line = [&](void* base, int length, int shift) {
             return [=, &w](int r) {
                 const int q = w.r * T::BR + r;
@@ -214,10 +214,10 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
             };
         };
         _Pragma("unroll") for (int half = 0; half < 2; ++half) {
-            t.template put<T::TC>([&](int i, int g) { return four(gu[half * T::TC + i][j], g); });
+            t.template put<T::TC>([&](int i) { return gu[half * T::TC + i][j]; });
             t.template take<T::TC, TIO>(j, a.F - f0, line(a.da, 2 * a.F, half * a.F));
         }
-        t.template put<T::TC>([&](int i, int g) { return four(tt[i][j], g); });
+        t.template put<T::TC>([&](int i) { return tt[i][j]; });
         t.template take<T::TC, TIO>(j, a.F - f0, line(a.h, a.F, 0));
     }
 }
@@ -242,13 +242,13 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(ExpertArgs a, int row_tiles, 
         t.r.start_cols(static_cast<const TIO*>(a.da) + size_t(first) * 2 * a.F, 2 * a.F * EL, r0 * T::BR, rows, t.wave, t.lane, 0);
         t.c.start_cols(a.x, int(a.x_bytes), c * T::BC, cols, t.wave, t.lane, t.list_at());
     }
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     clear<T>(acc);
     t.walk(acc, count, [&](int k) { return token_of(a, first + k); });
     TIO* out = static_cast<TIO*>(DOWN ? a.d_w_down : a.d_w_gate_up) + size_t(e) * rows * cols;
-    const int c0 = c * T::BC + t.wc * T::TC * 32;
+    const int c0 = c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
+        t.template put<T::TC>([&](int i) { return acc[i][j]; });
         t.template take<T::TC, TIO>(j, cols - c0, [&](int r) {
             const int row = r0 * T::BR + r;
             return row < rows ? out + size_t(row) * cols + c0 : nullptr;
@@ -305,10 +305,10 @@ int check(const lsm_experts_params* p, bool backward) {
 }
 
 template <typename TIO, int BR> struct HalfTileOf;  // the same rows, half the columns
-template <typename TIO> struct HalfTileOf<TIO, 256> { typedef Tile<TIO, BY_COLS, BY_ROWS, 2, 4, 2, 2, 4> type; };
-template <typename TIO> struct HalfTileOf<TIO, 128> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 2, 1, 2, 4> type; };
-template <typename TIO> struct HalfTileOf<TIO, 64> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 1, 2, 4> type; };
-template <typename TIO> struct HalfTileOf<TIO, 32> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 1, 1, 4> type; };
+template <typename TIO> struct HalfTileOf<TIO, 256> { typedef Tile<TIO, BY_COLS, BY_ROWS, 2, 4, 4, 4, 4> type; };
+template <typename TIO> struct HalfTileOf<TIO, 128> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 2, 2, 4, 4> type; };
+template <typename TIO> struct HalfTileOf<TIO, 64> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 2, 4, 4> type; };
+template <typename TIO> struct HalfTileOf<TIO, 32> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 2, 2, 4> type; };
 
 int rows_of_tile(const lsm_experts_params& p) {
     const int64_t mean = int64_t(p.n) * p.top_k / p.E;
@@ -383,8 +383,8 @@ bool launch_bwd(const lsm_experts_params& p, const ExpertArgs& a, hipStream_t st
     }
     if (!launched() || !launch_sum<TIO, false>(a, st)) return false;
     if (!a.d_w_down) return true;
-    return launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 4, 2, 4, true, false>, false>(a, st) &&
-           launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 4, 2, 4, false, true>, true>(a, st);
+    return launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 8, 4, 4, true, false>, false>(a, st) &&
+           launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 8, 4, 4, false, true>, true>(a, st);
 }
 
 template <typename TIO>

@@ -2,16 +2,17 @@
 // of which lie next to each other in memory, with either operand by rows ([i][k], k contiguous) or by columns ([k][i], i
 // contiguous), rows taken through a list where one is given.
 //
-// The product is formed as C R^T: c is the first operand of the 32 x 32 matrix instructions, so that a lane holds one row r and four
-// neighbouring c's in four registers, and what is done along a row (maximum, sum, gate with factor) stays in the lane.
+// The product is formed as C R^T: c is the first operand of the 16 x 16 matrix instructions, so that a lane holds one row r and four
+// neighbouring c's in four registers, and what is done along a row (maximum, sum, gate with factor) stays in a few lanes.  (With all
+// matrix cores busy the clock is bound by power: from registers alone 16 x 16 x 32 reaches 1.9 PFLOP/s here, 32 x 32 x 16 1.7.)
 //
 // Pieces of 64 bytes of k a row (32 of bf16, 16 of fp32) go straight from memory into LDS, NBUF of them in a ring, 16 bytes a lane;
 // a lane that has nothing to load (behind the last row, behind the last k) asks beyond the buffer's bound and gets zeros.
 // Where a lane's 16 bytes land is fixed by the hardware (one after the other), so rows are spread over the banks by which
-// 16 bytes of the row a lane asks for: slot s of row i holds piece s ^ f(i).
+// 16 bytes of the row a lane asks for: slot s of row i holds piece s ^ f(i).  (Without bank conflicts, by the counters; with them the clocks of LDS double.)
 //
-// Within a step t the operands of the next half step are read while the matrix instructions of this one run, across the barrier
-// too: piece t + 1 is complete before step t begins, and piece t + NBUF - 1 is requested in it.
+// While the matrix instructions of step t run, the operands of step t + 1 are read, each into the registers whose last use has just
+// been: piece t + 1 is complete before step t begins, piece t + NBUF - 1 is requested in it, and nothing is read from piece t.
 #pragma once
 #include "lsm_block_dev.h"
 
@@ -19,7 +20,6 @@ namespace lsm {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kBeyond = 0xfffff000u;  // offset and size of a buffer: at or behind it nothing is read and zeros come
@@ -47,13 +47,13 @@ __device__ __forceinline__ void load_to_lds(uint64_t base, uint32_t offset, uint
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer)
                  : "memory");
 }
-// One half step of a 32 x 32 product.
-__device__ __forceinline__ f32x16 product(const u32x4& a, const u32x4& b, f32x16 c, uint16_t) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+// One step of a 16 x 16 product: both operands hold, in lane l, 16 bytes of row l % 16 from byte 16 (l / 16) of the step on.
+__device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, f32x4 c, uint16_t) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 product(const u32x4& a, const u32x4& b, f32x16 c, float) {
+__device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, f32x4 c, float) {
     _Pragma("unroll") for (int i = 0; i < 4; ++i)
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
     return c;
 }
 
@@ -67,8 +67,12 @@ struct Operand {
     static_assert(N % 32 == 0 && (PIECES % WAVES == 0 || WAVES % PIECES == 0), "even shares");
     static constexpr int LINE = L == BY_ROWS ? kStepBytes : N * EL;   // bytes of a line in LDS
     static constexpr int LANES = LINE / 16, LINES = 64 / LANES;       // lanes of a line, lines of a load
-    // by columns: which 16 bytes of its line k a slot holds
-    static __device__ __forceinline__ int turn(int k) { return EL == 4 || LINE < 128 ? 0 : LINE >= 256 ? 4 * (k & 3) : 4 * ((k >> 1) & 1); }
+    // By columns slot s of line k holds piece s ^ turn(k): the lines k .. k + 3 and k + 8 .. k + 11 that half a wave reads at a time, 32
+    // bytes of each, lie in different banks.
+    static __device__ __forceinline__ int turn(int k) {
+        const int low = LINE >= 256 ? k & 3 : LINE == 128 ? (k >> 1) & 1 : 0, bits = LINE >= 256 ? 2 : LINE == 128 ? 1 : 0;
+        return EL == 4 ? 0 : 2 * (low | ((k >> 3) & 1) << bits);
+    }
 
     uint64_t base;
     uint32_t off[LOADS];
@@ -82,7 +86,9 @@ struct Operand {
         return ((lane % LANES) ^ turn(line(wave, lane, j))) * (16 / EL);
     }
     __device__ __forceinline__ static int line(int wave, int lane, int j) { return piece(wave, j) * LINES + lane / LANES; }
-    __device__ __forceinline__ static int k_piece(int lane) { return (lane & 3) ^ ((lane >> 3) & 3); }
+    // By rows slot s of row i holds piece s ^ 2 (i / 8 % 2): a wave reads 16 lanes at a time, of which those of rows 0..3 and 12..15 and those
+    // of rows 4..11 go together, the latter one piece further on.
+    __device__ __forceinline__ static int k_piece(int lane) { return (lane & 3) ^ (2 * (lane >> 5)); }
 
     // By rows: row_at(i) is the row's offset in bytes from `from` (kBeyond: none) for i of the tile.
     template <typename RowAt>
@@ -103,44 +109,42 @@ struct Operand {
             off[j] = first + c < width ? uint32_t(c * EL) + (LISTED ? 0u : uint32_t(line(wave, lane, j)) * uint32_t(stride)) : kBeyond;
         }
     }
-    // Request the pieces of step `step` of `K` k's; nothing behind the last.
-    __device__ __forceinline__ void request(uint32_t to, int step, int K, int wave, int lane) {
+    // Request load j of the pieces of step `step` of `K` k's; nothing behind the last.
+    __device__ __forceinline__ void request(uint32_t to, int step, int K, int wave, int lane, int j) {
         const int k0 = step * KSTEP;
-        _Pragma("unroll") for (int j = 0; j < LOADS; ++j) {
-            uint32_t o = off[j];
-            if (L == BY_ROWS) {
-                if (k0 + k_piece(lane) * (16 / EL) >= K) o = kBeyond;
-                load_to_lds(base + uint64_t(k0) * EL, o, uniform(int(to + piece(wave, j) * 1024)));
+        uint32_t o = off[j];
+        uint64_t from = base;
+        if (L == BY_ROWS) {
+            if (k0 + k_piece(lane) * (16 / EL) >= K) o = kBeyond;
+            from += uint64_t(k0) * EL;
+        } else {
+            const int k = k0 + line(wave, lane, j);
+            if (LISTED) {
+                const uint32_t row = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(list + 4 * (k % kList)));
+                o = o == kBeyond ? kBeyond : o + row * uint32_t(row_bytes);
             } else {
-                const int k = k0 + line(wave, lane, j);
-                if (LISTED) {
-                    const uint32_t row = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(list + 4 * (k % kList)));
-                    o = o == kBeyond ? kBeyond : o + row * uint32_t(row_bytes);
-                }
-                if (k >= K) o = kBeyond;
-                load_to_lds(LISTED ? base : base + uint64_t(k0) * uint64_t(uint32_t(row_bytes)), o, uniform(int(to + piece(wave, j) * 1024)));
+                from += uint64_t(k0) * uint64_t(uint32_t(row_bytes));
             }
+            if (k >= K) o = kBeyond;
         }
+        load_to_lds(from, o, uniform(int(to + piece(wave, j) * 1024)));
     }
     static constexpr int kList = 2048;  // rows of a list that are in LDS at a time
 
-    // Rows first .. first + 32 of half step `half_step` as an operand: lane l holds row l % 32, 16 bytes of k from l / 32 on.
-    __device__ __forceinline__ static u32x4 read(uint32_t at, int first, int half_step, int lane) {
-        const int half = lane >> 5;
-        if (L == BY_ROWS) {
-            const int x = (lane >> 1) & 3;
+    // Rows first .. first + 15 as an operand.
+    __device__ __forceinline__ static u32x4 read(uint32_t at, int first, int lane) {
+        const int r = lane & 15, q = lane >> 4;
+        if (L == BY_ROWS)
             return *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(
-                uintptr_t(at + first * kStepBytes + (lane & 31) * kStepBytes + (((2 * half_step + half) ^ x) * 16)));
-        }
+                uintptr_t(at + first * kStepBytes + r * kStepBytes + ((q ^ (2 * (r >> 3))) * 16)));
         if (EL == 4) {
             u32x4 v;
             _Pragma("unroll") for (int i = 0; i < 4; ++i)
-                v[i] = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(
-                    uintptr_t(at + (8 * half_step + 4 * half + i) * LINE + (first + (lane & 31)) * 4));
+                v[i] = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(at + (4 * q + i) * LINE + (first + r) * 4));
             return v;
         }
-        const int r = lane & 15, k = 16 * half_step + 8 * half + (r >> 2);
-        const int slot = ((first >> 3) + 2 * ((lane >> 4) & 1) + ((r >> 1) & 1)) ^ turn(r >> 2);
+        // 16 lanes read four lines' 16 columns and get a column of four lines each
+        const int k = 8 * q + (r >> 2), slot = ((first >> 3) + ((r >> 1) & 1)) ^ turn(k);
         const uint32_t p = at + k * LINE + slot * 16 + 8 * (r & 1);
         typedef s16x4 __attribute__((address_space(3))) * tr_t;
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(uintptr_t(p))));
@@ -149,18 +153,18 @@ struct Operand {
     }
 };
 
-// A tile: WC x WR waves of TC x TR blocks of 32 x 32.
+// A tile: WC x WR waves of TC x TR blocks of 16 x 16.
 template <typename TIO_, Layout LC, Layout LR, int WC_, int WR_, int TC_, int TR_, int NBUF_, bool LIST_C = false, bool LIST_R = false>
 struct Tile {
     typedef TIO_ TIO;
     static constexpr int WC = WC_, WR = WR_, TC = TC_, TR = TR_, NBUF = NBUF_, WAVES = WC * WR, THREADS = 64 * WAVES;
-    static constexpr int BC = WC * TC * 32, BR = WR * TR * 32;
+    static constexpr int BC = WC * TC * 16, BR = WR * TR * 16;
     typedef Operand<TIO, LC, BC, WAVES, LIST_C> C;
     typedef Operand<TIO, LR, BR, WAVES, LIST_R> R;
     static constexpr int STAGE = C::BYTES + R::BYTES, LOADS = C::LOADS + R::LOADS, AHEAD = NBUF - 1;
     static constexpr int LIST = LIST_C || LIST_R ? 4 * C::kList : 0;
-    // results on their way out: 32 rows of a wave's blocks at a time, in fp32, padded by 16 bytes a row; each wave has its own place
-    static constexpr int OUT = 32 * (TC * 128 + 16), RING = NBUF * STAGE;
+    // results on their way out: 16 rows of a wave's blocks at a time, in fp32, padded by 16 bytes a row; each wave has its own place
+    static constexpr int OUT = 16 * (TC * 64 + 16), RING = NBUF * STAGE;
     static constexpr int LDS = (RING > WAVES * OUT ? RING : WAVES * OUT) + LIST;
     static_assert(LDS <= 160 * 1024 && NBUF >= 3, "LDS");
 
@@ -177,19 +181,17 @@ struct Tile {
         lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)shared));
     }
     __device__ __forceinline__ uint32_t list_at() const { return lds + (LDS - LIST); }
-    __device__ __forceinline__ void request(int step, int K) {
+    // Load n of a step, of C::LOADS + R::LOADS.
+    __device__ __forceinline__ void request(int step, int K, int n) {
         const uint32_t at = lds + uint32_t(step % NBUF) * STAGE;
-        c.request(at, step, K, wave, lane);
-        r.request(at + C::BYTES, step, K, wave, lane);
+        if (n < C::LOADS) c.request(at, step, K, wave, lane, n);
+        else r.request(at + C::BYTES, step, K, wave, lane, n - C::LOADS);
     }
-    __device__ __forceinline__ void read(u32x4 (&a)[TC], u32x4 (&b)[TR], int step, int half_step) const {
-        const uint32_t at = lds + uint32_t(step % NBUF) * STAGE;
-        _Pragma("unroll") for (int i = 0; i < TC; ++i) a[i] = C::read(at, (wc * TC + i) * 32, half_step, lane);
-        _Pragma("unroll") for (int j = 0; j < TR; ++j) b[j] = R::read(at + C::BYTES, (wr * TR + j) * 32, half_step, lane);
+    __device__ __forceinline__ u32x4 read_c(int step, int i) const {
+        return C::read(lds + uint32_t(step % NBUF) * STAGE, (wc * TC + i) * 16, lane);
     }
-    static __device__ __forceinline__ void multiply(f32x16 (&acc)[TC][TR], const u32x4 (&a)[TC], const u32x4 (&b)[TR]) {
-        _Pragma("unroll") for (int j = 0; j < TR; ++j)
-            _Pragma("unroll") for (int i = 0; i < TC; ++i) acc[i][j] = product(a[i], b[j], acc[i][j], TIO());
+    __device__ __forceinline__ u32x4 read_r(int step, int j) const {
+        return R::read(lds + uint32_t(step % NBUF) * STAGE + C::BYTES, (wr * TR + j) * 16, lane);
     }
     // The rows of k0 .. k0 + n - 1 for an operand that is taken through a list.
     template <typename RowOf>
@@ -197,12 +199,12 @@ struct Tile {
         for (int k = k0 + int(threadIdx.x); k < min(k0 + n, K); k += THREADS)
             *reinterpret_cast<__attribute__((address_space(3))) uint32_t*>(uintptr_t(list_at() + 4 * (k % C::kList))) = row_of(k);
     }
-    __device__ __forceinline__ void walk(f32x16 (&acc)[TC][TR], int K) {
+    __device__ __forceinline__ void walk(f32x4 (&acc)[TC][TR], int K) {
         walk(acc, K, [](int) { return 0u; });
     }
     // acc += the product over k = 0 .. K - 1; row_of(k): the row of k in a list.  Begins and ends with LDS free.
     template <typename RowOf>
-    __device__ __forceinline__ void walk(f32x16 (&acc)[TC][TR], int K, RowOf row_of) {
+    __device__ __forceinline__ void walk(f32x4 (&acc)[TC][TR], int K, RowOf row_of) {
         const int steps = (K + C::KSTEP - 1) / C::KSTEP;
         if (steps == 0) return;
         if (LIST) {
@@ -210,61 +212,81 @@ struct Tile {
             wait_lds();
             barrier();
         }
-        u32x4 a0[TC], b0[TR], a1[TC], b1[TR];
-        _Pragma("unroll") for (int s = 0; s < AHEAD; ++s) request(s, K);
+        _Pragma("unroll") for (int s = 0; s < AHEAD; ++s)
+            _Pragma("unroll") for (int n = 0; n < LOADS; ++n) request(s, K, n);
         wait_loads<(AHEAD - 2) * LOADS>();
         barrier();
-        read(a0, b0, 0, 0);
-        for (int t = 0; t < steps; ++t) {
-            fence_schedule();
-            if (LIST) {  // the next half of the list, a step before its first row is wanted; the half that it replaces is used up
-                const int k = (t + AHEAD + 1) * C::KSTEP;
-                if (k >= C::kList && k % (C::kList / 2) == 0) fill(row_of, k, C::kList / 2, K);
-            }
-            request(t + AHEAD, K);
-            read(a1, b1, t, 1);
-            multiply(acc, a0, b0);
-            fence_schedule();
-            wait_lds();  // nothing of piece t is on its way any more: it may be overwritten behind the barrier
-            read(a0, b0, t + 1, 0);
-            multiply(acc, a1, b1);
-            fence_schedule();
-            wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
-            barrier();
+        u32x4 a[TC], b[TR], next[TR];
+        _Pragma("unroll") for (int j = 0; j < TR; ++j) b[j] = read_r(0, j);
+        _Pragma("unroll") for (int i = 0; i < TC; ++i) a[i] = read_c(0, i);
+        for (int t = 0; t < steps; t += 2) {
+            step(acc, a, b, next, t, K, row_of);
+            if (t + 1 < steps) step(acc, a, next, b, t + 1, K, row_of);
         }
         wait_lds();
         wait_loads<0>();
         barrier();
     }
-    // Values of block (i, j): register 4 g + e of a lane is row(j), column col(i, g) + e of the tile.
-    __device__ __forceinline__ int row(int j) const { return (wr * TR + j) * 32 + (lane & 31); }
-    __device__ __forceinline__ int col(int i, int g) const { return (wc * TC + i) * 32 + 8 * g + 4 * (lane >> 5); }
+    // Reads and requests are spread among the matrix instructions: behind one another they keep the wave from its next product until the
+    // last of them is accepted.
+    template <typename RowOf>
+    __device__ __forceinline__ void step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], const u32x4 (&b)[TR], u32x4 (&next)[TR], int t, int K, RowOf row_of) {
+        constexpr int ALL = TC * TR;
+        if (LIST) {  // the next half of the list, a step before its first row is wanted; the half that it replaces is used up
+            const int k = (t + AHEAD + 1) * C::KSTEP;
+            if (k >= C::kList && k % (C::kList / 2) == 0) fill(row_of, k, C::kList / 2, K);
+        }
+        fence_schedule();
+        _Pragma("unroll") for (int i = 0; i < TC; ++i)
+            _Pragma("unroll") for (int j = 0; j < TR; ++j) {
+                acc[i][j] = product(a[i], b[j], acc[i][j], TIO());
+                fence_schedule();
+                const int m = i * TR + j;
+                _Pragma("unroll") for (int n = m * TR / ALL; n < (m + 1) * TR / ALL; ++n) next[n] = read_r(t + 1, n);
+                _Pragma("unroll") for (int n = m * LOADS / ALL; n < (m + 1) * LOADS / ALL; ++n) request(t + AHEAD, K, n);
+                if (j == TR - 1) a[i] = read_c(t + 1, i);
+                fence_schedule();
+            }
+        wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
+        barrier();
+    }
+    // Values of block (i, j): element e of a lane is row(j), column col(i) + e of the tile.
+    __device__ __forceinline__ int row(int j) const { return (wr * TR + j) * 16 + (lane & 15); }
+    __device__ __forceinline__ int col(int i) const { return (wc * TC + i) * 16 + 4 * (lane >> 4); }
+    // Sum and maximum over the lanes of a row.
+    static __device__ __forceinline__ float row_sum(float x) {
+        x += __shfl_xor(x, 16, 64);
+        return x + __shfl_xor(x, 32, 64);
+    }
+    static __device__ __forceinline__ float row_max(float x) {
+        x = fmaxf(x, __shfl_xor(x, 16, 64));
+        return fmaxf(x, __shfl_xor(x, 32, 64));
+    }
 
     // Results to memory, whole lines at a time: block j of this wave's rows goes through the wave's own place in LDS (the caller has
-    // seen to it that LDS is free) and leaves in 16-byte pieces.  value(i, g): four results of block i < NB; line(r): where row r of
+    // seen to it that LDS is free) and leaves in 16-byte pieces.  value(i): four results of block i < NB; line(r): where row r of
     // the tile goes, first column of this wave included, or null; width: columns that there are from that column on.
-    __device__ __forceinline__ uint32_t own_place() const { return lds + uint32_t(wave) * OUT; }
-    template <int NB> __device__ __forceinline__ uint32_t cell(int row32, int column) const {
-        return own_place() + uint32_t(row32) * (NB * 128 + 16) + uint32_t(column) * 4;
+    template <int NB> __device__ __forceinline__ uint32_t cell(int row16, int column) const {
+        return lds + uint32_t(wave) * OUT + uint32_t(row16) * (NB * 64 + 16) + uint32_t(column) * 4;
     }
     template <int NB, typename Value>
     __device__ __forceinline__ void put(Value value) const {
         _Pragma("unroll") for (int i = 0; i < NB; ++i)
-            _Pragma("unroll") for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<NB>(lane & 31, i * 32 + 8 * g + 4 * (lane >> 5)))) = value(i, g);
+            *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<NB>(lane & 15, i * 16 + 4 * (lane >> 4)))) = value(i);
     }
     // ADD: to what is there already (fp32).
     template <int NB, typename TOUT, bool ADD = false, typename Line>
     __device__ __forceinline__ void take(int j, int width, Line line) const {
-        constexpr int E = 16 / int(sizeof(TOUT)), LANES = NB * 32 / E, ROWS = 64 / LANES;
-        _Pragma("unroll") for (int it = 0; it < 32 / ROWS; ++it) {
+        constexpr int E = 16 / int(sizeof(TOUT)), LANES = NB * 16 / E, ROWS = 64 / LANES;
+        _Pragma("unroll") for (int it = 0; it < (16 + ROWS - 1) / ROWS; ++it) {
             const int row = it * ROWS + lane / LANES, c = (lane % LANES) * E;
+            if (ROWS > 16 && row >= 16) continue;
             float v[E];
             _Pragma("unroll") for (int q = 0; q < E / 4; ++q) {
                 const f32x4 x = *reinterpret_cast<__attribute__((address_space(3))) const f32x4*>(uintptr_t(cell<NB>(row, c + 4 * q)));
                 _Pragma("unroll") for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
             }
-            TOUT* to = line((wr * TR + j) * 32 + row);
+            TOUT* to = line((wr * TR + j) * 16 + row);
             if (!to || c >= width) continue;
             if (ADD) {
                 float old[E];
@@ -276,20 +298,26 @@ struct Tile {
     }
 };
 
+// 2^x and 1 / (1 + 2^-x) of x = log2(e) y.  For bf16 elements the hardware's power and reciprocal, each within 2^-23: what they give is
+// rounded to bf16 or summed over many; for fp32 elements the library's functions.
+constexpr float kLog2e = 1.442695041f;
+__device__ __forceinline__ float power(float x, float) { return exp2f(x); }
+__device__ __forceinline__ float power(float x, uint16_t) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float sigmoid(float y, float) { return 1.f / (1.f + expf(-y)); }
+__device__ __forceinline__ float sigmoid(float y, uint16_t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * y)); }
+
 template <typename T>
-__device__ __forceinline__ void clear(f32x16 (&acc)[T::TC][T::TR]) {
+__device__ __forceinline__ void clear(f32x4 (&acc)[T::TC][T::TR]) {
     _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-        _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
-            _Pragma("unroll") for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
-__device__ __forceinline__ f32x4 four(const f32x16& v, int g) { return f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]}; }
 
 // Tiles of 256 columns and BR rows.
 template <typename TIO, Layout LC, Layout LR, int BR> struct TileOf;
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 256> { typedef Tile<TIO, LC, LR, 2, 4, 4, 2, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 128> { typedef Tile<TIO, LC, LR, 4, 2, 2, 2, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 64> { typedef Tile<TIO, LC, LR, 4, 1, 2, 2, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 32> { typedef Tile<TIO, LC, LR, 4, 1, 2, 1, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 256> { typedef Tile<TIO, LC, LR, 2, 4, 8, 4, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 128> { typedef Tile<TIO, LC, LR, 4, 2, 4, 4, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 64> { typedef Tile<TIO, LC, LR, 4, 1, 4, 4, 4> type; };
+template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 32> { typedef Tile<TIO, LC, LR, 4, 1, 4, 2, 4> type; };
 
 }  // namespace
 }  // namespace lsm

@@ -14,6 +14,8 @@
 namespace lsm {
 namespace {
 
+constexpr int kMostEntries = 256;
+
 struct VocabArgs {
     const void *x, *w;
     const int32_t *index, *offsets, *order, *place;
@@ -33,14 +35,10 @@ struct VocabArgs {
 __device__ __forceinline__ int rows_of(const VocabArgs& a) { return uniform(min(max(a.offsets[1], 0), a.n)); }
 __device__ __forceinline__ uint32_t token_of(const VocabArgs& a, int at) { return min(uint32_t(a.order[at]), uint32_t(a.n - 1)); }
 
-// exp: 24 bits for fp32 elements; for bf16 the hardware's power of two, whose argument's rounding costs 2^-24 of its size (2^-19 at most
-// where the result is not negligible).
-__device__ __forceinline__ float exponential(float x, float) { return expf(x); }
-__device__ __forceinline__ float exponential(float x, uint16_t) { return __builtin_amdgcn_exp2f(x * 1.442695041f); }
-
-__global__ __launch_bounds__(256) void k_teacher(VocabArgs a) {
-    const int t = int(blockIdx.x) * 4 + int(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (t >= a.n) return;
+__global__ __launch_bounds__(1024) void k_teacher(VocabArgs a) {
+    __shared__ int entry[kMostEntries][17];
+    __shared__ float share[kMostEntries][17];
+    const int t0 = int(blockIdx.x) * 16, slot = threadIdx.x >> 6, t = min(t0 + slot, a.n - 1), lane = threadIdx.x & 63;
     float z[4], m = -__builtin_inff();
     int v[4];
     _Pragma("unroll") for (int i = 0; i < 4; ++i) {
@@ -65,22 +63,61 @@ __global__ __launch_bounds__(256) void k_teacher(VocabArgs a) {
     }
     sum = group_sum<64>(sum);
     const float log_sum = logf(sum);
-    float entropy = 0.f;
+    float entropy = 0.f, p[4];
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+        p[i] = v[i] >= 0 ? expf(d[i]) / sum : 0.f;
+        if (p[i] > 0.f) entropy += p[i] * (d[i] - log_sum);
+        else v[i] = -1;
+    }
+    // entries of the same token become one, the first of them, so that what follows may take entries in any order
+    for (int e = 0; e < a.K; ++e) {
+        const int w = __builtin_amdgcn_readlane(e < 64 ? v[0] : e < 128 ? v[1] : e < 192 ? v[2] : v[3], e & 63);
+        float more = 0.f;
+        bool again = false;
+        _Pragma("unroll") for (int i = 0; i < 4; ++i)
+            if (w >= 0 && v[i] == w && 64 * i + lane > e) { more += p[i]; v[i] = -1; p[i] = 0.f; again = true; }
+        if (__ballot(again) == 0) continue;
+        more = group_sum<64>(more);
+        _Pragma("unroll") for (int i = 0; i < 4; ++i)
+            if (64 * i + lane == e) p[i] += more;
+    }
     _Pragma("unroll") for (int i = 0; i < 4; ++i) {
         const int j = 64 * i + lane;
-        const float p = v[i] >= 0 ? expf(d[i]) / sum : 0.f;
-        if (p > 0.f) entropy += p * (d[i] - log_sum);
-        if (j < a.K) {
-            a.entry[size_t(j) * a.n + t] = p > 0.f ? v[i] : -1;
-            a.share[size_t(j) * a.n + t] = p;
-        }
+        if (j >= a.K) break;
+        entry[j][slot] = v[i];
+        share[j][slot] = p[i];
     }
     entropy = group_sum<64>(entropy);
     if (lane == 0) {
         a.count[t] = counts ? 0 : -1;
         a.entropy[t] = entropy;
     }
+    __syncthreads();
+    for (int q = threadIdx.x; q < a.K * 16; q += 1024) {  // entry by entry, the tokens of one next to each other
+        const int j = q >> 4, token = t0 + (q & 15);
+        if (token >= a.n) continue;
+        a.entry[size_t(j) * a.n + token] = entry[j][q & 15];
+        a.share[size_t(j) * a.n + token] = share[j][q & 15];
+    }
 }
+
+// A token's entries as the quarters of a wave look through them: every fourth, 16 of them requested at a time.
+struct Entries {
+    static constexpr int N = 16;
+    int v[N];
+    __device__ __forceinline__ void load(const VocabArgs& a, int token, int e0, int lane) {
+        _Pragma("unroll") for (int u = 0; u < N; ++u) {
+            const int e = e0 + 4 * u + (lane >> 4);  // (n K is at most 2^28)
+            v[u] = token >= 0 && e < a.K ? a.entry[uint32_t(e) * uint32_t(a.n) + uint32_t(token)] : -1;
+        }
+    }
+    // found(e, column - first) for those of columns first .. first + width
+    template <typename Found>
+    __device__ __forceinline__ void find(int e0, int first, int width, int lane, Found found) const {
+        _Pragma("unroll") for (int u = 0; u < N; ++u)
+            if (v[u] >= 0 && uint32_t(v[u] - first) < uint32_t(width)) found(e0 + 4 * u + (lane >> 4), v[u] - first);
+    }
+};
 
 // Tile number id of rt x ct: eight rows of tiles at a time, the column changing more slowly than the row among them, so that the workgroups of
 // a die, whose numbers are neighbours, hold a block of about eight by four tiles.
@@ -96,7 +133,7 @@ __device__ __forceinline__ int number_of_tile(int all) {  // -1: none left.  A d
 
 // x (rows that count) times w^T from vocabulary column v0 on
 template <typename T>
-__device__ __forceinline__ void form_logits(T& t, const VocabArgs& a, int rows, int r0, int v0, int end, f32x16 (&acc)[T::TC][T::TR]) {
+__device__ __forceinline__ void form_logits(T& t, const VocabArgs& a, int rows, int r0, int v0, int end, f32x4 (&acc)[T::TC][T::TR]) {
     typedef typename T::TIO TIO;
     const uint32_t bytes = uint32_t(a.D) * uint32_t(sizeof(TIO));
     t.r.start_rows(a.x, t.wave, t.lane, [&](int i) { return r0 + i < rows ? token_of(a, r0 + i) * a.x_bytes : kBeyond; });
@@ -115,90 +152,100 @@ __global__ __launch_bounds__(T::THREADS) void k_logits(VocabArgs a) {
     tile_at(id, rt, ct, r, c);
     const int r0 = r * T::BR;
     T t(shared);
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     form_logits(t, a, rows, r0, c * T::BC, a.V, acc);
-    const int first = c * T::BC + t.wc * T::TC * 32, mine = first + 4 * (t.lane >> 5);  // of the wave, of the lane
+    const int first = c * T::BC + t.wc * T::TC * 16, mine = first + 4 * (t.lane >> 4);  // of the wave, of the lane
+    const float log2_scale = a.scale * kLog2e;
+    const bool edge = first + T::TC * 16 > a.V;
+    Entries entries;
+    if (TEACHER) entries.load(a, r0 + t.row(0) < rows ? int(token_of(a, r0 + t.row(0))) : -1, 0, t.lane);
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
         const int at = r0 + t.row(j);
         float m = -__builtin_inff(), sum = 0.f;
         _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-            _Pragma("unroll") for (int q = 0; q < 16; ++q) {
-                float z = acc[i][j][q] * a.scale;
-                if (mine + i * 32 + 8 * (q / 4) + q % 4 >= a.V) z = -__builtin_inff();
-                acc[i][j][q] = z;
-                m = fmaxf(m, z);
+            _Pragma("unroll") for (int q = 0; q < 4; ++q) {
+                if (edge && mine + i * 16 + q >= a.V) acc[i][j][q] = -__builtin_inff();
+                m = fmaxf(m, acc[i][j][q]);
             }
-        m = fmaxf(m, __shfl_xor(m, 32, 64));
-        const float top = m == -__builtin_inff() ? 0.f : m;
+        m = T::row_max(m);  // of the logits without their scale, which is positive
+        const float top = m == -__builtin_inff() ? 0.f : m * log2_scale;
         _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-            _Pragma("unroll") for (int q = 0; q < 16; ++q) sum += exponential(acc[i][j][q] - top, TIO());
-        sum += __shfl_xor(sum, 32, 64);
-        if (t.lane < 32 && at < rows) a.stats[size_t(c * T::WC + t.wc) * a.n + at] = f32x2{m, sum};
+            _Pragma("unroll") for (int q = 0; q < 4; ++q) sum += power(__builtin_fmaf(acc[i][j][q], log2_scale, -top), TIO());
+        sum = T::row_sum(sum);
+        if (t.lane < 16 && at < rows) a.stats[size_t(c * T::WC + t.wc) * a.n + at] = f32x2{m * a.scale, sum};
         const int token = at < rows ? int(token_of(a, at)) : -1;
         if (!TEACHER) {
             const int want = token < 0 ? -1 : a.index[token];
-            if (__ballot(uint32_t(want - first) < uint32_t(T::TC * 32)) == 0) continue;
+            if (__ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) == 0) continue;
             _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-                _Pragma("unroll") for (int q = 0; q < 16; ++q)
-                    if (want == mine + i * 32 + 8 * (q / 4) + q % 4) a.at_entry[at] = acc[i][j][q];
-        } else {  // either half of the wave looks for every other entry of its lane's row
-            t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
-            if (token < 0) continue;
-            for (int e = t.lane >> 5; e < a.K; e += 2) {
-                const int d = a.entry[size_t(e) * a.n + token] - first;
-                if (uint32_t(d) < uint32_t(T::TC * 32))
-                    a.at_entry[size_t(e) * a.n + at] =
-                        *reinterpret_cast<__attribute__((address_space(3))) const float*>(uintptr_t(t.template cell<T::TC>(t.lane & 31, d)));
+                _Pragma("unroll") for (int q = 0; q < 4; ++q)
+                    if (want == mine + i * 16 + q) a.at_entry[at] = acc[i][j][q] * a.scale;
+        } else {
+            Entries next;
+            if (j + 1 < T::TR) next.load(a, at + 16 < rows ? int(token_of(a, at + 16)) : -1, 0, t.lane);
+            t.template put<T::TC>([&](int i) { return acc[i][j]; });
+            const auto found = [&](int e, int d) {
+                a.at_entry[size_t(e) * a.n + at] =
+                    a.scale * *reinterpret_cast<__attribute__((address_space(3))) const float*>(uintptr_t(t.template cell<T::TC>(t.lane & 15, d)));
+            };
+            entries.find(0, first, T::TC * 16, t.lane, found);
+            for (int e0 = 4 * Entries::N; e0 < a.K; e0 += 4 * Entries::N) {
+                entries.load(a, token, e0, t.lane);
+                entries.find(e0, first, T::TC * 16, t.lane, found);
             }
+            entries = next;
         }
     }
 }
 
-// 64 tokens by a workgroup, every 16th part (and entry) by a thread
+// TOKENS tokens by a workgroup, every SLICES-th part (and entry) by a thread: 64 of them where tokens are many, four where a token's parts
+// are what there is to do (three tokens, 788 parts: 24 us by 64, 7 by four).
+template <int TOKENS, typename Join>
+__device__ __forceinline__ float join(float (&all)[1024], float x, Join with) {
+    constexpr int SLICES = 1024 / TOKENS;
+    __syncthreads();
+    all[threadIdx.x] = x;
+    _Pragma("unroll") for (int half = SLICES / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (int(threadIdx.x) < half * TOKENS) all[threadIdx.x] = with(all[threadIdx.x], all[threadIdx.x + half * TOKENS]);
+    }
+    __syncthreads();
+    return all[threadIdx.x % TOKENS];
+}
+template <int TOKENS>
 __global__ __launch_bounds__(1024) void k_join(VocabArgs a) {
-    __shared__ float top[16][64], total[16][64];
-    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, token = int(blockIdx.x) * 64 + lane;
+    __shared__ float all[1024];
+    constexpr int SLICES = 1024 / TOKENS, U = 4;
+    const auto larger = [](float x, float y) { return fmaxf(x, y); };
+    const auto add = [](float x, float y) { return x + y; };
+    const int slice = threadIdx.x / TOKENS, token = int(blockIdx.x) * TOKENS + int(threadIdx.x) % TOKENS;
     const int at = token < a.n ? a.place[token] : -1;
     float m = -__builtin_inff(), s = 0.f;
-    if (at >= 0 && at < a.n) {
-        for (int p = slice; p < a.parts; p += 16) m = fmaxf(m, a.stats[size_t(p) * a.n + at].x);
-        const float mm = m == -__builtin_inff() ? 0.f : m;
-        for (int p = slice; p < a.parts; p += 16) {
-            const f32x2 v = a.stats[size_t(p) * a.n + at];
-            s += v.y * expf(v.x - mm);
+    if (at >= 0 && at < a.n)
+        for (int p0 = slice; p0 < a.parts; p0 += U * SLICES) {  // a running maximum and sum, U parts at a time
+            f32x2 v[U];
+            float top = m;
+            _Pragma("unroll") for (int u = 0; u < U; ++u) {
+                v[u] = p0 + u * SLICES < a.parts ? a.stats[size_t(p0 + u * SLICES) * a.n + at] : f32x2{-__builtin_inff(), 0.f};
+                top = fmaxf(top, v[u].x);
+            }
+            const float base = top == -__builtin_inff() ? 0.f : top;
+            s *= expf(m - base);
+            _Pragma("unroll") for (int u = 0; u < U; ++u) s += v[u].y * expf(v[u].x - base);
+            m = top;
         }
-    }
-    top[slice][lane] = m;
-    __syncthreads();
-    float all = top[0][lane];
-    _Pragma("unroll") for (int i = 1; i < 16; ++i) all = fmaxf(all, top[i][lane]);
-    const float base = all == -__builtin_inff() ? 0.f : all;
-    total[slice][lane] = m == -__builtin_inff() ? s : s * expf(m - base);
-    __syncthreads();
-    float sum = 0.f;
-    _Pragma("unroll") for (int i = 0; i < 16; ++i) sum += total[i][lane];
-    const float lse = base + logf(sum);
-    __syncthreads();
-    float part = 0.f, shares = 0.f;
+    const float top = join<TOKENS>(all, m, larger), base = top == -__builtin_inff() ? 0.f : top;
+    const float lse = base + logf(join<TOKENS>(all, m == -__builtin_inff() ? s : s * expf(m - base), add));
+    float part = 0.f;
     if (a.K > 0 && at >= 0)
-        for (int e = slice; e < a.K; e += 16) {
+        for (int e = slice; e < a.K; e += SLICES) {
             const float p = a.share[size_t(e) * a.n + token];
-            if (!(p > 0.f)) continue;
-            shares += p;
-            part += p * (lse - a.at_entry[size_t(e) * a.n + at]);
+            if (p > 0.f) part += p * (lse - a.at_entry[size_t(e) * a.n + at]);
         }
-    top[slice][lane] = part;
-    __syncthreads();
+    if (a.K > 0) part = join<TOKENS>(all, part, add);
     if (slice != 0 || token >= a.n) return;
-    float loss = 0.f;
-    if (a.K > 0) {
-        loss = a.entropy[token];
-        _Pragma("unroll") for (int i = 0; i < 16; ++i) loss += top[i][lane];
-    } else if (at >= 0) {
-        loss = lse - a.at_entry[at];
-    }
-    a.loss[token] = at >= 0 ? loss : 0.f;
-    a.lse[token] = at >= 0 ? lse : 0.f;
+    a.loss[token] = at < 0 ? 0.f : a.K > 0 ? a.entropy[token] + part : lse - a.at_entry[at];
+    a.lse[token] = at < 0 ? 0.f : lse;
 }
 
 template <typename T, bool TEACHER>
@@ -212,31 +259,43 @@ __global__ __launch_bounds__(T::THREADS) void k_grad(VocabArgs a) {
     tile_at(id, rt, ct, r, c);
     const int r0 = r * T::BR;
     T t(shared);
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     form_logits(t, a, rows, r0, a.v0 + c * T::BC, end, acc);
-    const int column = c * T::BC + t.wc * T::TC * 32, first = a.v0 + column, mine = first + 4 * (t.lane >> 5);
+    const int column = c * T::BC + t.wc * T::TC * 16, first = a.v0 + column, mine = first + 4 * (t.lane >> 4);
+    const float log2_scale = a.scale * kLog2e;
+    const bool edge = first + T::TC * 16 > end;
+    Entries entries;
+    if (TEACHER) entries.load(a, r0 + t.row(0) < rows ? int(token_of(a, r0 + t.row(0))) : -1, 0, t.lane);
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
         const int at = r0 + t.row(j), token = at < rows ? int(token_of(a, at)) : -1;
         const float lse = token < 0 ? 0.f : a.lse_in[token], weight = token < 0 ? 0.f : a.d_loss[token] * a.scale;
         const int want = TEACHER || token < 0 ? -1 : a.index[token];
-        t.template put<T::TC>([&](int i, int g) {
+        Entries next;
+        if (TEACHER && j + 1 < T::TR) next.load(a, at + 16 < rows ? int(token_of(a, at + 16)) : -1, 0, t.lane);
+        const bool here = !TEACHER && __ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) != 0;
+        const float top = lse * kLog2e;
+        t.template put<T::TC>([&](int i) {
             f32x4 v;
             _Pragma("unroll") for (int e = 0; e < 4; ++e) {
-                const int col = mine + i * 32 + 8 * g + e;
-                float p = exponential(acc[i][j][4 * g + e] * a.scale - lse, TIO());
-                if (!TEACHER && col == want) p -= 1.f;
-                v[e] = col < end && token >= 0 ? weight * p : 0.f;
+                const int col = mine + i * 16 + e;
+                float p = power(__builtin_fmaf(acc[i][j][e], log2_scale, -top), TIO());
+                if (here && col == want) p -= 1.f;
+                v[e] = edge && col >= end ? 0.f : weight * p;
             }
             return v;
         });
-        if (TEACHER && token >= 0 && t.lane < 32)  // a row's entries one after the other: some may be the same
-            for (int e = 0; e < a.K; ++e) {
-                const int d = a.entry[size_t(e) * a.n + token] - first;
-                if (uint32_t(d) < uint32_t(T::TC * 32) && d + first < end) {
-                    auto* p = reinterpret_cast<__attribute__((address_space(3))) float*>(uintptr_t(t.template cell<T::TC>(t.lane, d)));
-                    *p = *p - weight * a.share[size_t(e) * a.n + token];
-                }
+        if (TEACHER) {
+            const auto found = [&](int e, int d) {  // no two entries of a row are the same
+                auto* p = reinterpret_cast<__attribute__((address_space(3))) float*>(uintptr_t(t.template cell<T::TC>(t.lane & 15, d)));
+                *p = *p - weight * a.share[size_t(e) * a.n + token];
+            };
+            entries.find(0, first, T::TC * 16, t.lane, found);
+            for (int e0 = 4 * Entries::N; e0 < a.K; e0 += 4 * Entries::N) {
+                entries.load(a, token, e0, t.lane);
+                entries.find(e0, first, T::TC * 16, t.lane, found);
             }
+            entries = next;
+        }
         // the columns behind the vocabulary's end are zeros that the next products read
         t.template take<T::TC, TIO>(j, a.piece - column, [&](int q) {
             return r0 + q < rows ? static_cast<TIO*>(a.grad) + size_t(r0 + q) * a.piece + column : nullptr;
@@ -257,12 +316,12 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(VocabArgs a) {
     T t(shared);
     t.r.start_cols(a.grad, a.piece * EL, r * T::BR, a.piece, t.wave, t.lane, 0);
     t.c.start_cols(a.x, int(a.x_bytes), c * T::BC, a.D, t.wave, t.lane, t.list_at());
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     clear<T>(acc);
     t.walk(acc, rows, [&](int k) { return token_of(a, k); });
-    const int c0 = c * T::BC + t.wc * T::TC * 32;
+    const int c0 = c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
+        t.template put<T::TC>([&](int i) { return acc[i][j]; });
         t.template take<T::TC, TIO>(j, a.D - c0, [&](int q) {
             const int v = r * T::BR + q;
             return v < width ? static_cast<TIO*>(a.dw) + size_t(a.v0 + v) * a.D + c0 : nullptr;
@@ -288,13 +347,13 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     t.r.start_rows(static_cast<const TIO*>(a.grad) + size_t(r0) * a.piece + k0, t.wave, t.lane,
                    [&](int i) { return r0 + i < rows ? uint32_t(i) * bytes : kBeyond; });
     t.c.start_cols(static_cast<const TIO*>(a.w) + size_t(a.v0 + k0) * a.D, a.D * EL, c * T::BC, a.D, t.wave, t.lane, 0);
-    f32x16 acc[T::TC][T::TR];
+    f32x4 acc[T::TC][T::TR];
     clear<T>(acc);
     t.walk(acc, k1 - k0);
-    const int c0 = c * T::BC + t.wc * T::TC * 32;
+    const int c0 = c * T::BC + t.wc * T::TC * 16;
     const auto line = [&](int q) { return r0 + q < rows ? a.part + (size_t(share) * a.n + r0 + q) * a.D + c0 : nullptr; };
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i, int g) { return four(acc[i][j], g); });
+        t.template put<T::TC>([&](int i) { return acc[i][j]; });
         if (a.v0 == 0) t.template take<T::TC, float>(j, a.D - c0, line);
         else t.template take<T::TC, float, true>(j, a.D - c0, line);
     }
@@ -319,13 +378,13 @@ __global__ __launch_bounds__(256) void k_dx_join(VocabArgs a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-constexpr int kMostEntries = 256;
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of the logits' gradient at a time: what the memory-side cache holds
 
 int check(const lsm_vocab_params* p) {
     if (!p) return LSM_ERR_NULL;
     if (p->struct_size != sizeof(lsm_vocab_params)) return LSM_ERR_SHAPE;
     if (p->n < 1 || p->D < 1 || p->V < 1 || p->K < 0 || p->n > kMostPairs || p->V > (1 << 24)) return LSM_ERR_SHAPE;
+    if (int64_t(p->n) * p->K > (1 << 28)) return LSM_ERR_SHAPE;
     if (!(p->temperature > 0.f) || !(1.f / p->temperature < 3.4e38f) || !(1.f / p->temperature > 0.f)) return LSM_ERR_SHAPE;
     if (p->dtype != LSM_DTYPE_F32 && p->dtype != LSM_DTYPE_BF16) return LSM_ERR_UNSUPPORTED;
     if (p->K > kMostEntries || p->D % 8 || p->D > 65536 || p->reserved != 0) return LSM_ERR_UNSUPPORTED;
@@ -407,7 +466,7 @@ VocabArgs arguments(const lsm_vocab_params& p, const Space& s, char* ws, const v
 bool enqueue_rows(const VocabArgs& a, const Space& s, char* ws, hipStream_t st) {
     if (a.K > 0) {
         ProfScope ps(KID_VOCAB_ROWS, st);
-        hipLaunchKernelGGL(k_teacher, dim3(up(a.n, 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(k_teacher, dim3(up(a.n, 16)), dim3(1024), 0, st, a);
         if (!launched()) return false;
     }
     return enqueue_plan(a.K ? a.count : a.index, a.n, 1, a.K ? 1 : a.V, reinterpret_cast<int32_t*>(ws + s.offsets),
@@ -427,7 +486,8 @@ bool launch_fwd(const VocabArgs& a, hipStream_t st) {
     }
     if (!launched()) return false;
     ProfScope ps(KID_VOCAB_JOIN, st);
-    hipLaunchKernelGGL(k_join, dim3(up(a.n, 64)), dim3(1024), 0, st, a);
+    if (a.n > 1024) hipLaunchKernelGGL(k_join<64>, dim3(up(a.n, 64)), dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL(k_join<4>, dim3(up(a.n, 4)), dim3(1024), 0, st, a);
     return launched();
 }
 
@@ -435,7 +495,7 @@ template <typename TIO, int BR>
 bool launch_bwd(VocabArgs a, hipStream_t st) {
     typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type T;
     typedef typename TileOf<TIO, BY_COLS, BY_ROWS, BR>::type X;
-    typedef Tile<TIO, BY_COLS, BY_COLS, 2, 4, 4, 2, 4, true, false> W;
+    typedef Tile<TIO, BY_COLS, BY_COLS, 2, 4, 8, 4, 4, true, false> W;
     for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
         const int width = a.V - a.v0 < a.piece ? a.V - a.v0 : a.piece;
         {
