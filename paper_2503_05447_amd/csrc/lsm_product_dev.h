@@ -65,6 +65,7 @@ struct Operand {
     static constexpr int EL = int(sizeof(TIO)), KSTEP = kStepBytes / EL, BYTES = N * kStepBytes;
     static constexpr int PIECES = N / 16, LOADS = PIECES >= WAVES ? PIECES / WAVES : 1;  // 1 KiB a load; of a wave
     static_assert(N % 32 == 0 && (PIECES % WAVES == 0 || WAVES % PIECES == 0), "even shares");
+    static constexpr int kList = 2048;  // rows of a list that are in LDS at a time
     static constexpr int LINE = L == BY_ROWS ? kStepBytes : N * EL;   // bytes of a line in LDS
     static constexpr int LANES = LINE / 16, LINES = 64 / LANES;       // lanes of a line, lines of a load
     // By columns slot s of line k holds piece s ^ turn(k): the lines k .. k + 3 and k + 8 .. k + 11 that half a wave reads at a time, 32
@@ -77,7 +78,8 @@ struct Operand {
     uint64_t base;
     uint32_t off[LOADS];
     int row_bytes;
-    int list;  // LDS address of the list of rows (LISTED, by columns)
+    int list;             // LDS address of the list of rows (LISTED, by columns)
+    uint32_t row[LOADS];  // LISTED: the rows of the next request
 
     __device__ __forceinline__ static int piece(int wave, int j) { return (wave * LOADS + j) % PIECES; }
     // the row (by rows) or the first of eight (four) neighbouring ones (by columns) that load j of this lane brings
@@ -109,6 +111,12 @@ struct Operand {
             off[j] = first + c < width ? uint32_t(c * EL) + (LISTED ? 0u : uint32_t(line(wave, lane, j)) * uint32_t(stride)) : kBeyond;
         }
     }
+    __device__ __forceinline__ uint32_t listed(int k) const {
+        return *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(list + 4 * (k % kList)));
+    }
+    __device__ __forceinline__ void first_rows(int wave, int lane) {
+        _Pragma("unroll") for (int j = 0; j < LOADS; ++j) row[j] = LISTED ? listed(line(wave, lane, j)) : 0;
+    }
     // Request load j of the pieces of step `step` of `K` k's; nothing behind the last.
     __device__ __forceinline__ void request(uint32_t to, int step, int K, int wave, int lane, int j) {
         const int k0 = step * KSTEP;
@@ -120,8 +128,9 @@ struct Operand {
         } else {
             const int k = k0 + line(wave, lane, j);
             if (LISTED) {
-                const uint32_t row = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(list + 4 * (k % kList)));
-                o = o == kBeyond ? kBeyond : o + row * uint32_t(row_bytes);
+                const uint32_t at = o + row[j] * uint32_t(row_bytes);
+                o = o == kBeyond ? kBeyond : at;
+                row[j] = listed(k + KSTEP);
             } else {
                 from += uint64_t(k0) * uint64_t(uint32_t(row_bytes));
             }
@@ -129,7 +138,6 @@ struct Operand {
         }
         load_to_lds(from, o, uniform(int(to + piece(wave, j) * 1024)));
     }
-    static constexpr int kList = 2048;  // rows of a list that are in LDS at a time
 
     // Rows first .. first + 15 as an operand.
     __device__ __forceinline__ static u32x4 read(uint32_t at, int first, int lane) {
@@ -211,6 +219,8 @@ struct Tile {
             fill(row_of, 0, C::kList, K);
             wait_lds();
             barrier();
+            c.first_rows(wave, lane);
+            r.first_rows(wave, lane);
         }
         _Pragma("unroll") for (int s = 0; s < AHEAD; ++s)
             _Pragma("unroll") for (int n = 0; n < LOADS; ++n) request(s, K, n);
@@ -232,8 +242,8 @@ struct Tile {
     template <typename RowOf>
     __device__ __forceinline__ void step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], const u32x4 (&b)[TR], u32x4 (&next)[TR], int t, int K, RowOf row_of) {
         constexpr int ALL = TC * TR;
-        if (LIST) {  // the next half of the list, a step before its first row is wanted; the half that it replaces is used up
-            const int k = (t + AHEAD + 1) * C::KSTEP;
+        if (LIST) {  // the next half of the list, a step before its first row is read; the half that it replaces is used up
+            const int k = (t + AHEAD + 2) * C::KSTEP;
             if (k >= C::kList && k % (C::kList / 2) == 0) fill(row_of, k, C::kList / 2, K);
         }
         fence_schedule();
