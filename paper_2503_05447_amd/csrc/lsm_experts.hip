@@ -7,8 +7,9 @@
 //   k_dx           the gradients of gate and factor times Wg, Wu, fp32, a row a pair
 //   k_dw           both weights' gradients, an expert's pairs being the long axis
 // An expert's rows are whole tiles but the last; a workgroup finds its expert and tile from the offsets.
+#include <type_traits>
+
 #include "lsm_product_dev.h"
-#include "lsm_train_dev.h"
 
 namespace lsm {
 namespace {
@@ -20,8 +21,9 @@ struct ExpertArgs {
     void *y, *d_w_gate_up, *d_w_down;
     float* d_weights;
     void *h, *da;           // [pairs][F]: activations (backward: times their weight); [pairs][2 F]
-    float *part, *weight_part;  // [pairs][D]; [tiles of F][pairs]
-    int n, D, F, E, top_k, parts;
+    void* part;           // [pairs][D]: fp32, or with bf16 elements fp16 times part_scale
+    float *part_scale, *weight_part;  // [stretches of D][pairs]; [tiles of F][pairs]
+    int n, D, F, E, top_k, parts, stretch;
     uint32_t x_bytes, dy_bytes;  // between rows
 };
 
@@ -115,15 +117,26 @@ __global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
     }
 }
 
-// rows of `parts` [pairs][D] = rows of R [pairs][K] times C^T
+// rows of `part` = the tile's
 template <typename T>
 __device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, const Where& w, f32x4 (&acc)[T::TC][T::TR]) {
-    const int d0 = w.c * T::BC + t.wc * T::TC * 16;
+    constexpr bool HALF = sizeof(typename T::TIO) == 2;
+    typedef typename std::conditional<HALF, half_t, float>::type TP;
+    const int stretch = w.c * T::WC + t.wc, d0 = stretch * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i) { return acc[i][j]; });
-        t.template take<T::TC, float>(j, a.D - d0, [&](int r) {
+        float scale = 1.f;
+        if (HALF) {
+            float m = 0.f;
+            _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+                _Pragma("unroll") for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_size(acc[i][j][e]));
+            scale = scale_for(T::row_max(m));
+            const int at = w.r * T::BR + t.row(j);
+            if (t.lane < 16 && at < w.count && d0 < a.D) a.part_scale[size_t(stretch) * (size_t(a.n) * a.top_k) + w.first + at] = 1.f / scale;
+        }
+        t.template put<T::TC>([&](int i) { return acc[i][j] * scale; });
+        t.template take<T::TC, TP>(j, a.D - d0, [&](int r) {
             const int at = w.r * T::BR + r;
-            return at < w.count ? a.part + size_t(w.first + at) * a.D + d0 : nullptr;
+            return at < w.count ? static_cast<TP*>(a.part) + size_t(w.first + at) * a.D + d0 : nullptr;
         });
     }
 }
@@ -177,6 +190,7 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
     Where w;
     if (!find_tile<T::BR>(a, (a.F + T::BC - 1) / T::BC, w)) return;
     f32x4 gu[H::TC][H::TR], tt[T::TC][T::TR];
+    float weight[T::TR];
     {
         H t(shared);
         start_gate_up(t, a, w);
@@ -191,10 +205,12 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
     t.c.start_cols(static_cast<const TIO*>(a.w_down) + size_t(w.e) * a.D * a.F, a.F * int(sizeof(TIO)), w.c * T::BC, a.F, t.wave, t.lane, 0);
     clear<T>(tt);
     t.walk(tt, a.D);
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
+        weight[j] = w.r * T::BR + t.row(j) < w.count ? a.weights[pair_of(a, w.first + w.r * T::BR + t.row(j))] : 0.f;
     const int f0 = w.c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
         const int at = w.r * T::BR + t.row(j);
-        const float p = at < w.count ? a.weights[pair_of(a, w.first + at)] : 0.f;
+        const float p = weight[j];
         float along = 0.f;
         _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
             _Pragma("unroll") for (int r = 0; r < 4; ++r) {
@@ -278,10 +294,13 @@ __global__ __launch_bounds__(256) void k_sum(ExpertArgs a) {
         const int at = a.place[size_t(t) * a.top_k + j];
         if (uint32_t(at) >= uint32_t(a.n * a.top_k)) continue;
         const float p = WEIGHTED ? a.weights[size_t(t) * a.top_k + j] : 1.f;
-        const f32x4* z = reinterpret_cast<const f32x4*>(a.part + size_t(at) * a.D + d);
-        _Pragma("unroll") for (int q = 0; q < E / 4; ++q) {
-            const f32x4 v = z[q];
-            _Pragma("unroll") for (int e = 0; e < 4; ++e) s[4 * q + e] += p * v[e];
+        if constexpr (E == 8) {
+            const float q = p * a.part_scale[size_t(d / a.stretch) * (size_t(a.n) * a.top_k) + at];
+            const f16x8 v = *reinterpret_cast<const f16x8*>(static_cast<const half_t*>(a.part) + size_t(at) * a.D + d);
+            _Pragma("unroll") for (int e = 0; e < 8; ++e) s[e] += q * float(v[e]);
+        } else {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part) + size_t(at) * a.D + d);
+            _Pragma("unroll") for (int e = 0; e < 4; ++e) s[e] += p * v[e];
         }
     }
     *reinterpret_cast<u32x4*>(static_cast<TIO*>(a.y) + size_t(t) * a.D + d) = pack(s);
@@ -304,35 +323,42 @@ int check(const lsm_experts_params* p, bool backward) {
     return LSM_OK;
 }
 
-template <typename TIO, int BR> struct HalfTileOf;  // the same rows, half the columns
-template <typename TIO> struct HalfTileOf<TIO, 256> { typedef Tile<TIO, BY_COLS, BY_ROWS, 2, 4, 4, 4, 4> type; };
-template <typename TIO> struct HalfTileOf<TIO, 128> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 2, 2, 4, 4> type; };
-template <typename TIO> struct HalfTileOf<TIO, 64> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 2, 4, 4> type; };
-template <typename TIO> struct HalfTileOf<TIO, 32> { typedef Tile<TIO, BY_COLS, BY_ROWS, 4, 1, 2, 2, 4> type; };
-
-int rows_of_tile(const lsm_experts_params& p) {
-    const int64_t mean = int64_t(p.n) * p.top_k / p.E;
-    return mean >= 192 ? 256 : mean >= 56 ? 128 : mean >= 28 ? 64 : 32;
+// Tiles of the products over pairs, whose rows are ragged, and of the weights' gradients.
+struct Plan { int up, down, hidden, dx, dw1, dw2; };
+int64_t tiles_of_rows(const lsm_experts_params& p, int rows) {  // about: every expert's last tile is half empty
+    const int64_t pairs = int64_t(p.n) * p.top_k, active = pairs < p.E ? pairs : p.E, full = pairs / rows + active / 2;
+    return full > active ? full : active;
 }
-int weight_parts(const lsm_experts_params& p) {  // waves along the features
-    const int br = rows_of_tile(p), wc = br == 256 ? 2 : 4;
-    return (p.F + 127) / 128 * wc;
+Plan plan_of(const lsm_experts_params& p) {
+    const bool f32 = p.dtype == LSM_DTYPE_F32;
+    const auto rows = [&](int cols, int K, int parts) {
+        return pick_tile(f32, K, [&](const TileSize& t) { return tiles_of_rows(p, t.rows) * up(cols, t.cols / parts); }, 0x7f);
+    };
+    const int64_t mean = (int64_t(p.n) * p.top_k + p.E - 1) / p.E;
+    const auto square = [&](int r, int c) {
+        return pick_tile(f32, mean, [&](const TileSize& t) { return int64_t(p.E) * up(r, t.rows) * up(c, t.cols); }, 1 << 0 | 1 << 2 | 1 << 5);
+    };
+    return Plan{rows(p.F, p.D, 2), rows(p.D, p.F, 1), rows(p.F, p.D + p.D / 2, 2), rows(p.D, 2 * p.F, 1), square(2 * p.F, p.D), square(p.D, p.F)};
 }
+int weight_parts(const lsm_experts_params& p, int kind) { return up(p.F, kTiles[kind].cols / 2) * kTiles[kind].waves; }
+int stretch_of(int kind) { return kTiles[kind].cols / kTiles[kind].waves; }
 // The most tiles there can be: every expert's last one may be almost empty.
-unsigned grid_of(const lsm_experts_params& p, int br, int cols) {
-    const int64_t pairs = int64_t(p.n) * p.top_k, tiles = pairs / br + (pairs < p.E ? pairs : int64_t(p.E));
+unsigned grid_of(const ExpertArgs& a, int rows, int cols) {
+    const int64_t pairs = int64_t(a.n) * a.top_k, tiles = pairs / rows + (pairs < a.E ? pairs : int64_t(a.E));
     return unsigned((tiles * cols + 7) / 8 * 8);
 }
 
-struct Space { size_t h, da, part, weight_part, bytes; };
+struct Space { size_t h, da, part, part_scale, weight_part, bytes; };
 Space space(const lsm_experts_params& p, bool backward) {
     const size_t pairs = size_t(p.n) * p.top_k, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4;
+    const Plan q = plan_of(p);
     Space s{};
     s.h = 0;
     s.part = align256(pairs * p.F * el);
-    s.da = s.part + align256(pairs * p.D * 4);
+    s.part_scale = s.part + align256(pairs * p.D * el);
+    s.da = s.part_scale + (el == 2 ? align256(pairs * up(p.D, stretch_of(backward ? q.dx : q.down)) * 4) : 0);
     s.weight_part = s.da + (backward ? align256(pairs * 2 * p.F * el) : 0);
-    s.bytes = s.weight_part + (backward ? align256(pairs * weight_parts(p) * 4) : 0);
+    s.bytes = s.weight_part + (backward ? align256(pairs * weight_parts(p, q.hidden) * 4) : 0);
     return s;
 }
 
@@ -345,56 +371,65 @@ bool launch_sum(const ExpertArgs& a, hipStream_t st) {
     return launched();
 }
 
-template <typename TIO, int BR>
-bool launch_fwd(const lsm_experts_params& p, const ExpertArgs& a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type T;
-    {
-        ProfScope ps(KID_EXPERTS_UP, st);
-        hipLaunchKernelGGL((k_up<T>), dim3(grid_of(p, BR, (a.F + T::BC / 2 - 1) / (T::BC / 2))), dim3(T::THREADS), 0, st, a);
-    }
-    if (!launched()) return false;
-    {
-        ProfScope ps(KID_EXPERTS_DOWN, st);
-        hipLaunchKernelGGL((k_down<T>), dim3(grid_of(p, BR, (a.D + T::BC - 1) / T::BC)), dim3(T::THREADS), 0, st, a);
-    }
-    return launched() && launch_sum<TIO, true>(a, st);
+template <typename TIO, int KIND>
+bool launch_up(const ExpertArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    ProfScope ps(KID_EXPERTS_UP, st);
+    hipLaunchKernelGGL((k_up<T>), dim3(grid_of(a, T::BR, up(a.F, T::BC / 2))), dim3(T::THREADS), 0, st, a);
+    return launched();
 }
-
-template <typename T, bool DOWN>
+template <typename TIO, int KIND>
+bool launch_down(const ExpertArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    ProfScope ps(KID_EXPERTS_DOWN, st);
+    hipLaunchKernelGGL((k_down<T>), dim3(grid_of(a, T::BR, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    return launched();
+}
+template <typename TIO, int KIND>
+bool launch_hidden(const ExpertArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type H;
+    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND, true>::type T;
+    ProfScope ps(KID_EXPERTS_HIDDEN_GRAD, st);
+    hipLaunchKernelGGL((k_hidden_grad<H, T>), dim3(grid_of(a, T::BR, up(a.F, T::BC))), dim3(T::THREADS), 0, st, a);
+    return launched();
+}
+template <typename TIO, int KIND>
+bool launch_dx(const ExpertArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND>::type T;
+    ProfScope ps(KID_EXPERTS_DX, st);
+    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of(a, T::BR, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    return launched();
+}
+template <typename TIO, int KIND, bool DOWN>
 bool launch_dw(const ExpertArgs& a, hipStream_t st) {
-    const int rows = DOWN ? a.D : 2 * a.F, cols = DOWN ? a.F : a.D, rt = (rows + T::BR - 1) / T::BR, ct = (cols + T::BC - 1) / T::BC;
+    typedef typename TileOf<TIO, BY_COLS, BY_COLS, KIND, false, !DOWN, DOWN>::type T;
+    const int rt = up(DOWN ? a.D : 2 * a.F, T::BR), ct = up(DOWN ? a.F : a.D, T::BC);
     ProfScope ps(KID_EXPERTS_DW, st);
     hipLaunchKernelGGL((k_dw<T, DOWN>), dim3(unsigned((int64_t(a.E) * rt * ct + 7) / 8 * 8)), dim3(T::THREADS), 0, st, a, rt, ct);
     return launched();
 }
-template <typename TIO, int BR>
-bool launch_bwd(const lsm_experts_params& p, const ExpertArgs& a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type H;
-    typedef typename HalfTileOf<TIO, BR>::type T;
-    {
-        ProfScope ps(KID_EXPERTS_HIDDEN_GRAD, st);
-        hipLaunchKernelGGL((k_hidden_grad<H, T>), dim3(grid_of(p, BR, (a.F + T::BC - 1) / T::BC)), dim3(T::THREADS), 0, st, a);
-    }
-    if (!launched()) return false;
-    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, BR>::type X;
-    {
-        ProfScope ps(KID_EXPERTS_DX, st);
-        hipLaunchKernelGGL((k_dx<X>), dim3(grid_of(p, BR, (a.D + X::BC - 1) / X::BC)), dim3(X::THREADS), 0, st, a);
-    }
-    if (!launched() || !launch_sum<TIO, false>(a, st)) return false;
-    if (!a.d_w_down) return true;
-    return launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 8, 4, 4, true, false>, false>(a, st) &&
-           launch_dw<Tile<TIO, BY_COLS, BY_COLS, 2, 4, 8, 4, 4, false, true>, true>(a, st);
-}
 
 template <typename TIO>
-bool launch(const lsm_experts_params& p, const ExpertArgs& a, bool backward, hipStream_t st) {
-    switch (rows_of_tile(p)) {
-        case 256: return backward ? launch_bwd<TIO, 256>(p, a, st) : launch_fwd<TIO, 256>(p, a, st);
-        case 128: return backward ? launch_bwd<TIO, 128>(p, a, st) : launch_fwd<TIO, 128>(p, a, st);
-        case 64: return backward ? launch_bwd<TIO, 64>(p, a, st) : launch_fwd<TIO, 64>(p, a, st);
-        default: return backward ? launch_bwd<TIO, 32>(p, a, st) : launch_fwd<TIO, 32>(p, a, st);
-    }
+bool launch(const lsm_experts_params& p, ExpertArgs a, bool backward, hipStream_t st) {
+    const Plan q = plan_of(p);
+    a.stretch = stretch_of(backward ? q.dx : q.down);
+    a.parts = weight_parts(p, q.hidden);
+#define LSM_KIND(call, kind)                                                                                     \
+    ((kind) == 0 ? call(0) : (kind) == 1 ? call(1) : (kind) == 2 ? call(2) : (kind) == 3 ? call(3) : (kind) == 4 ? call(4) \
+                                                                                     : (kind) == 5 ? call(5) : call(6))
+#define LSM_UP(K) launch_up<TIO, K>(a, st)
+#define LSM_DOWN(K) launch_down<TIO, K>(a, st)
+#define LSM_HIDDEN(K) launch_hidden<TIO, K>(a, st)
+#define LSM_DX(K) launch_dx<TIO, K>(a, st)
+    if (!backward) return LSM_KIND(LSM_UP, q.up) && LSM_KIND(LSM_DOWN, q.down) && launch_sum<TIO, true>(a, st);
+    if (!(LSM_KIND(LSM_HIDDEN, q.hidden) && LSM_KIND(LSM_DX, q.dx) && launch_sum<TIO, false>(a, st))) return false;
+    if (!a.d_w_down) return true;
+    return (q.dw1 == 0 ? launch_dw<TIO, 0, false>(a, st) : q.dw1 == 2 ? launch_dw<TIO, 2, false>(a, st) : launch_dw<TIO, 5, false>(a, st)) &&
+           (q.dw2 == 0 ? launch_dw<TIO, 0, true>(a, st) : q.dw2 == 2 ? launch_dw<TIO, 2, true>(a, st) : launch_dw<TIO, 5, true>(a, st));
+#undef LSM_UP
+#undef LSM_DOWN
+#undef LSM_HIDDEN
+#undef LSM_DX
 }
 
 }  // namespace
@@ -428,7 +463,7 @@ int lsm_moe_experts(const lsm_experts_params* p, const void* x, const float* wei
     ExpertArgs a{};
     a.x = x; a.w_gate_up = w_gate_up; a.w_down = w_down; a.residual = residual; a.weights = weights;
     a.offsets = offsets; a.order = order; a.place = place; a.y = y;
-    a.h = ws + s.h; a.part = reinterpret_cast<float*>(ws + s.part);
+    a.h = ws + s.h; a.part = ws + s.part; a.part_scale = reinterpret_cast<float*>(ws + s.part_scale);
     a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k;
     a.x_bytes = uint32_t(p->x_stride) * el;
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -456,9 +491,9 @@ int lsm_moe_experts_bwd(const lsm_experts_params* p, const void* x, const float*
     a.x = x; a.w_gate_up = w_gate_up; a.w_down = w_down; a.d_y = d_y; a.weights = weights;
     a.offsets = offsets; a.order = order; a.place = place; a.y = dx; a.d_weights = d_weights;
     a.d_w_gate_up = d_w_gate_up; a.d_w_down = d_w_down;
-    a.h = ws + s.h; a.part = reinterpret_cast<float*>(ws + s.part);
+    a.h = ws + s.h; a.part = ws + s.part; a.part_scale = reinterpret_cast<float*>(ws + s.part_scale);
     a.da = ws + s.da; a.weight_part = reinterpret_cast<float*>(ws + s.weight_part);
-    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k; a.parts = weight_parts(*p);
+    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k;
     a.x_bytes = uint32_t(p->x_stride) * el;
     a.dy_bytes = uint32_t(p->dy_stride) * el;
     const hipStream_t st = static_cast<hipStream_t>(stream);

@@ -14,16 +14,18 @@
 // While the matrix instructions of step t run, the operands of step t + 1 are read, each into the registers whose last use has just
 // been: piece t + 1 is complete before step t begins, piece t + NBUF - 1 is requested in it, and nothing is read from piece t.
 #pragma once
-#include "lsm_block_dev.h"
+#include "lsm_train_dev.h"
 
 namespace lsm {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half_t;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kBeyond = 0xfffff000u;  // offset and size of a buffer: at or behind it nothing is read and zeros come
-constexpr int kStepBytes = 64;             // of k, a row and step
+constexpr int kStepBytes = kTileStepBytes;
 
 enum Layout { BY_ROWS, BY_COLS };
 
@@ -117,9 +119,8 @@ struct Operand {
     __device__ __forceinline__ void first_rows(int wave, int lane) {
         _Pragma("unroll") for (int j = 0; j < LOADS; ++j) row[j] = LISTED ? listed(line(wave, lane, j)) : 0;
     }
-    // Request load j of the pieces of step `step` of `K` k's; nothing behind the last.
-    __device__ __forceinline__ void request(uint32_t to, int step, int K, int wave, int lane, int j) {
-        const int k0 = step * KSTEP;
+    // Request load j of the pieces from k0 on, of K k's; nothing behind the last.
+    __device__ __forceinline__ void request(uint32_t to, int k0, int K, int wave, int lane, int j) {
         uint32_t o = off[j];
         uint64_t from = base;
         if (L == BY_ROWS) {
@@ -192,8 +193,8 @@ struct Tile {
     // Load n of a step, of C::LOADS + R::LOADS.
     __device__ __forceinline__ void request(int step, int K, int n) {
         const uint32_t at = lds + uint32_t(step % NBUF) * STAGE;
-        if (n < C::LOADS) c.request(at, step, K, wave, lane, n);
-        else r.request(at + C::BYTES, step, K, wave, lane, n - C::LOADS);
+        if (n < C::LOADS) c.request(at, step * C::KSTEP, K, wave, lane, n);
+        else r.request(at + C::BYTES, step * C::KSTEP, K, wave, lane, n - C::LOADS);
     }
     __device__ __forceinline__ u32x4 read_c(int step, int i) const {
         return C::read(lds + uint32_t(step % NBUF) * STAGE, (wc * TC + i) * 16, lane);
@@ -229,23 +230,30 @@ struct Tile {
         u32x4 a[TC], b[TR], next[TR];
         _Pragma("unroll") for (int j = 0; j < TR; ++j) b[j] = read_r(0, j);
         _Pragma("unroll") for (int i = 0; i < TC; ++i) a[i] = read_c(0, i);
-        for (int t = 0; t < steps; t += 2) {
-            step(acc, a, b, next, t, K, row_of);
-            if (t + 1 < steps) step(acc, a, next, b, t + 1, K, row_of);
+        if constexpr (SQUARE) {
+            for (int t = 0; t < steps; ++t) square_step(acc, a, b, t, K, row_of);
+        } else {
+            for (int t = 0; t < steps; t += 2) {
+                step(acc, a, b, next, t, K, row_of);
+                if (t + 1 < steps) step(acc, a, next, b, t + 1, K, row_of);
+            }
         }
         wait_lds();
         wait_loads<0>();
         barrier();
+    }
+    template <typename RowOf>
+    __device__ __forceinline__ void refill(RowOf row_of, int t, int K) const {
+        if (!LIST) return;  // the next half of the list, a step before its first row is read; the half that it replaces is used up
+        const int k = (t + AHEAD + 2) * C::KSTEP;
+        if (k >= C::kList && k % (C::kList / 2) == 0) fill(row_of, k, C::kList / 2, K);
     }
     // Reads and requests are spread among the matrix instructions: behind one another they keep the wave from its next product until the
     // last of them is accepted.
     template <typename RowOf>
     __device__ __forceinline__ void step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], const u32x4 (&b)[TR], u32x4 (&next)[TR], int t, int K, RowOf row_of) {
         constexpr int ALL = TC * TR;
-        if (LIST) {  // the next half of the list, a step before its first row is read; the half that it replaces is used up
-            const int k = (t + AHEAD + 2) * C::KSTEP;
-            if (k >= C::kList && k % (C::kList / 2) == 0) fill(row_of, k, C::kList / 2, K);
-        }
+        refill(row_of, t, K);
         fence_schedule();
         _Pragma("unroll") for (int i = 0; i < TC; ++i)
             _Pragma("unroll") for (int j = 0; j < TR; ++j) {
@@ -257,6 +265,30 @@ struct Tile {
                 if (j == TR - 1) a[i] = read_c(t + 1, i);
                 fence_schedule();
             }
+        wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
+        barrier();
+    }
+    // The same for as many blocks along either side, without a second set of registers for r: first all products with row or column 0, then
+    // those with 1 and so on, so that operands i of both sides are free, and read anew, when theirs are done.
+    static constexpr bool SQUARE = TC == TR;
+    template <typename RowOf>
+    __device__ __forceinline__ void square_step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], u32x4 (&b)[TR], int t, int K, RowOf row_of) {
+        constexpr int ALL = TC * TR;
+        refill(row_of, t, K);
+        fence_schedule();
+        int m = 0;
+        _Pragma("unroll") for (int d = 0; d < TC; ++d) {
+            _Pragma("unroll") for (int q = 0; q < 2 * (TC - d) - 1; ++q, ++m) {
+                const int i = q & 1 ? d + (q + 1) / 2 : d, j = q & 1 ? d : d + q / 2;
+                acc[i][j] = product(a[i], b[j], acc[i][j], TIO());
+                fence_schedule();
+                _Pragma("unroll") for (int n = m * LOADS / ALL; n < (m + 1) * LOADS / ALL; ++n) request(t + AHEAD, K, n);
+                fence_schedule();
+            }
+            b[d] = read_r(t + 1, d);
+            a[d] = read_c(t + 1, d);
+            fence_schedule();
+        }
         wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
         barrier();
     }
@@ -284,7 +316,7 @@ struct Tile {
         _Pragma("unroll") for (int i = 0; i < NB; ++i)
             *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<NB>(lane & 15, i * 16 + 4 * (lane >> 4)))) = value(i);
     }
-    // ADD: to what is there already (fp32).
+    // ADD: to what is there already (TOUT's own sum).
     template <int NB, typename TOUT, bool ADD = false, typename Line>
     __device__ __forceinline__ void take(int j, int width, Line line) const {
         constexpr int E = 16 / int(sizeof(TOUT)), LANES = NB * 16 / E, ROWS = 64 / LANES;
@@ -298,6 +330,12 @@ struct Tile {
             }
             TOUT* to = line((wr * TR + j) * 16 + row);
             if (!to || c >= width) continue;
+            if constexpr (sizeof(TOUT) == 2 && !__is_same(TOUT, uint16_t)) {
+                f16x8 h;
+                _Pragma("unroll") for (int e = 0; e < E; ++e) h[e] = half_t(v[e]);
+                *reinterpret_cast<f16x8*>(to + c) = h;
+                continue;
+            }
             if (ADD) {
                 float old[E];
                 unpack(*reinterpret_cast<const u32x4*>(to + c), old);
@@ -307,6 +345,17 @@ struct Tile {
         }
     }
 };
+
+// Rows of one call's own use in 16 bits: fp16 times a power of two for each stretch of a row, so that the stretch's largest finite number is
+// about 2^14.  Off by 2^-12 of a number's size, an eighth of what bf16 is, at half of fp32's traffic.
+__device__ __forceinline__ float finite_size(float x) {
+    const float a = fabsf(x);
+    return a < __builtin_inff() ? a : 0.f;
+}
+__device__ __forceinline__ float scale_for(float largest) {  // 2^(14 - exponent of largest)
+    const int e = int(__float_as_uint(largest) >> 23);
+    return __uint_as_float(uint32_t(min(268 - e, 240)) << 23);
+}
 
 // 2^x and 1 / (1 + 2^-x) of x = log2(e) y.  For bf16 elements the hardware's power and reciprocal, each within 2^-23: what they give is
 // rounded to bf16 or summed over many; for fp32 elements the library's functions.
@@ -322,12 +371,22 @@ __device__ __forceinline__ void clear(f32x4 (&acc)[T::TC][T::TR]) {
         _Pragma("unroll") for (int j = 0; j < T::TR; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// Tiles of 256 columns and BR rows.
-template <typename TIO, Layout LC, Layout LR, int BR> struct TileOf;
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 256> { typedef Tile<TIO, LC, LR, 2, 4, 8, 4, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 128> { typedef Tile<TIO, LC, LR, 4, 2, 4, 4, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 64> { typedef Tile<TIO, LC, LR, 4, 1, 4, 4, 4> type; };
-template <typename TIO, Layout LC, Layout LR> struct TileOf<TIO, LC, LR, 32> { typedef Tile<TIO, LC, LR, 4, 1, 4, 2, 4> type; };
+// The tiles there are, by number (kTiles in lsm_train_dev.h has their sizes).  HALF: half the columns, for columns that go with pairs of them.
+template <typename TIO, Layout LC, Layout LR, int KIND, bool HALF = false, bool LIST_C = false, bool LIST_R = false> struct TileOf;
+#define LSM_TILE(KIND, WC, WR, TC, TR)                                                                                      \
+    template <typename TIO, Layout LC, Layout LR, bool HALF, bool LIST_C, bool LIST_R>                                        \
+    struct TileOf<TIO, LC, LR, KIND, HALF, LIST_C, LIST_R> {                                                                  \
+        typedef Tile<TIO, LC, LR, WC, WR, HALF ? (TC) / 2 : (TC), TR, 4, LIST_C, LIST_R> type;                                \
+        static_assert(kTiles[KIND].rows == (WR) * (TR) * 16 && kTiles[KIND].cols == (WC) * (TC) * 16 && kTiles[KIND].waves == (WC), ""); \
+    }
+LSM_TILE(0, 2, 4, 8, 4);
+LSM_TILE(1, 4, 2, 4, 4);
+LSM_TILE(2, 2, 2, 4, 4);
+LSM_TILE(3, 4, 1, 4, 4);
+LSM_TILE(4, 4, 1, 4, 2);
+LSM_TILE(5, 2, 2, 2, 2);
+LSM_TILE(6, 4, 1, 2, 2);
+#undef LSM_TILE
 
 }  // namespace
 }  // namespace lsm

@@ -9,7 +9,6 @@
 //   k_dx_join   the shares' sum
 // Bound: the matrix products, three forward and backward and a fourth for the logits formed again; for few tokens the weights, read once.
 #include "lsm_product_dev.h"
-#include "lsm_train_dev.h"
 
 namespace lsm {
 namespace {
@@ -157,10 +156,13 @@ __global__ __launch_bounds__(T::THREADS) void k_logits(VocabArgs a) {
     const int first = c * T::BC + t.wc * T::TC * 16, mine = first + 4 * (t.lane >> 4);  // of the wave, of the lane
     const float log2_scale = a.scale * kLog2e;
     const bool edge = first + T::TC * 16 > a.V;
+    int tokens[T::TR], wants[T::TR];
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) tokens[j] = r0 + t.row(j) < rows ? int(token_of(a, r0 + t.row(j))) : -1;
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) wants[j] = TEACHER || tokens[j] < 0 ? -1 : a.index[tokens[j]];
     Entries entries;
-    if (TEACHER) entries.load(a, r0 + t.row(0) < rows ? int(token_of(a, r0 + t.row(0))) : -1, 0, t.lane);
+    if (TEACHER) entries.load(a, tokens[0], 0, t.lane);
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        const int at = r0 + t.row(j);
+        const int at = r0 + t.row(j), token = tokens[j];
         float m = -__builtin_inff(), sum = 0.f;
         _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
             _Pragma("unroll") for (int q = 0; q < 4; ++q) {
@@ -173,16 +175,15 @@ __global__ __launch_bounds__(T::THREADS) void k_logits(VocabArgs a) {
             _Pragma("unroll") for (int q = 0; q < 4; ++q) sum += power(__builtin_fmaf(acc[i][j][q], log2_scale, -top), TIO());
         sum = T::row_sum(sum);
         if (t.lane < 16 && at < rows) a.stats[size_t(c * T::WC + t.wc) * a.n + at] = f32x2{m * a.scale, sum};
-        const int token = at < rows ? int(token_of(a, at)) : -1;
         if (!TEACHER) {
-            const int want = token < 0 ? -1 : a.index[token];
+            const int want = wants[j];
             if (__ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) == 0) continue;
             _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
                 _Pragma("unroll") for (int q = 0; q < 4; ++q)
                     if (want == mine + i * 16 + q) a.at_entry[at] = acc[i][j][q] * a.scale;
         } else {
             Entries next;
-            if (j + 1 < T::TR) next.load(a, at + 16 < rows ? int(token_of(a, at + 16)) : -1, 0, t.lane);
+            if (j + 1 < T::TR) next.load(a, tokens[(j + 1) % T::TR], 0, t.lane);
             t.template put<T::TC>([&](int i) { return acc[i][j]; });
             const auto found = [&](int e, int d) {
                 a.at_entry[size_t(e) * a.n + at] =
@@ -264,16 +265,22 @@ __global__ __launch_bounds__(T::THREADS) void k_grad(VocabArgs a) {
     const int column = c * T::BC + t.wc * T::TC * 16, first = a.v0 + column, mine = first + 4 * (t.lane >> 4);
     const float log2_scale = a.scale * kLog2e;
     const bool edge = first + T::TC * 16 > end;
-    Entries entries;
-    if (TEACHER) entries.load(a, r0 + t.row(0) < rows ? int(token_of(a, r0 + t.row(0))) : -1, 0, t.lane);
+    int tokens[T::TR], wants[T::TR];
+    float tops[T::TR], weights[T::TR];
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) tokens[j] = r0 + t.row(j) < rows ? int(token_of(a, r0 + t.row(j))) : -1;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        const int at = r0 + t.row(j), token = at < rows ? int(token_of(a, at)) : -1;
-        const float lse = token < 0 ? 0.f : a.lse_in[token], weight = token < 0 ? 0.f : a.d_loss[token] * a.scale;
-        const int want = TEACHER || token < 0 ? -1 : a.index[token];
+        wants[j] = TEACHER || tokens[j] < 0 ? -1 : a.index[tokens[j]];
+        tops[j] = tokens[j] < 0 ? 0.f : a.lse_in[tokens[j]] * kLog2e;
+        weights[j] = tokens[j] < 0 ? 0.f : a.d_loss[tokens[j]] * a.scale;
+    }
+    Entries entries;
+    if (TEACHER) entries.load(a, tokens[0], 0, t.lane);
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        const int token = tokens[j], want = wants[j];
+        const float top = tops[j], weight = weights[j];
         Entries next;
-        if (TEACHER && j + 1 < T::TR) next.load(a, at + 16 < rows ? int(token_of(a, at + 16)) : -1, 0, t.lane);
+        if (TEACHER && j + 1 < T::TR) next.load(a, tokens[(j + 1) % T::TR], 0, t.lane);
         const bool here = !TEACHER && __ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) != 0;
-        const float top = lse * kLog2e;
         t.template put<T::TC>([&](int i) {
             f32x4 v;
             _Pragma("unroll") for (int e = 0; e < 4; ++e) {
@@ -393,32 +400,41 @@ int check(const lsm_vocab_params* p) {
     if (p->x_stride % 8) return LSM_ERR_ALIGN;
     return LSM_OK;
 }
-int rows_of_tile(const lsm_vocab_params& p) { return p.n > 160 ? 256 : p.n > 64 ? 128 : p.n > 32 ? 64 : 32; }
-int waves_along(int br) { return br == 256 ? 2 : 4; }
-int up(int64_t x, int64_t to) { return int((x + to - 1) / to); }
-
-struct Split { int piece, shares; };
-Split split(const lsm_vocab_params& p) {
-    const int64_t el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4;
-    int64_t most = kPieceBytes / (p.n * el) / 256 * 256;
+// Tiles of the logits, of their gradient, of dw and dx; the vocabulary of a piece and its shares for dx.
+struct Plan { int logits, grad, dw, dx, piece, shares; };
+Plan plan_of(const lsm_vocab_params& p) {
+    const bool f32 = p.dtype == LSM_DTYPE_F32;
+    Plan q{};
+    q.logits = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.V, t.cols); }, 0x7f);
+    int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256 * 256;
     if (most < 256) most = 256;
     const int pieces = up(p.V, most);
-    Split s{up(up(p.V, pieces), 256) * 256, 1};
-    // shares of a piece's vocabulary: the fewest with which the last round of workgroups is nine tenths full, or the best of eight
-    const int br = rows_of_tile(p), room = br >= 128 ? 256 : 512;
-    const int64_t tiles = int64_t(up(p.n, br)) * up(p.D, 256);
-    double best = 0;
-    for (int k = 1; k <= 64 && k * 512 <= s.piece + 511; ++k) {
-        const double full = double(tiles * k) / (double(up(tiles * k, room)) * room);
-        if (full > best + 0.02) { best = full; s.shares = k; }
-        if (best >= 0.9 || (k >= 8 && tiles * k >= room)) break;
-    }
-    return s;
+    q.piece = up(up(p.V, pieces), 256) * 256;
+    q.grad = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(q.piece, t.cols); }, 0x7f);
+    q.dw = pick_tile(f32, p.n, [&](const TileSize& t) { return int64_t(up(q.piece, t.rows)) * up(p.D, t.cols); }, 1 << 0 | 1 << 2 | 1 << 5);
+    // dx: shares of a piece's vocabulary, the fewest with which the last round of workgroups is nine tenths full, or the best of some
+    const auto shares = [&](const TileSize& t) {
+        const int64_t tiles = int64_t(up(p.n, t.rows)) * up(p.D, t.cols), room = 256 * t.at_once;
+        double best = 0;
+        int least = 1;
+        for (int k = 1; k <= 64 && k * 512 <= q.piece + 511; ++k) {
+            const double full = double(tiles * k) / (double(up(tiles * k, room)) * room);
+            if (full > best + 0.02) { best = full; least = k; }
+            if (best >= 0.9 || (k >= 8 && tiles * k >= room)) break;
+        }
+        return least;
+    };
+    q.dx = pick_tile_of(f32, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.D, t.cols) * shares(t); },
+                     [&](const TileSize& t) { return up(q.piece, shares(t)); }, 0x7f);
+    q.shares = shares(kTiles[q.dx]);
+    return q;
 }
+int parts_of(const lsm_vocab_params& p, int kind) { return up(p.V, kTiles[kind].cols) * kTiles[kind].waves; }
 
 struct Space { size_t offsets, order, place, hist, count, entry, share, entropy, stats, at_entry, grad, part, bytes; };
 Space space(const lsm_vocab_params& p, bool backward) {
     const size_t n = p.n, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4, K = p.K;
+    const Plan q = plan_of(p);
     Space s{};
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
@@ -431,10 +447,9 @@ Space space(const lsm_vocab_params& p, bool backward) {
     s.share = take(K * n * 4);
     s.entropy = take(K ? n * 4 : 0);
     if (!backward) {
-        s.stats = take(size_t(up(p.V, 256)) * waves_along(rows_of_tile(p)) * n * sizeof(f32x2));
+        s.stats = take(size_t(parts_of(p, q.logits)) * n * sizeof(f32x2));
         s.at_entry = take((K ? K : 1) * n * 4);
     } else {
-        const Split q = split(p);
         s.grad = take(n * q.piece * el);
         s.part = take(size_t(q.shares) * n * p.D * 4);
     }
@@ -459,7 +474,6 @@ VocabArgs arguments(const lsm_vocab_params& p, const Space& s, char* ws, const v
     a.n = p.n; a.D = p.D; a.V = p.V; a.K = p.K;
     a.x_bytes = uint32_t(p.x_stride) * (p.dtype == LSM_DTYPE_BF16 ? 2 : 4);
     a.scale = 1.f / p.temperature;
-    a.parts = up(p.V, 256) * waves_along(rows_of_tile(p));
     return a;
 }
 // The tokens that count.
@@ -475,57 +489,71 @@ bool enqueue_rows(const VocabArgs& a, const Space& s, char* ws, hipStream_t st) 
 }
 unsigned grid_of(int64_t tiles) { return unsigned((tiles + 7) / 8 * 8); }
 
-template <typename TIO, int BR>
-bool launch_fwd(const VocabArgs& a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type T;
-    {
-        ProfScope ps(KID_VOCAB_LOGITS, st);
-        const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(a.V, T::BC));
-        if (a.K) hipLaunchKernelGGL((k_logits<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
-        else hipLaunchKernelGGL((k_logits<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
-    }
-    if (!launched()) return false;
-    ProfScope ps(KID_VOCAB_JOIN, st);
-    if (a.n > 1024) hipLaunchKernelGGL(k_join<64>, dim3(up(a.n, 64)), dim3(1024), 0, st, a);
-    else hipLaunchKernelGGL(k_join<4>, dim3(up(a.n, 4)), dim3(1024), 0, st, a);
+template <typename TIO, int KIND>
+bool launch_logits(const VocabArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    ProfScope ps(KID_VOCAB_LOGITS, st);
+    const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(a.V, T::BC));
+    if (a.K) hipLaunchKernelGGL((k_logits<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((k_logits<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
+    return launched();
+}
+template <typename TIO, int KIND>
+bool launch_grad(const VocabArgs& a, int width, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    ProfScope ps(KID_VOCAB_GRAD, st);
+    const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(width, T::BC));
+    if (a.K) hipLaunchKernelGGL((k_grad<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((k_grad<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
+    return launched();
+}
+template <typename TIO, int KIND>
+bool launch_dw(const VocabArgs& a, int width, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_COLS, BY_COLS, KIND, false, true>::type T;
+    ProfScope ps(KID_VOCAB_DW, st);
+    hipLaunchKernelGGL((k_dw<T>), dim3(grid_of(int64_t(up(width, T::BR)) * up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    return launched();
+}
+template <typename TIO, int KIND>
+bool launch_dx(const VocabArgs& a, hipStream_t st) {
+    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND>::type T;
+    ProfScope ps(KID_VOCAB_DX, st);
+    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of(int64_t(up(a.n, T::BR)) * up(a.D, T::BC) * a.shares)), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 
-template <typename TIO, int BR>
-bool launch_bwd(VocabArgs a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, BR>::type T;
-    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, BR>::type X;
-    typedef Tile<TIO, BY_COLS, BY_COLS, 2, 4, 8, 4, 4, true, false> W;
+template <typename TIO>
+bool launch(VocabArgs a, const lsm_vocab_params& p, bool backward, hipStream_t st) {
+    const Plan q = plan_of(p);
+#define LSM_KIND(call, kind)                                                                                     \
+    ((kind) == 0 ? call(0) : (kind) == 1 ? call(1) : (kind) == 2 ? call(2) : (kind) == 3 ? call(3) : (kind) == 4 ? call(4) \
+                                                                                     : (kind) == 5 ? call(5) : call(6))
+#define LSM_LOGITS(K) launch_logits<TIO, K>(a, st)
+#define LSM_GRAD(K) launch_grad<TIO, K>(a, width, st)
+#define LSM_DX(K) launch_dx<TIO, K>(a, st)
+    if (!backward) {
+        a.parts = parts_of(p, q.logits);
+        if (!LSM_KIND(LSM_LOGITS, q.logits)) return false;
+        ProfScope ps(KID_VOCAB_JOIN, st);
+        if (a.n > 1024) hipLaunchKernelGGL(k_join<64>, dim3(up(a.n, 64)), dim3(1024), 0, st, a);
+        else hipLaunchKernelGGL(k_join<4>, dim3(up(a.n, 4)), dim3(1024), 0, st, a);
+        return launched();
+    }
+    a.piece = q.piece;
+    a.shares = q.shares;
     for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
         const int width = a.V - a.v0 < a.piece ? a.V - a.v0 : a.piece;
-        {
-            ProfScope ps(KID_VOCAB_GRAD, st);
-            const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(width, T::BC));
-            if (a.K) hipLaunchKernelGGL((k_grad<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
-            else hipLaunchKernelGGL((k_grad<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
-        }
-        if (!launched()) return false;
-        if (a.dw) {
-            ProfScope ps(KID_VOCAB_DW, st);
-            hipLaunchKernelGGL((k_dw<W>), dim3(grid_of(int64_t(up(width, W::BR)) * up(a.D, W::BC))), dim3(W::THREADS), 0, st, a);
-            if (!launched()) return false;
-        }
-        ProfScope ps(KID_VOCAB_DX, st);
-        hipLaunchKernelGGL((k_dx<X>), dim3(grid_of(int64_t(up(a.n, X::BR)) * up(a.D, X::BC) * a.shares)), dim3(X::THREADS), 0, st, a);
-        if (!launched()) return false;
+        if (!LSM_KIND(LSM_GRAD, q.grad)) return false;
+        if (a.dw && !(q.dw == 0 ? launch_dw<TIO, 0>(a, width, st) : q.dw == 2 ? launch_dw<TIO, 2>(a, width, st) : launch_dw<TIO, 5>(a, width, st)))
+            return false;
+        if (!LSM_KIND(LSM_DX, q.dx)) return false;
     }
     ProfScope ps(KID_VOCAB_JOIN, st);
     hipLaunchKernelGGL((k_dx_join<TIO>), dim3(up(int64_t(a.n) * (a.D / kPiece<TIO>), 256)), dim3(256), 0, st, a);
     return launched();
-}
-template <typename TIO>
-bool launch(const VocabArgs& a, int br, bool backward, hipStream_t st) {
-    switch (br) {
-        case 256: return backward ? launch_bwd<TIO, 256>(a, st) : launch_fwd<TIO, 256>(a, st);
-        case 128: return backward ? launch_bwd<TIO, 128>(a, st) : launch_fwd<TIO, 128>(a, st);
-        case 64: return backward ? launch_bwd<TIO, 64>(a, st) : launch_fwd<TIO, 64>(a, st);
-        default: return backward ? launch_bwd<TIO, 32>(a, st) : launch_fwd<TIO, 32>(a, st);
-    }
+#undef LSM_LOGITS
+#undef LSM_GRAD
+#undef LSM_DX
 }
 
 }  // namespace
@@ -558,8 +586,7 @@ int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, cons
     a.lse = lse;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (!enqueue_rows(a, s, ws, st)) return LSM_ERR_LAUNCH;
-    const int br = rows_of_tile(*p);
-    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, br, false, st) : launch<float>(a, br, false, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, *p, false, st) : launch<float>(a, *p, false, st)) ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 int lsm_vocab_loss_bwd(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,
@@ -576,17 +603,13 @@ int lsm_vocab_loss_bwd(const lsm_vocab_params* p, const void* x, const void* w, 
     if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
     VocabArgs a = arguments(*p, s, ws, x, w, index, teacher);
-    const Split q = split(*p);
-    a.piece = q.piece;
-    a.shares = q.shares;
     a.lse_in = lse;
     a.d_loss = d_loss;
     a.dx = dx;
     a.dw = dw;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (!enqueue_rows(a, s, ws, st)) return LSM_ERR_LAUNCH;
-    const int br = rows_of_tile(*p);
-    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, br, true, st) : launch<float>(a, br, true, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, *p, true, st) : launch<float>(a, *p, true, st)) ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 }  // extern "C"
