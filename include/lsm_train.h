@@ -38,7 +38,7 @@ int lsm_moe_route(const lsm_route_params* p, const void* logits, float* weights,
 
 /*
  * Backward of L = <weights, d_weights>, from the logits and the experts chosen by the forward call.
- *   chosen     [n, top_k] int32, no expert twice for a token; outside [0, E): no expert                in
+ *   chosen     [n, top_k] int32; outside [0, E): no expert; one that stands twice counts once in S, its gradients add   in
  *   d_weights  [n, top_k] fp32; not used where there is no expert                                    in
  *   d_logits   [n, E] dtype                                                                          out
  */

@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void k_route_bwd(const TIO* logits, const int*
         const int e = chosen[size_t(t) * top_k + j];
         const float dw = d_weights[size_t(t) * top_k + j];
         _Pragma("unroll") for (int r = 0; r < kHeld; ++r)
-            if (e == G * r + g && e < E) { d[r] = dw; in[r] = true; }
+            if (e == G * r + g && e < E) { d[r] += dw; in[r] = true; }
     }
     uint32_t most = 0;
     _Pragma("unroll") for (int r = 0; r < kHeld; ++r)

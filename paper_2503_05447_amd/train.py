@@ -10,8 +10,9 @@ from operator import index
 
 import torch
 
-from .binding import LsmError, _alloc_on, _check, _ptr, _stream_handle, library
-from .block import _dtype, _workspace
+from .binding import LsmError, _alloc_on, _ptr, _stream_handle, library
+from .binding import _check as _check_dense
+from .block import _dtype, _workspace as _any_workspace
 
 
 class _RouteParams(ctypes.Structure):
@@ -47,11 +48,30 @@ def _vocab_params(*sizes):
     return p, library().lsm_vocab_loss_workspace_bytes(p), library().lsm_vocab_loss_bwd_workspace_bytes(p)
 
 
+def _here(t, name):
+    """The launches go to the current device: a tensor of another one is refused."""
+    if t.is_cuda and t.device.index is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+
+
+def _check(t, shape, dtype, name):
+    _check_dense(t, shape, dtype, name)
+    if t is not None:
+        _here(t, name)
+
+
+def _workspace(workspace, need, like):
+    if workspace is not None:
+        _here(workspace, "workspace")
+    return _any_workspace(workspace, need, like)
+
+
 def _rows(t, name):
     """Elements between the rows of a [n, D] device tensor that is dense along D."""
     if t.dim() != 2 or not t.is_cuda or t.stride(1) != 1 and t.shape[1] != 1:
         raise ValueError("%s: need a [n,D] device tensor, dense along D, got %s with strides %s on %s"
                          % (name, tuple(t.shape), t.stride(), t.device))
+    _here(t, name)
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
