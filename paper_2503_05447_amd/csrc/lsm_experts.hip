@@ -290,17 +290,29 @@ __global__ __launch_bounds__(256) void k_sum(ExpertArgs a) {
     float s[E];
     if (WEIGHTED && a.residual) unpack(*reinterpret_cast<const u32x4*>(static_cast<const TIO*>(a.residual) + size_t(t) * a.D + d), s);
     else _Pragma("unroll") for (int e = 0; e < E; ++e) s[e] = 0.f;
-    for (int j = 0; j < a.top_k; ++j) {
-        const int at = a.place[size_t(t) * a.top_k + j];
-        if (uint32_t(at) >= uint32_t(a.n * a.top_k)) continue;
-        const float p = WEIGHTED ? a.weights[size_t(t) * a.top_k + j] : 1.f;
-        if constexpr (E == 8) {
-            const float q = p * a.part_scale[size_t(d / a.stretch) * (size_t(a.n) * a.top_k) + at];
-            const f16x8 v = *reinterpret_cast<const f16x8*>(static_cast<const half_t*>(a.part) + size_t(at) * a.D + d);
-            _Pragma("unroll") for (int e = 0; e < 8; ++e) s[e] += q * float(v[e]);
-        } else {
-            const f32x4 v = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part) + size_t(at) * a.D + d);
-            _Pragma("unroll") for (int e = 0; e < 4; ++e) s[e] += p * v[e];
+    constexpr int U = 4;  // pairs requested at a time
+    for (int j0 = 0; j0 < a.top_k; j0 += U) {
+        int at[U];
+        float p[U];
+        u32x4 z[U];
+        _Pragma("unroll") for (int u = 0; u < U; ++u) {
+            at[u] = j0 + u < a.top_k ? a.place[size_t(t) * a.top_k + j0 + u] : -1;
+            if (uint32_t(at[u]) >= uint32_t(a.n * a.top_k)) at[u] = -1;
+            p[u] = !WEIGHTED ? 1.f : at[u] < 0 ? 0.f : a.weights[size_t(t) * a.top_k + j0 + u];
+        }
+        _Pragma("unroll") for (int u = 0; u < U; ++u) {
+            if (at[u] < 0) continue;
+            if (E == 8) p[u] *= a.part_scale[size_t(d / a.stretch) * (size_t(a.n) * a.top_k) + at[u]];
+            z[u] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.part) + (size_t(at[u]) * a.D + d) * sizeof(TIO));
+        }
+        _Pragma("unroll") for (int u = 0; u < U; ++u) {
+            if (at[u] < 0) continue;
+            if constexpr (E == 8) {
+                const f16x8 v = __builtin_bit_cast(f16x8, z[u]);
+                _Pragma("unroll") for (int e = 0; e < 8; ++e) s[e] += p[u] * float(v[e]);
+            } else {
+                _Pragma("unroll") for (int e = 0; e < 4; ++e) s[e] += p[u] * __uint_as_float(z[u][e]);
+            }
         }
     }
     *reinterpret_cast<u32x4*>(static_cast<TIO*>(a.y) + size_t(t) * a.D + d) = pack(s);
@@ -332,11 +344,11 @@ int64_t tiles_of_rows(const lsm_experts_params& p, int rows) {  // about: every 
 Plan plan_of(const lsm_experts_params& p) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
     const auto rows = [&](int cols, int K, int parts) {
-        return pick_tile(f32, K, [&](const TileSize& t) { return tiles_of_rows(p, t.rows) * up(cols, t.cols / parts); }, 0x7f);
+        return pick_tile(f32, K, [&](const TileSize& t) { return tiles_of_rows(p, t.rows) * up(cols, t.cols / parts); }, f32 ? 0x7e : 0x7f);
     };
     const int64_t mean = (int64_t(p.n) * p.top_k + p.E - 1) / p.E;
     const auto square = [&](int r, int c) {
-        return pick_tile(f32, mean, [&](const TileSize& t) { return int64_t(p.E) * up(r, t.rows) * up(c, t.cols); }, 1 << 0 | 1 << 2 | 1 << 5);
+        return pick_tile(f32, mean, [&](const TileSize& t) { return int64_t(p.E) * up(r, t.rows) * up(c, t.cols); }, (f32 ? 0 : 1 << 0) | 1 << 2 | 1 << 5);
     };
     return Plan{rows(p.F, p.D, 2), rows(p.D, p.F, 1), rows(p.F, p.D + p.D / 2, 2), rows(p.D, 2 * p.F, 1), square(2 * p.F, p.D), square(p.D, p.F)};
 }

@@ -166,6 +166,7 @@ struct Operand {
 template <typename TIO_, Layout LC, Layout LR, int WC_, int WR_, int TC_, int TR_, int NBUF_, bool LIST_C = false, bool LIST_R = false>
 struct Tile {
     typedef TIO_ TIO;
+    static constexpr bool SQUARE = TC_ == TR_;
     static constexpr int WC = WC_, WR = WR_, TC = TC_, TR = TR_, NBUF = NBUF_, WAVES = WC * WR, THREADS = 64 * WAVES;
     static constexpr int BC = WC * TC * 16, BR = WR * TR * 16;
     typedef Operand<TIO, LC, BC, WAVES, LIST_C> C;
@@ -230,17 +231,36 @@ struct Tile {
         u32x4 a[TC], b[TR], next[TR];
         _Pragma("unroll") for (int j = 0; j < TR; ++j) b[j] = read_r(0, j);
         _Pragma("unroll") for (int i = 0; i < TC; ++i) a[i] = read_c(0, i);
-        if constexpr (SQUARE) {
-            for (int t = 0; t < steps; ++t) square_step(acc, a, b, t, K, row_of);
-        } else {
-            for (int t = 0; t < steps; t += 2) {
-                step(acc, a, b, next, t, K, row_of);
-                if (t + 1 < steps) step(acc, a, next, b, t + 1, K, row_of);
+        if constexpr (FOLD > 0) {
+            f32x4 part[TC][TR];
+            for (int t0 = 0; t0 < steps; t0 += FOLD) {
+                _Pragma("unroll") for (int i = 0; i < TC; ++i)
+                    _Pragma("unroll") for (int j = 0; j < TR; ++j) part[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                walk_steps(part, a, b, next, t0, min(t0 + FOLD, steps), K, row_of);
+                _Pragma("unroll") for (int i = 0; i < TC; ++i)
+                    _Pragma("unroll") for (int j = 0; j < TR; ++j) acc[i][j] += part[i][j];
             }
+        } else {
+            walk_steps(acc, a, b, next, 0, steps, K, row_of);
         }
         wait_lds();
         wait_loads<0>();
         barrier();
+    }
+    // fp32 elements: sums of 128 k's are added up apart, so that a sum over some thousand is as exact as one over a few hundred (an even
+    // number of steps).
+    static constexpr int FOLD = sizeof(TIO) == 4 ? 8 : 0;
+    template <typename RowOf>
+    __device__ __forceinline__ void walk_steps(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], u32x4 (&b)[TR], u32x4 (&next)[TR], int t0, int t1, int K,
+                                               RowOf row_of) {
+        if constexpr (SQUARE) {
+            for (int t = t0; t < t1; ++t) square_step(acc, a, b, t, K, row_of);
+        } else {
+            for (int t = t0; t < t1; t += 2) {
+                step(acc, a, b, next, t, K, row_of);
+                if (t + 1 < t1) step(acc, a, next, b, t + 1, K, row_of);
+            }
+        }
     }
     template <typename RowOf>
     __device__ __forceinline__ void refill(RowOf row_of, int t, int K) const {
@@ -270,7 +290,6 @@ struct Tile {
     }
     // The same for as many blocks along either side, without a second set of registers for r: first all products with row or column 0, then
     // those with 1 and so on, so that operands i of both sides are free, and read anew, when theirs are done.
-    static constexpr bool SQUARE = TC == TR;
     template <typename RowOf>
     __device__ __forceinline__ void square_step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], u32x4 (&b)[TR], int t, int K, RowOf row_of) {
         constexpr int ALL = TC * TR;
@@ -311,15 +330,25 @@ struct Tile {
     template <int NB> __device__ __forceinline__ uint32_t cell(int row16, int column) const {
         return lds + uint32_t(wave) * OUT + uint32_t(row16) * (NB * 64 + 16) + uint32_t(column) * 4;
     }
+    // Between what lanes of a wave write there and what others read: no lane's part may be moved across, nor taken apart from the others' as
+    // where branches follow one another on the same condition.
+    static __device__ __forceinline__ void wave_meets() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
     template <int NB, typename Value>
     __device__ __forceinline__ void put(Value value) const {
+        wave_meets();
         _Pragma("unroll") for (int i = 0; i < NB; ++i)
             *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<NB>(lane & 15, i * 16 + 4 * (lane >> 4)))) = value(i);
+        wave_meets();
     }
     // ADD: to what is there already (TOUT's own sum).
     template <int NB, typename TOUT, bool ADD = false, typename Line>
     __device__ __forceinline__ void take(int j, int width, Line line) const {
         constexpr int E = 16 / int(sizeof(TOUT)), LANES = NB * 16 / E, ROWS = 64 / LANES;
+        wave_meets();
         _Pragma("unroll") for (int it = 0; it < (16 + ROWS - 1) / ROWS; ++it) {
             const int row = it * ROWS + lane / LANES, c = (lane % LANES) * E;
             if (ROWS > 16 && row >= 16) continue;
@@ -373,6 +402,7 @@ __device__ __forceinline__ void clear(f32x4 (&acc)[T::TC][T::TR]) {
 
 // The tiles there are, by number (kTiles in lsm_train_dev.h has their sizes).  HALF: half the columns, for columns that go with pairs of them.
 template <typename TIO, Layout LC, Layout LR, int KIND, bool HALF = false, bool LIST_C = false, bool LIST_R = false> struct TileOf;
+// (fp32 has no tile of 256 x 256: its sums are kept in two sets of registers.)
 #define LSM_TILE(KIND, WC, WR, TC, TR)                                                                                      \
     template <typename TIO, Layout LC, Layout LR, bool HALF, bool LIST_C, bool LIST_R>                                        \
     struct TileOf<TIO, LC, LR, KIND, HALF, LIST_C, LIST_R> {                                                                  \
@@ -387,6 +417,8 @@ LSM_TILE(4, 4, 1, 4, 2);
 LSM_TILE(5, 2, 2, 2, 2);
 LSM_TILE(6, 4, 1, 2, 2);
 #undef LSM_TILE
+template <Layout LC, Layout LR, bool HALF, bool LIST_C, bool LIST_R>
+struct TileOf<float, LC, LR, 0, HALF, LIST_C, LIST_R> : TileOf<float, LC, LR, 2, HALF, LIST_C, LIST_R> {};
 
 }  // namespace
 }  // namespace lsm

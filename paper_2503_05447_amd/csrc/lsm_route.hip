@@ -174,10 +174,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_place(PlanArgs a) {
         const int rows = kPlanThreads / G > 0 ? kPlanThreads / G : 1, g = int(threadIdx.x) % G, r0 = int(threadIdx.x) / G;
         int b = 0, s = 0;
         if (r0 < rows)
-            for (int r = r0; r < int(gridDim.x); r += rows) {
-                const int c = a.hist[size_t(r) * G + g];
-                s += c;
-                if (r < int(blockIdx.x)) b += c;
+            for (int r = r0; r < int(gridDim.x); r += 8 * rows) {  // eight of them requested at a time
+                int c[8];
+                _Pragma("unroll") for (int u = 0; u < 8; ++u) c[u] = r + u * rows < int(gridDim.x) ? a.hist[size_t(r + u * rows) * G + g] : 0;
+                _Pragma("unroll") for (int u = 0; u < 8; ++u) {
+                    s += c[u];
+                    if (r + u * rows < int(blockIdx.x)) b += c[u];
+                }
             }
         if (r0 < rows) {
             atomicAdd(&before[g], b);
@@ -250,7 +253,7 @@ int check(const lsm_route_params* p, bool logits) {
 
 int plan_share(int64_t count) {  // items of a block
     if (count <= kPlanAlone) return kPlanAlone;
-    const int64_t each = (count + kPlanBlocks - 1) / kPlanBlocks, unit = 2048;
+    const int64_t each = (count + kPlanBlocks - 1) / kPlanBlocks, unit = 64 * kPlanWaves;
     return int((each + unit - 1) / unit * unit);
 }
 

@@ -37,7 +37,8 @@ int pick_tile_of(bool f32, Tiles tiles, Length length, unsigned kinds) {
         const double share = n > 512 ? n / 256 + 0.3 : double(up(int64_t(n), 256));
         const double busy = share * (f32 ? 3.5 * t.rows * t.cols / 65536. : step_bf16[k]);
         const double brought = n * kTileStepBytes * (t.cols + t.rows / 4) / 12e6;
-        double step = rounds * 0.35;
+        // a lone step, and what its workgroups' requests take where there are few of them
+        double step = rounds * 0.3 + share * kTileStepBytes * (t.cols + t.rows / 4) / 160e3;
         if (step < busy) step = busy;
         if (step < brought) step = brought;
         const double time = steps * step + rounds * 7.;

@@ -34,13 +34,14 @@ struct VocabArgs {
 __device__ __forceinline__ int rows_of(const VocabArgs& a) { return uniform(min(max(a.offsets[1], 0), a.n)); }
 __device__ __forceinline__ uint32_t token_of(const VocabArgs& a, int at) { return min(uint32_t(a.order[at]), uint32_t(a.n - 1)); }
 
+template <int R>  // entries a lane
 __global__ __launch_bounds__(1024) void k_teacher(VocabArgs a) {
-    __shared__ int entry[kMostEntries][17];
-    __shared__ float share[kMostEntries][17];
+    __shared__ int entry[64 * R][17];
+    __shared__ float share[64 * R][17];
     const int t0 = int(blockIdx.x) * 16, slot = threadIdx.x >> 6, t = min(t0 + slot, a.n - 1), lane = threadIdx.x & 63;
-    float z[4], m = -__builtin_inff();
-    int v[4];
-    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+    float z[R], m = -__builtin_inff();
+    int v[R];
+    _Pragma("unroll") for (int i = 0; i < R; ++i) {
         const int j = 64 * i + lane;
         v[i] = -1;
         z[i] = -__builtin_inff();
@@ -55,32 +56,35 @@ __global__ __launch_bounds__(1024) void k_teacher(VocabArgs a) {
     }
     for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
     const bool counts = m > -__builtin_inff();
-    float sum = 0.f, d[4];
-    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+    float sum = 0.f, d[R];
+    _Pragma("unroll") for (int i = 0; i < R; ++i) {
         d[i] = v[i] >= 0 ? (z[i] - m) * a.scale : -__builtin_inff();
         sum += v[i] >= 0 ? expf(d[i]) : 0.f;
     }
     sum = group_sum<64>(sum);
     const float log_sum = logf(sum);
-    float entropy = 0.f, p[4];
-    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+    float entropy = 0.f, p[R];
+    _Pragma("unroll") for (int i = 0; i < R; ++i) {
         p[i] = v[i] >= 0 ? expf(d[i]) / sum : 0.f;
         if (p[i] > 0.f) entropy += p[i] * (d[i] - log_sum);
         else v[i] = -1;
     }
     // entries of the same token become one, the first of them, so that what follows may take entries in any order
     for (int e = 0; e < a.K; ++e) {
-        const int w = __builtin_amdgcn_readlane(e < 64 ? v[0] : e < 128 ? v[1] : e < 192 ? v[2] : v[3], e & 63);
+        int w = v[0];
+        _Pragma("unroll") for (int i = 1; i < R; ++i)
+            if (e >= 64 * i) w = v[i];
+        w = __builtin_amdgcn_readlane(w, e & 63);
         float more = 0.f;
         bool again = false;
-        _Pragma("unroll") for (int i = 0; i < 4; ++i)
+        _Pragma("unroll") for (int i = 0; i < R; ++i)
             if (w >= 0 && v[i] == w && 64 * i + lane > e) { more += p[i]; v[i] = -1; p[i] = 0.f; again = true; }
         if (__ballot(again) == 0) continue;
         more = group_sum<64>(more);
-        _Pragma("unroll") for (int i = 0; i < 4; ++i)
+        _Pragma("unroll") for (int i = 0; i < R; ++i)
             if (64 * i + lane == e) p[i] += more;
     }
-    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+    _Pragma("unroll") for (int i = 0; i < R; ++i) {
         const int j = 64 * i + lane;
         if (j >= a.K) break;
         entry[j][slot] = v[i];
@@ -405,13 +409,13 @@ struct Plan { int logits, grad, dw, dx, piece, shares; };
 Plan plan_of(const lsm_vocab_params& p) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
     Plan q{};
-    q.logits = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.V, t.cols); }, 0x7f);
+    q.logits = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.V, t.cols); }, f32 ? 0x7e : 0x7f);
     int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256 * 256;
     if (most < 256) most = 256;
     const int pieces = up(p.V, most);
     q.piece = up(up(p.V, pieces), 256) * 256;
-    q.grad = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(q.piece, t.cols); }, 0x7f);
-    q.dw = pick_tile(f32, p.n, [&](const TileSize& t) { return int64_t(up(q.piece, t.rows)) * up(p.D, t.cols); }, 1 << 0 | 1 << 2 | 1 << 5);
+    q.grad = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(q.piece, t.cols); }, f32 ? 0x7e : 0x7f);
+    q.dw = pick_tile(f32, p.n, [&](const TileSize& t) { return int64_t(up(q.piece, t.rows)) * up(p.D, t.cols); }, (f32 ? 0 : 1 << 0) | 1 << 2 | 1 << 5);
     // dx: shares of a piece's vocabulary, the fewest with which the last round of workgroups is nine tenths full, or the best of some
     const auto shares = [&](const TileSize& t) {
         const int64_t tiles = int64_t(up(p.n, t.rows)) * up(p.D, t.cols), room = 256 * t.at_once;
@@ -425,7 +429,7 @@ Plan plan_of(const lsm_vocab_params& p) {
         return least;
     };
     q.dx = pick_tile_of(f32, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.D, t.cols) * shares(t); },
-                     [&](const TileSize& t) { return up(q.piece, shares(t)); }, 0x7f);
+                     [&](const TileSize& t) { return up(q.piece, shares(t)); }, f32 ? 0x7e : 0x7f);
     q.shares = shares(kTiles[q.dx]);
     return q;
 }
@@ -480,7 +484,8 @@ VocabArgs arguments(const lsm_vocab_params& p, const Space& s, char* ws, const v
 bool enqueue_rows(const VocabArgs& a, const Space& s, char* ws, hipStream_t st) {
     if (a.K > 0) {
         ProfScope ps(KID_VOCAB_ROWS, st);
-        hipLaunchKernelGGL(k_teacher, dim3(up(a.n, 16)), dim3(1024), 0, st, a);
+        if (a.K <= 64) hipLaunchKernelGGL(k_teacher<1>, dim3(up(a.n, 16)), dim3(1024), 0, st, a);
+        else hipLaunchKernelGGL(k_teacher<4>, dim3(up(a.n, 16)), dim3(1024), 0, st, a);
         if (!launched()) return false;
     }
     return enqueue_plan(a.K ? a.count : a.index, a.n, 1, a.K ? 1 : a.V, reinterpret_cast<int32_t*>(ws + s.offsets),
