@@ -34,41 +34,47 @@ __device__ __forceinline__ uint32_t token_of(const ExpertArgs& a, int at) { retu
 
 struct Where { int e, first, count, r, c; };  // expert, its first place and its pairs, the tile's number along rows and columns
 
-// The tile of this workgroup, of all experts' tiles of BR rows x `cols` columns in the order expert, column, row.  Workgroups are dealt out
-// to the eight dies in turn; a die gets neighbouring tiles, which share operands in its L2.  False: there is none left.
+// The tiles of a workgroup, of all experts' tiles of BR rows x `cols` columns in the order expert, column, row.  Workgroups are dealt out
+// to the eight dies in turn; a die gets neighbouring tiles, which share operands in its L2.
 template <int BR>
-__device__ __forceinline__ bool find_tile(const ExpertArgs& a, int cols, Where& w) {
-    const int lane = threadIdx.x & 63;
-    int o[5], tiles[4], own = 0;
-    _Pragma("unroll") for (int i = 0; i < 5; ++i) o[i] = offset_of(a, min(4 * lane + i, a.E));
-    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
-        tiles[i] = max(o[i + 1] - o[i] + BR - 1, 0) / BR;
-        own += tiles[i];
-    }
-    int upto = own;
-    for (int off = 1; off < 64; off <<= 1) {
-        const int t = __shfl_up(upto, off, 64);
-        if (lane >= off) upto += t;
-    }
-    const int all = __builtin_amdgcn_readlane(upto, 63) * cols, die = (all + 7) / 8;
-    const int slot = int(blockIdx.x) / 8, id = (int(blockIdx.x) % 8) * die + slot;
-    if (slot >= die || id >= all) return false;
-    const int at = lanes(__ballot(upto * cols <= id));
-    int rest = id - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at)) * cols;
-    _Pragma("unroll") for (int i = 0; i < 4; ++i) {
-        const int t = __builtin_amdgcn_readlane(tiles[i], at);
-        if (rest < t * cols) {
-            w.e = 4 * at + i;
-            w.first = __builtin_amdgcn_readlane(o[i], at);
-            w.count = __builtin_amdgcn_readlane(o[i + 1], at) - w.first;
-            w.c = rest / t;
-            w.r = rest - w.c * t;
-            return true;
+struct Finder {
+    int o[5], tiles[4], upto, own;  // of four experts a lane: where they begin, their row tiles; row tiles up to and of this lane
+    __device__ __forceinline__ Finder(const ExpertArgs& a) {
+        const int lane = threadIdx.x & 63;
+        own = 0;
+        _Pragma("unroll") for (int i = 0; i < 5; ++i) o[i] = offset_of(a, min(4 * lane + i, a.E));
+        _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+            tiles[i] = max(o[i + 1] - o[i] + BR - 1, 0) / BR;
+            own += tiles[i];
         }
-        rest -= t * cols;
+        upto = own;
+        for (int off = 1; off < 64; off <<= 1) {
+            const int t = __shfl_up(upto, off, 64);
+            if (lane >= off) upto += t;
+        }
     }
-    return false;
-}
+    // The n-th tile of this workgroup; false: there is none.
+    __device__ __forceinline__ bool find(int n, int cols, Where& w) const {
+        const int all = __builtin_amdgcn_readlane(upto, 63) * cols, die = (all + 7) / 8;
+        const int at = int(blockIdx.x) / 8 + n * (int(gridDim.x) / 8), id = (int(blockIdx.x) % 8) * die + at;
+        if (at >= die || id >= all) return false;
+        const int l = lanes(__ballot(upto * cols <= id));
+        int rest = id - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(own, l)) * cols;
+        _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+            const int t = __builtin_amdgcn_readlane(tiles[i], l);
+            if (rest < t * cols) {
+                w.e = 4 * l + i;
+                w.first = __builtin_amdgcn_readlane(o[i], l);
+                w.count = __builtin_amdgcn_readlane(o[i + 1], l) - w.first;
+                w.c = rest / t;
+                w.r = rest - w.c * t;
+                return true;
+            }
+            rest -= t * cols;
+        }
+        return false;
+    }
+};
 
 // The rows of gate and factor for the same features are blocks i and i + TC / 2 of one wave.
 template <typename T>
@@ -77,43 +83,59 @@ __device__ __forceinline__ uint32_t gate_up_row(const ExpertArgs& a, int c, int 
     const int wave = q / (T::TC * 16), i = q / 16 % T::TC, f = c * (T::BC / 2) + (wave * HALF + i % HALF) * 16 + q % 16;
     return f < a.F ? uint32_t((i >= HALF ? a.F : 0) + f) * uint32_t(a.D) * uint32_t(sizeof(typename T::TIO)) : kBeyond;
 }
+// pair_at(i): the pair of row i of the tile
+template <typename T, typename PairAt>
+__device__ __forceinline__ void start_gate_up(const T& t, typename T::C& c, typename T::R& r, const ExpertArgs& a, const Where& w, PairAt pair_at) {
+    typedef typename T::TIO TIO;
+    r.start_rows(a.x, t.wave, t.lane, [&](int i) { return w.r * T::BR + i < w.count ? pair_at(i) / uint32_t(a.top_k) * a.x_bytes : kBeyond; });
+    c.start_rows(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, t.wave, t.lane,
+                 [&](int q) { return gate_up_row<T>(a, w.c, q); });
+}
 template <typename T>
 __device__ __forceinline__ void start_gate_up(T& t, const ExpertArgs& a, const Where& w) {
-    typedef typename T::TIO TIO;
-    t.r.start_rows(a.x, t.wave, t.lane, [&](int i) {
-        const int at = w.r * T::BR + i;
-        return at < w.count ? token_of(a, w.first + at) * a.x_bytes : kBeyond;
-    });
-    t.c.start_rows(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, t.wave, t.lane,
-                   [&](int q) { return gate_up_row<T>(a, w.c, q); });
+    start_gate_up(t, t.c, t.r, a, w, [&](int i) { return pair_of(a, w.first + w.r * T::BR + i); });
 }
 
 template <typename T>
 __global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
     typedef typename T::TIO TIO;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
+    const int cols = (a.F + T::BC / 2 - 1) / (T::BC / 2);
+    const Finder<T::BR> finder(a);
     Where w;
-    if (!find_tile<T::BR>(a, (a.F + T::BC / 2 - 1) / (T::BC / 2), w)) return;
+    if (!finder.find(0, cols, w)) return;
     T t(shared);
     start_gate_up(t, a, w);
-    f32x4 acc[T::TC][T::TR];
-    clear<T>(acc);
-    t.walk(acc, a.D);
-    constexpr int HALF = T::TC / 2;
-    const int f0 = w.c * (T::BC / 2) + t.wc * HALF * 16;
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<HALF>([&](int i) {
-            f32x4 h;
-            _Pragma("unroll") for (int e = 0; e < 4; ++e) {
-                const float gate = acc[i][j][e];
-                h[e] = gate * sigmoid(gate, TIO()) * acc[i + HALF][j][e];
-            }
-            return h;
+    for (int n = 1;; ++n) {
+        Where next{};
+        const bool more = T::FOLLOWED && finder.find(n, cols, next);
+        if (more) t.bring(a.order + next.first + next.r * T::BR, next.count - next.r * T::BR);
+        else next.count = 0;
+        f32x4 acc[T::TC][T::TR];
+        clear<T>(acc);
+        t.walk(acc, a.D, typename T::Nothing(), [&]() {
+            start_gate_up(t, t.c2, t.r2, a, next, [&](int i) { return min(uint32_t(t.brought(i)), uint32_t(a.n * a.top_k - 1)); });
         });
-        t.template take<HALF, TIO>(j, a.F - f0, [&](int r) {
-            const int at = w.r * T::BR + r;
-            return at < w.count ? static_cast<TIO*>(a.h) + size_t(w.first + at) * a.F + f0 : nullptr;
-        });
+        constexpr int HALF = T::TC / 2;
+        const int f0 = w.c * (T::BC / 2) + t.wc * HALF * 16;
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
+            t.template store<HALF, TIO>(
+                j, a.F - f0,
+                [&](int i) {
+                    f32x4 h;
+                    _Pragma("unroll") for (int e = 0; e < 4; ++e) {
+                        const float gate = acc[i][j][e];
+                        h[e] = gate * sigmoid(gate, TIO()) * acc[i + HALF][j][e];
+                    }
+                    return h;
+                },
+                [&](int r) {
+                    const int at = w.r * T::BR + r;
+                    return at < w.count ? static_cast<TIO*>(a.h) + size_t(w.first + at) * a.F + f0 : nullptr;
+                });
+        if (!more) return;
+        t.go_on();
+        w = next;
     }
 }
 
@@ -123,62 +145,79 @@ __device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, con
     constexpr bool HALF = sizeof(typename T::TIO) == 2;
     typedef typename std::conditional<HALF, half_t, float>::type TP;
     const int stretch = w.c * T::WC + t.wc, d0 = stretch * T::TC * 16;
+    float scale[T::TR];
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        float scale = 1.f;
-        if (HALF) {
-            float m = 0.f;
-            _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-                _Pragma("unroll") for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_size(acc[i][j][e]));
-            scale = scale_for(T::row_max(m));
-            const int at = w.r * T::BR + t.row(j);
-            if (t.lane < 16 && at < w.count && d0 < a.D) a.part_scale[size_t(stretch) * (size_t(a.n) * a.top_k) + w.first + at] = 1.f / scale;
-        }
-        t.template put<T::TC>([&](int i) { return acc[i][j] * scale; });
-        t.template take<T::TC, TP>(j, a.D - d0, [&](int r) {
-            const int at = w.r * T::BR + r;
-            return at < w.count ? static_cast<TP*>(a.part) + size_t(w.first + at) * a.D + d0 : nullptr;
-        });
+        scale[j] = 1.f;
+        if (!HALF) continue;
+        float m = 0.f;
+        _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+            _Pragma("unroll") for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_size(acc[i][j][e]));
+        scale[j] = scale_for(T::row_max(m));
+    }
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+        t.template store<T::TC, TP>(
+            j, a.D - d0, [&](int i) { return acc[i][j] * scale[j]; },
+            [&](int r) {
+                const int at = w.r * T::BR + r;
+                return at < w.count ? static_cast<TP*>(a.part) + size_t(w.first + at) * a.D + d0 : nullptr;
+            });
+        const int at = w.r * T::BR + t.row(j);
+        if (HALF && t.lane < 16 && at < w.count && d0 < a.D)
+            a.part_scale[size_t(stretch) * (size_t(a.n) * a.top_k) + w.first + at] = 1.f / scale[j];
     }
 }
 // rows of the pairs of this tile, `bytes` each, one after the other
 template <typename T>
-__device__ __forceinline__ void start_pairs(T& t, const void* rows, const Where& w, uint32_t bytes) {
-    t.r.start_rows(static_cast<const char*>(rows) + size_t(w.first + w.r * T::BR) * bytes, t.wave, t.lane,
-                   [&](int i) { return w.r * T::BR + i < w.count ? uint32_t(i) * bytes : kBeyond; });
+__device__ __forceinline__ void start_pairs(const T& t, typename T::R& r, const void* rows, const Where& w, uint32_t bytes) {
+    r.start_rows(static_cast<const char*>(rows) + size_t(w.first + w.r * T::BR) * bytes, t.wave, t.lane,
+                 [&](int i) { return w.r * T::BR + i < w.count ? uint32_t(i) * bytes : kBeyond; });
+}
+
+// `part` of all tiles of [pairs][D]: start(t, c, r, w) sets a tile's operands, K long
+template <typename T, typename Start>
+__device__ __forceinline__ void part_tiles(char* shared, const ExpertArgs& a, int K, Start start) {
+    const int cols = (a.D + T::BC - 1) / T::BC;
+    const Finder<T::BR> finder(a);
+    Where w;
+    if (!finder.find(0, cols, w)) return;
+    T t(shared);
+    start(t, t.c, t.r, w);
+    for (int n = 1;; ++n) {
+        Where next{};
+        const bool more = T::FOLLOWED && finder.find(n, cols, next);
+        if (!more) next.count = 0;
+        f32x4 acc[T::TC][T::TR];
+        clear<T>(acc);
+        t.walk(acc, K, typename T::Nothing(), [&]() { start(t, t.c2, t.r2, next); });
+        finish_part(t, a, w, acc);
+        if (!more) return;
+        t.go_on();
+        w = next;
+    }
 }
 
 template <typename T>
 __global__ __launch_bounds__(T::THREADS) void k_down(ExpertArgs a) {
     typedef typename T::TIO TIO;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
-    Where w;
-    if (!find_tile<T::BR>(a, (a.D + T::BC - 1) / T::BC, w)) return;
-    T t(shared);
     const uint32_t bytes = uint32_t(a.F) * uint32_t(sizeof(TIO));
-    start_pairs(t, a.h, w, bytes);
-    t.c.start_rows(static_cast<const TIO*>(a.w_down) + size_t(w.e) * a.D * a.F, t.wave, t.lane, [&](int q) {
-        const int d = w.c * T::BC + q;
-        return d < a.D ? uint32_t(d) * bytes : kBeyond;
+    part_tiles<T>(shared, a, a.F, [&](const T& t, typename T::C& c, typename T::R& r, const Where& w) {
+        start_pairs(t, r, a.h, w, bytes);
+        c.start_rows(static_cast<const TIO*>(a.w_down) + size_t(w.e) * a.D * a.F, t.wave, t.lane, [&](int q) {
+            const int d = w.c * T::BC + q;
+            return d < a.D ? uint32_t(d) * bytes : kBeyond;
+        });
     });
-    f32x4 acc[T::TC][T::TR];
-    clear<T>(acc);
-    t.walk(acc, a.F);
-    finish_part(t, a, w, acc);
 }
 
 template <typename T>
 __global__ __launch_bounds__(T::THREADS) void k_dx(ExpertArgs a) {
     typedef typename T::TIO TIO;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
-    Where w;
-    if (!find_tile<T::BR>(a, (a.D + T::BC - 1) / T::BC, w)) return;
-    T t(shared);
-    start_pairs(t, a.da, w, 2 * uint32_t(a.F) * uint32_t(sizeof(TIO)));
-    t.c.start_cols(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, a.D * int(sizeof(TIO)), w.c * T::BC, a.D, t.wave, t.lane, 0);
-    f32x4 acc[T::TC][T::TR];
-    clear<T>(acc);
-    t.walk(acc, 2 * a.F);
-    finish_part(t, a, w, acc);
+    part_tiles<T>(shared, a, 2 * a.F, [&](const T& t, typename T::C& c, typename T::R& r, const Where& w) {
+        start_pairs(t, r, a.da, w, 2 * uint32_t(a.F) * uint32_t(sizeof(TIO)));
+        c.start_cols(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, a.D * int(sizeof(TIO)), w.c * T::BC, a.D, t.wave, t.lane, 0);
+    });
 }
 
 // H: the products of gate and factor; T: that of dy with the columns of Wd for the same features.
@@ -188,7 +227,7 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
     static_assert(H::TC == 2 * T::TC && H::TR == T::TR && H::WC == T::WC && H::WR == T::WR, "the same features in the same lanes");
     __shared__ __attribute__((aligned(1024))) char shared[H::LDS > T::LDS ? H::LDS : T::LDS];
     Where w;
-    if (!find_tile<T::BR>(a, (a.F + T::BC - 1) / T::BC, w)) return;
+    if (!Finder<T::BR>(a).find(0, (a.F + T::BC - 1) / T::BC, w)) return;
     f32x4 gu[H::TC][H::TR], tt[T::TC][T::TR];
     float weight[T::TR];
     {
@@ -229,12 +268,9 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
                 return q < w.count ? static_cast<TIO*>(base) + size_t(w.first + q) * length + shift + f0 : nullptr;
             };
         };
-        _Pragma("unroll") for (int half = 0; half < 2; ++half) {
-            t.template put<T::TC>([&](int i) { return gu[half * T::TC + i][j]; });
-            t.template take<T::TC, TIO>(j, a.F - f0, line(a.da, 2 * a.F, half * a.F));
-        }
-        t.template put<T::TC>([&](int i) { return tt[i][j]; });
-        t.template take<T::TC, TIO>(j, a.F - f0, line(a.h, a.F, 0));
+        _Pragma("unroll") for (int half = 0; half < 2; ++half)
+            t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return gu[half * T::TC + i][j]; }, line(a.da, 2 * a.F, half * a.F));
+        t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return tt[i][j]; }, line(a.h, a.F, 0));
     }
 }
 
@@ -264,8 +300,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(ExpertArgs a, int row_tiles, 
     TIO* out = static_cast<TIO*>(DOWN ? a.d_w_down : a.d_w_gate_up) + size_t(e) * rows * cols;
     const int c0 = c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i) { return acc[i][j]; });
-        t.template take<T::TC, TIO>(j, cols - c0, [&](int r) {
+        t.template store<T::TC, TIO>(j, cols - c0, [&](int i) { return acc[i][j]; }, [&](int r) {
             const int row = r0 * T::BR + r;
             return row < rows ? out + size_t(row) * cols + c0 : nullptr;
         });
@@ -359,6 +394,11 @@ unsigned grid_of(const ExpertArgs& a, int rows, int cols) {
     const int64_t pairs = int64_t(a.n) * a.top_k, tiles = pairs / rows + (pairs < a.E ? pairs : int64_t(a.E));
     return unsigned((tiles * cols + 7) / 8 * 8);
 }
+template <typename T>
+unsigned grid_of(const ExpertArgs& a, int cols) {
+    const unsigned all = grid_of(a, T::BR, cols);
+    return T::FOLLOWED && all > 256 ? 256 : all;  // one for each compute unit
+}
 
 struct Space { size_t h, da, part, part_scale, weight_part, bytes; };
 Space space(const lsm_experts_params& p, bool backward) {
@@ -385,16 +425,16 @@ bool launch_sum(const ExpertArgs& a, hipStream_t st) {
 
 template <typename TIO, int KIND>
 bool launch_up(const ExpertArgs& a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND, false, false, false, true>::type T;
     ProfScope ps(KID_EXPERTS_UP, st);
-    hipLaunchKernelGGL((k_up<T>), dim3(grid_of(a, T::BR, up(a.F, T::BC / 2))), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_up<T>), dim3(grid_of<T>(a, up(a.F, T::BC / 2))), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND>
 bool launch_down(const ExpertArgs& a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND, false, false, false, true>::type T;
     ProfScope ps(KID_EXPERTS_DOWN, st);
-    hipLaunchKernelGGL((k_down<T>), dim3(grid_of(a, T::BR, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_down<T>), dim3(grid_of<T>(a, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND>
@@ -402,14 +442,14 @@ bool launch_hidden(const ExpertArgs& a, hipStream_t st) {
     typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type H;
     typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND, true>::type T;
     ProfScope ps(KID_EXPERTS_HIDDEN_GRAD, st);
-    hipLaunchKernelGGL((k_hidden_grad<H, T>), dim3(grid_of(a, T::BR, up(a.F, T::BC))), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_hidden_grad<H, T>), dim3(grid_of<T>(a, up(a.F, T::BC))), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND>
 bool launch_dx(const ExpertArgs& a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND>::type T;
+    typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND, false, false, false, true>::type T;
     ProfScope ps(KID_EXPERTS_DX, st);
-    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of(a, T::BR, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of<T>(a, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND, bool DOWN>

@@ -11,6 +11,8 @@
 // Where a lane's 16 bytes land is fixed by the hardware (one after the other), so rows are spread over the banks by which
 // 16 bytes of the row a lane asks for: slot s of row i holds piece s ^ f(i).  (Without bank conflicts, by the counters; with them the clocks of LDS double.)
 //
+// Where tiles follow one another in a workgroup there are as many workgroups as there is room for.
+//
 // While the matrix instructions of step t run, the operands of step t + 1 are read, each into the registers whose last use has just
 // been: piece t + 1 is complete before step t begins, piece t + NBUF - 1 is requested in it, and nothing is read from piece t.
 #pragma once
@@ -48,6 +50,12 @@ __device__ __forceinline__ void load_to_lds(uint64_t base, uint32_t offset, uint
     const u32x4 buffer = {uint32_t(from), uint32_t(from >> 32) & 0xffffu, kBeyond, 0x00020000u};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer)
                  : "memory");
+}
+// The same with 4 bytes a lane, to `to` + 4 lane.
+__device__ __forceinline__ void load4_to_lds(uint64_t base, uint32_t offset, uint32_t to) {
+    const uint64_t from = uniform(base);
+    const u32x4 buffer = {uint32_t(from), uint32_t(from >> 32) & 0xffffu, kBeyond, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer) : "memory");
 }
 // One step of a 16 x 16 product: both operands hold, in lane l, 16 bytes of row l % 16 from byte 16 (l / 16) of the step on.
 __device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, f32x4 c, uint16_t) {
@@ -162,25 +170,30 @@ struct Operand {
     }
 };
 
-// A tile: WC x WR waves of TC x TR blocks of 16 x 16.
-template <typename TIO_, Layout LC, Layout LR, int WC_, int WR_, int TC_, int TR_, int NBUF_, bool LIST_C = false, bool LIST_R = false>
+// A tile: WC x WR waves of TC x TR blocks of 16 x 16.  FOLLOWED: the workgroup goes on to another tile with the same kinds of operands and
+// the same K; the first pieces of that one are requested in the last steps of this one, and come while its results are written.
+template <typename TIO_, Layout LC, Layout LR, int WC_, int WR_, int TC_, int TR_, int NBUF_, bool LIST_C = false, bool LIST_R = false,
+          bool FOLLOWED_ = false>
 struct Tile {
     typedef TIO_ TIO;
-    static constexpr bool SQUARE = TC_ == TR_;
+    static constexpr bool FOLLOWED = FOLLOWED_;
     static constexpr int WC = WC_, WR = WR_, TC = TC_, TR = TR_, NBUF = NBUF_, WAVES = WC * WR, THREADS = 64 * WAVES;
     static constexpr int BC = WC * TC * 16, BR = WR * TR * 16;
     typedef Operand<TIO, LC, BC, WAVES, LIST_C> C;
     typedef Operand<TIO, LR, BR, WAVES, LIST_R> R;
-    static constexpr int STAGE = C::BYTES + R::BYTES, LOADS = C::LOADS + R::LOADS, AHEAD = NBUF - 1;
-    static constexpr int LIST = LIST_C || LIST_R ? 4 * C::kList : 0;
-    // results on their way out: 16 rows of a wave's blocks at a time, in fp32, padded by 16 bytes a row; each wave has its own place
-    static constexpr int OUT = 16 * (TC * 64 + 16), RING = NBUF * STAGE;
-    static constexpr int LDS = (RING > WAVES * OUT ? RING : WAVES * OUT) + LIST;
-    static_assert(LDS <= 160 * 1024 && NBUF >= 3, "LDS");
+    static constexpr int STAGE = C::BYTES + R::BYTES, LOADS = C::LOADS + R::LOADS, AHEAD = NBUF - 1, RING = NBUF * STAGE;
+    static constexpr int LIST = LIST_C || LIST_R ? 4 * C::kList : 0, ROWS = FOLLOWED ? 4 * BR : 0;  // the following tile's rows
+    static constexpr int LDS = RING + LIST + ROWS;
+    static_assert(LDS <= 160 * 1024 && NBUF >= 3 && !(FOLLOWED && LIST), "LDS");
+    // Results on their way out: 16 rows of CHUNK of a wave's blocks at a time, in fp32; each wave has its own place in the ring, where
+    // another tile follows in the one piece of it that nothing is on its way to.
+    static constexpr int CHUNK = FOLLOWED && TC > 4 ? 4 : TC, PAD = FOLLOWED ? 0 : 16;
+    static_assert(WAVES * 16 * (64 * CHUNK + PAD) <= (FOLLOWED ? STAGE : RING), "LDS");
 
-    C c;
-    R r;
-    int wave, lane, wc, wr;
+    C c, c2;
+    R r, r2;
+    int wave, lane, wc, wr, slot = 0;  // slot: of step 0 in the ring
+    bool ahead = false;                // the first pieces are there
     uint32_t lds;
 
     __device__ __forceinline__ Tile(const char* shared) {
@@ -190,44 +203,80 @@ struct Tile {
         wr = wave / WC;
         lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)shared));
     }
-    __device__ __forceinline__ uint32_t list_at() const { return lds + (LDS - LIST); }
-    // Load n of a step, of C::LOADS + R::LOADS.
-    __device__ __forceinline__ void request(int step, int K, int n) {
-        const uint32_t at = lds + uint32_t(step % NBUF) * STAGE;
-        if (n < C::LOADS) c.request(at, step * C::KSTEP, K, wave, lane, n);
-        else r.request(at + C::BYTES, step * C::KSTEP, K, wave, lane, n - C::LOADS);
+    __device__ __forceinline__ uint32_t list_at() const { return lds + RING; }
+    __device__ __forceinline__ uint32_t at(int step) const { return lds + uint32_t((slot + step) % NBUF) * STAGE; }
+
+    // The numbers list[i] for rows i < n of the following tile, to LDS, and one of them.
+    __device__ __forceinline__ void bring(const int32_t* list, int n) const {
+        if (wave < (BR + 63) / 64)
+            load4_to_lds(reinterpret_cast<uint64_t>(list), 64 * wave + lane < n ? uint32_t(4 * (64 * wave + lane)) : kBeyond,
+                         uniform(int(lds + RING + LIST + 256 * wave)));
     }
-    __device__ __forceinline__ u32x4 read_c(int step, int i) const {
-        return C::read(lds + uint32_t(step % NBUF) * STAGE, (wc * TC + i) * 16, lane);
+    __device__ __forceinline__ int brought(int i) const {
+        return *reinterpret_cast<__attribute__((address_space(3))) const int*>(uintptr_t(lds + RING + LIST + 4 * i));
     }
-    __device__ __forceinline__ u32x4 read_r(int step, int j) const {
-        return R::read(lds + uint32_t(step % NBUF) * STAGE + C::BYTES, (wr * TR + j) * 16, lane);
+
+    // Load n of step t of `steps`; behind them of the following tile's.
+    __device__ __forceinline__ void request(int t, int steps, int K, int n) {
+        const bool own = !FOLLOWED || t < steps;
+        const int k0 = (own ? t : t - steps) * C::KSTEP;
+        if (n < C::LOADS) {
+            if constexpr (FOLLOWED) {
+                C x = c;
+                x.base = own ? c.base : c2.base;
+                x.off[n] = own ? c.off[n] : c2.off[n];
+                x.request(at(t), k0, K, wave, lane, n);
+            } else {
+                c.request(at(t), k0, K, wave, lane, n);
+            }
+        } else {
+            const int m = n - C::LOADS;
+            if constexpr (FOLLOWED) {
+                R x = r;
+                x.base = own ? r.base : r2.base;
+                x.off[m] = own ? r.off[m] : r2.off[m];
+                x.request(at(t) + C::BYTES, k0, K, wave, lane, m);
+            } else {
+                r.request(at(t) + C::BYTES, k0, K, wave, lane, m);
+            }
+        }
     }
+    __device__ __forceinline__ u32x4 read_c(int step, int i) const { return C::read(at(step), (wc * TC + i) * 16, lane); }
+    __device__ __forceinline__ u32x4 read_r(int step, int j) const { return R::read(at(step) + C::BYTES, (wr * TR + j) * 16, lane); }
     // The rows of k0 .. k0 + n - 1 for an operand that is taken through a list.
     template <typename RowOf>
     __device__ __forceinline__ void fill(RowOf row_of, int k0, int n, int K) const {
         for (int k = k0 + int(threadIdx.x); k < min(k0 + n, K); k += THREADS)
             *reinterpret_cast<__attribute__((address_space(3))) uint32_t*>(uintptr_t(list_at() + 4 * (k % C::kList))) = row_of(k);
+        wait_lds();
     }
-    __device__ __forceinline__ void walk(f32x4 (&acc)[TC][TR], int K) {
-        walk(acc, K, [](int) { return 0u; });
-    }
-    // acc += the product over k = 0 .. K - 1; row_of(k): the row of k in a list.  Begins and ends with LDS free.
+    struct Nothing {
+        __device__ __forceinline__ uint32_t operator()(int) const { return 0; }
+        __device__ __forceinline__ void operator()() const {}
+    };
+    __device__ __forceinline__ void walk(f32x4 (&acc)[TC][TR], int K) { walk(acc, K, Nothing(), Nothing()); }
     template <typename RowOf>
-    __device__ __forceinline__ void walk(f32x4 (&acc)[TC][TR], int K, RowOf row_of) {
-        const int steps = (K + C::KSTEP - 1) / C::KSTEP;
+    __device__ __forceinline__ void walk(f32x4 (&acc)[TC][TR], int K, RowOf row_of) { walk(acc, K, row_of, Nothing()); }
+
+    // acc += the product over k = 0 .. K - 1; row_of(k): the row of k in a list; follow(): sets c2 and r2, called when what was brought
+    // is there.  Begins with LDS free, but for what is ahead, and ends so.
+    template <typename RowOf, typename Follow>
+    __device__ __forceinline__ void walk(f32x4 (&acc)[TC][TR], int K, RowOf row_of, Follow follow) {
+        int steps = (K + C::KSTEP - 1) / C::KSTEP;
+        if (FOLLOWED) steps = max(steps, AHEAD + 2);  // so that two ends of steps are between bring() and follow()
         if (steps == 0) return;
         if (LIST) {
             fill(row_of, 0, C::kList, K);
-            wait_lds();
             barrier();
             c.first_rows(wave, lane);
             r.first_rows(wave, lane);
         }
-        _Pragma("unroll") for (int s = 0; s < AHEAD; ++s)
-            _Pragma("unroll") for (int n = 0; n < LOADS; ++n) request(s, K, n);
-        wait_loads<(AHEAD - 2) * LOADS>();
-        barrier();
+        if (!FOLLOWED || !ahead) {
+            _Pragma("unroll") for (int s = 0; s < AHEAD; ++s)
+                _Pragma("unroll") for (int n = 0; n < LOADS; ++n) request(s, steps, K, n);
+            wait_loads<(AHEAD - 2) * LOADS>();
+            barrier();
+        }
         u32x4 a[TC], b[TR], next[TR];
         _Pragma("unroll") for (int j = 0; j < TR; ++j) b[j] = read_r(0, j);
         _Pragma("unroll") for (int i = 0; i < TC; ++i) a[i] = read_c(0, i);
@@ -236,30 +285,41 @@ struct Tile {
             for (int t0 = 0; t0 < steps; t0 += FOLD) {
                 _Pragma("unroll") for (int i = 0; i < TC; ++i)
                     _Pragma("unroll") for (int j = 0; j < TR; ++j) part[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-                walk_steps(part, a, b, next, t0, min(t0 + FOLD, steps), K, row_of);
+                walk_steps(part, a, b, next, t0, min(t0 + FOLD, steps), steps, K, row_of);
                 _Pragma("unroll") for (int i = 0; i < TC; ++i)
                     _Pragma("unroll") for (int j = 0; j < TR; ++j) acc[i][j] += part[i][j];
             }
+        } else if constexpr (FOLLOWED) {
+            walk_steps(acc, a, b, next, 0, steps - AHEAD, steps, K, row_of);
+            follow();
+            walk_steps(acc, a, b, next, steps - AHEAD, steps, steps, K, row_of);
         } else {
-            walk_steps(acc, a, b, next, 0, steps, K, row_of);
+            walk_steps(acc, a, b, next, 0, steps, steps, K, row_of);
         }
-        wait_lds();
-        wait_loads<0>();
-        barrier();
+        slot = (slot + steps) % NBUF;
+        if (!FOLLOWED) {
+            wait_lds();
+            wait_loads<0>();
+            barrier();
+        }
     }
-    // fp32 elements: sums of 128 k's are added up apart, so that a sum over some thousand is as exact as one over a few hundred (an even
-    // number of steps).
+    // fp32 elements: sums of 128 k's are added up apart, so that a sum over some thousand is as exact as one over a few hundred.
     static constexpr int FOLD = sizeof(TIO) == 4 ? 8 : 0;
+
     template <typename RowOf>
-    __device__ __forceinline__ void walk_steps(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], u32x4 (&b)[TR], u32x4 (&next)[TR], int t0, int t1, int K,
-                                               RowOf row_of) {
-        if constexpr (SQUARE) {
-            for (int t = t0; t < t1; ++t) square_step(acc, a, b, t, K, row_of);
+    __device__ __forceinline__ void walk_steps(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], u32x4 (&b)[TR], u32x4 (&next)[TR], int t0, int t1, int steps,
+                                               int K, RowOf row_of) {
+        int t = t0;
+        if constexpr (TC == TR || FOLLOWED || LIST > 0) {
+            for (; t < t1; ++t) lean_step(acc, a, b, t, steps, K, row_of);
         } else {
-            for (int t = t0; t < t1; t += 2) {
-                step(acc, a, b, next, t, K, row_of);
-                if (t + 1 < t1) step(acc, a, next, b, t + 1, K, row_of);
+            for (; t + 1 < t1; t += 2) {
+                step(acc, a, b, next, t, steps, K, row_of);
+                step(acc, a, next, b, t + 1, steps, K, row_of);
             }
+            if (t >= t1) return;
+            step(acc, a, b, next, t, steps, K, row_of);
+            _Pragma("unroll") for (int j = 0; j < TR; ++j) b[j] = next[j];
         }
     }
     template <typename RowOf>
@@ -268,10 +328,15 @@ struct Tile {
         const int k = (t + AHEAD + 2) * C::KSTEP;
         if (k >= C::kList && k % (C::kList / 2) == 0) fill(row_of, k, C::kList / 2, K);
     }
+    __device__ __forceinline__ void end_step(int t) const {
+        if (!FOLLOWED || !ahead || t > 0) wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
+        barrier();
+    }
     // Reads and requests are spread among the matrix instructions: behind one another they keep the wave from its next product until the
     // last of them is accepted.
     template <typename RowOf>
-    __device__ __forceinline__ void step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], const u32x4 (&b)[TR], u32x4 (&next)[TR], int t, int K, RowOf row_of) {
+    __device__ __forceinline__ void step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], const u32x4 (&b)[TR], u32x4 (&next)[TR], int t, int steps, int K,
+                                         RowOf row_of) {
         constexpr int ALL = TC * TR;
         refill(row_of, t, K);
         fence_schedule();
@@ -281,36 +346,48 @@ struct Tile {
                 fence_schedule();
                 const int m = i * TR + j;
                 _Pragma("unroll") for (int n = m * TR / ALL; n < (m + 1) * TR / ALL; ++n) next[n] = read_r(t + 1, n);
-                _Pragma("unroll") for (int n = m * LOADS / ALL; n < (m + 1) * LOADS / ALL; ++n) request(t + AHEAD, K, n);
+                _Pragma("unroll") for (int n = m * LOADS / ALL; n < (m + 1) * LOADS / ALL; ++n) request(t + AHEAD, steps, K, n);
                 if (j == TR - 1) a[i] = read_c(t + 1, i);
                 fence_schedule();
             }
-        wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
-        barrier();
+        end_step(t);
     }
-    // The same for as many blocks along either side, without a second set of registers for r: first all products with row or column 0, then
-    // those with 1 and so on, so that operands i of both sides are free, and read anew, when theirs are done.
+    // The same without a second set of registers for r: first all products with the first operand of the shorter side (and as many of the
+    // longer one as belong to it), then those with the second and so on, so that operands are free, and read anew, long before all
+    // products are formed.  (8 x 4 blocks alone, with registers to spare: 4 % slower, but through a list 2 % faster; followed, the second set costs 29 to 59
+    // registers in scratch and 15 to 20 %.)
     template <typename RowOf>
-    __device__ __forceinline__ void square_step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], u32x4 (&b)[TR], int t, int K, RowOf row_of) {
-        constexpr int ALL = TC * TR;
+    __device__ __forceinline__ void lean_step(f32x4 (&acc)[TC][TR], u32x4 (&a)[TC], u32x4 (&b)[TR], int t, int steps, int K, RowOf row_of) {
+        constexpr int GROUPS = TC < TR ? TC : TR, A = TC / GROUPS, B = TR / GROUPS, ALL = TC * TR;
         refill(row_of, t, K);
         fence_schedule();
         int m = 0;
-        _Pragma("unroll") for (int d = 0; d < TC; ++d) {
-            _Pragma("unroll") for (int q = 0; q < 2 * (TC - d) - 1; ++q, ++m) {
-                const int i = q & 1 ? d + (q + 1) / 2 : d, j = q & 1 ? d : d + q / 2;
-                acc[i][j] = product(a[i], b[j], acc[i][j], TIO());
-                fence_schedule();
-                _Pragma("unroll") for (int n = m * LOADS / ALL; n < (m + 1) * LOADS / ALL; ++n) request(t + AHEAD, K, n);
-                fence_schedule();
-            }
-            b[d] = read_r(t + 1, d);
-            a[d] = read_c(t + 1, d);
+        const auto multiply = [&](int i, int j) {
+            acc[i][j] = product(a[i], b[j], acc[i][j], TIO());
+            fence_schedule();
+            _Pragma("unroll") for (int n = m * LOADS / ALL; n < (m + 1) * LOADS / ALL; ++n) request(t + AHEAD, steps, K, n);
+            fence_schedule();
+            ++m;
+        };
+        _Pragma("unroll") for (int d = 0; d < GROUPS; ++d) {
+            _Pragma("unroll") for (int j = d * B; j < (d + 1) * B; ++j)
+                _Pragma("unroll") for (int i = d * A; i < TC; ++i) multiply(i, j);
+            _Pragma("unroll") for (int j = d * B; j < (d + 1) * B; ++j) b[j] = read_r(t + 1, j);
+            _Pragma("unroll") for (int j = (d + 1) * B; j < TR; ++j)
+                _Pragma("unroll") for (int i = d * A; i < (d + 1) * A; ++i) multiply(i, j);
+            _Pragma("unroll") for (int i = d * A; i < (d + 1) * A; ++i) a[i] = read_c(t + 1, i);
             fence_schedule();
         }
-        wait_loads<(AHEAD - 2) * LOADS>();  // piece t + 2 is there
+        end_step(t);
+    }
+    // On to the following tile, when all that this wave had to write is on its way.
+    __device__ __forceinline__ void go_on() {
+        c = c2;
+        r = r2;
+        ahead = true;
         barrier();
     }
+
     // Values of block (i, j): element e of a lane is row(j), column col(i) + e of the tile.
     __device__ __forceinline__ int row(int j) const { return (wr * TR + j) * 16 + (lane & 15); }
     __device__ __forceinline__ int col(int i) const { return (wc * TC + i) * 16 + 4 * (lane >> 4); }
@@ -324,11 +401,13 @@ struct Tile {
         return fmaxf(x, __shfl_xor(x, 32, 64));
     }
 
-    // Results to memory, whole lines at a time: block j of this wave's rows goes through the wave's own place in LDS (the caller has
-    // seen to it that LDS is free) and leaves in 16-byte pieces.  value(i): four results of block i < NB; line(r): where row r of
-    // the tile goes, first column of this wave included, or null; width: columns that there are from that column on.
-    template <int NB> __device__ __forceinline__ uint32_t cell(int row16, int column) const {
-        return lds + uint32_t(wave) * OUT + uint32_t(row16) * (NB * 64 + 16) + uint32_t(column) * 4;
+    // Results to memory, whole lines at a time: row block j of N neighbouring blocks goes through the wave's own place in LDS and leaves
+    // in 16-byte pieces.  Rows are 16 bytes further apart than they are long or, where there is no room for that, piece p of row r is at
+    // p ^ r: neither the lanes of a column nor those of a row meet in a bank.
+    template <int N> __device__ __forceinline__ uint32_t cell(int row16, int column) const {
+        static_assert(N <= CHUNK, "the wave's own place");
+        const uint32_t own = (FOLLOWED ? at(AHEAD) : lds) + uint32_t(wave) * (16 * (64 * CHUNK + PAD)) + uint32_t(row16) * (N * 64 + PAD);
+        return own + uint32_t(FOLLOWED ? ((column >> 2) ^ (row16 % (4 * N))) * 16 + (column & 3) * 4 : column * 4);
     }
     // Between what lanes of a wave write there and what others read: no lane's part may be moved across, nor taken apart from the others' as
     // where branches follow one another on the same condition.
@@ -337,24 +416,26 @@ struct Tile {
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    template <int NB, typename Value>
+    // value(i): four results of block i of the N.
+    template <int N, typename Value>
     __device__ __forceinline__ void put(Value value) const {
         wave_meets();
-        _Pragma("unroll") for (int i = 0; i < NB; ++i)
-            *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<NB>(lane & 15, i * 16 + 4 * (lane >> 4)))) = value(i);
+        _Pragma("unroll") for (int i = 0; i < N; ++i)
+            *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(uintptr_t(cell<N>(lane & 15, i * 16 + 4 * (lane >> 4)))) = value(i);
         wave_meets();
     }
+    // line(r): where row r of the tile goes, from the first of the N blocks' columns on, or null; width: columns that there are from there on.
     // ADD: to what is there already (TOUT's own sum).
-    template <int NB, typename TOUT, bool ADD = false, typename Line>
+    template <int N, typename TOUT, bool ADD = false, typename Line>
     __device__ __forceinline__ void take(int j, int width, Line line) const {
-        constexpr int E = 16 / int(sizeof(TOUT)), LANES = NB * 16 / E, ROWS = 64 / LANES;
+        constexpr int E = 16 / int(sizeof(TOUT)), LANES = N * 16 / E, ROWS_ = 64 / LANES;
         wave_meets();
-        _Pragma("unroll") for (int it = 0; it < (16 + ROWS - 1) / ROWS; ++it) {
-            const int row = it * ROWS + lane / LANES, c = (lane % LANES) * E;
-            if (ROWS > 16 && row >= 16) continue;
+        _Pragma("unroll") for (int it = 0; it < (16 + ROWS_ - 1) / ROWS_; ++it) {
+            const int row = it * ROWS_ + lane / LANES, c = (lane % LANES) * E;
+            if (ROWS_ > 16 && row >= 16) continue;
             float v[E];
             _Pragma("unroll") for (int q = 0; q < E / 4; ++q) {
-                const f32x4 x = *reinterpret_cast<__attribute__((address_space(3))) const f32x4*>(uintptr_t(cell<NB>(row, c + 4 * q)));
+                const f32x4 x = *reinterpret_cast<__attribute__((address_space(3))) const f32x4*>(uintptr_t(cell<N>(row, c + 4 * q)));
                 _Pragma("unroll") for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
             }
             TOUT* to = line((wr * TR + j) * 16 + row);
@@ -371,6 +452,23 @@ struct Tile {
                 _Pragma("unroll") for (int e = 0; e < E; ++e) v[e] += old[e];
             }
             *reinterpret_cast<u32x4*>(to + c) = pack(v);
+        }
+    }
+    // What was requested ahead is there before the first result is written: a wait for it later would be one for the results too.
+    __device__ __forceinline__ void settle() const {
+        if (FOLLOWED) wait_loads<0>();
+    }
+    // B blocks, CHUNK at a time; width, line from the first of them on.
+    template <int B, typename TOUT, bool ADD = false, typename Value, typename Line>
+    __device__ __forceinline__ void store(int j, int width, Value value, Line line) const {
+        constexpr int N = CHUNK < B ? CHUNK : B;
+        _Pragma("unroll") for (int i0 = 0; i0 < B; i0 += N) {
+            put<N>([&](int i) { return value(i0 + i); });
+            if (j == 0 && i0 == 0) settle();
+            take<N, TOUT, ADD>(j, width - i0 * 16, [&](int r) {
+                TOUT* p = line(r);
+                return p ? p + i0 * 16 : nullptr;
+            });
         }
     }
 };
@@ -401,12 +499,12 @@ __device__ __forceinline__ void clear(f32x4 (&acc)[T::TC][T::TR]) {
 }
 
 // The tiles there are, by number (kTiles in lsm_train_dev.h has their sizes).  HALF: half the columns, for columns that go with pairs of them.
-template <typename TIO, Layout LC, Layout LR, int KIND, bool HALF = false, bool LIST_C = false, bool LIST_R = false> struct TileOf;
+template <typename TIO, Layout LC, Layout LR, int KIND, bool HALF = false, bool LIST_C = false, bool LIST_R = false, bool FOLLOWED = false> struct TileOf;
 // (fp32 has no tile of 256 x 256: its sums are kept in two sets of registers.)
 #define LSM_TILE(KIND, WC, WR, TC, TR)                                                                                      \
-    template <typename TIO, Layout LC, Layout LR, bool HALF, bool LIST_C, bool LIST_R>                                        \
-    struct TileOf<TIO, LC, LR, KIND, HALF, LIST_C, LIST_R> {                                                                  \
-        typedef Tile<TIO, LC, LR, WC, WR, HALF ? (TC) / 2 : (TC), TR, 4, LIST_C, LIST_R> type;                                \
+    template <typename TIO, Layout LC, Layout LR, bool HALF, bool LIST_C, bool LIST_R, bool FOLLOWED>                         \
+    struct TileOf<TIO, LC, LR, KIND, HALF, LIST_C, LIST_R, FOLLOWED> {                                                                  \
+        typedef Tile<TIO, LC, LR, WC, WR, HALF ? (TC) / 2 : (TC), TR, 4, LIST_C, LIST_R, FOLLOWED && (KIND) == 0> type;       \
         static_assert(kTiles[KIND].rows == (WR) * (TR) * 16 && kTiles[KIND].cols == (WC) * (TC) * 16 && kTiles[KIND].waves == (WC), ""); \
     }
 LSM_TILE(0, 2, 4, 8, 4);
@@ -417,8 +515,9 @@ LSM_TILE(4, 4, 1, 4, 2);
 LSM_TILE(5, 2, 2, 2, 2);
 LSM_TILE(6, 4, 1, 2, 2);
 #undef LSM_TILE
-template <Layout LC, Layout LR, bool HALF, bool LIST_C, bool LIST_R>
-struct TileOf<float, LC, LR, 0, HALF, LIST_C, LIST_R> : TileOf<float, LC, LR, 2, HALF, LIST_C, LIST_R> {};
+template <Layout LC, Layout LR, bool HALF, bool LIST_C, bool LIST_R, bool FOLLOWED>
+struct TileOf<float, LC, LR, 0, HALF, LIST_C, LIST_R, FOLLOWED> : TileOf<float, LC, LR, 2, HALF, LIST_C, LIST_R> {};
+// FOLLOWED: the largest tiles, one workgroup a compute unit, on and on; the others' workgroups are each other's company.
 
 }  // namespace
 }  // namespace lsm

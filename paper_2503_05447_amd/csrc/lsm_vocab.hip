@@ -114,11 +114,20 @@ struct Entries {
             v[u] = token >= 0 && e < a.K ? a.entry[uint32_t(e) * uint32_t(a.n) + uint32_t(token)] : -1;
         }
     }
-    // found(e, column - first) for those of columns first .. first + width
+    // found(e, column - first) for those of columns first .. first + width, the lanes' first ones together, then their second ones: what they
+    // load for it is waited for a few times and not for every place (4096 tokens, 64 entries: 385 -> 300 us for the gradient).
     template <typename Found>
     __device__ __forceinline__ void find(int e0, int first, int width, int lane, Found found) const {
-        _Pragma("unroll") for (int u = 0; u < N; ++u)
-            if (v[u] >= 0 && uint32_t(v[u] - first) < uint32_t(width)) found(e0 + 4 * u + (lane >> 4), v[u] - first);
+        uint32_t hits = 0;
+        _Pragma("unroll") for (int u = 0; u < N; ++u) hits |= v[u] >= 0 && uint32_t(v[u] - first) < uint32_t(width) ? 1u << u : 0u;
+        while (__ballot(hits != 0)) {
+            if (hits == 0) continue;
+            const int u = __builtin_ctz(hits);
+            int d = 0;
+            _Pragma("unroll") for (int i = 0; i < N; ++i) d = u == i ? v[i] : d;
+            found(e0 + 4 * u + (lane >> 4), d - first);
+            hits &= hits - 1;
+        }
     }
 };
 
@@ -129,78 +138,103 @@ __device__ __forceinline__ void tile_at(int id, int rt, int ct, int& r, int& c) 
     c = rest / rows;
     r = 8 * band + rest - c * rows;
 }
-__device__ __forceinline__ int number_of_tile(int all) {  // -1: none left.  A die's numbers are neighbours
-    const int die = (all + 7) / 8, slot = int(blockIdx.x) / 8, id = (int(blockIdx.x) % 8) * die + slot;
-    return slot < die && id < all ? id : -1;
+__device__ __forceinline__ int number_of_tile(int all, int n = 0) {  // the n-th of this workgroup; -1: none left.  A die's numbers are neighbours
+    const int die = (all + 7) / 8, at = int(blockIdx.x) / 8 + n * (int(gridDim.x) / 8), id = (int(blockIdx.x) % 8) * die + at;
+    return at < die && id < all ? id : -1;
 }
 
-// x (rows that count) times w^T from vocabulary column v0 on
-template <typename T>
-__device__ __forceinline__ void form_logits(T& t, const VocabArgs& a, int rows, int r0, int v0, int end, f32x4 (&acc)[T::TC][T::TR]) {
+// The logits of all tiles of the tokens that count and the vocabulary from v0 to end, one after the other: finish(t, rows, r0, c, acc) with
+// the tile's first row, its number along the columns and its logits, still without their scale.
+template <typename T, typename Finish>
+__device__ __forceinline__ void logit_tiles(char* shared, const VocabArgs& a, int v0, int end, Finish finish) {
     typedef typename T::TIO TIO;
-    const uint32_t bytes = uint32_t(a.D) * uint32_t(sizeof(TIO));
-    t.r.start_rows(a.x, t.wave, t.lane, [&](int i) { return r0 + i < rows ? token_of(a, r0 + i) * a.x_bytes : kBeyond; });
-    t.c.start_rows(static_cast<const TIO*>(a.w) + size_t(v0) * a.D, t.wave, t.lane, [&](int q) { return v0 + q < end ? uint32_t(q) * bytes : kBeyond; });
-    clear<T>(acc);
-    t.walk(acc, a.D);
+    const int rows = rows_of(a), rt = (rows + T::BR - 1) / T::BR, ct = (end - v0 + T::BC - 1) / T::BC;
+    int id = number_of_tile(rt * ct), r, c;
+    if (id < 0) return;
+    tile_at(id, rt, ct, r, c);
+    T t(shared);
+    const auto start = [&](typename T::C& to_c, typename T::R& to_r, bool there, int r0, int c0, auto token_at) {
+        const uint32_t bytes = uint32_t(a.D) * uint32_t(sizeof(TIO));
+        to_r.start_rows(a.x, t.wave, t.lane, [&](int i) { return there && r0 + i < rows ? token_at(i) * a.x_bytes : kBeyond; });
+        to_c.start_rows(static_cast<const TIO*>(a.w) + size_t(v0 + c0) * a.D, t.wave, t.lane,
+                        [&](int q) { return there && v0 + c0 + q < end ? uint32_t(q) * bytes : kBeyond; });
+    };
+    start(t.c, t.r, true, r * T::BR, c * T::BC, [&](int i) { return token_of(a, r * T::BR + i); });
+    for (int n = 1;; ++n) {
+        int next = -1, r2 = 0, c2 = 0;
+        if (T::FOLLOWED) next = number_of_tile(rt * ct, n);
+        if (next >= 0) {
+            tile_at(next, rt, ct, r2, c2);
+            t.bring(a.order + r2 * T::BR, rows - r2 * T::BR);
+        }
+        f32x4 acc[T::TC][T::TR];
+        clear<T>(acc);
+        t.walk(acc, a.D, typename T::Nothing(), [&]() {
+            start(t.c2, t.r2, next >= 0, r2 * T::BR, c2 * T::BC, [&](int i) { return min(uint32_t(t.brought(i)), uint32_t(a.n - 1)); });
+        });
+        finish(t, rows, r * T::BR, c, acc);
+        if (next < 0) return;
+        t.go_on();
+        r = r2;
+        c = c2;
+    }
 }
 
 template <typename T, bool TEACHER>
 __global__ __launch_bounds__(T::THREADS) void k_logits(VocabArgs a) {
     typedef typename T::TIO TIO;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
-    const int rows = rows_of(a), rt = (rows + T::BR - 1) / T::BR, ct = (a.V + T::BC - 1) / T::BC, id = number_of_tile(rt * ct);
-    if (id < 0) return;
-    int r, c;
-    tile_at(id, rt, ct, r, c);
-    const int r0 = r * T::BR;
-    T t(shared);
-    f32x4 acc[T::TC][T::TR];
-    form_logits(t, a, rows, r0, c * T::BC, a.V, acc);
-    const int first = c * T::BC + t.wc * T::TC * 16, mine = first + 4 * (t.lane >> 4);  // of the wave, of the lane
-    const float log2_scale = a.scale * kLog2e;
-    const bool edge = first + T::TC * 16 > a.V;
-    int tokens[T::TR], wants[T::TR];
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) tokens[j] = r0 + t.row(j) < rows ? int(token_of(a, r0 + t.row(j))) : -1;
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) wants[j] = TEACHER || tokens[j] < 0 ? -1 : a.index[tokens[j]];
-    Entries entries;
-    if (TEACHER) entries.load(a, tokens[0], 0, t.lane);
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        const int at = r0 + t.row(j), token = tokens[j];
-        float m = -__builtin_inff(), sum = 0.f;
-        _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-            _Pragma("unroll") for (int q = 0; q < 4; ++q) {
-                if (edge && mine + i * 16 + q >= a.V) acc[i][j][q] = -__builtin_inff();
-                m = fmaxf(m, acc[i][j][q]);
-            }
-        m = T::row_max(m);  // of the logits without their scale, which is positive
-        const float top = m == -__builtin_inff() ? 0.f : m * log2_scale;
-        _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-            _Pragma("unroll") for (int q = 0; q < 4; ++q) sum += power(__builtin_fmaf(acc[i][j][q], log2_scale, -top), TIO());
-        sum = T::row_sum(sum);
-        if (t.lane < 16 && at < rows) a.stats[size_t(c * T::WC + t.wc) * a.n + at] = f32x2{m * a.scale, sum};
-        if (!TEACHER) {
-            const int want = wants[j];
-            if (__ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) == 0) continue;
+    logit_tiles<T>(shared, a, 0, a.V, [&](const T& t, int rows, int r0, int c, f32x4 (&acc)[T::TC][T::TR]) {
+        const int first = c * T::BC + t.wc * T::TC * 16, mine = first + 4 * (t.lane >> 4);  // of the wave, of the lane
+        const float log2_scale = a.scale * kLog2e;
+        const bool edge = first + T::TC * 16 > a.V;
+        int tokens[T::TR], wants[T::TR];
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) tokens[j] = r0 + t.row(j) < rows ? int(token_of(a, r0 + t.row(j))) : -1;
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) wants[j] = TEACHER || tokens[j] < 0 ? -1 : a.index[tokens[j]];
+        Entries entries;
+        if (TEACHER) entries.load(a, tokens[0], 0, t.lane);
+        t.settle();
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+            const int at = r0 + t.row(j), token = tokens[j];
+            float m = -__builtin_inff(), sum = 0.f;
             _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-                _Pragma("unroll") for (int q = 0; q < 4; ++q)
-                    if (want == mine + i * 16 + q) a.at_entry[at] = acc[i][j][q] * a.scale;
-        } else {
-            Entries next;
-            if (j + 1 < T::TR) next.load(a, tokens[(j + 1) % T::TR], 0, t.lane);
-            t.template put<T::TC>([&](int i) { return acc[i][j]; });
-            const auto found = [&](int e, int d) {
-                a.at_entry[size_t(e) * a.n + at] =
-                    a.scale * *reinterpret_cast<__attribute__((address_space(3))) const float*>(uintptr_t(t.template cell<T::TC>(t.lane & 15, d)));
-            };
-            entries.find(0, first, T::TC * 16, t.lane, found);
-            for (int e0 = 4 * Entries::N; e0 < a.K; e0 += 4 * Entries::N) {
-                entries.load(a, token, e0, t.lane);
-                entries.find(e0, first, T::TC * 16, t.lane, found);
+                _Pragma("unroll") for (int q = 0; q < 4; ++q) {
+                    if (edge && mine + i * 16 + q >= a.V) acc[i][j][q] = -__builtin_inff();
+                    m = fmaxf(m, acc[i][j][q]);
+                }
+            m = T::row_max(m);  // of the logits without their scale, which is positive
+            const float top = m == -__builtin_inff() ? 0.f : m * log2_scale;
+            _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+                _Pragma("unroll") for (int q = 0; q < 4; ++q) sum += power(__builtin_fmaf(acc[i][j][q], log2_scale, -top), TIO());
+            sum = T::row_sum(sum);
+            if (t.lane < 16 && at < rows) a.stats[size_t(c * T::WC + t.wc) * a.n + at] = f32x2{m * a.scale, sum};
+            if (!TEACHER) {
+                const int want = wants[j];
+                if (__ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) == 0) continue;
+                _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+                    _Pragma("unroll") for (int q = 0; q < 4; ++q)
+                        if (want == mine + i * 16 + q) a.at_entry[at] = acc[i][j][q] * a.scale;
+            } else {
+                Entries next;
+                if (j + 1 < T::TR) next.load(a, tokens[(j + 1) % T::TR], 0, t.lane);
+                constexpr int N = T::CHUNK;
+                _Pragma("unroll") for (int i0 = 0; i0 < T::TC; i0 += N) {
+                    t.template put<N>([&](int i) { return acc[i0 + i][j]; });
+                    const auto found = [&](int e, int d) {
+                        a.at_entry[size_t(e) * a.n + at] =
+                            a.scale * *reinterpret_cast<__attribute__((address_space(3))) const float*>(uintptr_t(t.template cell<N>(t.lane & 15, d)));
+                    };
+                    entries.find(0, first + i0 * 16, N * 16, t.lane, found);
+                    for (int e0 = 4 * Entries::N; e0 < a.K; e0 += 4 * Entries::N) {
+                        Entries more;
+                        more.load(a, token, e0, t.lane);
+                        more.find(e0, first + i0 * 16, N * 16, t.lane, found);
+                    }
+                }
+                entries = next;
             }
-            entries = next;
         }
-    }
+    });
 }
 
 // TOKENS tokens by a workgroup, every SLICES-th part (and entry) by a thread: 64 of them where tokens are many, four where a token's parts
@@ -258,60 +292,59 @@ __global__ __launch_bounds__(T::THREADS) void k_grad(VocabArgs a) {
     typedef typename T::TIO TIO;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
     const int end = min(a.V, a.v0 + a.piece);
-    const int rows = rows_of(a), rt = (rows + T::BR - 1) / T::BR, ct = (end - a.v0 + T::BC - 1) / T::BC, id = number_of_tile(rt * ct);
-    if (id < 0) return;
-    int r, c;
-    tile_at(id, rt, ct, r, c);
-    const int r0 = r * T::BR;
-    T t(shared);
-    f32x4 acc[T::TC][T::TR];
-    form_logits(t, a, rows, r0, a.v0 + c * T::BC, end, acc);
-    const int column = c * T::BC + t.wc * T::TC * 16, first = a.v0 + column, mine = first + 4 * (t.lane >> 4);
-    const float log2_scale = a.scale * kLog2e;
-    const bool edge = first + T::TC * 16 > end;
-    int tokens[T::TR], wants[T::TR];
-    float tops[T::TR], weights[T::TR];
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) tokens[j] = r0 + t.row(j) < rows ? int(token_of(a, r0 + t.row(j))) : -1;
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        wants[j] = TEACHER || tokens[j] < 0 ? -1 : a.index[tokens[j]];
-        tops[j] = tokens[j] < 0 ? 0.f : a.lse_in[tokens[j]] * kLog2e;
-        weights[j] = tokens[j] < 0 ? 0.f : a.d_loss[tokens[j]] * a.scale;
-    }
-    Entries entries;
-    if (TEACHER) entries.load(a, tokens[0], 0, t.lane);
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        const int token = tokens[j], want = wants[j];
-        const float top = tops[j], weight = weights[j];
-        Entries next;
-        if (TEACHER && j + 1 < T::TR) next.load(a, tokens[(j + 1) % T::TR], 0, t.lane);
-        const bool here = !TEACHER && __ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) != 0;
-        t.template put<T::TC>([&](int i) {
-            f32x4 v;
-            _Pragma("unroll") for (int e = 0; e < 4; ++e) {
-                const int col = mine + i * 16 + e;
-                float p = power(__builtin_fmaf(acc[i][j][e], log2_scale, -top), TIO());
-                if (here && col == want) p -= 1.f;
-                v[e] = edge && col >= end ? 0.f : weight * p;
-            }
-            return v;
-        });
-        if (TEACHER) {
-            const auto found = [&](int e, int d) {  // no two entries of a row are the same
-                auto* p = reinterpret_cast<__attribute__((address_space(3))) float*>(uintptr_t(t.template cell<T::TC>(t.lane & 15, d)));
-                *p = *p - weight * a.share[size_t(e) * a.n + token];
-            };
-            entries.find(0, first, T::TC * 16, t.lane, found);
-            for (int e0 = 4 * Entries::N; e0 < a.K; e0 += 4 * Entries::N) {
-                entries.load(a, token, e0, t.lane);
-                entries.find(e0, first, T::TC * 16, t.lane, found);
-            }
-            entries = next;
+    logit_tiles<T>(shared, a, a.v0, end, [&](const T& t, int rows, int r0, int c, f32x4 (&acc)[T::TC][T::TR]) {
+        const int column = c * T::BC + t.wc * T::TC * 16, first = a.v0 + column, mine = first + 4 * (t.lane >> 4);
+        const float log2_scale = a.scale * kLog2e;
+        const bool edge = first + T::TC * 16 > end;
+        int tokens[T::TR], wants[T::TR];
+        float tops[T::TR], weights[T::TR];
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) tokens[j] = r0 + t.row(j) < rows ? int(token_of(a, r0 + t.row(j))) : -1;
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+            wants[j] = TEACHER || tokens[j] < 0 ? -1 : a.index[tokens[j]];
+            tops[j] = tokens[j] < 0 ? 0.f : a.lse_in[tokens[j]] * kLog2e;
+            weights[j] = tokens[j] < 0 ? 0.f : a.d_loss[tokens[j]] * a.scale;
         }
-        // the columns behind the vocabulary's end are zeros that the next products read
-        t.template take<T::TC, TIO>(j, a.piece - column, [&](int q) {
-            return r0 + q < rows ? static_cast<TIO*>(a.grad) + size_t(r0 + q) * a.piece + column : nullptr;
-        });
-    }
+        Entries entries;
+        if (TEACHER) entries.load(a, tokens[0], 0, t.lane);
+        t.settle();
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+            const int token = tokens[j], want = wants[j];
+            const float top = tops[j], weight = weights[j];
+            Entries next;
+            if (TEACHER && j + 1 < T::TR) next.load(a, tokens[(j + 1) % T::TR], 0, t.lane);
+            const bool here = !TEACHER && __ballot(uint32_t(want - first) < uint32_t(T::TC * 16)) != 0;
+            constexpr int N = T::CHUNK;
+            _Pragma("unroll") for (int i0 = 0; i0 < T::TC; i0 += N) {
+                t.template put<N>([&](int i) {
+                    f32x4 v;
+                    _Pragma("unroll") for (int e = 0; e < 4; ++e) {
+                        const int col = mine + (i0 + i) * 16 + e;
+                        float p = power(__builtin_fmaf(acc[i0 + i][j][e], log2_scale, -top), TIO());
+                        if (here && col == want) p -= 1.f;
+                        v[e] = edge && col >= end ? 0.f : weight * p;
+                    }
+                    return v;
+                });
+                if (TEACHER) {
+                    const auto found = [&](int e, int d) {  // no two entries of a row are the same
+                        auto* p = reinterpret_cast<__attribute__((address_space(3))) float*>(uintptr_t(t.template cell<N>(t.lane & 15, d)));
+                        *p = *p - weight * a.share[size_t(e) * a.n + token];
+                    };
+                    entries.find(0, first + i0 * 16, N * 16, t.lane, found);
+                    for (int e0 = 4 * Entries::N; e0 < a.K; e0 += 4 * Entries::N) {
+                        Entries more;
+                        more.load(a, token, e0, t.lane);
+                        more.find(e0, first + i0 * 16, N * 16, t.lane, found);
+                    }
+                }
+                // the columns behind the vocabulary's end are zeros that the next products read
+                t.template take<N, TIO>(j, a.piece - column - i0 * 16, [&](int q) {
+                    return r0 + q < rows ? static_cast<TIO*>(a.grad) + size_t(r0 + q) * a.piece + column + i0 * 16 : nullptr;
+                });
+            }
+            if (TEACHER) entries = next;
+        }
+    });
 }
 
 template <typename T>
@@ -332,8 +365,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(VocabArgs a) {
     t.walk(acc, rows, [&](int k) { return token_of(a, k); });
     const int c0 = c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i) { return acc[i][j]; });
-        t.template take<T::TC, TIO>(j, a.D - c0, [&](int q) {
+        t.template store<T::TC, TIO>(j, a.D - c0, [&](int i) { return acc[i][j]; }, [&](int q) {
             const int v = r * T::BR + q;
             return v < width ? static_cast<TIO*>(a.dw) + size_t(a.v0 + v) * a.D + c0 : nullptr;
         });
@@ -364,9 +396,8 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     const int c0 = c * T::BC + t.wc * T::TC * 16;
     const auto line = [&](int q) { return r0 + q < rows ? a.part + (size_t(share) * a.n + r0 + q) * a.D + c0 : nullptr; };
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template put<T::TC>([&](int i) { return acc[i][j]; });
-        if (a.v0 == 0) t.template take<T::TC, float>(j, a.D - c0, line);
-        else t.template take<T::TC, float, true>(j, a.D - c0, line);
+        if (a.v0 == 0) t.template store<T::TC, float>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
+        else t.template store<T::TC, float, true>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
     }
 }
 
@@ -492,38 +523,44 @@ bool enqueue_rows(const VocabArgs& a, const Space& s, char* ws, hipStream_t st) 
                         reinterpret_cast<int32_t*>(ws + s.order), reinterpret_cast<int32_t*>(ws + s.place),
                         reinterpret_cast<int32_t*>(ws + s.hist), st);
 }
-unsigned grid_of(int64_t tiles) { return unsigned((tiles + 7) / 8 * 8); }
+template <typename T>
+unsigned grid_of(int64_t tiles) {
+    const unsigned all = unsigned((tiles + 7) / 8 * 8);
+    return T::FOLLOWED && all > 256 ? 256 : all;  // one for each compute unit
+}
 
 template <typename TIO, int KIND>
 bool launch_logits(const VocabArgs& a, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND, false, false, false, true>::type T;
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type TT;  // with a teacher: its entries need the registers
     ProfScope ps(KID_VOCAB_LOGITS, st);
-    const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(a.V, T::BC));
-    if (a.K) hipLaunchKernelGGL((k_logits<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
-    else hipLaunchKernelGGL((k_logits<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
+    const int64_t tiles = int64_t(up(a.n, T::BR)) * up(a.V, T::BC);
+    if (a.K) hipLaunchKernelGGL((k_logits<TT, true>), dim3(grid_of<TT>(tiles)), dim3(T::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((k_logits<T, false>), dim3(grid_of<T>(tiles)), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND>
 bool launch_grad(const VocabArgs& a, int width, hipStream_t st) {
-    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type T;
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND, false, false, false, true>::type T;
+    typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND>::type TT;  // with a teacher: its entries need the registers
     ProfScope ps(KID_VOCAB_GRAD, st);
-    const unsigned grid = grid_of(int64_t(up(a.n, T::BR)) * up(width, T::BC));
-    if (a.K) hipLaunchKernelGGL((k_grad<T, true>), dim3(grid), dim3(T::THREADS), 0, st, a);
-    else hipLaunchKernelGGL((k_grad<T, false>), dim3(grid), dim3(T::THREADS), 0, st, a);
+    const int64_t tiles = int64_t(up(a.n, T::BR)) * up(width, T::BC);
+    if (a.K) hipLaunchKernelGGL((k_grad<TT, true>), dim3(grid_of<TT>(tiles)), dim3(T::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((k_grad<T, false>), dim3(grid_of<T>(tiles)), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND>
 bool launch_dw(const VocabArgs& a, int width, hipStream_t st) {
     typedef typename TileOf<TIO, BY_COLS, BY_COLS, KIND, false, true>::type T;
     ProfScope ps(KID_VOCAB_DW, st);
-    hipLaunchKernelGGL((k_dw<T>), dim3(grid_of(int64_t(up(width, T::BR)) * up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_dw<T>), dim3(grid_of<T>(int64_t(up(width, T::BR)) * up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND>
 bool launch_dx(const VocabArgs& a, hipStream_t st) {
     typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND>::type T;
     ProfScope ps(KID_VOCAB_DX, st);
-    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of(int64_t(up(a.n, T::BR)) * up(a.D, T::BC) * a.shares)), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of<T>(int64_t(up(a.n, T::BR)) * up(a.D, T::BC) * a.shares)), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 
