@@ -51,7 +51,7 @@ int lsm_moe_route_bwd(const lsm_route_params* p, const void* logits, const int32
  *   offsets    [E + 1] int32: the pairs of expert e are at offsets[e] .. offsets[e + 1] - 1            out
  *   order      [n top_k] int32: the pair at each place; -1 behind offsets[E]                          out
  *   place      [n, top_k] int32: the place of each pair, -1 where it is left out                       out
- *   workspace  at least lsm_moe_plan_workspace_bytes(p) (0 for invalid params)
+ *   workspace  at least lsm_moe_plan_workspace_bytes(p) (0 for invalid params, and where none is needed: up to 8192 pairs)
  * Of p only n, E and top_k count.
  */
 size_t lsm_moe_plan_workspace_bytes(const lsm_route_params* p);

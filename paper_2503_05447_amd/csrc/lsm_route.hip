@@ -336,7 +336,7 @@ int lsm_moe_route_bwd(const lsm_route_params* p, const void* logits, const int32
 
 size_t lsm_moe_plan_workspace_bytes(const lsm_route_params* p) {
     using namespace lsm;
-    return check(p, false) == LSM_OK ? plan_space(int64_t(p->n) * p->top_k, p->E) + 256 : 0;
+    return check(p, false) == LSM_OK ? plan_space(int64_t(p->n) * p->top_k, p->E) : 0;
 }
 int lsm_moe_plan(const lsm_route_params* p, const int32_t* chosen, int32_t* offsets, int32_t* order, int32_t* place,
                  void* workspace, size_t workspace_bytes, void* stream) {
@@ -345,7 +345,8 @@ int lsm_moe_plan(const lsm_route_params* p, const int32_t* chosen, int32_t* offs
     if (rc != LSM_OK) return rc;
     if (!chosen || !offsets || !order || !place) return LSM_ERR_NULL;
     if (misaligned(chosen) || misaligned(offsets) || misaligned(order) || misaligned(place) || misaligned(workspace)) return LSM_ERR_ALIGN;
-    if (!workspace || workspace_bytes < lsm_moe_plan_workspace_bytes(p)) return LSM_ERR_WORKSPACE;
+    const size_t need = lsm_moe_plan_workspace_bytes(p);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return LSM_ERR_WORKSPACE;
     return enqueue_plan(chosen, int64_t(p->n) * p->top_k, p->E, p->E, offsets, order, place, static_cast<int32_t*>(workspace),
                         static_cast<hipStream_t>(stream)) ? LSM_OK : LSM_ERR_LAUNCH;
 }

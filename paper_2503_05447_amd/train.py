@@ -10,9 +10,8 @@ from operator import index
 
 import torch
 
-from .binding import LsmError, _alloc_on, _ptr, _stream_handle, library
-from .binding import _check as _check_dense
-from .block import _dtype, _workspace as _any_workspace
+from .binding import LsmError, _alloc_on, _ptr, _raw_stream_calls, _stream_handle, library
+from .block import _dtype
 
 
 class _RouteParams(ctypes.Structure):
@@ -27,6 +26,11 @@ class _ExpertsParams(ctypes.Structure):
 class _VocabParams(ctypes.Structure):
     _fields_ = ([("struct_size", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in ("n", "D", "V", "K", "dtype")]
                 + [("temperature", ctypes.c_float), ("reserved", ctypes.c_int32), ("x_stride", ctypes.c_int64)])
+
+
+def _current_device():
+    device = _raw_stream_calls()[1]
+    return device() if device is not None else torch.cuda.current_device()
 
 
 # Parameter blocks by reference, kept by the numbers in them (sizes only, no pointers), and the workspaces they ask for.
@@ -48,30 +52,41 @@ def _vocab_params(*sizes):
     return p, library().lsm_vocab_loss_workspace_bytes(p), library().lsm_vocab_loss_bwd_workspace_bytes(p)
 
 
-def _here(t, name):
-    """The launches go to the current device: a tensor of another one is refused."""
-    if t.is_cuda and t.device.index is not None and t.device.index != torch.cuda.current_device():
-        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+def _device(t, name):
+    """Number of the device that a call's first tensor is on; the launches go to the current one."""
+    if not t.is_cuda:
+        raise ValueError("%s: need a device tensor, got one on %s" % (name, t.device))
+    dev, current = t.get_device(), _current_device()
+    if dev != current and dev >= 0:
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, dev, current))
+    return dev
 
 
-def _check(t, shape, dtype, name):
-    _check_dense(t, shape, dtype, name)
-    if t is not None:
-        _here(t, name)
+def _check(t, shape, dtype, dev, name):
+    """A call's marshalling is most of its time for a few tokens: what is asked is asked in one line."""
+    if t is not None and (t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous()):
+        raise ValueError("%s: need a contiguous tensor %s of %s on device %d, got %s %s on %s"
+                         % (name, tuple(shape), dtype, dev, tuple(t.shape), t.dtype, t.device))
 
 
 def _workspace(workspace, need, like):
-    if workspace is not None:
-        _here(workspace, "workspace")
-    return _any_workspace(workspace, need, like)
+    """The caller's workspace, or a new one beside `like` (None where none is needed)."""
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
+    if workspace.get_device() != like.get_device() or not workspace.is_contiguous():
+        raise ValueError("workspace: need a contiguous tensor on %s, got one on %s" % (like.device, workspace.device))
+    return workspace
 
 
-def _rows(t, name):
-    """Elements between the rows of a [n, D] device tensor that is dense along D."""
-    if t.dim() != 2 or not t.is_cuda or t.stride(1) != 1 and t.shape[1] != 1:
-        raise ValueError("%s: need a [n,D] device tensor, dense along D, got %s with strides %s on %s"
-                         % (name, tuple(t.shape), t.stride(), t.device))
-    _here(t, name)
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _rows(t, dev, name):
+    """Elements between the rows of a [n, D] tensor that is dense along D."""
+    if t.dim() != 2 or t.get_device() != dev or t.stride(1) != 1 and t.shape[1] != 1:
+        raise ValueError("%s: need a [n,D] tensor, dense along D, on device %d, got %s with strides %s on %s"
+                         % (name, dev, tuple(t.shape), t.stride(), t.device))
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
@@ -90,11 +105,11 @@ def lsm_moe_route(logits, top_k, renormalise=True, stream=None):
         raise ValueError("logits: need [n,E], got %s" % (tuple(logits.shape),))
     n, E = logits.shape
     dt, k = _dtype(logits, "logits"), index(top_k)
-    _check(logits, (n, E), logits.dtype, "logits")
+    _check(logits, (n, E), logits.dtype, _device(logits, "logits"), "logits")
     p, _ = _route_params(n, E, k, dt, 1 if renormalise else 0)
     with _alloc_on(stream):
         weights = torch.empty((n, max(k, 0)), dtype=torch.float32, device=logits.device)
-        chosen = torch.empty((n, max(k, 0)), dtype=torch.int32, device=logits.device)
+        chosen = torch.empty_like(weights, dtype=torch.int32)
     _done(library().lsm_moe_route(p, _ptr(logits), _ptr(weights), _ptr(chosen), _stream_handle(stream)), "lsm_moe_route")
     return weights, chosen
 
@@ -107,9 +122,10 @@ def lsm_moe_route_bwd(logits, chosen, d_weights, renormalise=True, stream=None):
     n, E = logits.shape
     k = chosen.shape[1]
     dt = _dtype(logits, "logits")
-    _check(logits, (n, E), logits.dtype, "logits")
-    _check(chosen, (n, k), torch.int32, "chosen")
-    _check(d_weights, (n, k), torch.float32, "d_weights")
+    dev = _device(logits, "logits")
+    _check(logits, (n, E), logits.dtype, dev, "logits")
+    _check(chosen, (n, k), torch.int32, dev, "chosen")
+    _check(d_weights, (n, k), torch.float32, dev, "d_weights")
     p, _ = _route_params(n, E, k, dt, 1 if renormalise else 0)
     with _alloc_on(stream):
         d_logits = torch.empty_like(logits)
@@ -127,14 +143,14 @@ def lsm_moe_plan(chosen, E, workspace=None, stream=None):
         raise ValueError("chosen: need [n,top_k], got %s" % (tuple(chosen.shape),))
     n, k = chosen.shape
     E = index(E)
-    _check(chosen, (n, k), torch.int32, "chosen")
+    _check(chosen, (n, k), torch.int32, _device(chosen, "chosen"), "chosen")
     p, need = _route_params(n, E, k, 0, 0)
     with _alloc_on(stream):
         workspace = _workspace(workspace, need, chosen)
         offsets = torch.empty(max(E, 0) + 1, dtype=torch.int32, device=chosen.device)
         order = torch.empty(n * k, dtype=torch.int32, device=chosen.device)
         place = torch.empty_like(chosen)
-    _done(library().lsm_moe_plan(p, _ptr(chosen), _ptr(offsets), _ptr(order), _ptr(place), _ptr(workspace), workspace.numel(),
+    _done(library().lsm_moe_plan(p, _ptr(chosen), _ptr(offsets), _ptr(order), _ptr(place), _ptr(workspace), _bytes(workspace),
                                  _stream_handle(stream)), "lsm_moe_plan")
     return offsets, order, place
 
@@ -148,16 +164,17 @@ def _experts(x, weights, plan, w_gate_up, w_down, d_y):
     k = weights.shape[1]
     dt = _dtype(x, "x")
     offsets, order, place = plan
-    _check(weights, (n, k), torch.float32, "weights")
-    _check(offsets, (E + 1,), torch.int32, "offsets")
-    _check(order, (n * k,), torch.int32, "order")
-    _check(place, (n, k), torch.int32, "place")
-    _check(w_gate_up, (E, 2 * F, D), x.dtype, "w_gate_up")
-    _check(w_down, (E, D, F), x.dtype, "w_down")
-    stride = _rows(x, "x")
+    dev, dtype = _device(x, "x"), x.dtype
+    _check(weights, (n, k), torch.float32, dev, "weights")
+    _check(offsets, (E + 1,), torch.int32, dev, "offsets")
+    _check(order, (n * k,), torch.int32, dev, "order")
+    _check(place, (n, k), torch.int32, dev, "place")
+    _check(w_gate_up, (E, 2 * F, D), dtype, dev, "w_gate_up")
+    _check(w_down, (E, D, F), dtype, dev, "w_down")
+    stride = _rows(x, dev, "x")
     if d_y is not None and (d_y.dtype != x.dtype or d_y.shape != x.shape):
         raise ValueError("d_y: need %s %s, got %s %s" % (tuple(x.shape), x.dtype, tuple(d_y.shape), d_y.dtype))
-    return _experts_params(n, D, F, E, k, dt, 0, stride, D if d_y is None else _rows(d_y, "d_y"))
+    return _experts_params(n, D, F, E, k, dt, 0, stride, D if d_y is None else _rows(d_y, dev, "d_y"))
 
 
 def lsm_moe_experts(x, weights, plan, w_gate_up, w_down, residual=None, y=None, workspace=None, stream=None):
@@ -168,15 +185,16 @@ def lsm_moe_experts(x, weights, plan, w_gate_up, w_down, residual=None, y=None, 
     w_gate_up [E,2F,D] (F rows of the gate, F rows of the factor), w_down [E,D,F], residual [n,D] or None of x's type; D and F
     multiples of 8, E at most 256, top_k at most 16."""
     p, need, _ = _experts(x, weights, plan, w_gate_up, w_down, None)
-    _check(residual, x.shape, x.dtype, "residual")
+    dev = x.get_device()
+    _check(residual, x.shape, x.dtype, dev, "residual")
     with _alloc_on(stream):
         workspace = _workspace(workspace, need, x)
         if y is None:
             y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         else:
-            _check(y, x.shape, x.dtype, "y")
+            _check(y, x.shape, x.dtype, dev, "y")
     _done(library().lsm_moe_experts(p, _ptr(x), _ptr(weights), *map(_ptr, plan), _ptr(w_gate_up), _ptr(w_down), _ptr(residual), _ptr(y),
-                                    _ptr(workspace), workspace.numel(), _stream_handle(stream)), "lsm_moe_experts")
+                                    _ptr(workspace), _bytes(workspace), _stream_handle(stream)), "lsm_moe_experts")
     return y
 
 
@@ -193,7 +211,7 @@ def lsm_moe_experts_bwd(x, weights, plan, w_gate_up, w_down, d_y, weight_grads=T
         d_weights = torch.empty_like(weights)
         d_gate_up, d_down = (torch.empty_like(w_gate_up), torch.empty_like(w_down)) if weight_grads else (None, None)
     _done(library().lsm_moe_experts_bwd(p, _ptr(x), _ptr(weights), *map(_ptr, plan), _ptr(w_gate_up), _ptr(w_down), _ptr(d_y), _ptr(dx),
-                                        _ptr(d_weights), _ptr(d_gate_up), _ptr(d_down), _ptr(workspace), workspace.numel(),
+                                        _ptr(d_weights), _ptr(d_gate_up), _ptr(d_down), _ptr(workspace), _bytes(workspace),
                                         _stream_handle(stream)), "lsm_moe_experts_bwd")
     return dict(dx=dx, d_weights=d_weights, d_w_gate_up=d_gate_up, d_w_down=d_down)
 
@@ -204,19 +222,20 @@ def _vocab(x, w, index_, teacher, temperature):
     n, D = x.shape
     V = w.shape[0]
     dt = _dtype(x, "x")
-    _check(w, (V, D), x.dtype, "w")
+    dev = _device(x, "x")
+    _check(w, (V, D), x.dtype, dev, "w")
     K = 0
     if teacher is None:
-        _check(index_, (n,), torch.int32, "target")
+        _check(index_, (n,), torch.int32, dev, "target")
     else:
         if index_.dim() != 2:
             raise ValueError("index: need [n,K], got %s" % (tuple(index_.shape),))
         K = index_.shape[1]
         if K == 0:
             raise ValueError("index: need at least one entry a token")
-        _check(index_, (n, K), torch.int32, "index")
-        _check(teacher, (n, K), torch.float32, "teacher")
-    return _vocab_params(n, D, V, K, dt, float(temperature), 0, _rows(x, "x"))
+        _check(index_, (n, K), torch.int32, dev, "index")
+        _check(teacher, (n, K), torch.float32, dev, "teacher")
+    return _vocab_params(n, D, V, K, dt, float(temperature), 0, _rows(x, dev, "x"))
 
 
 def _vocab_fwd(x, w, index_, teacher, temperature, workspace, stream, name):
@@ -226,20 +245,20 @@ def _vocab_fwd(x, w, index_, teacher, temperature, workspace, stream, name):
         loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
         lse = torch.empty_like(loss)
     _done(library().lsm_vocab_loss(p, _ptr(x), _ptr(w), _ptr(index_), _ptr(teacher), _ptr(loss), _ptr(lse), _ptr(workspace),
-                                   workspace.numel(), _stream_handle(stream)), name)
+                                   _bytes(workspace), _stream_handle(stream)), name)
     return loss, lse
 
 
 def _vocab_bwd(x, w, index_, teacher, lse, d_loss, temperature, weight_grad, workspace, stream, name):
     p, _, need = _vocab(x, w, index_, teacher, temperature)
-    _check(lse, (x.shape[0],), torch.float32, "lse")
-    _check(d_loss, (x.shape[0],), torch.float32, "d_loss")
+    _check(lse, (x.shape[0],), torch.float32, x.get_device(), "lse")
+    _check(d_loss, (x.shape[0],), torch.float32, x.get_device(), "d_loss")
     with _alloc_on(stream):
         workspace = _workspace(workspace, need, x)
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         dw = torch.empty_like(w) if weight_grad else None
     _done(library().lsm_vocab_loss_bwd(p, _ptr(x), _ptr(w), _ptr(index_), _ptr(teacher), _ptr(lse), _ptr(d_loss), _ptr(dx), _ptr(dw),
-                                       _ptr(workspace), workspace.numel(), _stream_handle(stream)), name)
+                                       _ptr(workspace), _bytes(workspace), _stream_handle(stream)), name)
     return dict(dx=dx, dw=dw)
 
 
