@@ -111,6 +111,15 @@ def test_values_and_gradients(dtype, n, D, F, E, k):
     check(make(n, D, F, E, k, dtype, seed=n + D, residual=n % 2 == 0))
 
 
+# sizes with which each of the seven tiles is the one chosen for each of the products, in either type
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,D,F,E,k", [(18, 264, 208, 64, 3), (2090, 136, 96, 64, 2), (11292, 40, 72, 8, 2), (7222, 40, 256, 33, 1),
+                                       (15443, 192, 40, 8, 2), (2647, 728, 48, 5, 2), (12, 168, 1048, 33, 2), (12665, 72, 80, 33, 3),
+                                       (154, 888, 40, 64, 1), (18941, 136, 40, 8, 2), (1200, 1032, 520, 4, 2), (6000, 264, 392, 3, 1)])
+def test_every_tile(dtype, n, D, F, E, k):
+    check(make(n, D, F, E, k, dtype, seed=n + F, skew=0.5, dropped=0.1))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_longer_list_than_is_held_at_a_time(dtype):
     """Weight gradients over 5000 pairs of an expert: the list of rows (2048 at a time) is filled again and again."""

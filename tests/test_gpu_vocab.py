@@ -114,6 +114,15 @@ def test_distillation(dtype, n, D, V, K):
     check(make(n, D, V, K, dtype, seed=n + V, left_out=0.2 if n > 3 else 0.0), tau=2.0 if n % 2 else 1.0)
 
 
+# sizes with which each of the seven tiles is the one chosen for each of the products, in either type
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [0, 70])
+@pytest.mark.parametrize("n,D,V", [(1, 24, 18658), (790, 24, 1331), (8195, 24, 452), (37, 24, 64137), (8173, 24, 1028), (2, 136, 54471), (1, 24, 2580),
+                                   (213, 24, 541), (82, 24, 2750), (1, 152, 2729), (18331, 464, 51), (1000, 520, 5003), (2500, 264, 3001)])
+def test_every_tile(dtype, K, n, D, V):
+    check(make(n, D, V, K, dtype, seed=n + V, left_out=0.1 if n > 3 else 0.0))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_temperatures(dtype):
     for tau in (0.5, 3.0):
