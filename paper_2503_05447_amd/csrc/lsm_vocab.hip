@@ -26,7 +26,9 @@ struct VocabArgs {
     float *loss, *lse;
     void *grad, *dx, *dw;     // gradient [n][piece]
     float* part;              // [shares][n][D]
-    int n, D, V, K, parts, piece, v0, shares;
+    int n, D, V, K, parts;
+    int v0, width, piece;     // the piece: its first column, how many, and how many the gradient's rows hold (a multiple of 256)
+    int shares, begun;        // of the piece's columns for dx; how many of them have a sum from pieces before
     uint32_t x_bytes;
     float scale;              // 1 / temperature
 };
@@ -291,7 +293,7 @@ template <typename T, bool TEACHER>
 __global__ __launch_bounds__(T::THREADS) void k_grad(VocabArgs a) {
     typedef typename T::TIO TIO;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
-    const int end = min(a.V, a.v0 + a.piece);
+    const int end = a.v0 + a.width;
     logit_tiles<T>(shared, a, a.v0, end, [&](const T& t, int rows, int r0, int c, f32x4 (&acc)[T::TC][T::TR]) {
         const int column = c * T::BC + t.wc * T::TC * 16, first = a.v0 + column, mine = first + 4 * (t.lane >> 4);
         const float log2_scale = a.scale * kLog2e;
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(VocabArgs a) {
     typedef typename T::TIO TIO;
     constexpr int EL = int(sizeof(TIO));
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
-    const int width = min(a.V - a.v0, a.piece), rows = rows_of(a);
+    const int width = a.width, rows = rows_of(a);
     const int rt = (width + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, id = number_of_tile(rt * ct);
     if (id < 0) return;
     int r, c;
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     typedef typename T::TIO TIO;
     constexpr int EL = int(sizeof(TIO)), STEP = kStepBytes / EL;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
-    const int width = min(a.V - a.v0, a.piece), rows = rows_of(a);
+    const int width = a.width, rows = rows_of(a);
     const int rt = (rows + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, id = number_of_tile(rt * ct * a.shares);
     if (id < 0) return;
     const int share = id / (rt * ct);
@@ -396,7 +398,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     const int c0 = c * T::BC + t.wc * T::TC * 16;
     const auto line = [&](int q) { return r0 + q < rows ? a.part + (size_t(share) * a.n + r0 + q) * a.D + c0 : nullptr; };
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        if (a.v0 == 0) t.template store<T::TC, float>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
+        if (share >= a.begun) t.template store<T::TC, float>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
         else t.template store<T::TC, float, true>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
     }
 }
@@ -411,7 +413,7 @@ __global__ __launch_bounds__(256) void k_dx_join(VocabArgs a) {
     float s[E];
     _Pragma("unroll") for (int e = 0; e < E; ++e) s[e] = 0.f;
     if (at >= 0 && at < a.n)
-        for (int q = 0; q < a.shares; ++q) {
+        for (int q = 0; q < a.begun; ++q) {
             const f32x4* z = reinterpret_cast<const f32x4*>(a.part + (size_t(q) * a.n + at) * a.D + d);
             _Pragma("unroll") for (int i = 0; i < E / 4; ++i)
                 _Pragma("unroll") for (int e = 0; e < 4; ++e) s[4 * i + e] += z[i][e];
@@ -435,41 +437,62 @@ int check(const lsm_vocab_params* p) {
     if (p->x_stride % 8) return LSM_ERR_ALIGN;
     return LSM_OK;
 }
-// Tiles of the logits, of their gradient, of dw and dx; the vocabulary of a piece and its shares for dx.
-struct Plan { int logits, grad, dw, dx, piece, shares; };
-Plan plan_of(const lsm_vocab_params& p) {
+int logits_tile(const lsm_vocab_params& p) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
-    Plan q{};
-    q.logits = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.V, t.cols); }, f32 ? 0x7e : 0x7f);
-    int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256 * 256;
-    if (most < 256) most = 256;
-    const int pieces = up(p.V, most);
-    q.piece = up(up(p.V, pieces), 256) * 256;
-    q.grad = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(q.piece, t.cols); }, f32 ? 0x7e : 0x7f);
-    q.dw = pick_tile(f32, p.n, [&](const TileSize& t) { return int64_t(up(q.piece, t.rows)) * up(p.D, t.cols); }, (f32 ? 0 : 1 << 0) | 1 << 2 | 1 << 5);
-    // dx: shares of a piece's vocabulary, the fewest with which the last round of workgroups is nine tenths full, or the best of some
+    return pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.V, t.cols); }, f32 ? 0x7e : 0x7f);
+}
+// A piece of the vocabulary backward, of the `left` columns from the piece before on: how many, the tiles of the logits' gradient, of dw and dx,
+// and into how many shares dx takes the piece.  dw's products are as long as there are tokens, so that a last round of a few tiles takes
+// as long as a full one: a piece ends with a full round where less than half of the next one would be left, and what is left is a
+// piece with smaller tiles (8191 tokens, 50257 x 2048: dw 1115 -> 920 us).
+struct Piece { int width, grad, dw, dx, shares; };
+Piece piece_of(const lsm_vocab_params& p, int left) {
+    const bool f32 = p.dtype == LSM_DTYPE_F32;
+    const unsigned kinds = f32 ? 0x7e : 0x7f;
+    Piece q{};
+    int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256;  // in tiles of 256 columns
+    if (most < 1) most = 1;
+    int64_t tiles = up(left, 256);
+    if (tiles > most) tiles = most;
+    const int64_t across = up(p.D, 256), round = 256 / across, over = tiles % (round ? round : 1);
+    if (!f32 && round > 1 && tiles > round && 2 * over < round) tiles -= over;
+    q.width = tiles * 256 < left ? int(tiles * 256) : left;
+    q.grad = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(q.width, t.cols); }, kinds);
+    q.dw = pick_tile(f32, p.n, [&](const TileSize& t) { return int64_t(up(q.width, t.rows)) * up(p.D, t.cols); },
+                     (f32 ? 0 : 1 << 0) | 1 << 2 | 1 << 5);
+    // the fewest shares with which the last round of workgroups is nine tenths full, or the best of some
     const auto shares = [&](const TileSize& t) {
-        const int64_t tiles = int64_t(up(p.n, t.rows)) * up(p.D, t.cols), room = 256 * t.at_once;
+        const int64_t n = int64_t(up(p.n, t.rows)) * up(p.D, t.cols), room = 256 * t.at_once;
         double best = 0;
         int least = 1;
-        for (int k = 1; k <= 64 && k * 512 <= q.piece + 511; ++k) {
-            const double full = double(tiles * k) / (double(up(tiles * k, room)) * room);
+        for (int k = 1; k <= 64 && k * 512 <= q.width + 511; ++k) {
+            const double full = double(n * k) / (double(up(n * k, room)) * room);
             if (full > best + 0.02) { best = full; least = k; }
-            if (best >= 0.9 || (k >= 8 && tiles * k >= room)) break;
+            if (best >= 0.9 || (k >= 8 && n * k >= room)) break;
         }
         return least;
     };
     q.dx = pick_tile_of(f32, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.D, t.cols) * shares(t); },
-                     [&](const TileSize& t) { return up(q.piece, shares(t)); }, f32 ? 0x7e : 0x7f);
+                        [&](const TileSize& t) { return up(q.width, shares(t)); }, kinds);
     q.shares = shares(kTiles[q.dx]);
     return q;
+}
+// The most of any piece: columns (whole tiles), shares.
+Piece largest_piece(const lsm_vocab_params& p) {
+    Piece most{};
+    for (int v = 0; v < p.V;) {
+        const Piece q = piece_of(p, p.V - v);
+        if (up(q.width, 256) * 256 > most.width) most.width = up(q.width, 256) * 256;
+        if (q.shares > most.shares) most.shares = q.shares;
+        v += q.width;
+    }
+    return most;
 }
 int parts_of(const lsm_vocab_params& p, int kind) { return up(p.V, kTiles[kind].cols) * kTiles[kind].waves; }
 
 struct Space { size_t offsets, order, place, hist, count, entry, share, entropy, stats, at_entry, grad, part, bytes; };
 Space space(const lsm_vocab_params& p, bool backward) {
     const size_t n = p.n, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4, K = p.K;
-    const Plan q = plan_of(p);
     Space s{};
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
@@ -482,10 +505,11 @@ Space space(const lsm_vocab_params& p, bool backward) {
     s.share = take(K * n * 4);
     s.entropy = take(K ? n * 4 : 0);
     if (!backward) {
-        s.stats = take(size_t(parts_of(p, q.logits)) * n * sizeof(f32x2));
+        s.stats = take(size_t(parts_of(p, logits_tile(p))) * n * sizeof(f32x2));
         s.at_entry = take((K ? K : 1) * n * 4);
     } else {
-        s.grad = take(n * q.piece * el);
+        const Piece q = largest_piece(p);
+        s.grad = take(n * q.width * el);
         s.part = take(size_t(q.shares) * n * p.D * 4);
     }
     s.bytes = at;
@@ -566,29 +590,32 @@ bool launch_dx(const VocabArgs& a, hipStream_t st) {
 
 template <typename TIO>
 bool launch(VocabArgs a, const lsm_vocab_params& p, bool backward, hipStream_t st) {
-    const Plan q = plan_of(p);
 #define LSM_KIND(call, kind)                                                                                     \
     ((kind) == 0 ? call(0) : (kind) == 1 ? call(1) : (kind) == 2 ? call(2) : (kind) == 3 ? call(3) : (kind) == 4 ? call(4) \
                                                                                      : (kind) == 5 ? call(5) : call(6))
 #define LSM_LOGITS(K) launch_logits<TIO, K>(a, st)
-#define LSM_GRAD(K) launch_grad<TIO, K>(a, width, st)
+#define LSM_GRAD(K) launch_grad<TIO, K>(a, q.width, st)
 #define LSM_DX(K) launch_dx<TIO, K>(a, st)
     if (!backward) {
-        a.parts = parts_of(p, q.logits);
-        if (!LSM_KIND(LSM_LOGITS, q.logits)) return false;
+        const int kind = logits_tile(p);
+        a.parts = parts_of(p, kind);
+        if (!LSM_KIND(LSM_LOGITS, kind)) return false;
         ProfScope ps(KID_VOCAB_JOIN, st);
         if (a.n > 1024) hipLaunchKernelGGL(k_join<64>, dim3(up(a.n, 64)), dim3(1024), 0, st, a);
         else hipLaunchKernelGGL(k_join<4>, dim3(up(a.n, 4)), dim3(1024), 0, st, a);
         return launched();
     }
-    a.piece = q.piece;
-    a.shares = q.shares;
-    for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
-        const int width = a.V - a.v0 < a.piece ? a.V - a.v0 : a.piece;
+    for (a.v0 = 0; a.v0 < a.V;) {
+        const Piece q = piece_of(p, a.V - a.v0);
+        a.width = q.width;
+        a.piece = up(q.width, 256) * 256;
+        a.shares = q.shares;
         if (!LSM_KIND(LSM_GRAD, q.grad)) return false;
-        if (a.dw && !(q.dw == 0 ? launch_dw<TIO, 0>(a, width, st) : q.dw == 2 ? launch_dw<TIO, 2>(a, width, st) : launch_dw<TIO, 5>(a, width, st)))
+        if (a.dw && !(q.dw == 0 ? launch_dw<TIO, 0>(a, q.width, st) : q.dw == 2 ? launch_dw<TIO, 2>(a, q.width, st) : launch_dw<TIO, 5>(a, q.width, st)))
             return false;
         if (!LSM_KIND(LSM_DX, q.dx)) return false;
+        if (a.shares > a.begun) a.begun = a.shares;
+        a.v0 += q.width;
     }
     ProfScope ps(KID_VOCAB_JOIN, st);
     hipLaunchKernelGGL((k_dx_join<TIO>), dim3(up(int64_t(a.n) * (a.D / kPiece<TIO>), 256)), dim3(256), 0, st, a);
