@@ -55,10 +55,10 @@ struct Finder {
     }
     // The n-th tile of this workgroup; false: there is none.
     __device__ __forceinline__ bool find(int n, int cols, Where& w) const {
-        const int all = __builtin_amdgcn_readlane(upto, 63) * cols, die = (all + 7) / 8;
+        const int all = min(__builtin_amdgcn_readlane(upto, 63), int(kMostTiles) / cols) * cols, die = (all + 7) / 8;
         const int at = int(blockIdx.x) / 8 + n * (int(gridDim.x) / 8), id = (int(blockIdx.x) % 8) * die + at;
         if (at >= die || id >= all) return false;
-        const int l = lanes(__ballot(upto * cols <= id));
+        const int l = lanes(__ballot(upto <= id / cols));
         int rest = id - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(own, l)) * cols;
         _Pragma("unroll") for (int i = 0; i < 4; ++i) {
             const int t = __builtin_amdgcn_readlane(tiles[i], l);
@@ -354,6 +354,7 @@ __global__ __launch_bounds__(256) void k_sum(ExpertArgs a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
+bool fits(const lsm_experts_params& p, bool backward);
 int check(const lsm_experts_params* p, bool backward) {
     if (!p) return LSM_ERR_NULL;
     if (p->struct_size != sizeof(lsm_experts_params)) return LSM_ERR_SHAPE;
@@ -367,7 +368,7 @@ int check(const lsm_experts_params* p, bool backward) {
         if (s < p->D || s > (int64_t(1) << 31) || p->n * s * el >= int64_t(kBeyond)) return LSM_ERR_SHAPE;
         if (s % 8) return LSM_ERR_ALIGN;
     }
-    return LSM_OK;
+    return fits(*p, backward) ? LSM_OK : LSM_ERR_SHAPE;
 }
 
 // Tiles of the products over pairs, whose rows are ragged, and of the weights' gradients.
@@ -390,13 +391,19 @@ Plan plan_of(const lsm_experts_params& p) {
 int weight_parts(const lsm_experts_params& p, int kind) { return up(p.F, kTiles[kind].cols / 2) * kTiles[kind].waves; }
 int stretch_of(int kind) { return kTiles[kind].cols / kTiles[kind].waves; }
 // The most tiles there can be: every expert's last one may be almost empty.
-unsigned grid_of(const ExpertArgs& a, int rows, int cols) {
-    const int64_t pairs = int64_t(a.n) * a.top_k, tiles = pairs / rows + (pairs < a.E ? pairs : int64_t(a.E));
-    return unsigned((tiles * cols + 7) / 8 * 8);
+int64_t most_tiles(int64_t pairs, int E, int rows, int cols) { return (pairs / rows + (pairs < E ? pairs : int64_t(E))) * cols; }
+bool fits(const lsm_experts_params& p, bool backward) {
+    const Plan q = plan_of(p);
+    const auto rows = [&](int kind, int cols, int parts) {
+        return most_tiles(int64_t(p.n) * p.top_k, p.E, kTiles[kind].rows, up(cols, kTiles[kind].cols / parts)) < kMostTiles;
+    };
+    const auto square = [&](int kind, int r, int c) { return int64_t(p.E) * up(r, kTiles[kind].rows) * up(c, kTiles[kind].cols) < kMostTiles; };
+    if (!backward) return rows(q.up, p.F, 2) && rows(q.down, p.D, 1);
+    return rows(q.hidden, p.F, 2) && rows(q.dx, p.D, 1) && square(q.dw1, 2 * p.F, p.D) && square(q.dw2, p.D, p.F);
 }
 template <typename T>
 unsigned grid_of(const ExpertArgs& a, int cols) {
-    const unsigned all = grid_of(a, T::BR, cols);
+    const unsigned all = unsigned((most_tiles(int64_t(a.n) * a.top_k, a.E, T::BR, cols) + 7) / 8 * 8);
     return T::FOLLOWED && all > 256 ? 256 : all;  // one for each compute unit
 }
 

@@ -67,8 +67,6 @@ __device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, f32x4 c
     return c;
 }
 
-typedef __attribute__((address_space(3))) char* lds_t;
-
 // N rows of an operand and a step's k of each, as a workgroup of WAVES waves brings them to LDS and reads them.
 template <typename TIO, Layout L, int N, int WAVES, bool LISTED>
 struct Operand {

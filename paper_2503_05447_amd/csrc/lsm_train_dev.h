@@ -18,6 +18,7 @@ struct TileSize { int rows, cols, waves, at_once; };
 constexpr TileSize kTiles[] = {{256, 256, 2, 1}, {128, 256, 4, 1}, {128, 128, 2, 2}, {64, 256, 4, 2}, {32, 256, 4, 2}, {64, 64, 2, 4}, {32, 128, 4, 4}};
 constexpr int kTileKinds = int(sizeof(kTiles) / sizeof(kTiles[0]));
 constexpr int kTileStepBytes = 64;  // of k, a row and step
+constexpr int64_t kMostTiles = kAxisThreads / 512;  // of a launch, a workgroup of at most 512 threads each
 inline int up(int64_t x, int64_t to) { return int((x + to - 1) / to); }
 
 // The tile with which a product takes least, of those in `kinds` (a bit each): tiles(size) of them, length(size) long.  In microseconds, as

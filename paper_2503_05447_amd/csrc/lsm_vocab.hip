@@ -117,7 +117,7 @@ struct Entries {
         }
     }
     // found(e, column - first) for those of columns first .. first + width, the lanes' first ones together, then their second ones: what they
-    // load for it is waited for a few times and not for every place (4096 tokens, 64 entries: 385 -> 300 us for the gradient).
+    // load for it is waited for a few times and not for every place (4096 tokens, 64 entries: 385 -> 310 us for the gradient).
     template <typename Found>
     __device__ __forceinline__ void find(int e0, int first, int width, int lane, Found found) const {
         uint32_t hits = 0;
@@ -424,7 +424,8 @@ __global__ __launch_bounds__(256) void k_dx_join(VocabArgs a) {
 // ---- host ------------------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of the logits' gradient at a time: what the memory-side cache holds
 
-int check(const lsm_vocab_params* p) {
+bool fits(const lsm_vocab_params& p, bool backward);
+int check(const lsm_vocab_params* p, bool backward) {
     if (!p) return LSM_ERR_NULL;
     if (p->struct_size != sizeof(lsm_vocab_params)) return LSM_ERR_SHAPE;
     if (p->n < 1 || p->D < 1 || p->V < 1 || p->K < 0 || p->n > kMostPairs || p->V > (1 << 24)) return LSM_ERR_SHAPE;
@@ -435,7 +436,7 @@ int check(const lsm_vocab_params* p) {
     const int64_t el = p->dtype == LSM_DTYPE_BF16 ? 2 : 4;
     if (p->x_stride < p->D || p->x_stride > (int64_t(1) << 31) || p->n * p->x_stride * el >= int64_t(kBeyond)) return LSM_ERR_SHAPE;
     if (p->x_stride % 8) return LSM_ERR_ALIGN;
-    return LSM_OK;
+    return fits(*p, backward) ? LSM_OK : LSM_ERR_SHAPE;
 }
 int logits_tile(const lsm_vocab_params& p) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
@@ -444,8 +445,8 @@ int logits_tile(const lsm_vocab_params& p) {
 // A piece of the vocabulary backward, of the `left` columns from the piece before on: how many, the tiles of the logits' gradient, of dw and dx,
 // and into how many shares dx takes the piece.  dw's products are as long as there are tokens, so that a last round of a few tiles takes
 // as long as a full one: a piece ends with a full round where less than half of the next one would be left, and what is left is a
-// piece with smaller tiles (8191 tokens, 50257 x 2048: dw 1115 -> 920 us).
-struct Piece { int width, grad, dw, dx, shares; };
+// piece with smaller tiles (8191 tokens, 50257 x 2048: dw 1140 -> 990 us).
+struct Piece { int width, grad, dw, dx, shares; int64_t tiles; };  // tiles: the most of its launches
 Piece piece_of(const lsm_vocab_params& p, int left) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
     const unsigned kinds = f32 ? 0x7e : 0x7f;
@@ -475,18 +476,27 @@ Piece piece_of(const lsm_vocab_params& p, int left) {
     q.dx = pick_tile_of(f32, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.D, t.cols) * shares(t); },
                         [&](const TileSize& t) { return up(q.width, shares(t)); }, kinds);
     q.shares = shares(kTiles[q.dx]);
+    const auto tiles_of = [](int rows, int cols, int kind) { return int64_t(up(rows, kTiles[kind].rows)) * up(cols, kTiles[kind].cols); };
+    for (const int64_t n : {tiles_of(p.n, q.width, q.grad), tiles_of(q.width, p.D, q.dw), tiles_of(p.n, p.D, q.dx) * q.shares})
+        if (n > q.tiles) q.tiles = n;
     return q;
 }
-// The most of any piece: columns (whole tiles), shares.
+// The most of any piece: columns (whole tiles), shares, tiles.
 Piece largest_piece(const lsm_vocab_params& p) {
     Piece most{};
     for (int v = 0; v < p.V;) {
         const Piece q = piece_of(p, p.V - v);
         if (up(q.width, 256) * 256 > most.width) most.width = up(q.width, 256) * 256;
         if (q.shares > most.shares) most.shares = q.shares;
+        if (q.tiles > most.tiles) most.tiles = q.tiles;
         v += q.width;
     }
     return most;
+}
+bool fits(const lsm_vocab_params& p, bool backward) {
+    if (backward) return largest_piece(p).tiles < kMostTiles;
+    const TileSize& t = kTiles[logits_tile(p)];
+    return int64_t(up(p.n, t.rows)) * up(p.V, t.cols) < kMostTiles;
 }
 int parts_of(const lsm_vocab_params& p, int kind) { return up(p.V, kTiles[kind].cols) * kTiles[kind].waves; }
 
@@ -632,17 +642,17 @@ extern "C" {
 
 size_t lsm_vocab_loss_workspace_bytes(const lsm_vocab_params* p) {
     using namespace lsm;
-    return check(p) == LSM_OK ? space(*p, false).bytes : 0;
+    return check(p, false) == LSM_OK ? space(*p, false).bytes : 0;
 }
 size_t lsm_vocab_loss_bwd_workspace_bytes(const lsm_vocab_params* p) {
     using namespace lsm;
-    return check(p) == LSM_OK ? space(*p, true).bytes : 0;
+    return check(p, true) == LSM_OK ? space(*p, true).bytes : 0;
 }
 
 int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,
                    float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     using namespace lsm;
-    const int rc = check(p);
+    const int rc = check(p, false);
     if (rc != LSM_OK) return rc;
     if (!x || !w || !index || !teacher != !p->K || !loss || !lse) return LSM_ERR_NULL;
     if (misaligned(x) || misaligned(w) || misaligned(index) || misaligned(teacher) || misaligned(loss) || misaligned(lse) || misaligned(workspace))
@@ -662,7 +672,7 @@ int lsm_vocab_loss_bwd(const lsm_vocab_params* p, const void* x, const void* w, 
                        const float* lse, const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes,
                        void* stream) {
     using namespace lsm;
-    const int rc = check(p);
+    const int rc = check(p, true);
     if (rc != LSM_OK) return rc;
     if (!x || !w || !index || !teacher != !p->K || !lse || !d_loss || !dx) return LSM_ERR_NULL;
     if (misaligned(x) || misaligned(w) || misaligned(index) || misaligned(teacher) || misaligned(lse) || misaligned(d_loss) || misaligned(dx) ||

@@ -110,6 +110,21 @@ def test_losses_refuse_bad_sizes():
         assert size(ctypes.byref(vocab(D=60))) == 0 and size(ctypes.byref(vocab(n=100000, V=131071))) > 0
 
 
+def test_products_that_no_launch_holds_are_refused():
+    """2^32 threads are the most of a launch, 512 the most of a tile: 2^23 tiles or more are refused before anything runs."""
+    many = experts(n=1 << 24, top_k=1, D=8, F=65536)             # 65536 x 512 tiles of the hidden layer
+    assert call("lsm_moe_experts", many, 10) == SHAPE and call("lsm_moe_experts_bwd", many, 13) == SHAPE
+    wide = experts(n=256, top_k=1, E=256, D=32768, F=32760, dtype=1)     # the weights' gradients alone
+    assert call("lsm_moe_experts_bwd", wide, 13) == SHAPE
+    assert call("lsm_vocab_loss", vocab(n=1 << 24, D=8, V=1 << 24, K=0, dtype=1), 7, a3=None) == SHAPE
+    assert call("lsm_vocab_loss_bwd", vocab(n=1, D=65536, V=1 << 24, K=0, dtype=1), 9, a3=None) == SHAPE
+    lib = pkg.library()
+    for size, p in ((lib.lsm_moe_experts_workspace_bytes, many), (lib.lsm_moe_experts_bwd_workspace_bytes, wide)):
+        assert size(ctypes.byref(p)) == 0
+    large = experts(n=1 << 19, top_k=8, E=64, D=2048, F=1024, dtype=1)
+    assert lib.lsm_moe_experts_workspace_bytes(ctypes.byref(large)) > 0 and lib.lsm_moe_experts_bwd_workspace_bytes(ctypes.byref(large)) > 0
+
+
 def test_the_logits_are_never_kept():
     """What a backward call asks for is a piece of the vocabulary, whatever the vocabulary's size."""
     size = pkg.library().lsm_vocab_loss_bwd_workspace_bytes
