@@ -20,17 +20,21 @@ struct ExpertArgs {
     const int32_t *offsets, *order, *place;
     void *y, *d_w_gate_up, *d_w_down;
     float* d_weights;
-    void *h, *da;           // [pairs][F]: activations (backward: times their weight); [pairs][2 F]
+    void *h, *da;         // [pairs][F]: activations (backward: times their weight); [pairs][2 F]; rows from line to line
     void* part;           // [pairs][D]: fp32, or with bf16 elements fp16 times part_scale
     float *part_scale, *weight_part;  // [stretches of D][pairs]; [tiles of F][pairs]
     int n, D, F, E, top_k, parts, stretch;
-    uint32_t x_bytes, dy_bytes;  // between rows
+    uint32_t x_bytes, dy_bytes, h_bytes, da_bytes;  // between rows
 };
 
 // What the plan says, kept inside the buffers whatever stands there.
 __device__ __forceinline__ int offset_of(const ExpertArgs& a, int e) { return min(max(a.offsets[e], 0), a.n * a.top_k); }
 __device__ __forceinline__ uint32_t pair_of(const ExpertArgs& a, int at) { return min(uint32_t(a.order[at]), uint32_t(a.n * a.top_k - 1)); }
 __device__ __forceinline__ uint32_t token_of(const ExpertArgs& a, int at) { return pair_of(a, at) / uint32_t(a.top_k); }
+
+template <typename TIO> __device__ __forceinline__ TIO* row_of(void* rows, int at, uint32_t bytes) {
+    return reinterpret_cast<TIO*>(static_cast<char*>(rows) + size_t(at) * bytes);
+}
 
 struct Where { int e, first, count, r, c; };  // expert, its first place and its pairs, the tile's number along rows and columns
 
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
                 },
                 [&](int r) {
                     const int at = w.r * T::BR + r;
-                    return at < w.count ? static_cast<TIO*>(a.h) + size_t(w.first + at) * a.F + f0 : nullptr;
+                    return at < w.count ? row_of<TIO>(a.h, w.first + at, a.h_bytes) + f0 : nullptr;
                 });
         if (!more) return;
         t.go_on();
@@ -202,7 +206,7 @@ __global__ __launch_bounds__(T::THREADS) void k_down(ExpertArgs a) {
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
     const uint32_t bytes = uint32_t(a.F) * uint32_t(sizeof(TIO));
     part_tiles<T>(shared, a, a.F, [&](const T& t, typename T::C& c, typename T::R& r, const Where& w) {
-        start_pairs(t, r, a.h, w, bytes);
+        start_pairs(t, r, a.h, w, a.h_bytes);
         c.start_rows(static_cast<const TIO*>(a.w_down) + size_t(w.e) * a.D * a.F, t.wave, t.lane, [&](int q) {
             const int d = w.c * T::BC + q;
             return d < a.D ? uint32_t(d) * bytes : kBeyond;
@@ -215,7 +219,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(ExpertArgs a) {
     typedef typename T::TIO TIO;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
     part_tiles<T>(shared, a, 2 * a.F, [&](const T& t, typename T::C& c, typename T::R& r, const Where& w) {
-        start_pairs(t, r, a.da, w, 2 * uint32_t(a.F) * uint32_t(sizeof(TIO)));
+        start_pairs(t, r, a.da, w, a.da_bytes);
         c.start_cols(static_cast<const TIO*>(a.w_gate_up) + size_t(w.e) * 2 * a.F * a.D, a.D * int(sizeof(TIO)), w.c * T::BC, a.D, t.wave, t.lane, 0);
     });
 }
@@ -262,15 +266,15 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
             }
         along = T::row_sum(along);
         if (t.lane < 16 && at < w.count) a.weight_part[size_t(w.c * T::WC + t.wc) * (size_t(a.n) * a.top_k) + w.first + at] = along;
-        const auto line = [&](void* base, int length, int shift) {
+        const auto line = [&](void* base, uint32_t bytes, int shift) {
             return [=, &w](int r) {
                 const int q = w.r * T::BR + r;
-                return q < w.count ? static_cast<TIO*>(base) + size_t(w.first + q) * length + shift + f0 : nullptr;
+                return q < w.count ? row_of<TIO>(base, w.first + q, bytes) + shift + f0 : nullptr;
             };
         };
         _Pragma("unroll") for (int half = 0; half < 2; ++half)
-            t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return gu[half * T::TC + i][j]; }, line(a.da, 2 * a.F, half * a.F));
-        t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return tt[i][j]; }, line(a.h, a.F, 0));
+            t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return gu[half * T::TC + i][j]; }, line(a.da, a.da_bytes, half * a.F));
+        t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return tt[i][j]; }, line(a.h, a.h_bytes, 0));
     }
 }
 
@@ -289,9 +293,9 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(ExpertArgs a, int row_tiles, 
     T t(shared);
     if (DOWN) {
         t.r.start_cols(a.d_y, int(a.dy_bytes), r0 * T::BR, rows, t.wave, t.lane, t.list_at());
-        t.c.start_cols(static_cast<const TIO*>(a.h) + size_t(first) * a.F, a.F * EL, c * T::BC, cols, t.wave, t.lane, 0);
+        t.c.start_cols(row_of<TIO>(a.h, first, a.h_bytes), int(a.h_bytes), c * T::BC, cols, t.wave, t.lane, 0);
     } else {
-        t.r.start_cols(static_cast<const TIO*>(a.da) + size_t(first) * 2 * a.F, 2 * a.F * EL, r0 * T::BR, rows, t.wave, t.lane, 0);
+        t.r.start_cols(row_of<TIO>(a.da, first, a.da_bytes), int(a.da_bytes), r0 * T::BR, rows, t.wave, t.lane, 0);
         t.c.start_cols(a.x, int(a.x_bytes), c * T::BC, cols, t.wave, t.lane, t.list_at());
     }
     f32x4 acc[T::TC][T::TR];
@@ -407,16 +411,20 @@ unsigned grid_of(const ExpertArgs& a, int cols) {
     return T::FOLLOWED && all > 256 ? 256 : all;  // one for each compute unit
 }
 
+// Rows of own buffers begin with a line of the caches: a step's 64 bytes of a row are in one line, where else they lie across two if the
+// width is not whole lines (2047 tokens, 64 experts of 1032: Wd h 173 -> 163 us).
+size_t line_bytes(size_t bytes) { return (bytes + 127) / 128 * 128; }
+
 struct Space { size_t h, da, part, part_scale, weight_part, bytes; };
 Space space(const lsm_experts_params& p, bool backward) {
     const size_t pairs = size_t(p.n) * p.top_k, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4;
     const Plan q = plan_of(p);
     Space s{};
     s.h = 0;
-    s.part = align256(pairs * p.F * el);
+    s.part = align256(pairs * line_bytes(p.F * el));
     s.part_scale = s.part + align256(pairs * p.D * el);
     s.da = s.part_scale + (el == 2 ? align256(pairs * up(p.D, stretch_of(backward ? q.dx : q.down)) * 4) : 0);
-    s.weight_part = s.da + (backward ? align256(pairs * 2 * p.F * el) : 0);
+    s.weight_part = s.da + (backward ? align256(pairs * line_bytes(2 * p.F * el)) : 0);
     s.bytes = s.weight_part + (backward ? align256(pairs * weight_parts(p, q.hidden) * 4) : 0);
     return s;
 }
@@ -525,6 +533,7 @@ int lsm_moe_experts(const lsm_experts_params* p, const void* x, const float* wei
     a.h = ws + s.h; a.part = ws + s.part; a.part_scale = reinterpret_cast<float*>(ws + s.part_scale);
     a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k;
     a.x_bytes = uint32_t(p->x_stride) * el;
+    a.h_bytes = uint32_t(line_bytes(p->F * el));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return (el == 2 ? launch<uint16_t>(*p, a, false, st) : launch<float>(*p, a, false, st)) ? LSM_OK : LSM_ERR_LAUNCH;
 }
@@ -554,7 +563,9 @@ int lsm_moe_experts_bwd(const lsm_experts_params* p, const void* x, const float*
     a.da = ws + s.da; a.weight_part = reinterpret_cast<float*>(ws + s.weight_part);
     a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k;
     a.x_bytes = uint32_t(p->x_stride) * el;
+    a.h_bytes = uint32_t(line_bytes(p->F * el));
     a.dy_bytes = uint32_t(p->dy_stride) * el;
+    a.da_bytes = uint32_t(line_bytes(2 * p->F * el));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return (el == 2 ? launch<uint16_t>(*p, a, true, st) : launch<float>(*p, a, true, st)) ? LSM_OK : LSM_ERR_LAUNCH;
 }

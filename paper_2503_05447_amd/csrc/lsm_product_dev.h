@@ -472,7 +472,7 @@ struct Tile {
 };
 
 // Rows of one call's own use in 16 bits: fp16 times a power of two for each stretch of a row, so that the stretch's largest finite number is
-// about 2^14.  Off by 2^-12 of a number's size, an eighth of what bf16 is, at half of fp32's traffic.
+// about 2^14.  Off by at most 2^-11 of a number's size, an eighth of what bf16 is, at half of fp32's traffic.
 __device__ __forceinline__ float finite_size(float x) {
     const float a = fabsf(x);
     return a < __builtin_inff() ? a : 0.f;
