@@ -77,10 +77,11 @@ struct Operand {
     static constexpr int LINE = L == BY_ROWS ? kStepBytes : N * EL;   // bytes of a line in LDS
     static constexpr int LANES = LINE / 16, LINES = 64 / LANES;       // lanes of a line, lines of a load
     // By columns slot s of line k holds piece s ^ turn(k): the lines k .. k + 3 and k + 8 .. k + 11 that half a wave reads at a time, 32
-    // bytes of each, lie in different banks.
+    // bytes of each, lie in different banks; of fp32 the lines k, k + 4, k + 8 and k + 12, 64 bytes of each.
     static __device__ __forceinline__ int turn(int k) {
         const int low = LINE >= 256 ? k & 3 : LINE == 128 ? (k >> 1) & 1 : 0, bits = LINE >= 256 ? 2 : LINE == 128 ? 1 : 0;
-        return EL == 4 ? 0 : 2 * (low | ((k >> 3) & 1) << bits);
+        if (EL == 4) return 4 * ((k >> 2) & (LINE >= 256 ? 3 : LINE == 128 ? 1 : 0));
+        return 2 * (low | ((k >> 3) & 1) << bits);
     }
 
     uint64_t base;
@@ -154,8 +155,9 @@ struct Operand {
                 uintptr_t(at + first * kStepBytes + r * kStepBytes + ((q ^ (2 * (r >> 3))) * 16)));
         if (EL == 4) {
             u32x4 v;
+            const uint32_t p = at + 4 * q * LINE + (((first + r) >> 2) ^ turn(4 * q)) * 16 + (r & 3) * 4;
             _Pragma("unroll") for (int i = 0; i < 4; ++i)
-                v[i] = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(at + (4 * q + i) * LINE + (first + r) * 4));
+                v[i] = *reinterpret_cast<__attribute__((address_space(3))) const uint32_t*>(uintptr_t(p + i * LINE));
             return v;
         }
         // 16 lanes read four lines' 16 columns and get a column of four lines each
