@@ -321,7 +321,12 @@ __global__ __launch_bounds__(256) void k_sum(ExpertArgs a) {
         const int at = a.place[id];
         float s = 0.f;
         if (uint32_t(at) < uint32_t(a.n * a.top_k))
-            for (int b = 0; b < a.parts; ++b) s += a.weight_part[size_t(b) * (size_t(a.n) * a.top_k) + at];
+            for (int b = 0; b < a.parts; b += 16) {  // requested together
+                float x[16];
+                _Pragma("unroll") for (int u = 0; u < 16; ++u)
+                    x[u] = b + u < a.parts ? a.weight_part[size_t(b + u) * (size_t(a.n) * a.top_k) + at] : 0.f;
+                _Pragma("unroll") for (int u = 0; u < 16; ++u) s += x[u];
+            }
         a.d_weights[id] = s;
     }
     if (id >= int64_t(a.n) * pieces) return;

@@ -143,9 +143,15 @@ struct PlanArgs {
     int32_t *offsets, *order, *place, *hist;  // hist: [blocks][groups + 1], the last for what is left out
     int count, groups, limit, share;          // share: items of a block, a multiple of 64 kPlanWaves
 };
-__device__ __forceinline__ int group_of(const PlanArgs& a, int i) {
-    const int id = a.id[i];
-    return id >= 0 && id < a.limit ? (a.groups == 1 ? 0 : id) : a.groups;
+// The groups of items i, i + step and so on below `end` (-1: no item), requested together (3000 pairs in one block: 18 -> 9 us, with the waves'
+// shares even; 16 at a time: as fast, but three tokens 1.5 us slower for the longer code).
+constexpr int kRead = 4;
+__device__ __forceinline__ void groups_of(const PlanArgs& a, int i, int step, int end, int (&g)[kRead]) {
+    _Pragma("unroll") for (int u = 0; u < kRead; ++u) g[u] = i + u * step < end ? a.id[i + u * step] : 0;
+    _Pragma("unroll") for (int u = 0; u < kRead; ++u) {
+        const int id = g[u];
+        g[u] = i + u * step >= end ? -1 : id >= 0 && id < a.limit ? (a.groups == 1 ? 0 : id) : a.groups;
+    }
 }
 
 __global__ __launch_bounds__(kPlanThreads) void k_plan_count(PlanArgs a) {
@@ -153,7 +159,12 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_count(PlanArgs a) {
     for (int g = threadIdx.x; g <= a.groups; g += kPlanThreads) n[g] = 0;
     __syncthreads();
     const int i0 = int(blockIdx.x) * a.share, i1 = min(a.count, i0 + a.share);
-    for (int i = i0 + int(threadIdx.x); i < i1; i += kPlanThreads) atomicAdd(&n[group_of(a, i)], 1);
+    for (int i = i0 + int(threadIdx.x); i < i1; i += kRead * kPlanThreads) {
+        int g[kRead];
+        groups_of(a, i, kPlanThreads, i1, g);
+        _Pragma("unroll") for (int u = 0; u < kRead; ++u)
+            if (g[u] >= 0) atomicAdd(&n[g[u]], 1);
+    }
     __syncthreads();
     for (int g = threadIdx.x; g <= a.groups; g += kPlanThreads) a.hist[size_t(blockIdx.x) * (a.groups + 1) + g] = n[g];
 }
@@ -169,7 +180,12 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_place(PlanArgs a) {
     }
     __syncthreads();
     const int i0 = int(blockIdx.x) * a.share, each = a.share / kPlanWaves, w0 = i0 + wave * each, w1 = min(a.count, w0 + each);
-    for (int i = w0 + lane; i < w1; i += 64) atomicAdd(&mine[wave][group_of(a, i)], 1);
+    for (int i = w0 + lane; i < w1; i += kRead * 64) {
+        int g[kRead];
+        groups_of(a, i, 64, w1, g);
+        _Pragma("unroll") for (int u = 0; u < kRead; ++u)
+            if (g[u] >= 0) atomicAdd(&mine[wave][g[u]], 1);
+    }
     if (gridDim.x > 1) {
         const int rows = kPlanThreads / G > 0 ? kPlanThreads / G : 1, g = int(threadIdx.x) % G, r0 = int(threadIdx.x) / G;
         int b = 0, s = 0;
@@ -219,23 +235,28 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_place(PlanArgs a) {
     }
     __syncthreads();
     volatile int* next = mine[wave];
-    for (int i = w0 + lane; i - lane < w1; i += 64) {
-        const bool there = i < w1;
-        const int g = there ? group_of(a, i) : -1;
-        unsigned long long same = __ballot(there);
-        for (int b = 0; (a.groups >> b) != 0; ++b) {
-            const unsigned long long set = __ballot((g >> b) & 1);
-            same &= (g >> b) & 1 ? set : ~set;
+    for (int first = w0; first < w1; first += kRead * 64) {
+        int groups[kRead];
+        groups_of(a, first + lane, 64, w1, groups);
+        _Pragma("unroll") for (int u = 0; u < kRead; ++u) {
+            if (first + u * 64 >= w1) break;
+            const int i = first + u * 64 + lane, g = groups[u];
+            const bool there = g >= 0;
+            unsigned long long same = __ballot(there);
+            for (int b = 0; (a.groups >> b) != 0; ++b) {
+                const unsigned long long set = __ballot((g >> b) & 1);
+                same &= (g >> b) & 1 ? set : ~set;
+            }
+            if (there) {
+                const int rank = lanes(same & ((1ull << lane) - 1)), at = next[g] + rank;
+                const bool in = g < a.groups;
+                a.order[at] = in ? i : -1;
+                a.place[i] = in ? at : -1;
+            }
+            __builtin_amdgcn_wave_barrier();
+            if (there && (same >> lane) == 1ull) next[g] = next[g] + lanes(same);  // the last of the equal ones
+            __builtin_amdgcn_wave_barrier();
         }
-        if (there) {
-            const int rank = lanes(same & ((1ull << lane) - 1)), at = next[g] + rank;
-            const bool in = g < a.groups;
-            a.order[at] = in ? i : -1;
-            a.place[i] = in ? at : -1;
-        }
-        __builtin_amdgcn_wave_barrier();
-        if (there && (same >> lane) == 1ull) next[g] = next[g] + lanes(same);  // the last of the equal ones
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -252,8 +273,7 @@ int check(const lsm_route_params* p, bool logits) {
 }
 
 int plan_share(int64_t count) {  // items of a block
-    if (count <= kPlanAlone) return kPlanAlone;
-    const int64_t each = (count + kPlanBlocks - 1) / kPlanBlocks, unit = 64 * kPlanWaves;
+    const int64_t each = count <= kPlanAlone ? count : (count + kPlanBlocks - 1) / kPlanBlocks, unit = 64 * kPlanWaves;
     return int((each + unit - 1) / unit * unit);
 }
 
