@@ -124,6 +124,20 @@ def test_every_tile(dtype, K, n, D, V):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V,K,where", [(70, 2047, 70, (490, 540)), (33, 1024, 256, (0, 1024)), (300, 513, 5, (508, 513)), (5, 70001, 66, (511, 514)),
+                                         (64, 4096, 64, (4032, 4096))])
+def test_entries_close_together(dtype, n, V, K, where):
+    """A teacher's tokens within a few columns, on both sides of a border, most of them several times, at the vocabulary's ends; some rows
+    with entries that do not count between them."""
+    import torch
+    a = make(n, 72, V, K, dtype, seed=n + K)
+    a["index"] = (where[0] + a["index"] % (where[1] - where[0])).int()
+    a["index"][::3, ::2] = torch.tensor([-1, V], dtype=torch.int32).cuda()[torch.arange((K + 1) // 2).cuda() % 2]
+    a["teacher"][1::4, 1::3] = -INF
+    check(a)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_temperatures(dtype):
     for tau in (0.5, 3.0):
         check(make(40, 64, 500, 0, dtype, seed=1), tau)
