@@ -15,6 +15,10 @@ namespace {
 
 constexpr int kMostEntries = 256, kGroup = 512;
 
+// dx of a piece: rows of a tile, in how many shares its columns are taken with all tokens, the most it is worth taking them in
+struct Shares { int rows, least, most; };
+constexpr int kPieceKinds = 3;  // whole pieces, one that ends with a full round, what is left
+
 struct VocabArgs {
     const void *x, *w;
     const int32_t *index, *offsets, *order, *place;
@@ -26,10 +30,11 @@ struct VocabArgs {
     float* at_entry;          // [max(K, 1)][n] logits
     float *loss, *lse;
     void *grad, *dx, *dw;     // gradient [n][piece]
-    float* part;              // [shares][n][D]
+    float* part;              // [shares][tokens that count][D]
     int n, D, V, K, parts, groups;  // groups: of kGroup columns
     int v0, width, piece;     // the piece: its first column, how many, and how many the gradient's rows hold (a multiple of 256)
-    int shares, begun;        // of the piece's columns for dx; how many of them have a sum from pieces before
+    Shares here, before[kPieceKinds];  // of this piece, of the kinds of pieces that were before
+    int kinds;                // of them
     uint32_t x_bytes;
     float scale;              // 1 / temperature
 };
@@ -389,19 +394,32 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(VocabArgs a) {
     }
 }
 
+// In how many shares a piece's columns are taken: where few of the tokens count, as many times more as workgroups would have nothing to do
+// (8191 tokens, 50257 x 2048, 60 % of them left out: dx 1118 -> 705 us).
+__device__ __forceinline__ int shares_of(const Shares& s, int n, int rows) {
+    const int all = (n + s.rows - 1) / s.rows, there = max((rows + s.rows - 1) / s.rows, 1);
+    return max(s.least, min(s.most, int(int64_t(s.least) * all / there)));
+}
+__device__ __forceinline__ int shares_before(const VocabArgs& a, int rows) {  // so many have a sum
+    int most = 0;
+    _Pragma("unroll") for (int i = 0; i < kPieceKinds; ++i)
+        if (i < a.kinds) most = max(most, shares_of(a.before[i], a.n, rows));
+    return most;
+}
+
 template <typename T>
 __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     typedef typename T::TIO TIO;
     constexpr int EL = int(sizeof(TIO)), STEP = kStepBytes / EL;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
     const int width = a.width, rows = rows_of(a);
-    const int rt = (rows + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, id = number_of_tile(rt * ct * a.shares);
+    const int rt = (rows + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, shares = shares_of(a.here, a.n, rows), id = number_of_tile(rt * ct * shares);
     if (id < 0) return;
     const int share = id / (rt * ct);
     int r, c;
     tile_at(id - share * rt * ct, rt, ct, r, c);
-    const int steps = (width + STEP - 1) / STEP, k0 = steps * share / a.shares * STEP, k1 = min(width, steps * (share + 1) / a.shares * STEP);
-    const int r0 = r * T::BR;
+    const int steps = (width + STEP - 1) / STEP, k0 = steps * share / shares * STEP, k1 = min(width, steps * (share + 1) / shares * STEP);
+    const int r0 = r * T::BR, begun = shares_before(a, rows);
     const uint32_t bytes = uint32_t(a.piece) * EL;
     T t(shared);
     t.r.start_rows(static_cast<const TIO*>(a.grad) + size_t(r0) * a.piece + k0, t.wave, t.lane,
@@ -411,9 +429,9 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     clear<T>(acc);
     t.walk(acc, k1 - k0);
     const int c0 = c * T::BC + t.wc * T::TC * 16;
-    const auto line = [&](int q) { return r0 + q < rows ? a.part + (size_t(share) * a.n + r0 + q) * a.D + c0 : nullptr; };
+    const auto line = [&](int q) { return r0 + q < rows ? a.part + (size_t(share) * rows + r0 + q) * a.D + c0 : nullptr; };
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        if (share >= a.begun) t.template store<T::TC, float>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
+        if (share >= begun) t.template store<T::TC, float>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
         else t.template store<T::TC, float, true>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
     }
 }
@@ -427,9 +445,10 @@ __global__ __launch_bounds__(256) void k_dx_join(VocabArgs a) {
     const int token = int(id / pieces), d = int(id - int64_t(token) * pieces) * E, at = a.place[token];
     float s[E];
     _Pragma("unroll") for (int e = 0; e < E; ++e) s[e] = 0.f;
-    if (at >= 0 && at < a.n)
-        for (int q = 0; q < a.begun; ++q) {
-            const f32x4* z = reinterpret_cast<const f32x4*>(a.part + (size_t(q) * a.n + at) * a.D + d);
+    const int rows = rows_of(a), begun = shares_before(a, rows);
+    if (at >= 0 && at < rows)
+        for (int q = 0; q < begun; ++q) {
+            const f32x4* z = reinterpret_cast<const f32x4*>(a.part + (size_t(q) * rows + at) * a.D + d);
             _Pragma("unroll") for (int i = 0; i < E / 4; ++i)
                 _Pragma("unroll") for (int e = 0; e < 4; ++e) s[4 * i + e] += z[i][e];
         }
@@ -461,7 +480,7 @@ int logits_tile(const lsm_vocab_params& p) {
 // and into how many shares dx takes the piece.  dw's products are as long as there are tokens, so that a last round of a few tiles takes
 // as long as a full one: a piece ends with a full round where less than half of the next one would be left, and what is left is a
 // piece with smaller tiles (8191 tokens, 50257 x 2048: dw 1140 -> 990 us).
-struct Piece { int width, grad, dw, dx, shares; int64_t tiles; };  // tiles: the most of its launches
+struct Piece { int width, grad, dw, dx, shares; int64_t tiles, rows; };  // tiles: the most of its launches; rows: of sums for dx
 Piece piece_of(const lsm_vocab_params& p, int left) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
     const unsigned kinds = f32 ? 0x7e : 0x7f;
@@ -492,17 +511,18 @@ Piece piece_of(const lsm_vocab_params& p, int left) {
                         [&](const TileSize& t) { return up(q.width, shares(t)); }, kinds);
     q.shares = shares(kTiles[q.dx]);
     const auto tiles_of = [](int rows, int cols, int kind) { return int64_t(up(rows, kTiles[kind].rows)) * up(cols, kTiles[kind].cols); };
+    q.rows = int64_t(q.shares) * up(p.n, kTiles[q.dx].rows) * kTiles[q.dx].rows;
     for (const int64_t n : {tiles_of(p.n, q.width, q.grad), tiles_of(q.width, p.D, q.dw), tiles_of(p.n, p.D, q.dx) * q.shares})
         if (n > q.tiles) q.tiles = n;
     return q;
 }
-// The most of any piece: columns (whole tiles), shares, tiles.
+// The most of any piece: columns (whole tiles), tiles, rows of sums.
 Piece largest_piece(const lsm_vocab_params& p) {
     Piece most{};
     for (int v = 0; v < p.V;) {
         const Piece q = piece_of(p, p.V - v);
         if (up(q.width, 256) * 256 > most.width) most.width = up(q.width, 256) * 256;
-        if (q.shares > most.shares) most.shares = q.shares;
+        if (q.rows > most.rows) most.rows = q.rows;
         if (q.tiles > most.tiles) most.tiles = q.tiles;
         v += q.width;
     }
@@ -538,7 +558,7 @@ Space space(const lsm_vocab_params& p, bool backward) {
     } else {
         const Piece q = largest_piece(p);
         s.grad = take(n * q.width * el);
-        s.part = take(size_t(q.shares) * n * p.D * 4);
+        s.part = take(size_t(q.rows) * p.D * 4);
     }
     s.bytes = at;
     return s;
@@ -613,7 +633,7 @@ template <typename TIO, int KIND>
 bool launch_dx(const VocabArgs& a, hipStream_t st) {
     typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND>::type T;
     ProfScope ps(KID_VOCAB_DX, st);
-    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of<T>(int64_t(up(a.n, T::BR)) * up(a.D, T::BC) * a.shares)), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of<T>(int64_t(up(a.n, T::BR)) * up(a.D, T::BC) * a.here.least)), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 
@@ -638,12 +658,16 @@ bool launch(VocabArgs a, const lsm_vocab_params& p, bool backward, hipStream_t s
         const Piece q = piece_of(p, a.V - a.v0);
         a.width = q.width;
         a.piece = up(q.width, 256) * 256;
-        a.shares = q.shares;
+        a.here = Shares{kTiles[q.dx].rows, q.shares, q.width / 512};
         if (!LSM_KIND(LSM_GRAD, q.grad)) return false;
         if (a.dw && !(q.dw == 0 ? launch_dw<TIO, 0>(a, q.width, st) : q.dw == 2 ? launch_dw<TIO, 2>(a, q.width, st) : launch_dw<TIO, 5>(a, q.width, st)))
             return false;
         if (!LSM_KIND(LSM_DX, q.dx)) return false;
-        if (a.shares > a.begun) a.begun = a.shares;
+        const Shares last = a.kinds ? a.before[a.kinds - 1] : Shares{};
+        if (last.rows != a.here.rows || last.least != a.here.least || last.most != a.here.most) {
+            if (a.kinds == kPieceKinds) return false;
+            a.before[a.kinds++] = a.here;
+        }
         a.v0 += q.width;
     }
     ProfScope ps(KID_VOCAB_JOIN, st);

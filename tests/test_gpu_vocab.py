@@ -168,6 +168,13 @@ def test_a_vocabulary_in_pieces(dtype):
     assert (got["dx"][gone] == 0).all() and (got["loss"][gone] == 0).all() and (got["lse"][gone] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,D,V,left_out", [(2100, 72, 20001, 0.9), (1500, 264, 9001, 0.7), (8000, 24, 5001, 0.997), (700, 520, 6000, 0.5), (3000, 72, 3001, 1.0)])
+def test_few_tokens_of_many_count(dtype, n, D, V, left_out):
+    """dx's sums are then in more shares of the vocabulary than with all tokens; with none there is nothing to do."""
+    check(make(n, D, V, 0, dtype, seed=n, left_out=left_out))
+
+
 @pytest.mark.parametrize("K", [0, 5])
 def test_tokens_left_out_are_not_read(K):
     import torch
