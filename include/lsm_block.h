@@ -101,8 +101,8 @@ typedef struct {
  *   y          [n, D]                                                                               out
  *   workspace  at least lsm_moe_step_workspace_bytes(p) (0 for invalid params)
  * The form for decoding: the active experts' weights are read once, whatever the tokens that share them; for the many tokens
- * of a prompt a grouped matrix product is the better tool.  Sums are fp32; with bf16 elements the hidden activations are kept
- * as a bf16 head and a bf16 remainder, so that the one rounding to bf16 is the result's.  A token with a router output of
+ * of a prompt, and for training, lsm_moe_experts of lsm_train.h is the better tool.  Sums are fp32; with bf16 elements the
+ * hidden activations are kept as a bf16 head and a bf16 remainder, so that the one rounding to bf16 is the result's.  A token with a router output of
  * NaN or +inf, or with none above -inf, gets a row of NaN (beside finite ones an expert of -inf has the weight 0); other tokens
  * are not affected.
  */

@@ -11,6 +11,9 @@
 // Where a lane's 16 bytes land is fixed by the hardware (one after the other), so rows are spread over the banks by which
 // 16 bytes of the row a lane asks for: slot s of row i holds piece s ^ f(i).  (Without bank conflicts, by the counters; with them the clocks of LDS double.)
 //
+// Bound by the matrix cores: from registers alone the instruction reaches 1.9 PFLOP/s here, the steps of a 256 x 256 tile 1.4, a whole product
+// 0.9 to 1.26 with its start, its results and a last round of tiles that is not full (a large library product 1.17 to 1.42).  fp32
+// products are bound by the instruction's 154 TFLOP/s, of which long ones reach 117.
 // Where tiles follow one another in a workgroup there are as many workgroups as there is room for.
 //
 // While the matrix instructions of step t run, the operands of step t + 1 are read, each into the registers whose last use has just
