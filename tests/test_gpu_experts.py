@@ -187,6 +187,65 @@ def test_large_and_small_numbers(dtype):
             assert torch.equal(got[name], base[name] * scale), name
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,E,k", [(70, 256, 16), (300, 129, 6), (9, 255, 3), (500, 253, 1)])
+def test_many_experts(dtype, n, E, k):
+    check(make(n, 64, 40, E, k, dtype, seed=E, skew=1.0, dropped=0.05))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_the_workspace_held_does_not_matter(dtype):
+    """Workspaces of NaN (all bits set), widths that are neither whole tiles nor whole lines of the caches."""
+    import torch
+    for n, D, F in ((37, 72, 104), (300, 136, 40), (2100, 264, 72)):
+        a = make(n, D, F, 5, 2, dtype, seed=n, dropped=0.2)
+        want = run(a)
+        plan = lsm().lsm_moe_plan(a["chosen"], 5)
+        what = a["x"], a["weights"], plan, a["w_gate_up"], a["w_down"]
+        ws = torch.full((1 << 26,), 255, dtype=torch.uint8, device="cuda")
+        y = lsm().lsm_moe_experts(*what, residual=a["residual"], workspace=ws)
+        ws.fill_(255)
+        got = dict(lsm().lsm_moe_experts_bwd(*what, a["d_y"], workspace=ws), y=y)
+        for name in want:
+            assert torch.equal(got[name], want[name]), (name, n)
+
+
+def test_rows_almost_four_gigabytes_apart():
+    """Offsets that need all of 32 bits: the last rows of x and d_y begin just below 2^32 bytes."""
+    import torch
+    a = make(16, 72, 40, 3, 2, "bf16", seed=21)
+    want = run(a)
+    stride = (1 << 27) - 256
+    far = torch.empty(16 * stride, dtype=torch.bfloat16, device="cuda")
+    for name in ("x", "d_y"):
+        b = dict(a)
+        b[name] = far.as_strided((16, 72), (stride, 1))
+        b[name].copy_(a[name])
+        got = run(b)
+        assert all(torch.equal(got[q], want[q]) for q in want), name
+
+
+def test_an_expert_of_almost_four_gigabytes():
+    """65528 x 16376: all zeros but the last eight features and columns, which are an expert of 8 x 8."""
+    import torch
+    D, F = 65528, 16376
+    small = make(5, 8, 8, 1, 1, "bf16", seed=22, residual=False)
+    big = dict(small, x=torch.zeros(5, D, dtype=torch.bfloat16, device="cuda"), d_y=torch.zeros(5, D, dtype=torch.bfloat16, device="cuda"),
+               w_gate_up=torch.zeros(1, 2 * F, D, dtype=torch.bfloat16, device="cuda"), w_down=torch.zeros(1, D, F, dtype=torch.bfloat16, device="cuda"))
+    big["x"][:, -8:], big["d_y"][:, -8:] = small["x"], small["d_y"]
+    big["w_gate_up"][0, F - 8:F, -8:], big["w_gate_up"][0, -8:, -8:] = small["w_gate_up"][0, :8], small["w_gate_up"][0, 8:]
+    big["w_down"][0, -8:, -8:] = small["w_down"][0]
+    got = run(big)
+    want, spread = reference(small)
+    cut = dict(y=got["y"][:, -8:], dx=got["dx"][:, -8:], d_weights=got["d_weights"], d_w_down=got["d_w_down"][:, -8:, -8:],
+               d_w_gate_up=torch.cat((got["d_w_gate_up"][:, F - 8:F, -8:], got["d_w_gate_up"][:, -8:, -8:]), 1))
+    for name in want:
+        compare(name, cut[name], want[name], spread[name], name != "d_weights")
+    for name in ("y", "dx"):
+        assert (got[name][:, :-8] == 0).all()
+    assert int((got["d_w_gate_up"] != 0).sum()) <= 2 * 64 and int((got["d_w_down"] != 0).sum()) <= 64
+
+
 def test_rows_further_apart():
     """x and d_y as columns of wider tensors, with numbers that are not finite between the rows."""
     import torch

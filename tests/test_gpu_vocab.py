@@ -250,6 +250,67 @@ def test_large_logits():
     assert ((got["loss"].double() - want["loss"]).abs() <= tol).all() and torch.isfinite(got["dx"]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [0, 7])
+def test_what_the_workspace_held_does_not_matter(dtype, K):
+    """Workspaces of NaN (all bits set), vocabularies that end inside a tile, tokens left out."""
+    import torch
+    for n, D, V in ((5, 72, 1001), (300, 136, 777), (2100, 72, 3001)):
+        a = make(n, D, V, K, dtype, seed=n, left_out=0.3)
+        want = run(a)
+        ws = torch.full((1 << 27,), 255, dtype=torch.uint8, device="cuda")
+        fwd, bwd, what = ((lsm().lsm_linear_cross_entropy, lsm().lsm_linear_cross_entropy_bwd, ()) if K == 0 else
+                          (lsm().lsm_linear_distill, lsm().lsm_linear_distill_bwd, (a["teacher"],)))
+        loss, lse = fwd(a["x"], a["w"], a["index"], *what, workspace=ws)
+        ws.fill_(255)
+        got = dict(bwd(a["x"], a["w"], a["index"], *what, lse, a["d_loss"], workspace=ws), loss=loss, lse=lse)
+        for name in want:
+            assert torch.equal(got[name], want[name]), (name, n)
+
+
+@pytest.mark.parametrize("K", [0, 7])
+def test_rows_almost_four_gigabytes_apart(K):
+    """Offsets that need all of 32 bits: the last row of x begins just below 2^32 bytes."""
+    import torch
+    a = make(16, 72, 300, K, "bf16", seed=31)
+    want = run(a)
+    stride = (1 << 27) - 256
+    far = torch.empty(16 * stride, dtype=torch.bfloat16, device="cuda")
+    b = dict(a, x=far.as_strided((16, 72), (stride, 1)))
+    b["x"].copy_(a["x"])
+    got = run(b)
+    assert all(torch.equal(got[q], want[q]) for q in want)
+
+
+def test_a_vocabulary_of_more_than_four_gigabytes():
+    """2^24 - 3 columns of 136: rows of w and its gradient behind 2^32 bytes, targets at both ends."""
+    import torch
+    V, D = (1 << 24) - 3, 136
+    gen = torch.Generator("cuda").manual_seed(32)
+    w = torch.zeros(V, D, dtype=torch.bfloat16, device="cuda")
+    w[-4:] = torch.randn(4, D, generator=gen, device="cuda", dtype=torch.bfloat16)
+    x = torch.randn(3, D, generator=gen, device="cuda", dtype=torch.bfloat16) / 8
+    target = torch.tensor([V - 1, 0, V - 3], dtype=torch.int32, device="cuda")
+    loss, lse = lsm().lsm_linear_cross_entropy(x, w, target)
+    got = lsm().lsm_linear_cross_entropy_bwd(x, w, target, lse, torch.ones(3, device="cuda"))
+    z = x.double() @ w[-4:].double().t().contiguous()                      # all other logits are 0
+    want = torch.log(torch.exp(z).sum(1) + (V - 4))
+    at = torch.stack((z[0, 3], torch.zeros_like(z[0, 0]), z[2, 1]))
+    # lse is about 16.6: fp32 sums of 2^24 terms, a few tens at a time, then of parts: within 64 x 2^-24 of the sum, and 2^-23 of 17
+    assert ((lse.double() - want).abs() <= 64 * 2.0 ** -24 + 17 * 2.0 ** -23).all() and ((loss.double() - (want - at)).abs() <= 2.0 ** -15).all()
+    g = torch.zeros(3, 4, dtype=torch.float64, device="cuda")
+    g += torch.exp(z - want[:, None])
+    g[0, 3] -= 1
+    g[2, 1] -= 1
+    dw = g.t().contiguous() @ x.double()
+    size = g.abs().t().contiguous() @ x.double().abs()                     # roundings of g and of the result, 2^-8 each, and 2^-18 of p
+    assert ((got["dw"][-4:].double() - dw).abs() <= 2.1 * 2.0 ** -8 * size).all()
+    row0 = (torch.exp(-want)[:, None] - torch.tensor([[0.0], [1.0], [0.0]], device="cuda").double()) * x.double()
+    assert ((got["dw"][0].double() - row0.sum(0)).abs() <= 2.1 * 2.0 ** -8 * row0.abs().sum(0)).all()
+    dx = g @ w[-4:].double()
+    assert ((got["dx"].double() - dx).abs() <= 2.1 * 2.0 ** -8 * (g.abs() @ w[-4:].double().abs())).all()
+
+
 def test_rows_further_apart_and_no_weight_gradient():
     import torch
     a = make(70, 64, 300, 0, "bf16", seed=9)
