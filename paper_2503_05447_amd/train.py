@@ -33,22 +33,30 @@ def _current_device():
     return device() if device is not None else torch.cuda.current_device()
 
 
+def _sized(params, sizes):
+    """A parameter block of `sizes`, by reference; ctypes itself would cut a number off at 32 bits."""
+    p = params(ctypes.sizeof(params), *sizes)
+    if any(getattr(p, f) != s for (f, t), s in zip(params._fields_[1:], sizes) if t is not ctypes.c_float):
+        raise ValueError("a size is beyond the 32 bits (strides: 64) that the library takes: %s" % (sizes,))
+    return ctypes.byref(p)
+
+
 # Parameter blocks by reference, kept by the numbers in them (sizes only, no pointers), and the workspaces they ask for.
 @functools.lru_cache(maxsize=256)
 def _route_params(*sizes):
-    p = ctypes.byref(_RouteParams(ctypes.sizeof(_RouteParams), *sizes))
+    p = _sized(_RouteParams, sizes)
     return p, library().lsm_moe_plan_workspace_bytes(p)
 
 
 @functools.lru_cache(maxsize=256)
 def _experts_params(*sizes):
-    p = ctypes.byref(_ExpertsParams(ctypes.sizeof(_ExpertsParams), *sizes))
+    p = _sized(_ExpertsParams, sizes)
     return p, library().lsm_moe_experts_workspace_bytes(p), library().lsm_moe_experts_bwd_workspace_bytes(p)
 
 
 @functools.lru_cache(maxsize=256)
 def _vocab_params(*sizes):
-    p = ctypes.byref(_VocabParams(ctypes.sizeof(_VocabParams), *sizes))
+    p = _sized(_VocabParams, sizes)
     return p, library().lsm_vocab_loss_workspace_bytes(p), library().lsm_vocab_loss_bwd_workspace_bytes(p)
 
 

@@ -217,6 +217,19 @@ def test_binding_refuses(seen):
     assert not seen
 
 
+def test_numbers_beyond_32_bits_are_refused(seen):
+    """They would be taken for their lowest 32 bits."""
+    with pytest.raises(ValueError):
+        pkg.lsm_moe_route(tensor(6, 9), (1 << 32) + 3)
+    with pytest.raises(ValueError):
+        pkg.lsm_moe_plan(tensor(6, 3, dtype=torch.int32), (1 << 32) + 9)
+    with pytest.raises(ValueError):
+        train._vocab_params(6, 64, (1 << 32) + 50, 0, 0, 1.0, 0, 64)
+    with pytest.raises(ValueError):
+        train._experts_params((1 << 32) + 6, 64, 40, 9, 3, 0, 0, 64, 64)
+    assert not seen
+
+
 def test_another_device_is_refused(seen, monkeypatch):
     class Elsewhere(OnDevice):
         def get_device(self):
