@@ -32,6 +32,7 @@ struct ExpertArgs {
     void* part;           // [pairs][D]: fp32, or with bf16 elements fp16 times part_scale
     float *part_scale, *weight_part;  // [stretches of D][pairs]; [tiles of F][pairs]
     int n, D, F, E, top_k, parts, stretch;
+    int halves;             // rows of a pair in h (forward) or da (backward): 2 where a remainder follows what was rounded
     uint32_t x_bytes, dy_bytes, h_bytes, da_bytes;  // between rows
 };
 
@@ -44,6 +45,17 @@ template <typename TIO> __device__ __forceinline__ TIO* row_of(void* rows, int a
     return reinterpret_cast<TIO*>(static_cast<char*>(rows) + size_t(at) * bytes);
 }
 
+// What rounding x to bf16 leaves; nothing where it is not finite.
+__device__ __forceinline__ float remainder_of(float x) {
+    const float r = x - bf16_lo(pack2(x, 0.f));
+    return fabsf(r) < __builtin_inff() ? r : 0.f;
+}
+__device__ __forceinline__ f32x4 remainders(const f32x4& x) {
+    return f32x4{remainder_of(x[0]), remainder_of(x[1]), remainder_of(x[2]), remainder_of(x[3])};
+}
+// Tiles that are taken for few rows: they can hold two of a pair.
+template <typename T> constexpr bool kMayHalve = sizeof(typename T::TIO) == 2 && T::BR <= 64;
+
 struct Where { int e, first, count, r, c; };  // expert, its first place and its pairs, the tile's number along rows and columns
 
 // The tiles of a workgroup, of all experts' tiles of BR rows x `cols` columns in the order expert, column, row.  Workgroups are dealt out
@@ -51,10 +63,10 @@ struct Where { int e, first, count, r, c; };  // expert, its first place and its
 template <int BR>
 struct Finder {
     int o[5], tiles[4], upto, own;  // of four experts a lane: where they begin, their row tiles; row tiles up to and of this lane
-    __device__ __forceinline__ Finder(const ExpertArgs& a) {
+    __device__ __forceinline__ Finder(const ExpertArgs& a, int halves = 1) {
         const int lane = threadIdx.x & 63;
         own = 0;
-        _Pragma("unroll") for (int i = 0; i < 5; ++i) o[i] = offset_of(a, min(4 * lane + i, a.E));
+        _Pragma("unroll") for (int i = 0; i < 5; ++i) o[i] = offset_of(a, min(4 * lane + i, a.E)) * halves;
         _Pragma("unroll") for (int i = 0; i < 4; ++i) {
             tiles[i] = max(o[i + 1] - o[i] + BR - 1, 0) / BR;
             own += tiles[i];
@@ -130,21 +142,23 @@ __global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
         });
         constexpr int HALF = T::TC / 2;
         const int f0 = w.c * (T::BC / 2) + t.wc * HALF * 16;
-        _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
-            t.template store<HALF, TIO>(
-                j, a.F - f0,
-                [&](int i) {
-                    f32x4 h;
-                    _Pragma("unroll") for (int e = 0; e < 4; ++e) {
-                        const float gate = acc[i][j][e];
-                        h[e] = gate * sigmoid(gate, TIO()) * acc[i + HALF][j][e];
-                    }
-                    return h;
-                },
-                [&](int r) {
+        const int halves = kMayHalve<T> ? a.halves : 1;
+        _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
+            _Pragma("unroll") for (int i = 0; i < HALF; ++i)
+                _Pragma("unroll") for (int e = 0; e < 4; ++e) {
+                    const float gate = acc[i][j][e];
+                    acc[i][j][e] = gate * sigmoid(gate, TIO()) * acc[i + HALF][j][e];
+                }
+            const auto line = [&](int half) {
+                return [=, &w](int r) {
                     const int at = w.r * T::BR + r;
-                    return at < w.count ? row_of<TIO>(a.h, w.first + at, a.h_bytes) + f0 : nullptr;
-                });
+                    return at < w.count ? row_of<TIO>(a.h, (w.first + at) * halves + half, a.h_bytes) + f0 : nullptr;
+                };
+            };
+            t.template store<HALF, TIO>(j, a.F - f0, [&](int i) { return acc[i][j]; }, line(0));
+            if constexpr (kMayHalve<T>)
+                if (halves == 2) t.template store<HALF, TIO>(j, a.F - f0, [&](int i) { return remainders(acc[i][j]); }, line(1));
+        }
         if (!more) return;
         t.go_on();
         w = next;
@@ -156,7 +170,13 @@ template <typename T>
 __device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, const Where& w, f32x4 (&acc)[T::TC][T::TR]) {
     constexpr bool HALF = sizeof(typename T::TIO) == 2;
     typedef typename std::conditional<HALF, half_t, float>::type TP;
-    const int stretch = w.c * T::WC + t.wc, d0 = stretch * T::TC * 16;
+    const int stretch = w.c * T::WC + t.wc, d0 = stretch * T::TC * 16, halves = kMayHalve<T> ? a.halves : 1;
+    if constexpr (kMayHalve<T>)
+        if (halves == 2)  // both rows of a pair, in neighbouring lanes
+            _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+                _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
+                    _Pragma("unroll") for (int e = 0; e < 4; ++e) acc[i][j][e] += dpp<0xB1>(acc[i][j][e]);
+    const auto pair_of_row = [=, &w](int row) { return row < w.count && (row & (halves - 1)) == 0 ? (w.first + row) >> (halves - 1) : -1; };
     float scale[T::TR];
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
         scale[j] = 1.f;
@@ -170,12 +190,11 @@ __device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, con
         t.template store<T::TC, TP>(
             j, a.D - d0, [&](int i) { return acc[i][j] * scale[j]; },
             [&](int r) {
-                const int at = w.r * T::BR + r;
-                return at < w.count ? static_cast<TP*>(a.part) + size_t(w.first + at) * a.D + d0 : nullptr;
+                const int at = pair_of_row(w.r * T::BR + r);
+                return at >= 0 ? static_cast<TP*>(a.part) + size_t(at) * a.D + d0 : nullptr;
             });
-        const int at = w.r * T::BR + t.row(j);
-        if (HALF && t.lane < 16 && at < w.count && d0 < a.D)
-            a.part_scale[size_t(stretch) * (size_t(a.n) * a.top_k) + w.first + at] = 1.f / scale[j];
+        const int at = pair_of_row(w.r * T::BR + t.row(j));
+        if (HALF && t.lane < 16 && at >= 0 && d0 < a.D) a.part_scale[size_t(stretch) * (size_t(a.n) * a.top_k) + at] = 1.f / scale[j];
     }
 }
 // rows of the pairs of this tile, `bytes` each, one after the other
@@ -189,7 +208,7 @@ __device__ __forceinline__ void start_pairs(const T& t, typename T::R& r, const 
 template <typename T, typename Start>
 __device__ __forceinline__ void part_tiles(char* shared, const ExpertArgs& a, int K, Start start) {
     const int cols = (a.D + T::BC - 1) / T::BC;
-    const Finder<T::BR> finder(a);
+    const Finder<T::BR> finder(a, kMayHalve<T> ? a.halves : 1);
     Where w;
     if (!finder.find(0, cols, w)) return;
     T t(shared);
@@ -274,15 +293,21 @@ __global__ __launch_bounds__(T::THREADS) void k_hidden_grad(ExpertArgs a) {
             }
         along = T::row_sum(along);
         if (t.lane < 16 && at < w.count) a.weight_part[size_t(w.c * T::WC + t.wc) * (size_t(a.n) * a.top_k) + w.first + at] = along;
-        const auto line = [&](void* base, uint32_t bytes, int shift) {
+        const int halves = kMayHalve<T> ? a.halves : 1;
+        const auto line = [&](void* base, uint32_t bytes, int shift, int by, int which) {
             return [=, &w](int r) {
                 const int q = w.r * T::BR + r;
-                return q < w.count ? row_of<TIO>(base, w.first + q, bytes) + shift + f0 : nullptr;
+                return q < w.count ? row_of<TIO>(base, (w.first + q) * by + which, bytes) + shift + f0 : nullptr;
             };
         };
         _Pragma("unroll") for (int half = 0; half < 2; ++half)
-            t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return gu[half * T::TC + i][j]; }, line(a.da, a.da_bytes, half * a.F));
-        t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return tt[i][j]; }, line(a.h, a.h_bytes, 0));
+            t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return gu[half * T::TC + i][j]; }, line(a.da, a.da_bytes, half * a.F, halves, 0));
+        if constexpr (kMayHalve<T>)
+            if (halves == 2)
+                _Pragma("unroll") for (int half = 0; half < 2; ++half)
+                    t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return remainders(gu[half * T::TC + i][j]); },
+                                                 line(a.da, a.da_bytes, half * a.F, halves, 1));
+        t.template store<T::TC, TIO>(j, a.F - f0, [&](int i) { return tt[i][j]; }, line(a.h, a.h_bytes, 0, 1, 0));
     }
 }
 
@@ -303,7 +328,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(ExpertArgs a, int row_tiles, 
         t.r.start_cols(a.d_y, int(a.dy_bytes), r0 * T::BR, rows, t.wave, t.lane, t.list_at());
         t.c.start_cols(row_of<TIO>(a.h, first, a.h_bytes), int(a.h_bytes), c * T::BC, cols, t.wave, t.lane, 0);
     } else {
-        t.r.start_cols(row_of<TIO>(a.da, first, a.da_bytes), int(a.da_bytes), r0 * T::BR, rows, t.wave, t.lane, 0);
+        t.r.start_cols(row_of<TIO>(a.da, first * a.halves, a.da_bytes), int(a.da_bytes) * a.halves, r0 * T::BR, rows, t.wave, t.lane, 0);
         t.c.start_cols(a.x, int(a.x_bytes), c * T::BC, cols, t.wave, t.lane, t.list_at());
     }
     f32x4 acc[T::TC][T::TR];
@@ -389,6 +414,11 @@ int check(const lsm_experts_params* p, bool backward) {
 }
 
 // Tiles of the products over pairs, whose rows are ragged, and of the weights' gradients.
+// Up to 16 tokens the rounding of what goes from one product into the next is kept as a row of its own behind it: an expert's rows are
+// still one tile, the weights are read once, and with bf16 elements the result's rounding is the only one that counts (without: errors
+// of 1.41 times it).
+int halves_of(const lsm_experts_params& p) { return p.dtype == LSM_DTYPE_BF16 && p.n <= 16 ? 2 : 1; }
+
 struct Plan { int up, down, hidden, dx, dw1, dw2; };
 int64_t tiles_of_rows(const lsm_experts_params& p, int rows) {  // about: every expert's last tile is half empty
     const int64_t pairs = int64_t(p.n) * p.top_k, active = pairs < p.E ? pairs : p.E, full = pairs / rows + active / 2;
@@ -397,7 +427,8 @@ int64_t tiles_of_rows(const lsm_experts_params& p, int rows) {  // about: every 
 Plan plan_of(const lsm_experts_params& p) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
     const auto rows = [&](int cols, int K, int parts) {
-        return pick_tile(f32, K, [&](const TileSize& t) { return tiles_of_rows(p, t.rows) * up(cols, t.cols / parts); }, f32 ? 0x7e : 0x7f);
+        return pick_tile(f32, K, [&](const TileSize& t) { return tiles_of_rows(p, t.rows) * up(cols, t.cols / parts); },
+                         halves_of(p) == 2 ? 0x78 : f32 ? 0x7e : 0x7f);
     };
     const int64_t mean = (int64_t(p.n) * p.top_k + p.E - 1) / p.E;
     const auto square = [&](int r, int c) {
@@ -408,19 +439,21 @@ Plan plan_of(const lsm_experts_params& p) {
 int weight_parts(const lsm_experts_params& p, int kind) { return up(p.F, kTiles[kind].cols / 2) * kTiles[kind].waves; }
 int stretch_of(int kind) { return kTiles[kind].cols / kTiles[kind].waves; }
 // The most tiles there can be: every expert's last one may be almost empty.
-int64_t most_tiles(int64_t pairs, int E, int rows, int cols) { return (pairs / rows + (pairs < E ? pairs : int64_t(E))) * cols; }
+int64_t most_tiles(int64_t pairs, int E, int rows, int cols, int halves) {
+    return (pairs * halves / rows + (pairs < E ? pairs : int64_t(E))) * cols;
+}
 bool fits(const lsm_experts_params& p, bool backward) {
     const Plan q = plan_of(p);
     const auto rows = [&](int kind, int cols, int parts) {
-        return most_tiles(int64_t(p.n) * p.top_k, p.E, kTiles[kind].rows, up(cols, kTiles[kind].cols / parts)) < kMostTiles;
+        return most_tiles(int64_t(p.n) * p.top_k, p.E, kTiles[kind].rows, up(cols, kTiles[kind].cols / parts), halves_of(p)) < kMostTiles;
     };
     const auto square = [&](int kind, int r, int c) { return int64_t(p.E) * up(r, kTiles[kind].rows) * up(c, kTiles[kind].cols) < kMostTiles; };
     if (!backward) return rows(q.up, p.F, 2) && rows(q.down, p.D, 1);
     return rows(q.hidden, p.F, 2) && rows(q.dx, p.D, 1) && square(q.dw1, 2 * p.F, p.D) && square(q.dw2, p.D, p.F);
 }
 template <typename T>
-unsigned grid_of(const ExpertArgs& a, int cols) {
-    const unsigned all = unsigned((most_tiles(int64_t(a.n) * a.top_k, a.E, T::BR, cols) + 7) / 8 * 8);
+unsigned grid_of(const ExpertArgs& a, int cols, int halves = 1) {
+    const unsigned all = unsigned((most_tiles(int64_t(a.n) * a.top_k, a.E, T::BR, cols, halves) + 7) / 8 * 8);
     return T::FOLLOWED && all > 256 ? 256 : all;  // one for each compute unit
 }
 
@@ -434,10 +467,10 @@ Space space(const lsm_experts_params& p, bool backward) {
     const Plan q = plan_of(p);
     Space s{};
     s.h = 0;
-    s.part = align256(pairs * line_bytes(p.F * el));
+    s.part = align256(pairs * (backward ? 1 : halves_of(p)) * line_bytes(p.F * el));
     s.part_scale = s.part + align256(pairs * p.D * el);
     s.da = s.part_scale + (el == 2 ? align256(pairs * up(p.D, stretch_of(backward ? q.dx : q.down)) * 4) : 0);
-    s.weight_part = s.da + (backward ? align256(pairs * line_bytes(2 * p.F * el)) : 0);
+    s.weight_part = s.da + (backward ? align256(pairs * halves_of(p) * line_bytes(2 * p.F * el)) : 0);
     s.bytes = s.weight_part + (backward ? align256(pairs * weight_parts(p, q.hidden) * 4) : 0);
     return s;
 }
@@ -462,7 +495,7 @@ template <typename TIO, int KIND>
 bool launch_down(const ExpertArgs& a, hipStream_t st) {
     typedef typename TileOf<TIO, BY_ROWS, BY_ROWS, KIND, false, false, false, true>::type T;
     ProfScope ps(KID_EXPERTS_DOWN, st);
-    hipLaunchKernelGGL((k_down<T>), dim3(grid_of<T>(a, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_down<T>), dim3(grid_of<T>(a, up(a.D, T::BC), a.halves)), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND>
@@ -477,7 +510,7 @@ template <typename TIO, int KIND>
 bool launch_dx(const ExpertArgs& a, hipStream_t st) {
     typedef typename TileOf<TIO, BY_COLS, BY_ROWS, KIND, false, false, false, true>::type T;
     ProfScope ps(KID_EXPERTS_DX, st);
-    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of<T>(a, up(a.D, T::BC))), dim3(T::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_dx<T>), dim3(grid_of<T>(a, up(a.D, T::BC), a.halves)), dim3(T::THREADS), 0, st, a);
     return launched();
 }
 template <typename TIO, int KIND, bool DOWN>
@@ -544,7 +577,7 @@ int lsm_moe_experts(const lsm_experts_params* p, const void* x, const float* wei
     a.x = x; a.w_gate_up = w_gate_up; a.w_down = w_down; a.residual = residual; a.weights = weights;
     a.offsets = offsets; a.order = order; a.place = place; a.y = y;
     a.h = ws + s.h; a.part = ws + s.part; a.part_scale = reinterpret_cast<float*>(ws + s.part_scale);
-    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k;
+    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k; a.halves = halves_of(*p);
     a.x_bytes = uint32_t(p->x_stride) * el;
     a.h_bytes = uint32_t(line_bytes(p->F * el));
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -574,7 +607,7 @@ int lsm_moe_experts_bwd(const lsm_experts_params* p, const void* x, const float*
     a.d_w_gate_up = d_w_gate_up; a.d_w_down = d_w_down;
     a.h = ws + s.h; a.part = ws + s.part; a.part_scale = reinterpret_cast<float*>(ws + s.part_scale);
     a.da = ws + s.da; a.weight_part = reinterpret_cast<float*>(ws + s.weight_part);
-    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k;
+    a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k; a.halves = halves_of(*p);
     a.x_bytes = uint32_t(p->x_stride) * el;
     a.h_bytes = uint32_t(line_bytes(p->F * el));
     a.dy_bytes = uint32_t(p->dy_stride) * el;

@@ -280,6 +280,23 @@ def test_gradients_against_differences():
         assert abs(float((got[grad].double() * way.double()).sum()) - want) <= 2e-3 * size, name
 
 
+@pytest.mark.parametrize("n,D,F,E,k", [(1, 256, 136, 4, 1), (1, 1032, 520, 16, 4), (5, 264, 2056, 8, 2), (16, 72, 264, 1, 1), (16, 520, 136, 40, 16)])
+def test_few_tokens_are_rounded_once(n, D, F, E, k):
+    """Up to 16 tokens only the result is rounded to bf16 (half a step, 2^-8 of it); a pair's row to half precision before that: with a
+    power of two for a stretch of it, so 2^-11 of each number, or 2^-25 of the stretch's largest; and what is left of a number that is rounded in two
+    halves is 2^-16 of it, spread over the sum as the spread of its products is.  fp32 sums as everywhere in this file."""
+    import torch
+    a = make(n, D, F, E, k, "bf16", seed=n + D, residual=False)
+    got = run(a)
+    want, spread = reference(a)
+    for name in ("y", "dx"):
+        parts = 2.0 ** -11 * 7 * spread[name].square().mean(-1, keepdim=True).sqrt().clamp(min=0)
+        scale = torch.maximum(spread[name], spread[name].square().mean(-1, keepdim=True).sqrt())
+        tol = 2.0 ** -8 * want[name].abs() + parts * k ** 0.5 + (10 * 2.0 ** -16 + 7 * 2.0 ** -16) * scale
+        err = (got[name].double() - want[name]).abs()
+        assert (err <= tol).all(), (name, float((err / tol.clamp(min=1e-300)).max()))
+
+
 def test_frozen_experts():
     import torch
     a = make(40, 64, 40, 3, 2, "bf16", seed=13)
