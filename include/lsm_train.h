@@ -145,7 +145,8 @@ int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, cons
  *   dx         [n, D]; 0 for tokens that are left out                                               out
  *   dw         [V, D], or NULL (not wanted)                                                        out
  *   workspace  at least lsm_vocab_loss_bwd_workspace_bytes(p) (0 for invalid params)
- * With bf16 elements the gradient of the logits is rounded to bf16 on its way into the next products.
+ * With bf16 elements the gradient of the logits is rounded to bf16 on its way into the next products (of up to 16 tokens: with what
+ * the rounding leaves).
  */
 size_t lsm_vocab_loss_bwd_workspace_bytes(const lsm_vocab_params* p);
 int lsm_vocab_loss_bwd(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,

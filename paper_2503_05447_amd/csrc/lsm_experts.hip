@@ -45,17 +45,9 @@ template <typename TIO> __device__ __forceinline__ TIO* row_of(void* rows, int a
     return reinterpret_cast<TIO*>(static_cast<char*>(rows) + size_t(at) * bytes);
 }
 
-// What rounding x to bf16 leaves; nothing where it is not finite.
-__device__ __forceinline__ float remainder_of(float x) {
-    const float r = x - bf16_lo(pack2(x, 0.f));
-    return fabsf(r) < __builtin_inff() ? r : 0.f;
-}
 __device__ __forceinline__ f32x4 remainders(const f32x4& x) {
     return f32x4{remainder_of(x[0]), remainder_of(x[1]), remainder_of(x[2]), remainder_of(x[3])};
 }
-// Tiles that are taken for few rows: they can hold two of a pair.
-template <typename T> constexpr bool kMayHalve = sizeof(typename T::TIO) == 2 && T::BR <= 64;
-
 struct Where { int e, first, count, r, c; };  // expert, its first place and its pairs, the tile's number along rows and columns
 
 // The tiles of a workgroup, of all experts' tiles of BR rows x `cols` columns in the order expert, column, row.  Workgroups are dealt out

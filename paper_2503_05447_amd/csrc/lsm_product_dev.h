@@ -173,6 +173,12 @@ struct Operand {
     }
 };
 
+// What rounding x to bf16 leaves; nothing where it is not finite.
+__device__ __forceinline__ float remainder_of(float x) {
+    const float r = x - bf16_lo(pack2(x, 0.f));
+    return fabsf(r) < __builtin_inff() ? r : 0.f;
+}
+
 // A tile: WC x WR waves of TC x TR blocks of 16 x 16.  FOLLOWED: the workgroup goes on to another tile with the same kinds of operands and
 // the same K; the first pieces of that one are requested in the last steps of this one, and come while its results are written.
 template <typename TIO_, Layout LC, Layout LR, int WC_, int WR_, int TC_, int TR_, int NBUF_, bool LIST_C = false, bool LIST_R = false,
@@ -428,8 +434,8 @@ struct Tile {
         wave_meets();
     }
     // line(r): where row r of the tile goes, from the first of the N blocks' columns on, or null; width: columns that there are from there on.
-    // ADD: to what is there already (TOUT's own sum).
-    template <int N, typename TOUT, bool ADD = false, typename Line>
+    // ADD: to what is there already (TOUT's own sum); REST: what rounding to bf16 leaves of the results.
+    template <int N, typename TOUT, bool ADD = false, bool REST = false, typename Line>
     __device__ __forceinline__ void take(int j, int width, Line line) const {
         constexpr int E = 16 / int(sizeof(TOUT)), LANES = N * 16 / E, ROWS_ = 64 / LANES;
         wave_meets();
@@ -439,7 +445,7 @@ struct Tile {
             float v[E];
             _Pragma("unroll") for (int q = 0; q < E / 4; ++q) {
                 const f32x4 x = *reinterpret_cast<__attribute__((address_space(3))) const f32x4*>(uintptr_t(cell<N>(row, c + 4 * q)));
-                _Pragma("unroll") for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
+                _Pragma("unroll") for (int e = 0; e < 4; ++e) v[4 * q + e] = REST ? remainder_of(x[e]) : x[e];
             }
             TOUT* to = line((wr * TR + j) * 16 + row);
             if (!to || c >= width) continue;
@@ -475,6 +481,9 @@ struct Tile {
         }
     }
 };
+
+// Tiles that are taken for few rows: they can hold two rows of a result, with what its rounding leaves.
+template <typename T> constexpr bool kMayHalve = sizeof(typename T::TIO) == 2 && T::BR <= 64;
 
 // Rows of one call's own use in 16 bits: fp16 times a power of two for each stretch of a row, so that the stretch's largest finite number is
 // about 2^14.  Off by at most 2^-11 of a number's size, an eighth of what bf16 is, at half of fp32's traffic.

@@ -41,6 +41,7 @@ struct VocabArgs {
     int v0, width, piece;     // the piece: its first column, how many, and how many the gradient's rows hold (a multiple of 256)
     Shares here, before[kPieceKinds];  // of this piece, of the kinds of pieces that were before
     int kinds;                // of them
+    int halves;               // rows of a token in grad: 2 where a remainder follows what was rounded
     uint32_t x_bytes;
     float scale;              // 1 / temperature
 };
@@ -367,9 +368,15 @@ __global__ __launch_bounds__(T::THREADS) void k_grad(VocabArgs a) {
                     });
                 }
                 // the columns behind the vocabulary's end are zeros that the next products read
-                t.template take<N, TIO>(j, a.piece - column - i0 * 16, [&](int q) {
-                    return r0 + q < rows ? static_cast<TIO*>(a.grad) + size_t(r0 + q) * a.piece + column + i0 * 16 : nullptr;
-                });
+                const int halves = kMayHalve<T> ? a.halves : 1;
+                const auto line = [&](int half) {
+                    return [=](int q) {
+                        return r0 + q < rows ? static_cast<TIO*>(a.grad) + size_t((r0 + q) * halves + half) * a.piece + column + i0 * 16 : nullptr;
+                    };
+                };
+                t.template take<N, TIO>(j, a.piece - column - i0 * 16, line(0));
+                if constexpr (kMayHalve<T>)
+                    if (halves == 2) t.template take<N, TIO, false, true>(j, a.piece - column - i0 * 16, line(1));
             }
         }
     });
@@ -390,7 +397,7 @@ __global__ __launch_bounds__(T::THREADS) void k_dw(VocabArgs a) {
     t.c.start_cols(a.x, int(a.x_bytes), c * T::BC, a.D, t.wave, t.lane, t.list_at());
     f32x4 acc[T::TC][T::TR];
     clear<T>(acc);
-    t.walk(acc, rows, [&](int k) { return token_of(a, k); });
+    t.walk(acc, rows * a.halves, [&](int k) { return token_of(a, k >> (a.halves - 1)); });
     const int c0 = c * T::BC + t.wc * T::TC * 16;
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
         t.template store<T::TC, TIO>(j, a.D - c0, [&](int i) { return acc[i][j]; }, [&](int q) {
@@ -418,14 +425,14 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     typedef typename T::TIO TIO;
     constexpr int EL = int(sizeof(TIO)), STEP = kStepBytes / EL;
     __shared__ __attribute__((aligned(1024))) char shared[T::LDS];
-    const int width = a.width, rows = rows_of(a);
-    const int rt = (rows + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, shares = shares_of(a.here, a.n, rows), id = number_of_tile(rt * ct * shares);
+    const int width = a.width, tokens = rows_of(a), halves = kMayHalve<T> ? a.halves : 1, rows = tokens * halves;
+    const int rt = (rows + T::BR - 1) / T::BR, ct = (a.D + T::BC - 1) / T::BC, shares = shares_of(a.here, a.n, tokens), id = number_of_tile(rt * ct * shares);
     if (id < 0) return;
     const int share = id / (rt * ct);
     int r, c;
     tile_at(id - share * rt * ct, rt, ct, r, c);
     const int steps = (width + STEP - 1) / STEP, k0 = steps * share / shares * STEP, k1 = min(width, steps * (share + 1) / shares * STEP);
-    const int r0 = r * T::BR, begun = shares_before(a, rows);
+    const int r0 = r * T::BR, begun = shares_before(a, tokens);
     const uint32_t bytes = uint32_t(a.piece) * EL;
     T t(shared);
     t.r.start_rows(static_cast<const TIO*>(a.grad) + size_t(r0) * a.piece + k0, t.wave, t.lane,
@@ -435,7 +442,15 @@ __global__ __launch_bounds__(T::THREADS) void k_dx(VocabArgs a) {
     clear<T>(acc);
     t.walk(acc, k1 - k0);
     const int c0 = c * T::BC + t.wc * T::TC * 16;
-    const auto line = [&](int q) { return r0 + q < rows ? a.part + (size_t(share) * rows + r0 + q) * a.D + c0 : nullptr; };
+    if constexpr (kMayHalve<T>)
+        if (halves == 2)  // both rows of a token, in neighbouring lanes
+            _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
+                _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
+                    _Pragma("unroll") for (int e = 0; e < 4; ++e) acc[i][j][e] += dpp<0xB1>(acc[i][j][e]);
+    const auto line = [&](int q) {
+        const int at = r0 + q;
+        return at < rows && (at & (halves - 1)) == 0 ? a.part + (size_t(share) * tokens + (at >> (halves - 1))) * a.D + c0 : nullptr;
+    };
     _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
         if (share >= begun) t.template store<T::TC, float>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
         else t.template store<T::TC, float, true>(j, a.D - c0, [&](int i) { return acc[i][j]; }, line);
@@ -486,10 +501,15 @@ int logits_tile(const lsm_vocab_params& p) {
 // and into how many shares dx takes the piece.  dw's products are as long as there are tokens, so that a last round of a few tiles takes
 // as long as a full one: a piece ends with a full round where less than half of the next one would be left, and what is left is a
 // piece with smaller tiles (8191 tokens, 50257 x 2048: dw 1140 -> 990 us).
+// Up to 16 tokens the rounding of the logits' gradient is kept as a row of its own behind it: the rows are still one tile, and with bf16 elements
+// the results' rounding is the only one that counts (without: errors of 1.41 times it, and of a single token up to twice, as all of
+// its results hang on its target's one number).
+int halves_of(const lsm_vocab_params& p) { return p.dtype == LSM_DTYPE_BF16 && p.n <= 16 ? 2 : 1; }
+
 struct Piece { int width, grad, dw, dx, shares; int64_t tiles, rows; };  // tiles: the most of its launches; rows: of sums for dx
 Piece piece_of(const lsm_vocab_params& p, int left) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
-    const unsigned kinds = f32 ? 0x7e : 0x7f;
+    const unsigned kinds = halves_of(p) == 2 ? 0x78 : f32 ? 0x7e : 0x7f;
     Piece q{};
     int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256;  // in tiles of 256 columns
     if (most < 1) most = 1;
@@ -563,7 +583,7 @@ Space space(const lsm_vocab_params& p, bool backward) {
         s.at_entry = take((K ? K : 1) * n * 4);
     } else {
         const Piece q = largest_piece(p);
-        s.grad = take(n * q.width * el);
+        s.grad = take(n * halves_of(p) * q.width * el);
         s.part = take(size_t(q.rows) * p.D * 4);
     }
     s.bytes = at;
@@ -586,6 +606,7 @@ VocabArgs arguments(const lsm_vocab_params& p, const Space& s, char* ws, const v
     a.grad = ws + s.grad;
     a.part = reinterpret_cast<float*>(ws + s.part);
     a.n = p.n; a.D = p.D; a.V = p.V; a.K = p.K; a.groups = groups_of(p);
+    a.halves = halves_of(p);
     a.x_bytes = uint32_t(p.x_stride) * (p.dtype == LSM_DTYPE_BF16 ? 2 : 4);
     a.scale = 1.f / p.temperature;
     return a;

@@ -137,6 +137,22 @@ def test_entries_close_together(dtype, n, V, K, where):
     check(a)
 
 
+@pytest.mark.parametrize("K", [0, 9])
+@pytest.mark.parametrize("n,D,V", [(1, 64, 777), (1, 1032, 50), (3, 264, 20001), (16, 136, 3001), (16, 2056, 700)])
+def test_few_tokens_are_rounded_once(n, D, V, K):
+    """Up to 16 tokens only dx and dw are rounded to bf16 (half a step, 2^-8); what is left of a number in two halves is 2^-16 of it.  fp32 as in
+    check()."""
+    import torch
+    a = make(n, D, V, K, "bf16", seed=n + V)
+    got = run(a)
+    want, spread, moved, length = reference(a)
+    for name in ("dx", "dw"):
+        tol = 2.0 ** -15 * moved[name] + (10 * 2.0 ** -23 * math.sqrt(length[name]) + 2.0 ** -20 + 7 * 2.0 ** -16) * spread[name]
+        err = (got[name].double() - want[name]).abs()
+        tol = tol + 2.0 ** -8 * want[name].abs() + 1e-30
+        assert (err <= tol).all(), (name, float((err / tol).max()))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_temperatures(dtype):
     for tau in (0.5, 3.0):
