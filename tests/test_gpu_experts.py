@@ -197,7 +197,7 @@ def test_many_experts(dtype, n, E, k):
 def test_what_the_workspace_held_does_not_matter(dtype):
     """Workspaces of NaN (all bits set), widths that are neither whole tiles nor whole lines of the caches."""
     import torch
-    for n, D, F in ((37, 72, 104), (300, 136, 40), (2100, 264, 72)):
+    for n, D, F in ((9, 72, 104), (37, 72, 104), (300, 136, 40), (2100, 264, 72)):
         a = make(n, D, F, 5, 2, dtype, seed=n, dropped=0.2)
         want = run(a)
         plan = lsm().lsm_moe_plan(a["chosen"], 5)
