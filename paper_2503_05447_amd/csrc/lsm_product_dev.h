@@ -389,11 +389,13 @@ struct Tile {
         }
         end_step(t);
     }
-    // On to the following tile, when all that this wave had to write is on its way.
+    // On to the following tile, when all that this wave had to write is on its way.  Pieces are requested into its place of the ring next, so
+    // what it wrote there is waited for: a wave that stores nothing (rows behind the last, columns behind the width) has read none of it back.
     __device__ __forceinline__ void go_on() {
         c = c2;
         r = r2;
         ahead = true;
+        wait_lds();
         barrier();
     }
 

@@ -120,6 +120,23 @@ def test_every_tile(dtype, n, D, F, E, k):
     check(make(n, D, F, E, k, dtype, seed=n + F, skew=0.5, dropped=0.1))
 
 
+# The largest tiles in more number than there are compute units, so that workgroups go on to a second and a third: 298 or 550 tiles of rows, one to
+# four of columns; products of 2, 3, 4, 5, 9 and 13 steps (a step is 32 numbers), of which those below five are filled up.
+@pytest.mark.parametrize("full,D,F", [(45, 128, 72), (45, 136, 72), (24, 264, 64), (24, 392, 264)])
+def test_tiles_that_follow_one_another(full, D, F):
+    """Every expert has `full` whole tiles of 256 rows and a last one of 1, 64, 65, 128, 129 or no rows: waves with rows behind the last, and columns
+    behind the widths, store nothing between two tiles."""
+    import torch
+    last = [1, 64, 65, 128, 129, 0, 0, 129, 128, 65, 64, 1]
+    experts = torch.cat([torch.full((256 * full + r,), e, dtype=torch.int32) for e, r in enumerate(last)] + [torch.full((37,), -1, dtype=torch.int32)])
+    n = experts.numel()
+    a = make(n, D, F, 12, 1, "bf16", seed=D + F)
+    gen = torch.Generator().manual_seed(full)
+    a["chosen"] = experts[torch.randperm(n, generator=gen)][:, None].cuda()
+    a["weights"] = (0.25 + torch.rand(n, 1, generator=gen)).cuda()
+    check(a)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_longer_list_than_is_held_at_a_time(dtype):
     """Weight gradients over 5000 pairs of an expert: the list of rows (2048 at a time) is filled again and again."""
