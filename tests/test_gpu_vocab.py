@@ -123,6 +123,16 @@ def test_every_tile(dtype, K, n, D, V):
     check(make(n, D, V, K, dtype, seed=n + V, left_out=0.1 if n > 3 else 0.0))
 
 
+# The largest tiles in more number than there are compute units, so that workgroups go on to a second and a third: `rows` of the tokens count, a
+# last tile of 1, 64, 129 or all of its 256 rows; products of 1, 5 and 9 steps (a step is 32 numbers), of which those below five are filled up.
+@pytest.mark.parametrize("n,D,V,rows", [(3000, 24, 9001, 2561), (3000, 24, 9001, 2816), (4001, 136, 9001, 3969), (6000, 264, 5001, 5184)])
+def test_tiles_that_follow_one_another(n, D, V, rows):
+    import torch
+    a = make(n, D, V, 0, "bf16", seed=rows)
+    a["index"][torch.randperm(n, generator=torch.Generator().manual_seed(V))[rows:].cuda()] = -100
+    check(a)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,V,K,where", [(70, 2047, 70, (490, 540)), (33, 1024, 256, (0, 1024)), (300, 513, 5, (508, 513)), (5, 70001, 66, (511, 514)),
                                          (64, 4096, 64, (4032, 4096))])
