@@ -82,9 +82,9 @@ typedef struct {
  *   residual   [n, D] or NULL (= 0)                                                                 in
  *   y          [n, D]                                                                               out
  *   workspace  at least lsm_moe_experts_workspace_bytes(p) (0 for invalid params)
- * Products of the elements as they are, sums in fp32; with bf16 elements the hidden activations (of more than 16 tokens; of fewer
- * what the rounding leaves goes along) and the result are rounded to bf16, and a pair's row of Wd h, before its weight, to the 11 bits of a half with a power of two for every 32 to 128 columns.  A
- * number that is not finite in x reaches the rows of its token alone.
+ * Products of the elements as they are, sums in fp32, over a token's pairs too; with bf16 elements the result is rounded to bf16, and in
+ * calls of more than 16 tokens the hidden activations as well (in smaller calls what their rounding leaves goes along).  A number that is
+ * not finite in x reaches the rows of its token alone.
  */
 size_t lsm_moe_experts_workspace_bytes(const lsm_experts_params* p);
 int lsm_moe_experts(const lsm_experts_params* p, const void* x, const float* weights, const int32_t* offsets, const int32_t* order,
@@ -100,7 +100,8 @@ int lsm_moe_experts(const lsm_experts_params* p, const void* x, const float* wei
  *   d_w_gate_up  [E, 2 F, D], d_w_down [E, D, F]; 0 for an expert without tokens                      out
  *   workspace    at least lsm_moe_experts_bwd_workspace_bytes(p) (0 for invalid params)
  * With bf16 elements the hidden activations' gradients, and the activations times their weight, are rounded to bf16 on their way
- * into the next product (dx of up to 16 tokens: with what the rounding leaves), and a pair's row of dx as the forward call's.  d_w_gate_up and d_w_down: both or neither (NULL: not wanted, as in a layer whose experts are frozen).
+ * into the next product (for dx in calls of up to 16 tokens: with what the rounding leaves).
+ * d_w_gate_up and d_w_down: both or neither (NULL: not wanted, as in a layer whose experts are frozen).
  */
 size_t lsm_moe_experts_bwd_workspace_bytes(const lsm_experts_params* p);
 int lsm_moe_experts_bwd(const lsm_experts_params* p, const void* x, const float* weights, const int32_t* offsets,

@@ -15,8 +15,8 @@
 // 776, 2 a token: 55, 37, 5, 86, 68, 7, 76 and 45 us, 50 to 82 TFLOP/s.
 // Nothing is saved by the forward call: gate and factor formed again cost 500 us there, kept they would be 0.5 GB a layer.  A pair's result is a
 // row of its own, added up by k_sum in a fixed order: adding to the token's row at once would need atomics, whose order is not fixed.
-#include <type_traits>
-
+// These rows are parts of a token's sum and stay in fp32: as fp16 with a power of two for each stretch of a row they would take half the bytes
+// (16384 tokens forward and backward 3520 -> 3365 us, five tokens 44.4 -> 46.1), and move one result in sixteen to a neighbouring bf16.
 #include "lsm_product_dev.h"
 
 namespace lsm {
@@ -29,9 +29,8 @@ struct ExpertArgs {
     void *y, *d_w_gate_up, *d_w_down;
     float* d_weights;
     void *h, *da;         // [pairs][F]: activations (backward: times their weight); [pairs][2 F]; rows from line to line
-    void* part;           // [pairs][D]: fp32, or with bf16 elements fp16 times part_scale
-    float *part_scale, *weight_part;  // [stretches of D][pairs]; [tiles of F][pairs]
-    int n, D, F, E, top_k, parts, stretch;
+    float *part, *weight_part;  // [pairs][D]; [tiles of F][pairs]
+    int n, D, F, E, top_k, parts;
     int halves;             // rows of a pair in h (forward) or da (backward): 2 where a remainder follows what was rounded
     uint32_t x_bytes, dy_bytes, h_bytes, da_bytes;  // between rows
 };
@@ -160,34 +159,17 @@ __global__ __launch_bounds__(T::THREADS) void k_up(ExpertArgs a) {
 // rows of `part` = the tile's
 template <typename T>
 __device__ __forceinline__ void finish_part(const T& t, const ExpertArgs& a, const Where& w, f32x4 (&acc)[T::TC][T::TR]) {
-    constexpr bool HALF = sizeof(typename T::TIO) == 2;
-    typedef typename std::conditional<HALF, half_t, float>::type TP;
-    const int stretch = w.c * T::WC + t.wc, d0 = stretch * T::TC * 16, halves = kMayHalve<T> ? a.halves : 1;
+    const int d0 = (w.c * T::WC + t.wc) * T::TC * 16, halves = kMayHalve<T> ? a.halves : 1;
     if constexpr (kMayHalve<T>)
         if (halves == 2)  // both rows of a pair, in neighbouring lanes
             _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
                 _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
                     _Pragma("unroll") for (int e = 0; e < 4; ++e) acc[i][j][e] += dpp<0xB1>(acc[i][j][e]);
-    const auto pair_of_row = [=, &w](int row) { return row < w.count && (row & (halves - 1)) == 0 ? (w.first + row) >> (halves - 1) : -1; };
-    float scale[T::TR];
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        scale[j] = 1.f;
-        if (!HALF) continue;
-        float m = 0.f;
-        _Pragma("unroll") for (int i = 0; i < T::TC; ++i)
-            _Pragma("unroll") for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_size(acc[i][j][e]));
-        scale[j] = scale_for(T::row_max(m));
-    }
-    _Pragma("unroll") for (int j = 0; j < T::TR; ++j) {
-        t.template store<T::TC, TP>(
-            j, a.D - d0, [&](int i) { return acc[i][j] * scale[j]; },
-            [&](int r) {
-                const int at = pair_of_row(w.r * T::BR + r);
-                return at >= 0 ? static_cast<TP*>(a.part) + size_t(at) * a.D + d0 : nullptr;
-            });
-        const int at = pair_of_row(w.r * T::BR + t.row(j));
-        if (HALF && t.lane < 16 && at >= 0 && d0 < a.D) a.part_scale[size_t(stretch) * (size_t(a.n) * a.top_k) + at] = 1.f / scale[j];
-    }
+    _Pragma("unroll") for (int j = 0; j < T::TR; ++j)
+        t.template store<T::TC, float>(j, a.D - d0, [&](int i) { return acc[i][j]; }, [&](int r) {
+            const int row = w.r * T::BR + r;
+            return row < w.count && (row & (halves - 1)) == 0 ? a.part + size_t((w.first + row) >> (halves - 1)) * a.D + d0 : nullptr;
+        });
 }
 // rows of the pairs of this tile, `bytes` each, one after the other
 template <typename T>
@@ -363,7 +345,7 @@ __global__ __launch_bounds__(256) void k_sum(ExpertArgs a) {
     for (int j0 = 0; j0 < a.top_k; j0 += U) {
         int at[U];
         float p[U];
-        u32x4 z[U];
+        f32x4 z[U][E / 4];
         _Pragma("unroll") for (int u = 0; u < U; ++u) {
             at[u] = j0 + u < a.top_k ? a.place[size_t(t) * a.top_k + j0 + u] : -1;
             if (uint32_t(at[u]) >= uint32_t(a.n * a.top_k)) at[u] = -1;
@@ -371,17 +353,13 @@ __global__ __launch_bounds__(256) void k_sum(ExpertArgs a) {
         }
         _Pragma("unroll") for (int u = 0; u < U; ++u) {
             if (at[u] < 0) continue;
-            if (E == 8) p[u] *= a.part_scale[size_t(d / a.stretch) * (size_t(a.n) * a.top_k) + at[u]];
-            z[u] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.part) + (size_t(at[u]) * a.D + d) * sizeof(TIO));
+            _Pragma("unroll") for (int i = 0; i < E / 4; ++i)
+                z[u][i] = *reinterpret_cast<const f32x4*>(a.part + size_t(at[u]) * a.D + d + 4 * i);
         }
         _Pragma("unroll") for (int u = 0; u < U; ++u) {
             if (at[u] < 0) continue;
-            if constexpr (E == 8) {
-                const f16x8 v = __builtin_bit_cast(f16x8, z[u]);
-                _Pragma("unroll") for (int e = 0; e < 8; ++e) s[e] += p[u] * float(v[e]);
-            } else {
-                _Pragma("unroll") for (int e = 0; e < 4; ++e) s[e] += p[u] * __uint_as_float(z[u][e]);
-            }
+            _Pragma("unroll") for (int i = 0; i < E / 4; ++i)
+                _Pragma("unroll") for (int e = 0; e < 4; ++e) s[4 * i + e] += p[u] * z[u][i][e];
         }
     }
     *reinterpret_cast<u32x4*>(static_cast<TIO*>(a.y) + size_t(t) * a.D + d) = pack(s);
@@ -429,7 +407,6 @@ Plan plan_of(const lsm_experts_params& p) {
     return Plan{rows(p.F, p.D, 2), rows(p.D, p.F, 1), rows(p.F, p.D + p.D / 2, 2), rows(p.D, 2 * p.F, 1), square(2 * p.F, p.D), square(p.D, p.F)};
 }
 int weight_parts(const lsm_experts_params& p, int kind) { return up(p.F, kTiles[kind].cols / 2) * kTiles[kind].waves; }
-int stretch_of(int kind) { return kTiles[kind].cols / kTiles[kind].waves; }
 // The most tiles there can be: every expert's last one may be almost empty.
 int64_t most_tiles(int64_t pairs, int E, int rows, int cols, int halves) {
     return (pairs * halves / rows + (pairs < E ? pairs : int64_t(E))) * cols;
@@ -453,15 +430,14 @@ unsigned grid_of(const ExpertArgs& a, int cols, int halves = 1) {
 // width is not whole lines (2047 tokens, 64 experts of 1032: Wd h 173 -> 163 us).
 size_t line_bytes(size_t bytes) { return (bytes + 127) / 128 * 128; }
 
-struct Space { size_t h, da, part, part_scale, weight_part, bytes; };
+struct Space { size_t h, da, part, weight_part, bytes; };
 Space space(const lsm_experts_params& p, bool backward) {
     const size_t pairs = size_t(p.n) * p.top_k, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4;
     const Plan q = plan_of(p);
     Space s{};
     s.h = 0;
     s.part = align256(pairs * (backward ? 1 : halves_of(p)) * line_bytes(p.F * el));
-    s.part_scale = s.part + align256(pairs * p.D * el);
-    s.da = s.part_scale + (el == 2 ? align256(pairs * up(p.D, stretch_of(backward ? q.dx : q.down)) * 4) : 0);
+    s.da = s.part + align256(pairs * p.D * 4);
     s.weight_part = s.da + (backward ? align256(pairs * halves_of(p) * line_bytes(2 * p.F * el)) : 0);
     s.bytes = s.weight_part + (backward ? align256(pairs * weight_parts(p, q.hidden) * 4) : 0);
     return s;
@@ -517,7 +493,6 @@ bool launch_dw(const ExpertArgs& a, hipStream_t st) {
 template <typename TIO>
 bool launch(const lsm_experts_params& p, ExpertArgs a, bool backward, hipStream_t st) {
     const Plan q = plan_of(p);
-    a.stretch = stretch_of(backward ? q.dx : q.down);
     a.parts = weight_parts(p, q.hidden);
 #define LSM_KIND(call, kind)                                                                                     \
     ((kind) == 0 ? call(0) : (kind) == 1 ? call(1) : (kind) == 2 ? call(2) : (kind) == 3 ? call(3) : (kind) == 4 ? call(4) \
@@ -568,7 +543,7 @@ int lsm_moe_experts(const lsm_experts_params* p, const void* x, const float* wei
     ExpertArgs a{};
     a.x = x; a.w_gate_up = w_gate_up; a.w_down = w_down; a.residual = residual; a.weights = weights;
     a.offsets = offsets; a.order = order; a.place = place; a.y = y;
-    a.h = ws + s.h; a.part = ws + s.part; a.part_scale = reinterpret_cast<float*>(ws + s.part_scale);
+    a.h = ws + s.h; a.part = reinterpret_cast<float*>(ws + s.part);
     a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k; a.halves = halves_of(*p);
     a.x_bytes = uint32_t(p->x_stride) * el;
     a.h_bytes = uint32_t(line_bytes(p->F * el));
@@ -597,7 +572,7 @@ int lsm_moe_experts_bwd(const lsm_experts_params* p, const void* x, const float*
     a.x = x; a.w_gate_up = w_gate_up; a.w_down = w_down; a.d_y = d_y; a.weights = weights;
     a.offsets = offsets; a.order = order; a.place = place; a.y = dx; a.d_weights = d_weights;
     a.d_w_gate_up = d_w_gate_up; a.d_w_down = d_w_down;
-    a.h = ws + s.h; a.part = ws + s.part; a.part_scale = reinterpret_cast<float*>(ws + s.part_scale);
+    a.h = ws + s.h; a.part = reinterpret_cast<float*>(ws + s.part);
     a.da = ws + s.da; a.weight_part = reinterpret_cast<float*>(ws + s.weight_part);
     a.n = p->n; a.D = p->D; a.F = p->F; a.E = p->E; a.top_k = p->top_k; a.halves = halves_of(*p);
     a.x_bytes = uint32_t(p->x_stride) * el;

@@ -26,8 +26,6 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 half_t;
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kBeyond = 0xfffff000u;  // offset and size of a buffer: at or behind it nothing is read and zeros come
 constexpr int kStepBytes = kTileStepBytes;
@@ -451,12 +449,6 @@ struct Tile {
             }
             TOUT* to = line((wr * TR + j) * 16 + row);
             if (!to || c >= width) continue;
-            if constexpr (sizeof(TOUT) == 2 && !__is_same(TOUT, uint16_t)) {
-                f16x8 h;
-                _Pragma("unroll") for (int e = 0; e < E; ++e) h[e] = half_t(v[e]);
-                *reinterpret_cast<f16x8*>(to + c) = h;
-                continue;
-            }
             if (ADD) {
                 float old[E];
                 unpack(*reinterpret_cast<const u32x4*>(to + c), old);
@@ -486,17 +478,6 @@ struct Tile {
 
 // Tiles that are taken for few rows: they can hold two rows of a result, with what its rounding leaves.
 template <typename T> constexpr bool kMayHalve = sizeof(typename T::TIO) == 2 && T::BR <= 64;
-
-// Rows of one call's own use in 16 bits: fp16 times a power of two for each stretch of a row, so that the stretch's largest finite number is
-// about 2^14.  Off by at most 2^-11 of a number's size, an eighth of what bf16 is, at half of fp32's traffic.
-__device__ __forceinline__ float finite_size(float x) {
-    const float a = fabsf(x);
-    return a < __builtin_inff() ? a : 0.f;
-}
-__device__ __forceinline__ float scale_for(float largest) {  // 2^(14 - exponent of largest)
-    const int e = int(__float_as_uint(largest) >> 23);
-    return __uint_as_float(uint32_t(min(268 - e, 240)) << 23);
-}
 
 // 2^x and 1 / (1 + 2^-x) of x = log2(e) y.  For bf16 elements the hardware's power and reciprocal, each within 2^-23: what they give is
 // rounded to bf16 or summed over many; for fp32 elements the library's functions.

@@ -10,8 +10,7 @@ beside that along d.  With bf16 elements one operand of the last product has bee
 rounded: the activations (y), their gradients (dx, d_w_gate_up), the weighted activations (d_w_down).  Each rounding is off by at
 most 2^-8 of the value, independently: the standard deviation of a result's error is at most 2^-8 / sqrt(3) times the root of the sum of
 the squared products, which is formed in 64 bits too; seven of those are asked (some million results), and half a step, 2^-8, of the stored value.
-The pairs' rows between product and sum (fp16 with a scale: 2^-12 of a value or of the row's largest 2^-25) are inside that.  Routing
-weights' gradients are fp32 sums of unrounded numbers."""
+Routing weights' gradients are fp32 sums of unrounded numbers."""
 import math
 
 import pytest
@@ -312,6 +311,55 @@ def test_few_tokens_are_rounded_once(n, D, F, E, k):
         tol = 2.0 ** -8 * want[name].abs() + parts * k ** 0.5 + (10 * 2.0 ** -16 + 7 * 2.0 ** -16) * scale
         err = (got[name].double() - want[name]).abs()
         assert (err <= tol).all(), (name, float((err / tol.clamp(min=1e-300)).max()))
+
+
+def half_step(want):
+    """Of bf16, at each value: numbers of 2^e to 2^(e + 1) are 2^(e - 7) apart."""
+    import torch
+    return torch.ldexp(torch.ones_like(want), torch.frexp(want)[1] - 9)
+
+
+@pytest.mark.parametrize("n,D,F,E,k", [(16, 1032, 264, 4, 1), (16, 520, 136, 40, 16), (5, 2056, 520, 8, 2), (1, 2056, 1032, 16, 4)])
+def test_nothing_but_the_result_of_few_tokens_is_rounded(n, D, F, E, k):
+    """Up to 16 tokens: half a step of the result at its own size, and beside that what a remainder's own rounding leaves of activations and their
+    gradients, 2^-17 of each at most (2^-8 of a remainder that is 2^-9 of them), independently: 7 / sqrt(3) 2^-17 of the products' root sum of squares,
+    and seven standard deviations of 2^-24 * 2 sqrt(2056) for the fp32 sums of two products behind one another, below 7 * 2^-17 of their root mean square."""
+    import torch
+    a = make(n, D, F, E, k, "bf16", seed=n + F, residual=False)
+    got = run(a)
+    want, spread = reference(a)
+    for name in ("y", "dx"):
+        scale = torch.maximum(spread[name], spread[name].square().mean(-1, keepdim=True).sqrt())
+        tol = half_step(want[name]) + (7 / math.sqrt(3) + 7) * 2.0 ** -17 * scale
+        bad = ~((got[name].double() - want[name]).abs() <= tol)
+        assert not bad.any(), (name, int(bad.sum()))
+
+
+@pytest.mark.parametrize("n,E,k", [(5, 4, 2), (70, 3, 1), (300, 2, 2), (9000, 12, 4)])
+def test_a_pairs_row_is_whole_until_it_is_added(n, E, k):
+    """Activations that bf16 holds: the gate is 64, whose sigmoid is 1, the factor a whole number up to 96.  What is rounded is then the result alone: half a
+    step of it at its own size, and 2^-18 of the products' sum of sizes, for no more than 64 fp32 roundings of 2^-24 behind one another."""
+    import torch
+    D, F = 264, 40
+    gen = torch.Generator().manual_seed(n)
+    a = make(n, D, F, E, k, "bf16", seed=n, residual=False)
+    a["x"][:, 0] = 1
+    a["x"][:, 1:7] = torch.tensor([-2.0, -1.0, 1.0, 2.0])[torch.randint(0, 4, (n, 6), generator=gen)].to(a["x"])
+    a["w_gate_up"].zero_()
+    a["w_gate_up"][:, :F, 0] = 64
+    a["w_gate_up"][:, F:, 1:7] = torch.randint(-8, 9, (E, F, 6), generator=gen).to(a["x"])
+    plan = lsm().lsm_moe_plan(a["chosen"], E)
+    got = lsm().lsm_moe_experts(a["x"], a["weights"], plan, a["w_gate_up"], a["w_down"])
+    want, size = torch.zeros(n, D, dtype=torch.float64, device="cuda"), torch.zeros(n, D, dtype=torch.float64, device="cuda")
+    for j in range(k):
+        e = a["chosen"][:, j].long()
+        h = 64 * (a["x"][:, 1:7].double()[:, None] * a["w_gate_up"].double()[e, F:, 1:7]).sum(-1)
+        for f in range(F):
+            one = a["weights"][:, j, None].double() * h[:, f, None] * a["w_down"].double()[e, :, f]
+            want += one
+            size += one.abs()
+    bad = ~((got.double() - want).abs() <= half_step(want) + 2.0 ** -18 * size)
+    assert not bad.any(), int(bad.sum())
 
 
 def test_frozen_experts():
