@@ -499,8 +499,10 @@ int logits_tile(const lsm_vocab_params& p) {
 }
 // A piece of the vocabulary backward, of the `left` columns from the piece before on: how many, the tiles of the logits' gradient, of dw and dx,
 // and into how many shares dx takes the piece.  dw's products are as long as there are tokens, so that a last round of a few tiles takes
-// as long as a full one: a piece ends with a full round where less than half of the next one would be left, and what is left is a
-// piece with smaller tiles (8191 tokens, 50257 x 2048: dw 1140 -> 990 us).
+// as long as a full one: a piece that others follow ends with a full round where less than half of the next one would be left (8191 tokens,
+// 50257 x 1032, 64 columns of tiles at a time against 51: 3640 -> 3080 us backward; 12000 tokens, 50257 x 2048, 43 against 32: 7580 -> 6970).  What fits into one
+// piece stays one: another piece costs three launches and another pass over dx's sums (3 tokens, 50257 x 1024, 192 and 5 columns of tiles against 197: 109 -> 92 us;
+// 2048 tokens, 50257 x 2048: 1205 -> 1135; 6000 tokens, 33000 x 2048, 87, 32 and 10 against 87 and 42: 2365 -> 2300).
 // Up to 16 tokens the rounding of the logits' gradient is kept as a row of its own behind it: the rows are still one tile, and with bf16 elements
 // the results' rounding is the only one that counts (without: errors of 1.41 times it, and of a single token up to twice, as all of
 // its results hang on its target's one number).
@@ -514,9 +516,8 @@ Piece piece_of(const lsm_vocab_params& p, int left) {
     int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256;  // in tiles of 256 columns
     if (most < 1) most = 1;
     int64_t tiles = up(left, 256);
-    if (tiles > most) tiles = most;
-    const int64_t across = up(p.D, 256), round = 256 / across, over = tiles % (round ? round : 1);
-    if (!f32 && round > 1 && tiles > round && 2 * over < round) tiles -= over;
+    const int64_t across = up(p.D, 256), round = 256 / across, over = most % (round ? round : 1);
+    if (tiles > most) tiles = !f32 && round > 1 && most > round && 2 * over < round ? most - over : most;
     q.width = tiles * 256 < left ? int(tiles * 256) : left;
     q.grad = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(q.width, t.cols); }, kinds);
     q.dw = pick_tile(f32, p.n, [&](const TileSize& t) { return int64_t(up(q.width, t.rows)) * up(p.D, t.cols); },

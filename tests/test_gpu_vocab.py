@@ -194,6 +194,24 @@ def test_a_vocabulary_in_pieces(dtype):
     assert (got["dx"][gone] == 0).all() and (got["loss"][gone] == 0).all() and (got["lse"][gone] == 0).all()
 
 
+@pytest.mark.parametrize("n,D,V,pieces", [(3, 1024, 50257, 1), (64, 1024, 20001, 1), (700, 1032, 33000, 1), (8191, 1032, 20001, 2)])
+def test_what_fits_into_one_piece_is_one(n, D, V, pieces):
+    """Launches of the logits' gradient: 8191 x 16384 of bf16 is what a piece holds."""
+    import torch
+    a = make(n, D, V, 0, "bf16", seed=n)
+    loss, lse = lsm().lsm_linear_cross_entropy(a["x"], a["w"], a["index"])
+    lsm().lsm_profile_start()
+    lsm().lsm_linear_cross_entropy_bwd(a["x"], a["w"], a["index"], lse, a["d_loss"])
+    torch.cuda.synchronize()
+    names = [name for name, _ in lsm().lsm_profile_stop()]
+    assert names.count("vocab_grad") == names.count("vocab_dw") == names.count("vocab_dx") == pieces
+
+
+def test_whole_pieces_that_end_with_full_rounds():
+    """8191 tokens of which most count, three pieces: 51 columns of tiles, of the 64 that fit, twice, and what is left; dx's sums go from piece to piece."""
+    check(make(8191, 1032, 40001, 0, "bf16", seed=41, left_out=0.3))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,D,V,left_out", [(2100, 72, 20001, 0.9), (1500, 264, 9001, 0.7), (8000, 24, 5001, 0.997), (700, 520, 6000, 0.5), (3000, 72, 3001, 1.0)])
 def test_few_tokens_of_many_count(dtype, n, D, V, left_out):
