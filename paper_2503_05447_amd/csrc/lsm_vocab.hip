@@ -23,7 +23,7 @@ constexpr int kMostEntries = 256, kGroup = 512;
 
 // dx of a piece: rows of a tile, in how many shares its columns are taken with all tokens, the most it is worth taking them in
 struct Shares { int rows, least, most; };
-constexpr int kPieceKinds = 3;  // whole pieces, one that ends with a full round, what is left
+constexpr int kPieceKinds = 2;  // whole pieces, what is left
 
 struct VocabArgs {
     const void *x, *w;
@@ -479,8 +479,9 @@ __global__ __launch_bounds__(256) void k_dx_join(VocabArgs a) {
 // ---- host ------------------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of the logits' gradient at a time: what the memory-side cache holds
 
-bool fits(const lsm_vocab_params& p, bool backward);
-int check(const lsm_vocab_params* p, bool backward) {
+struct Pieces;
+bool fits(const lsm_vocab_params& p, Pieces* backward);
+int check(const lsm_vocab_params* p, Pieces* backward) {  // backward: where its pieces go, null for the forward call
     if (!p) return LSM_ERR_NULL;
     if (p->struct_size != sizeof(lsm_vocab_params)) return LSM_ERR_SHAPE;
     if (p->n < 1 || p->D < 1 || p->V < 1 || p->K < 0 || p->n > kMostPairs || p->V > (1 << 24)) return LSM_ERR_SHAPE;
@@ -497,28 +498,18 @@ int logits_tile(const lsm_vocab_params& p) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
     return pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(p.V, t.cols); }, f32 ? 0x7e : 0x7f);
 }
-// A piece of the vocabulary backward, of the `left` columns from the piece before on: how many, the tiles of the logits' gradient, of dw and dx,
-// and into how many shares dx takes the piece.  dw's products are as long as there are tokens, so that a last round of a few tiles takes
-// as long as a full one: a piece that others follow ends with a full round where less than half of the next one would be left (8191 tokens,
-// 50257 x 1032, 64 columns of tiles at a time against 51: 3640 -> 3080 us backward; 12000 tokens, 50257 x 2048, 43 against 32: 7580 -> 6970).  What fits into one
-// piece stays one: another piece costs three launches and another pass over dx's sums (3 tokens, 50257 x 1024, 192 and 5 columns of tiles against 197: 109 -> 92 us;
-// 2048 tokens, 50257 x 2048: 1205 -> 1135; 6000 tokens, 33000 x 2048, 87, 32 and 10 against 87 and 42: 2365 -> 2300).
 // Up to 16 tokens the rounding of the logits' gradient is kept as a row of its own behind it: the rows are still one tile, and with bf16 elements
 // the results' rounding is the only one that counts (without: errors of 1.41 times it, and of a single token up to twice, as all of
 // its results hang on its target's one number).
 int halves_of(const lsm_vocab_params& p) { return p.dtype == LSM_DTYPE_BF16 && p.n <= 16 ? 2 : 1; }
 
+// A piece of the vocabulary backward: how many columns, the tiles of the logits' gradient, of dw and dx, into how many shares dx takes the piece.
 struct Piece { int width, grad, dw, dx, shares; int64_t tiles, rows; };  // tiles: the most of its launches; rows: of sums for dx
-Piece piece_of(const lsm_vocab_params& p, int left) {
+Piece piece_of(const lsm_vocab_params& p, int width) {
     const bool f32 = p.dtype == LSM_DTYPE_F32;
     const unsigned kinds = halves_of(p) == 2 ? 0x78 : f32 ? 0x7e : 0x7f;
     Piece q{};
-    int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256;  // in tiles of 256 columns
-    if (most < 1) most = 1;
-    int64_t tiles = up(left, 256);
-    const int64_t across = up(p.D, 256), round = 256 / across, over = most % (round ? round : 1);
-    if (tiles > most) tiles = !f32 && round > 1 && most > round && 2 * over < round ? most - over : most;
-    q.width = tiles * 256 < left ? int(tiles * 256) : left;
+    q.width = width;
     q.grad = pick_tile(f32, p.D, [&](const TileSize& t) { return int64_t(up(p.n, t.rows)) * up(q.width, t.cols); }, kinds);
     q.dw = pick_tile(f32, p.n, [&](const TileSize& t) { return int64_t(up(q.width, t.rows)) * up(p.D, t.cols); },
                      (f32 ? 0 : 1 << 0) | 1 << 2 | 1 << 5);
@@ -543,20 +534,37 @@ Piece piece_of(const lsm_vocab_params& p, int left) {
         if (n > q.tiles) q.tiles = n;
     return q;
 }
+// The pieces of a call: `count` whole ones and what is left of the vocabulary, one column at least.
+// dw's products are as long as there are tokens, so that a last round of a few tiles takes as long as a full one: a whole piece ends with a
+// full round where less than half of the next one would be left (8191 tokens, 50257 x 1032, 64 columns of tiles at a time against 51: 3640 -> 3080 us
+// backward; 12000 tokens, 50257 x 2048, 43 against 32: 7580 -> 6970).  What fits into one piece stays one: another piece costs three launches and another
+// pass over dx's sums (3 tokens, 50257 x 1024, 192 and 5 columns of tiles against 197: 109 -> 92 us; 2048 tokens, 50257 x 2048: 1205 -> 1135; 6000
+// tokens, 33000 x 2048, 87, 32 and 10 against 87 and 42: 2365 -> 2300).
+struct Pieces { Piece whole, last; int count; };
+Pieces pieces_of(const lsm_vocab_params& p) {
+    const bool f32 = p.dtype == LSM_DTYPE_F32;
+    int64_t most = kPieceBytes / (int64_t(p.n) * (f32 ? 4 : 2)) / 256;  // in tiles of 256 columns
+    if (most < 1) most = 1;
+    const int64_t tiles = up(p.V, 256), round = 256 / up(p.D, 256), over = most % (round ? round : 1);
+    const int64_t whole = !f32 && round > 1 && most > round && 2 * over < round ? most - over : most;
+    Pieces q{};
+    q.count = tiles > most ? up(tiles - most, whole) : 0;
+    if (q.count) q.whole = piece_of(p, int(whole * 256));
+    q.last = piece_of(p, int(p.V - q.count * whole * 256));
+    return q;
+}
 // The most of any piece: columns (whole tiles), tiles, rows of sums.
-Piece largest_piece(const lsm_vocab_params& p) {
+Piece largest_of(const Pieces& all) {
     Piece most{};
-    for (int v = 0; v < p.V;) {
-        const Piece q = piece_of(p, p.V - v);
+    for (const Piece& q : {all.whole, all.last}) {
         if (up(q.width, 256) * 256 > most.width) most.width = up(q.width, 256) * 256;
         if (q.rows > most.rows) most.rows = q.rows;
         if (q.tiles > most.tiles) most.tiles = q.tiles;
-        v += q.width;
     }
     return most;
 }
-bool fits(const lsm_vocab_params& p, bool backward) {
-    if (backward) return largest_piece(p).tiles < kMostTiles;
+bool fits(const lsm_vocab_params& p, Pieces* backward) {
+    if (backward) return largest_of(*backward = pieces_of(p)).tiles < kMostTiles;
     const TileSize& t = kTiles[logits_tile(p)];
     return int64_t(up(p.n, t.rows)) * up(p.V, t.cols) < kMostTiles;
 }
@@ -565,7 +573,7 @@ int parts_of(const lsm_vocab_params& p, int kind) { return up(p.V, kTiles[kind].
 int groups_of(const lsm_vocab_params& p) { return up(p.V, kGroup); }
 
 struct Space { size_t offsets, order, place, hist, count, entry, share, begin, entropy, stats, at_entry, grad, part, bytes; };
-Space space(const lsm_vocab_params& p, bool backward) {
+Space space(const lsm_vocab_params& p, const Pieces* backward) {
     const size_t n = p.n, el = p.dtype == LSM_DTYPE_BF16 ? 2 : 4, K = p.K;
     Space s{};
     size_t at = 0;
@@ -583,7 +591,7 @@ Space space(const lsm_vocab_params& p, bool backward) {
         s.stats = take(size_t(parts_of(p, logits_tile(p))) * n * sizeof(f32x2));
         s.at_entry = take((K ? K : 1) * n * 4);
     } else {
-        const Piece q = largest_piece(p);
+        const Piece q = largest_of(*backward);
         s.grad = take(n * halves_of(p) * q.width * el);
         s.part = take(size_t(q.rows) * p.D * 4);
     }
@@ -666,7 +674,7 @@ bool launch_dx(const VocabArgs& a, hipStream_t st) {
 }
 
 template <typename TIO>
-bool launch(VocabArgs a, const lsm_vocab_params& p, bool backward, hipStream_t st) {
+bool launch(VocabArgs a, const lsm_vocab_params& p, const Pieces* backward, hipStream_t st) {
 #define LSM_KIND(call, kind)                                                                                     \
     ((kind) == 0 ? call(0) : (kind) == 1 ? call(1) : (kind) == 2 ? call(2) : (kind) == 3 ? call(3) : (kind) == 4 ? call(4) \
                                                                                      : (kind) == 5 ? call(5) : call(6))
@@ -682,8 +690,8 @@ bool launch(VocabArgs a, const lsm_vocab_params& p, bool backward, hipStream_t s
         else hipLaunchKernelGGL(k_join<4>, dim3(up(a.n, 4)), dim3(1024), 0, st, a);
         return launched();
     }
-    for (a.v0 = 0; a.v0 < a.V;) {
-        const Piece q = piece_of(p, a.V - a.v0);
+    for (int i = 0; i <= backward->count; ++i) {
+        const Piece& q = i < backward->count ? backward->whole : backward->last;
         a.width = q.width;
         a.piece = up(q.width, 256) * 256;
         a.here = Shares{kTiles[q.dx].rows, q.shares, q.width / 512};
@@ -691,11 +699,7 @@ bool launch(VocabArgs a, const lsm_vocab_params& p, bool backward, hipStream_t s
         if (a.dw && !(q.dw == 0 ? launch_dw<TIO, 0>(a, q.width, st) : q.dw == 2 ? launch_dw<TIO, 2>(a, q.width, st) : launch_dw<TIO, 5>(a, q.width, st)))
             return false;
         if (!LSM_KIND(LSM_DX, q.dx)) return false;
-        const Shares last = a.kinds ? a.before[a.kinds - 1] : Shares{};
-        if (last.rows != a.here.rows || last.least != a.here.least || last.most != a.here.most) {
-            if (a.kinds == kPieceKinds) return false;
-            a.before[a.kinds++] = a.here;
-        }
+        if (i == 0 || i == backward->count) a.before[a.kinds++] = a.here;
         a.v0 += q.width;
     }
     ProfScope ps(KID_VOCAB_JOIN, st);
@@ -713,22 +717,23 @@ extern "C" {
 
 size_t lsm_vocab_loss_workspace_bytes(const lsm_vocab_params* p) {
     using namespace lsm;
-    return check(p, false) == LSM_OK ? space(*p, false).bytes : 0;
+    return check(p, nullptr) == LSM_OK ? space(*p, nullptr).bytes : 0;
 }
 size_t lsm_vocab_loss_bwd_workspace_bytes(const lsm_vocab_params* p) {
     using namespace lsm;
-    return check(p, true) == LSM_OK ? space(*p, true).bytes : 0;
+    Pieces pieces;
+    return check(p, &pieces) == LSM_OK ? space(*p, &pieces).bytes : 0;
 }
 
 int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,
                    float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     using namespace lsm;
-    const int rc = check(p, false);
+    const int rc = check(p, nullptr);
     if (rc != LSM_OK) return rc;
     if (!x || !w || !index || !teacher != !p->K || !loss || !lse) return LSM_ERR_NULL;
     if (misaligned(x) || misaligned(w) || misaligned(index) || misaligned(teacher) || misaligned(loss) || misaligned(lse) || misaligned(workspace))
         return LSM_ERR_ALIGN;
-    const Space s = space(*p, false);
+    const Space s = space(*p, nullptr);
     if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
     VocabArgs a = arguments(*p, s, ws, x, w, index, teacher);
@@ -736,20 +741,21 @@ int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, cons
     a.lse = lse;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (!enqueue_rows(a, s, ws, st)) return LSM_ERR_LAUNCH;
-    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, *p, false, st) : launch<float>(a, *p, false, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, *p, nullptr, st) : launch<float>(a, *p, nullptr, st)) ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 int lsm_vocab_loss_bwd(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,
                        const float* lse, const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes,
                        void* stream) {
     using namespace lsm;
-    const int rc = check(p, true);
+    Pieces pieces;
+    const int rc = check(p, &pieces);
     if (rc != LSM_OK) return rc;
     if (!x || !w || !index || !teacher != !p->K || !lse || !d_loss || !dx) return LSM_ERR_NULL;
     if (misaligned(x) || misaligned(w) || misaligned(index) || misaligned(teacher) || misaligned(lse) || misaligned(d_loss) || misaligned(dx) ||
         misaligned(dw) || misaligned(workspace))
         return LSM_ERR_ALIGN;
-    const Space s = space(*p, true);
+    const Space s = space(*p, &pieces);
     if (!workspace || workspace_bytes < s.bytes) return LSM_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
     VocabArgs a = arguments(*p, s, ws, x, w, index, teacher);
@@ -759,7 +765,7 @@ int lsm_vocab_loss_bwd(const lsm_vocab_params* p, const void* x, const void* w, 
     a.dw = dw;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (!enqueue_rows(a, s, ws, st)) return LSM_ERR_LAUNCH;
-    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, *p, true, st) : launch<float>(a, *p, true, st)) ? LSM_OK : LSM_ERR_LAUNCH;
+    return (p->dtype == LSM_DTYPE_BF16 ? launch<uint16_t>(a, *p, &pieces, st) : launch<float>(a, *p, &pieces, st)) ? LSM_OK : LSM_ERR_LAUNCH;
 }
 
 }  // extern "C"
