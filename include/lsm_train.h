@@ -116,7 +116,7 @@ typedef struct {
     int32_t  n, D, V;     /* tokens (1..2^24), their width (a multiple of 8, at most 65536), vocabulary (1..2^24)  */
     int32_t  K;           /* 0: one target a token; 1..256: so many logits of a teacher, n * K at most 2^28       */
     int32_t  dtype;       /* lsm_dtype of x, w and their gradients                                            */
-    float    temperature; /* > 0: divides the logits, the teacher's too                                       */
+    float    temperature; /* 2^-127 or more: divides the logits, the teacher's too                            */
     int32_t  reserved;    /* 0                                                                               */
     int64_t  x_stride;    /* elements between rows of x, >= D, a multiple of 8; n * x_stride * element size below 2^32 - 4096 */
 } lsm_vocab_params;
@@ -134,7 +134,7 @@ typedef struct {
  *   workspace  at least lsm_vocab_loss_workspace_bytes(p) (0 for invalid params)
  * An index outside [0, V) is no target and no entry, nor is a teacher's logit of -inf or NaN (+inf counts as the largest finite
  * number); entries of the same index add up.  A token without target or entries is left out: its row of x is not read, loss and lse
- * are 0.  Sums are fp32.
+ * are 0.  Sums are fp32.  A token with a logit of 2^127 or more (or NaN) gets a loss that is not finite.
  */
 size_t lsm_vocab_loss_workspace_bytes(const lsm_vocab_params* p);
 int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,

@@ -486,7 +486,7 @@ int check(const lsm_vocab_params* p, Pieces* backward) {  // backward: where its
     if (p->struct_size != sizeof(lsm_vocab_params)) return LSM_ERR_SHAPE;
     if (p->n < 1 || p->D < 1 || p->V < 1 || p->K < 0 || p->n > kMostPairs || p->V > (1 << 24)) return LSM_ERR_SHAPE;
     if (int64_t(p->n) * p->K > (1 << 28)) return LSM_ERR_SHAPE;
-    if (!(p->temperature > 0.f) || !(1.f / p->temperature < 3.4e38f) || !(1.f / p->temperature > 0.f)) return LSM_ERR_SHAPE;
+    if (!(p->temperature > 0.f) || !(1.f / p->temperature * kLog2e < 3.4e38f) || !(1.f / p->temperature > 0.f)) return LSM_ERR_SHAPE;  // (the kernels' own scale)
     if (p->dtype != LSM_DTYPE_F32 && p->dtype != LSM_DTYPE_BF16) return LSM_ERR_UNSUPPORTED;
     if (p->K > kMostEntries || p->D % 8 || p->D > 65536 || p->reserved != 0) return LSM_ERR_UNSUPPORTED;
     const int64_t el = p->dtype == LSM_DTYPE_BF16 ? 2 : 4;

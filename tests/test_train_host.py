@@ -110,6 +110,17 @@ def test_losses_refuse_bad_sizes():
         assert size(ctypes.byref(vocab(D=60))) == 0 and size(ctypes.byref(vocab(n=100000, V=131071))) > 0
 
 
+def test_temperatures_whose_scale_is_not_finite_are_refused():
+    """The kernels raise 2 to a power: 1 / (temperature log 2) is a number of fp32 from 2^-127.4 on."""
+    for name, n in (("lsm_vocab_loss", 7), ("lsm_vocab_loss_bwd", 9)):
+        for bad in (3.5e-39, 4.0e-39, 2.0 ** -128):
+            assert call(name, vocab(temperature=bad), n, a3=None) == SHAPE, (name, bad)
+    for size in (pkg.library().lsm_vocab_loss_workspace_bytes, pkg.library().lsm_vocab_loss_bwd_workspace_bytes):
+        assert size(ctypes.byref(vocab(temperature=3.5e-39))) == 0
+        for good in (2.0 ** -127, 2.0 ** -100, 1.0, 2.0 ** 126):
+            assert size(ctypes.byref(vocab(temperature=good))) > 0
+
+
 def test_products_that_no_launch_holds_are_refused():
     """2^32 threads are the most of a launch, 512 the most of a tile: 2^23 tiles or more are refused before anything runs."""
     many = experts(n=1 << 24, top_k=1, D=8, F=65536)             # 65536 x 512 tiles of the hidden layer
