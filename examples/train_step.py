@@ -3,11 +3,12 @@ backward.
 
 A layer: projection -> lsm_qk_norm_rope -> lsm_chunk_fwd -> projection, then lsm_moe_route -> lsm_moe_plan -> lsm_moe_experts; at the end
 lsm_linear_cross_entropy, or with a teacher's best logits lsm_linear_distill.  Each operator's backward call is wrapped for torch's
-automatic differentiation; projections, norms of the residual stream and the optimizer are torch.
+automatic differentiation, once: a derivative of the gradients is refused.  Projections, norms of the residual stream and the optimizer are torch.
 
     python examples/train_step.py [--batch 4] [--tokens 2048] [--steps 10] [--teacher 32]
 """
 import argparse
+import functools
 import os
 import sys
 import time
@@ -16,6 +17,17 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2503_05447_amd as lsm  # noqa: E402
+
+
+def once(backward):
+    """The operators' gradients are constants to automatic differentiation: under create_graph what follows from them would silently be
+    differentiated as if they were, whether or not the gradients that come in require one."""
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        if torch.is_grad_enabled():
+            raise RuntimeError("the gradients of these operators cannot be differentiated again (create_graph)")
+        return backward(ctx, *grads)
+    return run
 
 
 class NormRotation(torch.autograd.Function):
@@ -27,6 +39,7 @@ class NormRotation(torch.autograd.Function):
         return lsm.lsm_qk_norm_rope(q, k, q_weight=q_weight, k_weight=k_weight, **ctx.how)
 
     @staticmethod
+    @once
     def backward(ctx, d_q, d_k):
         q, k, q_weight, k_weight = ctx.saved_tensors
         g = lsm.lsm_qk_norm_rope_bwd(q, k, d_q.contiguous(), d_k.contiguous(), q_weight=q_weight, k_weight=k_weight, **ctx.how)
@@ -41,6 +54,7 @@ class Mixer(torch.autograd.Function):
         return lsm.lsm_chunk_fwd(q, k, v, g, lsm.DECAY_SCALAR, layout=lsm.LAYOUT_BTHD)[0]
 
     @staticmethod
+    @once
     def backward(ctx, d_o):
         r = lsm.lsm_chunk_bwd(*ctx.saved_tensors, lsm.DECAY_SCALAR, d_o.contiguous(), layout=lsm.LAYOUT_BTHD)
         return r["dq"], r["dk"], r["dv"], r["dg"]
@@ -56,6 +70,7 @@ class Experts(torch.autograd.Function):
         return lsm.lsm_moe_experts(x, weights, ctx.plan, w_gate_up, w_down, residual=residual)
 
     @staticmethod
+    @once
     def backward(ctx, d_y):
         x, logits, weights, chosen, w_gate_up, w_down = ctx.saved_tensors
         g = lsm.lsm_moe_experts_bwd(x, weights, ctx.plan, w_gate_up, w_down, d_y.contiguous())
@@ -71,6 +86,7 @@ class CrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once
     def backward(ctx, d_loss):
         x, w, target, lse = ctx.saved_tensors
         g = lsm.lsm_linear_cross_entropy_bwd(x, w, target, lse, d_loss.contiguous())
@@ -87,6 +103,7 @@ class Distill(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once
     def backward(ctx, d_loss):
         x, w, index, teacher, lse = ctx.saved_tensors
         g = lsm.lsm_linear_distill_bwd(x, w, index, teacher, lse, d_loss.contiguous(), ctx.temperature)
