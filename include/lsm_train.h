@@ -20,7 +20,7 @@ extern "C" {
 
 typedef struct {
     uint32_t struct_size; /* = sizeof(lsm_route_params)                                                        */
-    int32_t  n, E, top_k; /* tokens (1..2^24), experts (1..256), how many of them a token goes to (1..16, at most E) */
+    int32_t  n, E, top_k; /* tokens, experts (1..256), how many of them a token goes to (1..16, at most E); n * top_k at most 2^24 */
     int32_t  dtype;       /* lsm_dtype of the logits and of their gradient                                    */
     int32_t  renormalise; /* 1: a token's weights sum to 1; 0: they are the softmax over all experts           */
 } lsm_route_params;
@@ -63,7 +63,7 @@ int lsm_moe_plan(const lsm_route_params* p, const int32_t* chosen, int32_t* offs
 
 typedef struct {
     uint32_t struct_size; /* = sizeof(lsm_experts_params)                                                     */
-    int32_t  n, D, F;     /* tokens, their width and the experts' (multiples of 8, at most 65536)             */
+    int32_t  n, D, F;     /* tokens, their width and the experts' (multiples of 8, at most 65536; 2 F D * element size below 2^32 - 4096) */
     int32_t  E, top_k;    /* experts (1..256), pairs of a token (1..16); n * top_k at most 2^24                */
     int32_t  dtype;       /* lsm_dtype of x, weights of the experts, y and all their gradients                */
     int32_t  reserved;    /* 0                                                                               */
@@ -125,7 +125,8 @@ typedef struct {
  * For every token:   z_v = <x, w_v> / temperature ,   lse = log sum_v exp(z_v) ,
  *     K = 0:   loss = lse - z_target ,
  *     K > 0:   loss = sum_j p_j (log p_j - (z_{index_j} - lse)) ,   p = softmax(teacher / temperature) over the token's entries
- * (the divergence of the model from the teacher, whose other tokens count as impossible).  The logits are never kept.
+ * (the divergence of the model from the teacher, whose other tokens count as impossible).  The logits are never kept; of every 32 to
+ * 128 of a token's the workspace holds a maximum and a sum, 8 bytes (16384 tokens, 131072 columns, bf16: 134 MB).
  *   x          [n, D], rows x_stride apart                                                          in
  *   w          [V, D]                                                                               in
  *   index      [n] (K = 0: the target) or [n, K] int32                                               in
@@ -133,8 +134,10 @@ typedef struct {
  *   loss, lse  [n] fp32                                                                             out
  *   workspace  at least lsm_vocab_loss_workspace_bytes(p) (0 for invalid params)
  * An index outside [0, V) is no target and no entry, nor is a teacher's logit of -inf or NaN (+inf counts as the largest finite
- * number); entries of the same index add up.  A token without target or entries is left out: its row of x is not read, loss and lse
- * are 0.  Sums are fp32.  A token with a logit of 2^127 or more (or NaN) gets a loss that is not finite.
+ * number).  Entries of the same index each count with their own p: their gradients add up, and the loss is the sum as it stands, which is
+ * less than the divergence from the teacher with such entries made one, by what their p log p differ.
+ * A token without target or entries is left out: its row of x is not read, loss and lse are 0.  Sums are fp32.  A token with a logit of
+ * 2^127 or more (or NaN) gets a loss that is not finite.
  */
 size_t lsm_vocab_loss_workspace_bytes(const lsm_vocab_params* p);
 int lsm_vocab_loss(const lsm_vocab_params* p, const void* x, const void* w, const int32_t* index, const float* teacher,
