@@ -397,9 +397,8 @@ struct Tile {
         barrier();
     }
 
-    // Values of block (i, j): element e of a lane is row(j), column col(i) + e of the tile.
+    // Values of block (i, j): element e of a lane is row(j), column 16 (wc TC + i) + 4 (lane / 16) + e of the tile.
     __device__ __forceinline__ int row(int j) const { return (wr * TR + j) * 16 + (lane & 15); }
-    __device__ __forceinline__ int col(int i) const { return (wc * TC + i) * 16 + 4 * (lane >> 4); }
     // Sum and maximum over the lanes of a row.
     static __device__ __forceinline__ float row_sum(float x) {
         x += __shfl_xor(x, 16, 64);

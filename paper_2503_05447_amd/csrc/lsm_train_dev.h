@@ -17,6 +17,10 @@ bool enqueue_plan(const int32_t* id, int64_t count, int groups, int limit, int32
 struct TileSize { int rows, cols, waves, at_once; };
 constexpr TileSize kTiles[] = {{256, 256, 2, 1}, {128, 256, 4, 1}, {128, 128, 2, 2}, {64, 256, 4, 2}, {32, 256, 4, 2}, {64, 64, 2, 4}, {32, 128, 4, 4}};
 constexpr int kTileKinds = int(sizeof(kTiles) / sizeof(kTiles[0]));
+// call(K) with the tile's number as a constant.
+#define LSM_KIND(call, kind)                                                                                     \
+    ((kind) == 0 ? call(0) : (kind) == 1 ? call(1) : (kind) == 2 ? call(2) : (kind) == 3 ? call(3) : (kind) == 4 ? call(4) \
+                                                                                     : (kind) == 5 ? call(5) : call(6))
 constexpr int kTileStepBytes = 64;  // of k, a row and step
 constexpr int64_t kMostTiles = kAxisThreads / 512;  // of a launch, a workgroup of at most 512 threads each
 inline int up(int64_t x, int64_t to) { return int((x + to - 1) / to); }

@@ -187,7 +187,7 @@ def _experts(x, weights, plan, w_gate_up, w_down, d_y):
 
 def lsm_moe_experts(x, weights, plan, w_gate_up, w_down, residual=None, y=None, workspace=None, stream=None):
     """y [n,D] = residual + sum_j weights[t,j] Wd_e (silu(Wg_e x_t) * (Wu_e x_t)) over the pairs of ``plan`` (lsm_moe_plan), for
-    any number of tokens (lsm_moe_step is the form for a decode step, with the routing in it).
+    any number of tokens (lsm_moe_step, with the routing in it, is the faster form for a decode step of up to 128).
 
     x [n,D] float32 or bfloat16, dense along D (rows may be further apart, by multiples of 8 elements); weights [n,top_k] float32;
     w_gate_up [E,2F,D] (F rows of the gate, F rows of the factor), w_down [E,D,F], residual [n,D] or None of x's type; D and F
