@@ -9,14 +9,14 @@
 // An expert's rows are whole tiles but the last; a workgroup finds its expert and tile from the offsets, which stay on the device.
 //
 // Bound: the matrix products for many tokens, the weights' bytes for few.  16384 tokens of 1024, 64 experts of 1024, 8 a token, bf16: up
-// 505 us (1.09 PFLOP/s), down 293 (0.94), sum 70 (4.8 TB/s), hidden_grad 1050 (0.79: one tile's products and the other's follow each
-// other, with a fresh start each), dx 517 (1.06), dw 830 for both (0.99: a mean of 2048 pairs is 64 steps a tile), against 1.17 to
-// 1.42 of large library products.  Five tokens: 25, 17 and 5 us for 168 and 84 MB of weights.  fp32, 1500 tokens of 512, 8 experts of
-// 776, 2 a token: 55, 37, 5, 86, 68, 7, 76 and 45 us, 50 to 82 TFLOP/s.
+// 511 us (1.08 PFLOP/s; matrix cores busy 0.59 of the clocks), down 327 (0.84, 0.45), sum 131 (4.6 TB/s), hidden_grad 1053 (0.78, 0.41: one tile's
+// products and the other's follow each other, with a fresh start each), dx 545 (1.01, 0.55), dw 830 to 915 for both (0.90 to 0.99, 0.56: a mean of 2048
+// pairs is 64 steps a tile), against 1.17 to 1.42 of large library products.  Five tokens: 26, 17 and 4 us for 168 and 84 MB of weights.  fp32, 1500
+// tokens of 512, 8 experts of 776, 2 a token: 55, 38, 5, 86, 69, 7 and 121 us, 50 to 82 TFLOP/s (busy 0.61 to 0.72).
 // Nothing is saved by the forward call: gate and factor formed again cost 500 us there, kept they would be 0.5 GB a layer.  A pair's result is a
 // row of its own, added up by k_sum in a fixed order: adding to the token's row at once would need atomics, whose order is not fixed.
 // These rows are parts of a token's sum and stay in fp32: as fp16 with a power of two for each stretch of a row they would take half the bytes
-// (16384 tokens forward and backward 3520 -> 3365 us, five tokens 44.4 -> 46.1), and move one result in sixteen to a neighbouring bf16.
+// (16384 tokens forward and backward 3520 -> 3365 us, five tokens 44.4 -> 46.1), and change five tokens' results by 5e-4 of their size.
 #include "lsm_product_dev.h"
 
 namespace lsm {

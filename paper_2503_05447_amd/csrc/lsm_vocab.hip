@@ -8,10 +8,11 @@
 //   k_dx        gradient w, the piece's vocabulary being the long axis, in several shares of it, added to the pieces before
 //   k_dx_join   the shares' sum
 // Bound: the matrix products, three forward and backward and a fourth for the logits formed again; for few tokens the weights, read once.
-// 8191 tokens of 2048 of which 5734 count, 50257 columns, bf16: logits 935 us (1.26 PFLOP/s, a plain library product of that size is
-// 1.24), grad 1115 (1.06: 576 MB leave through LDS), dw 980 (1.20), dx 1190 (0.99: 184 tiles of 256 x 256 for 256 compute units); join 10,
-// dx's sum 15, the plan 12 a call.  700 tokens of 512, 32003 columns, fp32: 211, 217, 196 and 204 us, 106 to 117 TFLOP/s.  Three tokens of
-// 1024, 50257 columns: 22 us, 4.7 TB/s.  4096 tokens of 1024 with a teacher's 64 entries, 32000 columns: 260, 272, 206 and 211 us.
+// 8191 tokens of 2048 of which 5734 count, 50257 columns, bf16: logits 946 us (1.25 PFLOP/s, a plain library product of that size is
+// 1.24; matrix cores busy 0.67 of the clocks), grad 1112 (1.06, 0.60: 576 MB leave through LDS), dw 994 (1.19, 0.64), dx 1174 (1.00, 0.65: 184 tiles of
+// 256 x 256 for 256 compute units); join 10, dx's sum 15, the plan 13 a call.  700 tokens of 512, 32003 columns, fp32: 218, 224, 202 and 215 us,
+// 103 to 113 TFLOP/s (busy 0.77 to 0.79).  Three tokens of 1024, 50257 columns: 22 us, 4.7 TB/s; backward 22, 33 and 20 us.  4096 tokens of 1024
+// with a teacher's 64 entries, 32000 columns: 260, 271, 206 and 206 us.
 // The logits' gradient is formed a piece of the vocabulary at a time, so that workspaces do not grow with it; that pieces of 256 MB fit the
 // memory-side cache makes no difference (512 MB and 1 GB: within 1 %).
 #include "lsm_product_dev.h"
