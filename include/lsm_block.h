@@ -101,9 +101,9 @@ typedef struct {
  *   y          [n, D]                                                                               out
  *   workspace  at least lsm_moe_step_workspace_bytes(p) (0 for invalid params)
  * The form for decoding: the active experts' weights are read once, whatever the tokens that share them.  Beside lsm_moe_route,
- * lsm_moe_plan and lsm_moe_experts of lsm_train.h it is the faster one for all the tokens that it takes (64 experts of 1024 x 1024, 8 a
- * token, bf16: one token 23 us against 59, 32 tokens 92 against 101, 128 tokens 106 against 104); they are the form for more tokens, and for
- * training.  Sums are fp32; with bf16 elements the hidden activations are kept as a bf16 head and a bf16 remainder, so that the one
+ * lsm_moe_plan and lsm_moe_experts of lsm_train.h it is the faster one up to about 100 tokens, and as fast at 128 (64 experts of 1024 x
+ * 1024, 8 a token, bf16: one token 23 us against 59, 32 tokens 92 against 101, 128 tokens 106 against 104); they are the form for more tokens,
+ * and for training.  Sums are fp32; with bf16 elements the hidden activations are kept as a bf16 head and a bf16 remainder, so that the one
  * rounding to bf16 is the result's.  A token with a router output of NaN or +inf, or with none above -inf, gets a row of NaN (beside
  * finite ones an expert of -inf has the weight 0); other tokens are not affected.
  */

@@ -72,7 +72,7 @@ typedef struct {
 } lsm_experts_params;
 
 /*
- * (Up to 128 tokens forward alone: lsm_moe_step of lsm_block.h is the faster form.)
+ * (Up to about 100 tokens forward alone lsm_moe_step of lsm_block.h is the faster form.)
  * For every token t:   y_t = residual_t + sum_j weights[t, j] Wd_e (silu(Wg_e x_t) * (Wu_e x_t)) ,   e the expert of pair (t, j),
  * over the pairs that the plan of lsm_moe_plan holds (offsets, order, place).
  *   x          [n, D], rows x_stride apart                                                          in

@@ -187,7 +187,7 @@ def _experts(x, weights, plan, w_gate_up, w_down, d_y):
 
 def lsm_moe_experts(x, weights, plan, w_gate_up, w_down, residual=None, y=None, workspace=None, stream=None):
     """y [n,D] = residual + sum_j weights[t,j] Wd_e (silu(Wg_e x_t) * (Wu_e x_t)) over the pairs of ``plan`` (lsm_moe_plan), for
-    any number of tokens (lsm_moe_step, with the routing in it, is the faster form for a decode step of up to 128).
+    any number of tokens (lsm_moe_step, with the routing in it, is the faster form for a decode step of up to about 100).
 
     x [n,D] float32 or bfloat16, dense along D (rows may be further apart, by multiples of 8 elements); weights [n,top_k] float32;
     w_gate_up [E,2F,D] (F rows of the gate, F rows of the factor), w_down [E,D,F], residual [n,D] or None of x's type; D and F
@@ -290,8 +290,8 @@ def lsm_linear_distill(x, w, index, teacher, temperature=1.0, workspace=None, st
 
     index [n,K] int32 and teacher [n,K] float32: tokens and logits, in any order, K at most 256; p = softmax(teacher / temperature) over
     a token's entries, loss = sum_j p_j (log p_j - log softmax(x w^T / temperature)[index_j]).  An entry whose index is outside [0, V) or
-    whose logit is -inf or NaN does not count; a token without any is left out (loss and lse 0).  x, w as in
-    lsm_linear_cross_entropy."""
+    whose logit is -inf or NaN does not count, entries of the same index each count with their own p; a token without any is left out (loss
+    and lse 0).  x, w as in lsm_linear_cross_entropy."""
     if teacher is None:
         raise ValueError("teacher is required")
     return _vocab_fwd(x, w, index, teacher, temperature, workspace, stream, "lsm_linear_distill")
